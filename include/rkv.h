@@ -338,6 +338,126 @@ int rkv_entropy_profile(const rkv_shape* shape, int32_t n_layers, int32_t n_q, c
                         const void* const* k, float* rows_out, float* h_out, uint32_t* status, void* ws,
                         size_t ws_bytes, void* stream);
 
+/* ---- Paged caches: the memory that eviction gives back, and the attention that reads a cache.
+ *
+ * A pool holds K and V rows of 128 bf16 or fp16 values in n_pages pages of page_size slots (any size from 1);
+ * row (page, head, slot) lies at k + page k_page + head k_head + slot k_slot elements (v likewise), so pages of
+ * [n_kv_heads, page_size, d] and of [page_size, n_kv_heads, d] and views into larger buffers serve alike, and the
+ * caches of rkv_decode_step are pools whose page is a sequence's whole cache.  Strides are multiples of 8 and not
+ * negative, pools 16-byte aligned, n_pages * page_size < 2^31.  Slot i of a sequence lies in page
+ * table[s][i / page_size] at i % page_size; a flat slot number is page * page_size + i % page_size. */
+typedef enum { RKV_BF16 = 0, RKV_F16 = 1 } rkv_dtype;
+typedef struct {
+  void* k;
+  void* v;
+  int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
+  int32_t n_pages, page_size, n_kv_heads, head_dim, dtype;
+} rkv_pages;
+
+/* Bits of rkv_resize.status. */
+#define RKV_PAGES_EXHAUSTED 1u /* more pages asked for than are free */
+#define RKV_PAGES_INVALID 2u   /* a length, the cursor, or a total is out of its range */
+
+/* Device pointers of one rkv_pages_resize call, int32 unless noted.
+ *  lens, new_lens [n_seqs]  slots each sequence holds now and shall hold;
+ *  table  [n_seqs, max_pages], rows table_stride apart: page ids, read and written;
+ *  ring   [n_pages]  page ids; cursor [2] = {head, count}: free are ring[(head + j) % n_pages], j < count;
+ *  lens_out [n_seqs], cursor_out [2]  the new state (may be lens and cursor themselves);
+ *  slots  [max_new]  flat slot numbers of the new tokens, sequence by sequence; -1 behind the last;
+ *  cu_new [n_seqs + 1]  where each sequence's new tokens begin in slots (cu_q of rkv_pages_attend);
+ *  status [1] uint32: 0, or RKV_PAGES_* bits. */
+typedef struct {
+  const int32_t* lens;
+  const int32_t* new_lens;
+  int32_t* lens_out;
+  int32_t* table;
+  int64_t table_stride;
+  int32_t* ring;
+  const int32_t* cursor;
+  int32_t* cursor_out;
+  int32_t* slots;
+  int32_t* cu_new;
+  uint32_t* status;
+  int32_t n_seqs, max_pages, n_pages, page_size, max_new;
+} rkv_resize;
+
+/* Block tables and slot map from request lengths, on the device.  With have = ceil(len / page_size) and want =
+ * ceil(new_len / page_size): a sequence that grows takes want - have pages from the front of the ring (in the order
+ * of the sequences, then of their pages) into table[s][have ..]; one that shrinks appends table[s][want .. have) to the
+ * ring's end; entries past a sequence's pages are left as they are.  Pages given back are free from the next
+ * call on.  New tokens are slots len .. new_len - 1 of each growing sequence.
+ * All or nothing: when the pages do not suffice (RKV_PAGES_EXHAUSTED), or when a length is negative or above max_pages *
+ * page_size, the cursor is outside [0, n_pages), the new tokens exceed max_new, or more pages would be free than
+ * there are (RKV_PAGES_INVALID), table and ring stay, lens_out and cursor_out repeat the old state, slots are -1 and
+ * cu_new 0.  Page ids are copied, never dereferenced.  Two kernels at most; no workspace.
+ * Errors: RKV_ERR_INVALID_ARG (null pointers, negative sizes, max_new < 0), RKV_ERR_UNSUPPORTED (n_seqs > 8192,
+ * n_pages * page_size or max_pages * page_size from 2^31), RKV_ERR_SHAPE (table_stride < max_pages), RKV_ERR_HIP. */
+int rkv_pages_resize(const rkv_resize* r, void* stream);
+
+/* New rows of one rkv_pages_write call: row (o, t, h), o < n_outer, t < n_tokens, lies at k + o k_outer + t k_token +
+ * h k_head elements and goes to slot slots[o n_tokens + t] (n_outer = 1: [tokens, heads, d]; the compacted caches of
+ * rkv_prefill_evict are n_outer = B, k_outer = Hkv n d, k_token = d, k_head = n d). */
+typedef struct {
+  const void* k;
+  const void* v;
+  int64_t k_outer, k_token, k_head, v_outer, v_token, v_head;
+  const int32_t* slots;
+  int32_t n_outer, n_tokens;
+} rkv_rows;
+
+/* Copies new K and V rows to their slots, bit-exactly.  A row whose slot is outside [0, n_pages * page_size) is
+ * skipped (padding).  Slots that are not skipped must be distinct.
+ * Errors: RKV_ERR_INVALID_ARG (null pointers, negative sizes or strides, unknown dtype), RKV_ERR_UNSUPPORTED (head_dim
+ * != 128, pointers not 16-byte aligned, strides not multiples of 8, 2^31 rows or slots), RKV_ERR_HIP. */
+int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream);
+
+/* One rkv_pages_attend call.  Device pointers:
+ *  q, out   [n_rows, Hq, d] of the pool's dtype, row (t, hq) at q + t q_token + hq q_head elements (out likewise);
+ *  lse      NULL, or fp32 [n_rows, Hq], dense;
+ *  table    int32 [n_seqs, max_pages], rows table_stride apart; lens int32 [n_seqs]: cached slots of each sequence, its
+ *           queries' own ones included;
+ *  cu_q     int32 [n_seqs + 1], not descending: sequence s has rows cu_q[s] .. cu_q[s+1] - 1; NULL: one row each (n_rows =
+ *           n_seqs).  Rows from cu_q[n_seqs] on are left as they are;
+ *  prefix_lens  NULL, or int32 [n_seqs]; first_keys NULL, or int32 [n_rows]; slopes NULL, or fp32 [Hq].
+ * causal 0 or 1; window 0 (none) or the number of slots a query sees, its own included; scale, softcap (0: none).
+ * max_q, max_kv: the most rows and slots of a sequence, or 0; they choose kernels and splits, never results: calls
+ * with other bounds differ in rounding alone. */
+typedef struct {
+  const void* q;
+  void* out;
+  float* lse;
+  int64_t q_token, q_head, out_token, out_head;
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* lens;
+  const int32_t* cu_q;
+  const int32_t* prefix_lens;
+  const int32_t* first_keys;
+  const float* slopes;
+  int32_t n_seqs, n_rows, n_q_heads, max_pages, max_q, max_kv, causal, window;
+  float scale, softcap;
+} rkv_attend;
+
+/* Attention of new tokens, one or many per sequence, over a paged cache.  Row i of a sequence with n slots and m rows
+ * has position p = n - m + i and sees the slots j of [lo, hi):
+ *   hi = causal ? max(p + 1, min(prefix_lens[s], n)) : n   (a prefix is seen from every position),
+ *   lo = max(0, p - window + 1 with a window, first_keys[row])   (first_keys: where the row's document begins);
+ *   x_j = scale q . k_j;  softcap c: x_j <- c tanh(x_j / c);  slopes: x_j <- x_j - slopes[hq] |p - j|;
+ *   out = sum_j softmax_j(x) v_j,  lse = log sum_j exp(x_j); a row that sees nothing: out 0, lse -infinity.
+ * Slots are the cache's: in a cache that an eviction compacted, windows, documents and distances count kept rows.
+ * Products on bf16 / fp16 MFMA with 32-bit accumulation; softmax statistics and sums in 32 bits; probabilities are
+ * rounded to the pool's dtype for the product with V, once, before they are divided by their unrounded sum.
+ * Page ids are checked: a slot whose page is outside [0, n_pages) reads as a row of zeros.  Slots outside a sequence's
+ * visible ones are never read into a result, whatever they hold; lens are cut to [0, max_pages * page_size].
+ * ws: device workspace of rkv_pages_attend_workspace_size bytes, 256-byte aligned, one for each call in flight, and for
+ * each captured graph that may run beside another; NULL where that size is 0.
+ * Errors: RKV_ERR_INVALID_ARG (null pointers, negative sizes or strides, unknown dtype, scale or softcap not finite,
+ * softcap < 0), RKV_ERR_SHAPE (Hq not a multiple of Hkv, n_rows != n_seqs without cu_q, table_stride < max_pages),
+ * RKV_ERR_UNSUPPORTED (head_dim != 128, q or out not 16-byte aligned, strides not multiples of 8, 2^31 slots or more),
+ * RKV_ERR_WORKSPACE, RKV_ERR_HIP.  Validation ends before the first launch. */
+int rkv_pages_attend_workspace_size(const rkv_pages* pages, const rkv_attend* a, size_t* bytes);
+int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size_t ws_bytes, void* stream);
+
 /* Implementation calls (measurement, no paper passage): kernel timing for benchmarks and tests.
  * rkv_profile_enable(stage) makes every following
  * launch of that stage record a pair of HIP events around it on the caller's stream

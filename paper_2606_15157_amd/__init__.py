@@ -16,10 +16,12 @@ from typing import Sequence
 from . import _abi
 from ._abi import FULL, STREAMING, SNAPKV, H2O, TOVA, H2O_FULL, PHASE_PREFILL, PHASE_DECODE, T_IDENTITY, T_PPL_CAP  # noqa: F401
 from ._abi import SCOPE_PREFILL, SCOPE_DECODE, SCOPE_BOTH, STATUS_TIMEOUT, STATUS_INVALID, STATUS_REPAIRED  # noqa: F401
+from ._abi import PAGES_EXHAUSTED, PAGES_INVALID  # noqa: F401
 from ._abi import RkvError, check
 
 __all__ = ["Plan", "allocate_budgets", "evict_prefill", "decode_step", "decode_init_from_prefill", "prefill_check",
            "rule_phases", "version", "entropy_profile", "entropy_budgets",
+           "PagedCache", "pages_init", "pages_resize", "pages_write", "pages_attend", "pages_init_from_prefill",
            "FULL", "STREAMING", "SNAPKV", "H2O", "TOVA", "H2O_FULL", "SCOPE_PREFILL", "SCOPE_DECODE", "SCOPE_BOTH",
            "RkvError"]
 
@@ -379,3 +381,203 @@ def decode_step(plan: Plan, state, q, k, v, position: int, *, victim_out=None, s
     assert len(q) == len(k) == len(v) == n
     check(_abi.lib().rkv_decode_step(plan.handle, C.byref(shape), C.byref(st), C.byref(inp), int(position),
                                      C.c_void_p(_stream_handle(stream, dev))))
+
+
+# ---- paged caches
+
+def _same_device(dev, *tensors):
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError("tensors must be on one device")
+
+
+def _int32(name, t, shape):
+    """Checks an int32 tensor of `shape` (None: any size), dense but for a table's row stride."""
+    if t.dtype is not _torch().int32 or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name} must be int32 {list(shape)}")
+    if t.numel() and t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _elsewhere(dev, stream):
+    """A context in which `dev` and `stream` are the current ones, or None where they are: what a call allocates then
+    belongs to the stream that uses it."""
+    torch = _torch()
+    if dev.type != "cuda":
+        raise ValueError("tensors must be on the GPU")
+    if stream is None:
+        return None if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+    if stream.device != dev:
+        raise ValueError("the stream is another device's")
+    return torch.cuda.stream(stream)
+
+
+def _raw_stream(dev):
+    return _torch().cuda.current_stream(dev).cuda_stream
+
+
+class PagedCache:
+    """A pool of K and V pages (rkv_pages): k_pages, v_pages bf16 or fp16 [n_pages, Hkv, page_size, 128], any strides that are
+    multiples of 8 with the last dimension dense.  Make one and keep it: its calls then marshal no pool again.  The decode
+    caches of `decode_step` ([B, Hkv, C, 128]) are pools of one page per sequence."""
+
+    def __init__(self, k_pages, v_pages):
+        torch = _torch()
+        if k_pages.dim() != 4 or k_pages.shape != v_pages.shape:
+            raise ValueError("k_pages and v_pages must have shape [n_pages, Hkv, page_size, d]")
+        if k_pages.dtype != v_pages.dtype or k_pages.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("pages must be bf16 or fp16")
+        if k_pages.stride(3) != 1 or v_pages.stride(3) != 1:
+            raise ValueError("pages must be dense in their last dimension")
+        _same_device(k_pages.device, v_pages)
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.device, self.dtype = k_pages.device, k_pages.dtype
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k_pages.shape
+        self._c = _abi.Pages(k_pages.data_ptr(), v_pages.data_ptr(), *k_pages.stride()[:3], *v_pages.stride()[:3], self.n_pages,
+                             self.page_size, self.n_kv_heads, self.head_dim, _abi.BF16 if self.dtype == torch.bfloat16 else _abi.F16)
+        self._ref = C.byref(self._c)
+
+
+def pages_init(n_seqs: int, max_pages: int, n_pages: int, page_size: int, device="cuda"):
+    """The tables of empty sequences and a full ring of free pages: {"table" int32 [n_seqs, max_pages], "lens" int32 [n_seqs],
+    "ring" int32 [n_pages], "cursor" int32 [2] (front of the ring, free pages), "page_size"}."""
+    torch = _torch()
+    return {"table": torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device),
+            "lens": torch.zeros(n_seqs, dtype=torch.int32, device=device),
+            "ring": torch.arange(n_pages, dtype=torch.int32, device=device),
+            "cursor": torch.tensor([0, n_pages], dtype=torch.int32, device=device), "page_size": int(page_size)}
+
+
+def pages_resize(pages, new_lens, max_new: int, *, in_place=True, stream=None):
+    """Block tables and slot map from request lengths (rkv_pages_resize): sequence s of `pages` (pages_init) gets new_lens[s]
+    slots; pages are taken from the ring's front and given back to its end.  Returns {"slots" int32 [max_new] of the new
+    tokens, -1 behind the last, "cu_new" int32 [n_seqs + 1], "status" int32 [1] (0, or PAGES_EXHAUSTED / PAGES_INVALID: nothing
+    changed), "lens", "cursor"}.  in_place: lens and cursor of `pages` become the new ones; else they stay, and the new ones
+    are only returned (the table's entries past the old lengths and the ring's behind the free ones are written all the same)."""
+    torch = _torch()
+    table, lens, ring, cursor = pages["table"], pages["lens"], pages["ring"], pages["cursor"]
+    dev = table.device
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return pages_resize(pages, new_lens, max_new, in_place=in_place)
+    n = lens.shape[0]
+    _same_device(dev, lens, ring, cursor, new_lens)
+    _int32("table", table, (n, None))
+    _int32("lens", lens, (n,))
+    _int32("new_lens", new_lens, (n,))
+    _int32("ring", ring, (None,))
+    _int32("cursor", cursor, (2,))
+    lens_out, cursor_out = (lens, cursor) if in_place else (torch.empty_like(lens), torch.empty_like(cursor))
+    slots = torch.empty(max_new, dtype=torch.int32, device=dev)
+    cu_new = torch.empty(n + 1, dtype=torch.int32, device=dev)
+    status = torch.empty(1, dtype=torch.int32, device=dev)
+    r = _abi.Resize(lens.data_ptr(), new_lens.data_ptr(), lens_out.data_ptr(), table.data_ptr(), table.stride(0), ring.data_ptr(),
+                    cursor.data_ptr(), cursor_out.data_ptr(), slots.data_ptr(), cu_new.data_ptr(), status.data_ptr(), n, table.shape[1],
+                    ring.shape[0], pages["page_size"], max_new)
+    check(_abi.lib().rkv_pages_resize(C.byref(r), _raw_stream(dev)))
+    return {"slots": slots, "cu_new": cu_new, "status": status, "lens": lens_out, "cursor": cursor_out}
+
+
+def pages_write(cache: PagedCache, k, v, slots, *, stream=None):
+    """Copies new rows to their slots (rkv_pages_write): k, v [T, Hkv, d], or [B, n, Hkv, d] with T = B n, of the pool's type and any
+    strides that are multiples of 8; slots int32 [T], distinct; rows with a slot outside the pool (-1) are skipped."""
+    dev = cache.device
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return pages_write(cache, k, v, slots)
+    if k.shape != v.shape or k.dim() not in (3, 4) or k.shape[-2:] != (cache.n_kv_heads, cache.head_dim):
+        raise ValueError("k and v must have shape [T, Hkv, d] or [B, n, Hkv, d]")
+    if k.dtype != cache.dtype or v.dtype != cache.dtype or k.stride(-1) != 1 or v.stride(-1) != 1:
+        raise ValueError("k and v must be of the pool's type and dense in their last dimension")
+    _same_device(dev, k, v, slots)
+    outer, n = (1, k.shape[0]) if k.dim() == 3 else k.shape[:2]
+    _int32("slots", slots, (outer * n,))
+    ks, vs = k.stride(), v.stride()
+    if k.dim() == 3:
+        ks, vs = (0, *ks), (0, *vs)
+    rows = _abi.Rows(k.data_ptr(), v.data_ptr(), *ks[:3], *vs[:3], slots.data_ptr(), outer, n)
+    check(_abi.lib().rkv_pages_write(cache._ref, C.byref(rows), _raw_stream(dev)))
+
+
+def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_kv=0, scale=None, causal=True, window=0, softcap=0.0,
+                 slopes=None, prefix_lens=None, first_keys=None, out=None, lse_out=None, return_lse=False, stream=None):
+    """Attention of new tokens over a paged cache (rkv_pages_attend).
+
+    q: [T, Hq, d] of the pool's type, any strides that are multiples of 8; table int32 [n_seqs, max_pages]; lens int32 [n_seqs],
+    the slots of each sequence with its new tokens' own among them; cu_q int32 [n_seqs + 1]: sequence s has rows cu_q[s] ..
+    cu_q[s + 1] - 1 (None: one row each).  max_q, max_kv: the most rows and slots of a sequence, if known: they choose the
+    kernel, never the result.  scale: 1 / sqrt(d) by default; window: slots a query sees, its own included (0: all);
+    softcap c: scores c tanh(x / c); slopes fp32 [Hq]: scores less slope times distance; prefix_lens int32 [n_seqs]: slots
+    every row of the sequence sees; first_keys int32 [T]: the first slot a row sees.  Returns out [T, Hq, d] (`out` if given: rows
+    behind the last sequence stay as they are; a row that sees nothing is 0), and with return_lse or lse_out also fp32
+    [T, Hq], the logarithm of the sum of exponentials (-inf for a row that sees nothing)."""
+    torch = _torch()
+    dev = cache.device
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return pages_attend(cache, q, table, lens, cu_q, max_q=max_q, max_kv=max_kv, scale=scale, causal=causal, window=window,
+                                softcap=softcap, slopes=slopes, prefix_lens=prefix_lens, first_keys=first_keys, out=out, lse_out=lse_out,
+                                return_lse=return_lse)
+    if q.dim() != 3 or q.shape[2] != cache.head_dim or q.dtype != cache.dtype or q.stride(2) != 1:
+        raise ValueError("q must have shape [T, Hq, d], the pool's type and a dense last dimension")
+    T, Hq, d = q.shape
+    n = lens.shape[0]
+    _same_device(dev, q, table, lens, cu_q, slopes, prefix_lens, first_keys, out, lse_out)
+    _int32("table", table, (n, None))
+    _int32("lens", lens, (n,))
+    for name, t, size in (("cu_q", cu_q, n + 1), ("prefix_lens", prefix_lens, n), ("first_keys", first_keys, T)):
+        if t is not None:
+            _int32(name, t, (size,))
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (Hq,) or not slopes.is_contiguous()):
+        raise ValueError("slopes must be contiguous fp32 [Hq]")
+    if out is None:
+        out = torch.empty((T, Hq, d), dtype=q.dtype, device=dev)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.stride(2) != 1:
+        raise ValueError("out must have q's shape and type and a dense last dimension")
+    if lse_out is None:
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev) if return_lse else None
+    elif lse_out.shape != (T, Hq) or lse_out.dtype != torch.float32 or not lse_out.is_contiguous():
+        raise ValueError("lse_out must be contiguous fp32 [T, Hq]")
+    else:
+        lse = lse_out
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    a = _abi.Attend(q.data_ptr(), out.data_ptr(), ptr(lse), q.stride(0), q.stride(1), out.stride(0), out.stride(1), table.data_ptr(),
+                    table.stride(0), lens.data_ptr(), ptr(cu_q), ptr(prefix_lens), ptr(first_keys), ptr(slopes), n, T, Hq, table.shape[1],
+                    max_q, max_kv, bool(causal), window, d ** -0.5 if scale is None else scale, softcap)
+    L = _abi.lib()
+    nbytes = C.c_size_t()
+    check(L.rkv_pages_attend_workspace_size(cache._ref, C.byref(a), C.byref(nbytes)))
+    ws = torch.empty(nbytes.value, dtype=torch.uint8, device=dev) if nbytes.value else None
+    check(L.rkv_pages_attend(cache._ref, C.byref(a), ptr(ws), nbytes.value, _raw_stream(dev)))
+    return out if lse is None else (out, lse)
+
+
+def pages_init_from_prefill(plan: Plan, prefill_out, *, page_size=16, extra=0, stream=None):
+    """Prefill -> paged caches: the compacted prompt cache of every layer of an evict_prefill result moves into pages, of which a
+    layer takes as many as its retained rows need, and `extra` more slots' worth per sequence stay free for new tokens.
+    Returns, per layer, (cache, pages): a PagedCache and its tables (pages_init) with lens at the layer's retained count."""
+    torch = _torch()
+    got = []
+    dev = prefill_out["k_out"][0].device
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return pages_init_from_prefill(plan, prefill_out, page_size=page_size, extra=extra)
+    for k, v in zip(prefill_out["k_out"], prefill_out["v_out"]):
+        B, Hkv, n, d = k.shape
+        per = -(-(n + extra) // page_size)
+        pages = pages_init(B, max(1, per), max(1, B * per), page_size, dev)
+        pool = torch.empty((2, max(1, B * per), Hkv, page_size, d), dtype=k.dtype, device=dev)
+        cache = PagedCache(pool[0], pool[1])
+        step = pages_resize(pages, torch.full((B,), n, dtype=torch.int32, device=dev), B * n)
+        pages_write(cache, k.permute(0, 2, 1, 3), v.permute(0, 2, 1, 3), step["slots"])
+        got.append((cache, pages))
+    return got

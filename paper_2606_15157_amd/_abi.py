@@ -16,12 +16,15 @@ PHASE_PREFILL, PHASE_DECODE = 0, 1
 SCOPE_PREFILL, SCOPE_DECODE, SCOPE_BOTH = 0, 1, 2
 T_IDENTITY, T_PPL_CAP = 0, 1
 STATUS_TIMEOUT, STATUS_INVALID, STATUS_REPAIRED = 1, 2, 4
+BF16, F16 = 0, 1
+PAGES_EXHAUSTED, PAGES_INVALID = 1, 2
 
 EXPORTED = [
     "rkv_allocate_budgets", "rkv_plan_create", "rkv_plan_destroy", "rkv_plan_num_layers",
     "rkv_plan_serialize", "rkv_plan_deserialize", "rkv_rule_phases", "rkv_plan_from_route",
     "rkv_plan_retained_counts", "rkv_prefill_workspace_size", "rkv_prefill_evict", "rkv_prefill_evict_noalloc", "rkv_prefill_check",
-    "rkv_decode_step", "rkv_decode_init_from_prefill", "rkv_entropy_workspace_size", "rkv_entropy_profile", "rkv_profile_enable", "rkv_profile_read", "rkv_last_error",
+    "rkv_decode_step", "rkv_decode_init_from_prefill", "rkv_entropy_workspace_size", "rkv_entropy_profile",
+    "rkv_pages_resize", "rkv_pages_write", "rkv_pages_attend_workspace_size", "rkv_pages_attend", "rkv_profile_enable", "rkv_profile_read", "rkv_last_error",
     "rkv_version",
 ]
 
@@ -62,6 +65,34 @@ class DecodeInput(C.Structure):
                 ("victim_out", C.POINTER(C.c_void_p))]
 
 
+def _fields(*groups):
+    return [(name, kind) for kind, names in groups for name in names.split()]
+
+
+class Pages(C.Structure):
+    _fields_ = _fields((C.c_void_p, "k v"), (C.c_int64, "k_page k_head k_slot v_page v_head v_slot"),
+                       (C.c_int32, "n_pages page_size n_kv_heads head_dim dtype"))
+
+
+class Resize(C.Structure):
+    _fields_ = _fields((C.c_void_p, "lens new_lens lens_out table"), (C.c_int64, "table_stride"),
+                       (C.c_void_p, "ring cursor cursor_out slots cu_new status"),
+                       (C.c_int32, "n_seqs max_pages n_pages page_size max_new"))
+
+
+class Rows(C.Structure):
+    _fields_ = _fields((C.c_void_p, "k v"), (C.c_int64, "k_outer k_token k_head v_outer v_token v_head"),
+                       (C.c_void_p, "slots"), (C.c_int32, "n_outer n_tokens"))
+
+
+class Attend(C.Structure):
+    _fields_ = _fields((C.c_void_p, "q out lse"), (C.c_int64, "q_token q_head out_token out_head"),
+                       (C.c_void_p, "table"), (C.c_int64, "table_stride"),
+                       (C.c_void_p, "lens cu_q prefix_lens first_keys slopes"),
+                       (C.c_int32, "n_seqs n_rows n_q_heads max_pages max_q max_kv causal window"),
+                       (C.c_float, "scale softcap"))
+
+
 _lib = None
 
 
@@ -97,6 +128,10 @@ def lib():
         L.rkv_entropy_profile.argtypes = [C.POINTER(Shape), C.c_int32, C.c_int32, C.POINTER(C.c_void_p),
                                           C.POINTER(C.c_void_p), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                           C.c_size_t, C.c_void_p]
+        L.rkv_pages_resize.argtypes = [C.POINTER(Resize), C.c_void_p]
+        L.rkv_pages_write.argtypes = [C.POINTER(Pages), C.POINTER(Rows), C.c_void_p]
+        L.rkv_pages_attend_workspace_size.argtypes = [C.POINTER(Pages), C.POINTER(Attend), C.POINTER(C.c_size_t)]
+        L.rkv_pages_attend.argtypes = [C.POINTER(Pages), C.POINTER(Attend), C.c_void_p, C.c_size_t, C.c_void_p]
         L.rkv_profile_enable.argtypes = [C.c_int32]
         L.rkv_profile_read.argtypes = [C.POINTER(C.c_int32), C.POINTER(C.c_double)]
         L.rkv_last_error.restype = C.c_char_p
@@ -107,6 +142,7 @@ def lib():
                      "rkv_prefill_workspace_size", "rkv_prefill_evict", "rkv_prefill_check", "rkv_decode_step",
                      "rkv_rule_phases", "rkv_plan_from_route", "rkv_decode_init_from_prefill", "rkv_prefill_evict_noalloc",
                      "rkv_entropy_workspace_size", "rkv_entropy_profile",
+                     "rkv_pages_resize", "rkv_pages_write", "rkv_pages_attend_workspace_size", "rkv_pages_attend",
                      "rkv_profile_enable", "rkv_profile_read", "rkv_version"):
             getattr(L, name).restype = C.c_int
         _lib = L

@@ -1,0 +1,130 @@
+// Host side of the paged caches: argument checks and launches of rkv_pages_resize, rkv_pages_write and
+// rkv_pages_attend.
+#include <hip/hip_runtime_api.h>
+
+#include <cmath>
+
+#include "rkv_internal.h"
+
+namespace {
+
+constexpr int64_t kIntEnd = int64_t(1) << 31;
+
+int launched(int err) {
+  if (err) return rkv::fail(RKV_ERR_HIP, std::string("kernel launch failed: ") + hipGetErrorString((hipError_t)err));
+  return RKV_OK;
+}
+
+// A 16-byte aligned pointer and strides (elements) of whole 16-byte pieces.
+int check_layout(const char* what, const void* ptr, std::initializer_list<int64_t> strides) {
+  for (int64_t s : strides)
+    if (s < 0) return rkv::fail(RKV_ERR_INVALID_ARG, std::string(what) + ": negative stride");
+  if ((uintptr_t)ptr % 16) return rkv::fail(RKV_ERR_UNSUPPORTED, std::string(what) + " must be 16-byte aligned");
+  for (int64_t s : strides)
+    if (s % 8) return rkv::fail(RKV_ERR_UNSUPPORTED, std::string(what) + ": strides must be multiples of 8 elements");
+  return RKV_OK;
+}
+
+int check_pages(const rkv_pages* p) {
+  if (!p) return rkv::fail(RKV_ERR_INVALID_ARG, "null pages");
+  if (!p->k || !p->v) return rkv::fail(RKV_ERR_INVALID_ARG, "null page pool");
+  if (p->n_pages < 1 || p->page_size < 1 || p->n_kv_heads < 1)
+    return rkv::fail(RKV_ERR_INVALID_ARG, "n_pages, page_size and n_kv_heads must be >= 1");
+  if (p->dtype != RKV_BF16 && p->dtype != RKV_F16) return rkv::fail(RKV_ERR_INVALID_ARG, "unknown dtype");
+  if (p->head_dim != rkv::kHeadDim) return rkv::fail(RKV_ERR_UNSUPPORTED, "head_dim must be 128");
+  if ((int64_t)p->n_pages * p->page_size >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "a pool holds fewer than 2^31 slots");
+  if (int st = check_layout("k pages", p->k, {p->k_page, p->k_head, p->k_slot})) return st;
+  return check_layout("v pages", p->v, {p->v_page, p->v_head, p->v_slot});
+}
+
+int check_attend(const rkv_pages* p, const rkv_attend* a) {
+  if (int st = check_pages(p)) return st;
+  if (!a) return rkv::fail(RKV_ERR_INVALID_ARG, "null attend");
+  if (a->n_seqs < 0 || a->n_rows < 0 || a->max_pages < 0 || a->max_q < 0 || a->max_kv < 0 || a->window < 0 || a->table_stride < 0)
+    return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
+  if (a->causal != 0 && a->causal != 1) return rkv::fail(RKV_ERR_INVALID_ARG, "causal must be 0 or 1");
+  if (!std::isfinite(a->scale) || !std::isfinite(a->softcap) || a->softcap < 0.f)
+    return rkv::fail(RKV_ERR_INVALID_ARG, "scale and softcap must be finite, softcap >= 0");
+  if (a->n_q_heads < 1 || a->n_q_heads % p->n_kv_heads)
+    return rkv::fail(RKV_ERR_SHAPE, "n_q_heads must be a positive multiple of n_kv_heads");
+  if (!a->cu_q && a->n_rows != a->n_seqs) return rkv::fail(RKV_ERR_SHAPE, "without cu_q every sequence has one row");
+  if (a->table_stride < a->max_pages) return rkv::fail(RKV_ERR_SHAPE, "table_stride is less than max_pages");
+  if ((int64_t)a->max_pages * p->page_size >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "a sequence holds fewer than 2^31 slots");
+  if ((int64_t)a->n_rows * a->n_q_heads >= kIntEnd / 2) return rkv::fail(RKV_ERR_UNSUPPORTED, "n_rows * n_q_heads must be below 2^30");
+  if (int st = check_layout("q", a->q, {a->q_token, a->q_head})) return st;
+  return check_layout("out", a->out, {a->out_token, a->out_head});
+}
+
+bool nothing_to_do(const rkv_attend* a) { return a->n_seqs == 0 || a->n_rows == 0; }
+
+rkv::AttendLaunch attend_launch(const rkv_pages* p, const rkv_attend* a) {
+  rkv::AttendLaunch L{};
+  L.p = *p;
+  L.a = *a;
+  L.group = a->n_q_heads / p->n_kv_heads;
+  L.by_page = rkv::fast_div(p->page_size);
+  L.by_group = rkv::fast_div(L.group);
+  return L;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rkv_pages_resize(const rkv_resize* r, void* stream) {
+  rkv::clear_error();
+  if (!r) return rkv::fail(RKV_ERR_INVALID_ARG, "null resize");
+  if (r->n_seqs < 0 || r->max_pages < 0 || r->max_new < 0 || r->table_stride < 0 || r->n_pages < 1 || r->page_size < 1)
+    return rkv::fail(RKV_ERR_INVALID_ARG, "negative size, or no pages");
+  if (!r->ring || !r->cursor || !r->cursor_out || !r->cu_new || !r->status || (r->max_new && !r->slots) ||
+      (r->n_seqs && (!r->lens || !r->new_lens || !r->lens_out)) || (r->n_seqs && r->max_pages && !r->table))
+    return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  if (r->n_seqs > rkv::kResizeMaxSeqs)
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "at most " + std::to_string(rkv::kResizeMaxSeqs) + " sequences");
+  if ((int64_t)r->n_pages * r->page_size >= kIntEnd || (int64_t)r->max_pages * r->page_size >= kIntEnd)
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "a pool and a sequence hold fewer than 2^31 slots");
+  if (r->table_stride < r->max_pages) return rkv::fail(RKV_ERR_SHAPE, "table_stride is less than max_pages");
+  return launched(rkv::launch_resize({*r, rkv::fast_div(r->page_size)}, stream));
+}
+
+int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream) {
+  rkv::clear_error();
+  if (int st = check_pages(pages)) return st;
+  if (!rows) return rkv::fail(RKV_ERR_INVALID_ARG, "null rows");
+  if (rows->n_outer < 0 || rows->n_tokens < 0) return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
+  if (rows->n_outer == 0 || rows->n_tokens == 0) return RKV_OK;
+  if (!rows->k || !rows->v || !rows->slots) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  if ((int64_t)rows->n_outer * rows->n_tokens >= kIntEnd / pages->n_kv_heads)
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "fewer than 2^31 rows a call");
+  if (int st = check_layout("k rows", rows->k, {rows->k_outer, rows->k_token, rows->k_head})) return st;
+  if (int st = check_layout("v rows", rows->v, {rows->v_outer, rows->v_token, rows->v_head})) return st;
+  rkv::WriteLaunch W{};
+  W.p = *pages;
+  W.r = *rows;
+  W.by_page = rkv::fast_div(pages->page_size);
+  W.by_head = rkv::fast_div(pages->n_kv_heads);
+  W.by_token = rkv::fast_div(rows->n_tokens);
+  W.n_items = rows->n_outer * rows->n_tokens * pages->n_kv_heads;
+  W.n_slots = pages->n_pages * pages->page_size;
+  return launched(rkv::launch_write(W, stream));
+}
+
+int rkv_pages_attend_workspace_size(const rkv_pages* pages, const rkv_attend* a, size_t* bytes) {
+  rkv::clear_error();
+  if (!bytes) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  if (int st = check_attend(pages, a)) return st;
+  *bytes = 0;
+  return RKV_OK;
+}
+
+int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size_t ws_bytes, void* stream) {
+  rkv::clear_error();
+  if (int st = check_attend(pages, a)) return st;
+  if (nothing_to_do(a)) return RKV_OK;
+  if (!a->q || !a->out || !a->lens || (a->max_pages && !a->table)) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  (void)ws;
+  (void)ws_bytes;
+  return launched(rkv::launch_attend(attend_launch(pages, a), stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,444 @@
+"""GPU parity of the paged caches (block tables and slot maps, rows to slots, attention over pages) against the float64
+oracle, and of a program that uses them together."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_15157_amd as rkv
+from oracle import pages as OG
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}     # half a step, relative
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def f64(t):
+    return t.detach().to("cpu", torch.float64).numpy()
+
+
+# ------------------------------------------------------------------ block tables and slot maps
+
+def run_resize(pages, new, max_new, **kw):
+    """One call against the oracle; returns what it returned."""
+    old = {k: pages[k].cpu().tolist() for k in ("table", "lens", "ring", "cursor")}
+    want = OG.resize(old["table"], old["lens"], old["ring"], old["cursor"], new, pages["page_size"], max_new)
+    got = rkv.pages_resize(pages, ints(new), max_new, **kw)
+    assert got["status"].tolist() == [want["status"]]
+    for k in ("slots", "cu_new", "lens", "cursor"):
+        assert got[k].tolist() == want[k], k
+    assert pages["table"].tolist() == want["table"]
+    assert pages["ring"].tolist() == want["ring"]
+    return got
+
+
+@pytest.mark.parametrize("n,page,most", [(1, 16, 100), (1, 1, 1), (7, 5, 33), (64, 16, 500), (65, 64, 3000), (200, 7, 900), (1025, 16, 60),
+                                         (8192, 16, 40)])
+def test_resize_follows_the_oracle_turn_by_turn(n, page, most):
+    """Requests grow, shrink, end and enter over several turns on one state."""
+    rng = np.random.default_rng(n * 31 + page)
+    width = -(-most // page)
+    pages = rkv.pages_init(n, width, n * width + 3, page)
+    lens = [0] * n
+    for turn in range(6):
+        new = [int(x) for x in rng.integers(0, most + 1, n)]
+        keep = rng.random(n) < 0.5
+        new = [min(most, a + 1) if k else b for a, b, k in zip(lens, new, keep)]
+        max_new = sum(max(0, b - a) for a, b in zip(lens, new)) + int(rng.integers(0, 9))
+        got = run_resize(pages, new, max_new)
+        if got["status"].item() == 0:
+            lens = new
+            rows = [pages["table"][s, :-(-x // page)].tolist() for s, x in enumerate(lens)]
+            held = [p for r in rows for p in r]
+            assert len(set(held)) == len(held)
+
+
+def test_resize_without_in_place_leaves_lengths_and_cursor():
+    pages = rkv.pages_init(3, 8, 20, 4)
+    run_resize(pages, [5, 9, 1], 15)
+    before = pages["lens"].tolist(), pages["cursor"].tolist()
+    got = run_resize(pages, [6, 0, 30], 30, in_place=False)
+    assert (pages["lens"].tolist(), pages["cursor"].tolist()) == before and got["lens"].tolist() == [6, 0, 30]
+
+
+@pytest.mark.parametrize("what", ["pages", "slots", "long", "negative", "head", "count", "old"])
+def test_resize_changes_nothing_when_it_cannot_serve_all(what):
+    pages = rkv.pages_init(4, 4, 9, 8)
+    run_resize(pages, [8, 3, 0, 17], 28)
+    new, max_new = [9, 3, 4, 17], 5
+    if what == "pages":
+        new, max_new = [32, 32, 32, 17], 100
+    elif what == "slots":
+        max_new = 4
+    elif what == "long":
+        new = [33, 3, 4, 17]
+    elif what == "negative":
+        new = [9, -1, 4, 17]
+    elif what == "head":
+        pages["cursor"][0] = 9
+    elif what == "count":
+        pages["cursor"][1] = -1
+    else:
+        pages["lens"][2] = 40
+    got = run_resize(pages, new, max_new)
+    assert got["status"].item() == (1 if what == "pages" else 2)
+    assert got["slots"].tolist() == [-1] * max_new
+
+
+def test_resize_of_many_new_tokens_and_a_ring_that_wraps():
+    """More slots than one workgroup fills, pages given back around the ring's end."""
+    pages = rkv.pages_init(40, 600, 40 * 40, 16)
+    rng = np.random.default_rng(5)
+    for turn in range(5):
+        new = [int(x) for x in rng.integers(0, 640, 40)]
+        run_resize(pages, new, 40 * 640)
+    new = [0] * 40
+    run_resize(pages, new, 0)
+    run_resize(pages, [9600, 9600] + [0] * 38, 20000)
+
+
+def test_resize_of_no_sequences():
+    pages = rkv.pages_init(0, 4, 9, 8)
+    got = rkv.pages_resize(pages, ints([]), 3)
+    assert got["slots"].tolist() == [-1] * 3 and got["cu_new"].tolist() == [0] and got["status"].item() == 0
+
+
+# ------------------------------------------------------------------ rows to slots
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,hkv,page,layout", [(1, 8, 16, "rows"), (7, 1, 1, "rows"), (300, 3, 7, "fused"), (130, 8, 100, "heads"),
+                                               (4099, 2, 64, "fused")])
+def test_write_puts_every_row_in_its_slot_and_touches_no_other(T, hkv, page, layout, dtype):
+    g = torch.Generator(device="cuda").manual_seed(T)
+    n_pages = -(-2 * T // page) + 2
+    pool = torch.randn((2, n_pages, hkv, page, 128), device="cuda", generator=g).to(dtype)
+    if layout == "heads":
+        k, v = (torch.randn((2, hkv, T // 2, 128), device="cuda", generator=g).to(dtype).permute(0, 2, 1, 3) for _ in range(2))
+    elif layout == "fused":
+        x = torch.randn((T, 2 * hkv + 4, 128), device="cuda", generator=g).to(dtype)
+        k, v = x[:, 4:4 + hkv], x[:, 4 + hkv:]
+    else:
+        k, v = (torch.randn((T, hkv, 128), device="cuda", generator=g).to(dtype) for _ in range(2))
+    slots = torch.randperm(n_pages * page, device="cuda", generator=g)[:T].to(torch.int32)
+    if T > 5:
+        slots[3], slots[T - 1], slots[4] = -1, n_pages * page, -7
+    want = pool.cpu().clone()
+    for x, src in ((want[0], k), (want[1], v)):
+        src = src.reshape(T, hkv, 128).cpu()
+        for t, s in enumerate(slots.tolist()):
+            if 0 <= s < n_pages * page:
+                x[s // page, :, s % page] = src[t]
+    rkv.pages_write(rkv.PagedCache(pool[0], pool[1]), k, v, slots)
+    assert torch.equal(pool.cpu().view(torch.int16), want.view(torch.int16))
+
+
+def test_write_and_attend_past_32_bit_offsets():
+    """A pool of more than 2^32 elements: the last page's rows."""
+    page, n_pages = 1024, (1 << 25) // 1024 + 2
+    pool = torch.empty((n_pages, 1, page, 128), dtype=torch.bfloat16, device="cuda")
+    k = torch.randn((70, 1, 128), device="cuda").to(torch.bfloat16)
+    slots = torch.arange(n_pages * page - 70, n_pages * page, dtype=torch.int32, device="cuda")
+    cache = rkv.PagedCache(pool, pool)
+    rkv.pages_write(cache, k, k, slots)
+    assert torch.equal(pool[-1, 0, -70:], k[:, 0])
+    q = torch.randn((1, 1, 128), device="cuda").to(torch.bfloat16)
+    out = rkv.pages_attend(cache, q, ints([[n_pages - 1]]), ints([page]), window=70)
+    small = rkv.PagedCache(k.view(1, 1, 70, 128), k.view(1, 1, 70, 128))
+    want = rkv.pages_attend(small, q, ints([[0]]), ints([70]))
+    assert (out - want).abs().max() <= 2 * 2.0 ** -8 * want.abs().max() + 2.0 ** -8 * k.abs().max()
+
+
+# ------------------------------------------------------------------ attention
+
+class Case:
+    """Pools whose every slot outside the sequences holds NaN, tables, and queries."""
+
+    def __init__(self, lens, hq=4, hkv=2, page=16, dtype=torch.bfloat16, seed=0, pad=0, spread=1.0, nhd=False):
+        rng = np.random.default_rng(seed)
+        self.lens, self.page, self.dtype = lens, page, dtype
+        counts = [-(-n // page) for _, n in lens]
+        n_pages = sum(counts) + 2
+        ids = rng.permutation(n_pages)
+        self.table = np.full((len(lens), max(counts + [1]) + 1), -1, dtype=np.int32)
+        shape = (n_pages, page, hkv, 128) if nhd else (n_pages, hkv, page, 128)
+        self.k, self.v = (torch.full(shape, NAN, dtype=dtype, device="cuda") for _ in range(2))
+        if nhd:
+            self.k, self.v = self.k.transpose(1, 2), self.v.transpose(1, 2)
+        at = 0
+        for s, (c, (_, n)) in enumerate(zip(counts, lens)):
+            self.table[s, :c] = ids[at:at + c]
+            at += c
+            for j in range(c):
+                m = min(page, n - j * page)
+                for x in (self.k, self.v):
+                    x[int(self.table[s, j]), :, :m] = torch.from_numpy(rng.standard_normal((hkv, m, 128)) * spread).to("cuda", dtype)
+        self.rows = sum(m for m, _ in lens)
+        self.q = torch.from_numpy(rng.standard_normal((self.rows + pad, hq, 128)) * spread).to("cuda", dtype)
+        self.cu = np.cumsum([0] + [m for m, _ in lens]).tolist()
+        self.cache = rkv.PagedCache(self.k, self.v)
+
+    def check(self, q=None, rows=None, **kw):
+        """The call against the oracle, every element within what the roundings may move it by."""
+        q = self.q if q is None else q
+        dev = {k: torch.tensor(np.asarray(x), device="cuda", dtype=torch.float32 if k == "slopes" else torch.int32)
+               for k, x in kw.items() if k in ("slopes", "prefix_lens", "first_keys") and x is not None}
+        same = {k: x for k, x in kw.items() if k not in dev}
+        lens = [n for _, n in self.lens]
+        out, lse = rkv.pages_attend(self.cache, q, ints(self.table.tolist()), ints(lens), ints(self.cu), return_lse=True, **{**same, **dev})
+        drop = {k: x for k, x in kw.items() if k not in ("max_q", "max_kv", "out", "lse_out")}
+        want, log, weight, reach = OG.attend(f64(self.k), f64(self.v), f64(q), self.table, lens, self.cu, **drop)
+        n = self.rows
+        compare(out[:n], lse[:n], want[:n], log[:n], weight[:n], reach[:n], self.dtype, kw.get("softcap", 0.0), kw.get("slopes"),
+                max([x for x in lens] + [1]))
+        return out, lse
+
+
+def compare(out, lse, want, log, weight, reach, dtype, softcap=0.0, slopes=None, most=1):
+    """A score is off by the fp32 sum of 128 products (each addition half a step of 2^-23 of what has been summed, at most
+    `reach`), its scaling, the cap (a few steps of the cap itself) and the bias (a step of slope times distance); the reference's
+    subtraction and the exponential add steps of the score's size and one of the result.  A probability's relative error is
+    that, plus half a step of its type where it is rounded for the product; the output's is half a step again."""
+    top = reach + (np.max(np.abs(slopes)) * most if slopes is not None else 0.0)
+    score = 2.0 ** -24 * (140 * reach + 8 * top + 16 * softcap + 8)
+    assert not torch.isnan(out).any() and not torch.isnan(lse).any()
+    got, empty = f64(lse), np.isneginf(log)
+    assert (np.isneginf(got) == empty).all()
+    # sums of up to 2^18 terms in 32 bits, in parts of at most a few thousand: below 2^-13 relative in all
+    off = np.where(empty, 0.0, got - np.where(empty, 0.0, log))
+    assert (np.abs(np.where(empty, 0.0, off)) <= score + 2.0 ** -13 * 0.01 + 2.0 ** -22 * np.abs(np.where(empty, 0.0, log))).all(), np.abs(off[~empty]).max()
+    u = HALF[dtype]
+    # a probability below the type's normal range keeps an absolute step only (fp16: 2^-25 of the largest one)
+    tiny = 2.0 ** -25 * most if dtype == torch.float16 else 0.0
+    bound = u * (weight + np.abs(want)) * 1.01 + (2 * score[..., None] + 2.0 ** -15) * weight + tiny
+    bad = np.abs(f64(out) - want) - bound
+    assert (bad <= 0).all(), (bad.max(), np.argwhere(bad > 0)[:4])
+
+
+ONE = [(1, 1), (1, 2), (1, 63), (1, 64), (1, 65), (1, 500), (1, 1025), (1, 16)]
+MANY = [(5, 5), (1, 130), (70, 200), (33, 33), (0, 40), (129, 300), (2, 2), (0, 0)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("page", [1, 7, 16, 48, 64, 100, 2000])
+def test_attention_over_any_page_size(page, dtype):
+    Case(ONE, page=page, dtype=dtype, seed=page).check(max_q=1)
+    Case(MANY, page=page, dtype=dtype, seed=page + 1).check()
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (6, 2), (10, 2), (8, 1), (16, 2), (24, 1), (40, 1), (33, 1)])
+def test_attention_over_head_layouts(hq, hkv):
+    Case(ONE, hq=hq, hkv=hkv, seed=hq).check()
+    Case([(1, 300), (3, 70), (40, 200), (0, 3)], hq=hq, hkv=hkv, seed=hq + 1).check()
+
+
+@pytest.mark.parametrize("lens", [ONE, MANY], ids=["one", "many"])
+@pytest.mark.parametrize("kw", [
+    dict(causal=False), dict(window=1), dict(window=64), dict(window=50), dict(softcap=2.0), dict(softcap=50.0), dict(scale=0.5),
+    dict(scale=-0.2), dict(prefix_lens=1000), dict(prefix_lens=37), dict(prefix_lens=37, window=20), dict(slopes=True),
+    dict(slopes=True, softcap=5.0, prefix_lens=64), dict(first_keys="half"), dict(first_keys="beyond"), dict(causal=False, window=33)],
+    ids=lambda d: "-".join(f"{k}{v}" for k, v in d.items()))
+def test_attention_masks_and_scores(lens, kw):
+    kw = dict(kw)
+    c = Case(lens, hq=6, hkv=2, page=16, seed=11)
+    if "slopes" in kw:
+        kw["slopes"] = np.array([2.0 ** -(i + 1) for i in range(6)], dtype=np.float32)
+    if "prefix_lens" in kw:
+        kw["prefix_lens"] = [kw["prefix_lens"]] * len(lens)
+    if "first_keys" in kw:
+        at = [n - m + i for m, n in lens for i in range(m)]
+        # half of them begin halfway, the others nowhere a row sees: its own slot's next
+        kw["first_keys"] = [p // 2 if kw["first_keys"] == "half" or t % 2 else p + 1 for t, p in enumerate(at)]
+    out, lse = c.check(**kw)
+    if kw.get("first_keys") and kw["first_keys"][0] > 0:
+        assert (out[0] == 0).all() and torch.isneginf(lse[0]).all()
+
+
+def test_queries_before_the_first_slot_see_nothing():
+    """More rows than slots: the first ones' positions are negative."""
+    out, lse = Case([(9, 4), (3, 0), (1, 20)], seed=2).check()
+    assert (out[:5] == 0).all() and torch.isneginf(lse[9:12]).all()
+
+
+@pytest.mark.parametrize("hints", [dict(), dict(max_q=1), dict(max_q=300, max_kv=400), dict(max_q=1, max_kv=1), dict(max_q=10 ** 6, max_kv=10 ** 6)])
+def test_bounds_change_no_result(hints):
+    """max_q and max_kv choose kernels only, wrong ones too."""
+    Case(MANY, seed=3).check(**hints)
+    Case([(1, 900), (1, 5), (1, 0)], seed=4, hq=8).check(**hints)
+
+
+def test_large_scores_and_sinks():
+    """Scores far apart: the running maximum moves late, early and by hundreds."""
+    Case([(1, 700), (40, 333)], seed=5, spread=4.0).check()
+    c = Case([(1, 4000), (20, 1000)], seed=6)
+    for s, j in ((0, 3900), (1, 3), (1, 970)):
+        c.k[int(c.table[s, j // 16]), :, j % 16] = 20 * c.q[0, ::2]
+    c.check()
+
+
+def test_long_sequences_in_few_rows():
+    Case([(1, 40000), (1, 17), (1, 9001)], hq=8, hkv=1, page=64, seed=7).check(max_q=1, max_kv=40000)
+    Case([(30, 20011)], hq=4, hkv=1, page=32, seed=8).check()
+
+
+@pytest.mark.parametrize("nhd", [False, True])
+def test_strided_tensors(nhd):
+    """Queries sliced from a fused projection, an output with gaps, pools of either order; rows behind the last sequence and gaps
+    stay as they were."""
+    c = Case([(3, 50), (1, 200), (20, 20)], hq=4, hkv=2, seed=9, pad=5, nhd=nhd)
+    wide = torch.randn((29, 9, 128), device="cuda").to(torch.bfloat16)
+    wide[:, 2:6] = c.q
+    held = torch.full((29, 7, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((29, 4), 7.0, device="cuda")
+    out, _ = c.check(q=wide[:, 2:6], out=held[:, 1:5, 128:], lse_out=lse)
+    assert (held[24:] == 7).all() and (lse[24:] == 7).all()
+    assert (held[:, 0] == 7).all() and (held[:, 5:] == 7).all() and (held[..., :128] == 7).all()
+
+
+def test_nan_and_infinity_where_no_row_looks():
+    """Slots before the window and behind the row's own hold NaN and infinities."""
+    c = Case([(1, 300), (1, 77)], seed=10)
+    want = c.check(window=40)[0]
+    for s, n in ((0, 300), (1, 77)):
+        for j in range(n - 40):
+            for x, bad in ((c.k, NAN), (c.v, math.inf if j % 2 else -math.inf)):
+                x[int(c.table[s, j // 16]), :, j % 16] = bad
+    got = rkv.pages_attend(c.cache, c.q, ints(c.table.tolist()), ints([300, 77]), window=40, max_q=1)
+    assert not torch.isnan(got).any() and torch.equal(got, want)
+
+
+def test_pages_outside_the_pool_read_as_zeros():
+    """Page ids that are no page: rows of zeros, and no fault; the other sequence's results are its own."""
+    c = Case([(2, 64), (2, 64)], seed=12)
+    c.table[0, 1], c.table[0, 2] = 1 << 30, -5
+    c.check()
+
+
+def test_sequences_that_share_pages():
+    c = Case([(1, 100), (4, 90)], seed=13)
+    c.table[1, :4] = c.table[0, :4]
+    c.check()
+
+
+def test_repeats_are_bit_equal_and_a_side_stream_serves():
+    c = Case([(1, 5000), (70, 900), (1, 1)], hq=8, seed=14)
+    args = (c.cache, c.q, ints(c.table.tolist()), ints([5000, 900, 1]), ints(c.cu))
+    want = rkv.pages_attend(*args)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [rkv.pages_attend(*args, stream=side) for _ in range(3)]
+    side.synchronize()
+    for x in got:
+        assert torch.equal(x, want)
+
+
+# ------------------------------------------------------------------ together
+
+def test_evicted_prompt_moves_into_pages_and_is_attended():
+    """evict_prefill, its caches into pages, new tokens written and attended, layer by layer with their own capacities."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    B, hkv, hq, L = 2, 2, 8, 400
+    rules, budgets = [rkv.SNAPKV, rkv.STREAMING, rkv.H2O, rkv.FULL], [77, 40, 130, 0]
+    plan = rkv.Plan(rules, budgets, window=32)
+    rand = lambda *s: torch.randn(s, device="cuda", generator=g).to(torch.bfloat16)  # noqa: E731
+    k, v, q = ([rand(B, h, n, 128) for _ in rules] for h, n in ((hkv, L), (hkv, L), (hq, 32)))
+    out = rkv.evict_prefill(plan, q, k, v, check_status=True)
+    layers = rkv.pages_init_from_prefill(plan, out, page_size=16, extra=3)
+    for l, (cache, pages) in enumerate(layers):
+        n = plan.retained_counts(L)[l]
+        assert pages["lens"].tolist() == [n] * B
+        new_k, new_v, new_q = rand(B * 3, hkv, 128), rand(B * 3, hkv, 128), rand(B * 3, hq, 128)
+        step = rkv.pages_resize(pages, pages["lens"] + 3, B * 3)
+        rkv.pages_write(cache, new_k, new_v, step["slots"])
+        got, lse = rkv.pages_attend(cache, new_q, pages["table"], pages["lens"], step["cu_new"], return_lse=True)
+        rows_k, rows_v = (torch.cat([out[x][l], new.view(B, 3, hkv, 128).transpose(1, 2)], 2) for x, new in (("k_out", new_k), ("v_out", new_v)))
+        want = OG.attend(f64(rows_k), f64(rows_v), f64(new_q), [[0], [1]], [n + 3] * B, [0, 3, 6])
+        compare(got, lse, *want, torch.bfloat16, most=n + 3)
+
+
+def test_decode_caches_are_read_in_place():
+    """The caches of decode_step as pools of one page a sequence."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    B, hkv, hq, L = 3, 2, 4, 300
+    plan = rkv.Plan([rkv.TOVA], [50], [rkv.TOVA], [50], window=32)
+    rand = lambda *s: torch.randn(s, device="cuda", generator=g).to(torch.bfloat16)  # noqa: E731
+    out = rkv.evict_prefill(plan, [rand(B, hq, 32, 128)], [rand(B, hkv, L, 128)], [rand(B, hkv, L, 128)], check_status=True)
+    state = rkv.decode_init_from_prefill(plan, out)
+    cache = rkv.PagedCache(state["k_cache"][0], state["v_cache"][0])
+    table, lens = torch.arange(B, dtype=torch.int32, device="cuda").view(B, 1), ints([50] * B)
+    for t in range(3):
+        q = rand(B, hq, 128)
+        rkv.decode_step(plan, state, [q], [rand(B, hkv, 128)], [rand(B, hkv, 128)], L + t)
+        got, lse = rkv.pages_attend(cache, q, table, lens, return_lse=True)
+        want = OG.attend(f64(state["k_cache"][0]), f64(state["v_cache"][0]), f64(q), table.tolist(), [50] * B)
+        compare(got, lse, *want, torch.bfloat16, most=50)
+
+
+def test_a_captured_step_replays():
+    """One decode step (tables, rows, attention) in a graph, replayed with eager work between, against the oracle."""
+    n, hkv, hq, page = 5, 2, 8, 4
+    pages = rkv.pages_init(n, 20, 100, page)
+    pool = torch.full((2, 100, hkv, page, 128), NAN, dtype=torch.bfloat16, device="cuda")
+    cache = rkv.PagedCache(pool[0], pool[1])
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *s: torch.randn(s, device="cuda", generator=g).to(torch.bfloat16)  # noqa: E731
+    start = [1, 0, 7, 30, 4]
+    step = rkv.pages_resize(pages, ints(start), 42)
+    seen = [rand(42, hkv, 128), rand(42, hkv, 128)]
+    rkv.pages_write(cache, *seen, step["slots"])
+    hist = [[[x[i] for i in range(sum(start[:s]), sum(start[:s + 1]))] for s in range(n)] for x in seen]
+    q, k, v = rand(n, hq, 128), rand(n, hkv, 128), rand(n, hkv, 128)
+    new_lens = torch.empty_like(pages["lens"])
+
+    def tick():
+        torch.add(pages["lens"], 1, out=new_lens)
+        step = rkv.pages_resize(pages, new_lens, n)
+        rkv.pages_write(cache, k, v, step["slots"])
+        return rkv.pages_attend(cache, q, pages["table"], pages["lens"], step["cu_new"], max_q=1, return_lse=True)
+
+    saved = {x: pages[x].clone() for x in ("table", "lens", "ring", "cursor")}
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = tick()
+    for x, t in saved.items():
+        pages[x].copy_(t)
+    for turn in range(6):
+        q.copy_(rand(n, hq, 128)), k.copy_(rand(n, hkv, 128)), v.copy_(rand(n, hkv, 128))
+        for x, src in zip(hist, (k, v)):
+            for s in range(n):
+                x[s].append(src[s].clone())
+        if turn % 2:
+            tick_out, tick_lse = tick()      # the program's own eager step
+        else:
+            graph.replay()
+            tick_out, tick_lse = out, lse
+        torch.cuda.synchronize()
+        lens = [a + turn + 1 for a in start]
+        assert pages["lens"].tolist() == lens
+        dense = [np.zeros((n, hkv, max(lens), 128)) for _ in range(2)]
+        for d, x in zip(dense, hist):
+            for s in range(n):
+                d[s, :, :lens[s]] = f64(torch.stack(x[s])).transpose(1, 0, 2)
+        want = OG.attend(*dense, f64(q), [[s] for s in range(n)], lens)
+        compare(tick_out, tick_lse, *want, torch.bfloat16, most=max(lens))
+
+
+def test_refusals_reach_python():
+    c = Case([(1, 4)], seed=15)
+    table, lens = ints(c.table.tolist()), ints([4])
+    with pytest.raises(rkv.RkvError):       # six heads over two is fine, three is not
+        rkv.pages_attend(c.cache, torch.zeros((1, 3, 128), dtype=torch.bfloat16, device="cuda"), table, lens)
+    odd = torch.zeros(1 * 4 * 128 + 4, dtype=torch.bfloat16, device="cuda")[4:].view(1, 4, 128)
+    with pytest.raises(rkv.RkvError):
+        rkv.pages_attend(c.cache, odd, table, lens)
+    for bad in (dict(lens=lens.long()), dict(table=table.t()), dict(cu_q=ints([0])), dict(first_keys=ints([0, 0])),
+                dict(slopes=torch.zeros(4, device="cuda", dtype=torch.float64)), dict(out=c.q[:, :2])):
+        kw = {"table": table, "lens": lens, **bad}
+        with pytest.raises(ValueError):
+            rkv.pages_attend(c.cache, c.q, kw.pop("table"), kw.pop("lens"), **kw)
