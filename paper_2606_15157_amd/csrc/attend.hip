@@ -12,6 +12,11 @@
 //
 // One pass with a running maximum m (log2 units), sum l and output O^T per row, rescaled only when a maximum outgrows the
 // reference by more than 8 (factors of exp2(8) at most in P, which has the exponent range for it).
+//
+// Many row tiles (prompts) are a workgroup each.  Up to kListed of them (decode steps, chunks) are dealt out by key tiles:
+// every workgroup adds up the same list of tiles' costs from cu_q and lens, which the host does not know, and takes an equal,
+// consecutive share, however ragged the batch.  A share's first and last rows may be part of an item: those partial sums go to
+// the workspace, and join_kernel adds them in the order of the keys.  Nothing depends on what an earlier call left there.
 #include <hip/hip_runtime.h>
 
 #include "lds_dma.h"
@@ -24,14 +29,18 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kRows = 128;                 // rows of a workgroup, 32 a wave
+constexpr int kRows = kAttendRows;         // rows of a workgroup, 32 a wave
 constexpr int kKeys = 64;                  // keys of a streamed tile
+constexpr int kShares = kAttendShares;
+constexpr int kListed = kAttendListed;
+constexpr int kLeast = 1;                  // key tiles of a share, at least
 constexpr int kTileBytes = kKeys * kHeadDim * 2;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGrow = 8.f;               // log2 units a maximum may outgrow the reference by
@@ -56,6 +65,8 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t at) { return *(const __attr
 __device__ __forceinline__ u32x2 lds_read_tr(uint32_t at) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at));
 }
+// log sum exp of a row from its running maximum (log2 units) and sum.
+__device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -__builtin_inff() : m / kLog2e + logf(l); }
 // All of this wave's DMA is in and its LDS reads are done, then the workgroup's.
 __device__ __forceinline__ void tile_sync() {
   wait_vmcnt<0>();
@@ -97,21 +108,39 @@ __device__ __forceinline__ int tile_sequence(const AttendLaunch& A, int tile) {
   return lo;
 }
 
-// kExtra: capped scores or a bias by distance.
+// The key tiles [t0, t1) that rows r0 .. r0 + 127 of a sequence of n_q tokens and n_kv slots may see (first_keys aside).
+__device__ __forceinline__ void tile_span(const AttendLaunch& A, int seq, int r0, int n_q, int n_kv, int& t0, int& t1) {
+  const rkv_attend& a = A.a;
+  const int first = n_kv - n_q + div_by(r0, A.by_group), last = n_kv - n_q + min(n_q - 1, div_by(r0 + kRows - 1, A.by_group));
+  int hi = n_kv;
+  if (a.causal) hi = min(n_kv, max(last + 1, a.prefix_lens ? a.prefix_lens[seq] : 0));
+  const int lo = a.window ? max(0, first - a.window + 1) : 0;
+  t0 = lo / kKeys;
+  t1 = max(t0, (hi + kKeys - 1) / kKeys);
+}
+__device__ __forceinline__ int slots_of(const AttendLaunch& A, int seq) {
+  return min(max(A.a.lens[seq], 0), A.a.max_pages * A.p.page_size);
+}
+__device__ __forceinline__ int end_row(const rkv_attend& a, int seq) { return a.cu_q ? first_row(a, seq + 1) : min(seq + 1, a.n_rows); }
+
+// A partial sum in the workspace: slot_rows rows of 128 floats (not divided by l), then their m and l.
+__device__ __forceinline__ float* part_slot(const AttendLaunch& A, int slot) {
+  return A.parts + (size_t)slot * A.slot_rows * (kHeadDim + 2);
+}
+
+struct Bounds {
+  int lo[4], hi[4];
+};
+
+// Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
+// partial sums go, null: the rows are finished.
 template <bool kF16, bool kExtra>
-__global__ __launch_bounds__(256, 2) void attend_kernel(const AttendLaunch A) {
-  __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];   // [buffer][K, V]
-  __shared__ int sLo[4], sHi[4];
+__device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
+                                            int r0, int h, int u0, int n, float* part) {
   const rkv_attend& a = A.a;
   const rkv_pages& p = A.p;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int h = blockIdx.x % p.n_kv_heads;
-  const int tile = A.n_tiles - 1 - blockIdx.x / p.n_kv_heads;   // a causal prompt's longest rows first
-  const int seq = __builtin_amdgcn_readfirstlane(tile_sequence(A, tile));
-  const int row0 = first_row(a, seq), n_q = (a.cu_q ? first_row(a, seq + 1) : min(seq + 1, a.n_rows)) - row0;
-  const int r0 = (tile - tile_start(A, seq)) * kRows, n_rows = n_q * A.group;
-  if (r0 < 0 || r0 >= n_rows) return;
-  const int n_kv = min(max(a.lens[seq], 0), a.max_pages * p.page_size);
+  const int n_rows = n_q * A.group, n_kv = slots_of(A, seq);
 
   // this lane's row (rows behind the last repeat it) and the slots it sees
   const int r = min(r0 + 32 * wv + col, n_rows - 1);
@@ -126,20 +155,28 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendLaunch A) {
     lo = 0x7fffffff;
     hi = 0;
   }
-  const int w_lo = wave_min(lo), w_hi = wave_max(hi);      // slots some row of the wave sees
-  const int all_lo = wave_max(lo), all_hi = wave_min(hi);  // and that every row sees
-  if (lane == 0) {
-    sLo[wv] = w_lo;
-    sHi[wv] = w_hi;
-  }
-  __syncthreads();
-  const int b_lo = min(min(sLo[0], sLo[1]), min(sLo[2], sLo[3])), b_hi = max(max(sHi[0], sHi[1]), max(sHi[2], sHi[3]));
-  const int t0 = b_hi > b_lo ? b_lo / kKeys : 0, t1 = b_hi > b_lo ? (b_hi + kKeys - 1) / kKeys : 0;
-
   u32x4 q[8];
   const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + row * a.q_token + hq * a.q_head;
 #pragma unroll
   for (int s = 0; s < 8; ++s) q[s] = *reinterpret_cast<const u32x4*>(qrow + 16 * s + 8 * half);
+
+  const int w_lo = wave_min(lo), w_hi = wave_max(hi);      // slots some row of the wave sees
+  const int all_lo = wave_max(lo), all_hi = wave_min(hi);  // and that every row sees
+  if (lane == 0) {
+    bounds.lo[wv] = w_lo;
+    bounds.hi[wv] = w_hi;
+  }
+  __syncthreads();
+  const int b_lo = min(min(bounds.lo[0], bounds.lo[1]), min(bounds.lo[2], bounds.lo[3]));
+  const int b_hi = max(max(bounds.hi[0], bounds.hi[1]), max(bounds.hi[2], bounds.hi[3]));
+  int t0, t1;
+  tile_span(A, seq, r0, n_q, n_kv, t0, t1);
+  if (n >= 0) {
+    t0 += u0;
+    t1 = min(t1, t0 + n);
+  }
+  t0 = max(t0, b_lo / kKeys);
+  t1 = min(t1, (b_hi + kKeys - 1) / kKeys);
 
   // The four rows this lane fetches of a tile: 16 wv + 4 j + lane / 16, 16 bytes of each.  K rows lie in LDS with chunk c at
   // c ^ (row % 16), V rows with c at c ^ 4 (row % 4): the reads below then touch every bank alike.
@@ -194,7 +231,7 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendLaunch A) {
       if (tl + 2 < t1) find(tl + 2);
     }
     const int key0 = tl * kKeys;
-    if (key0 + kKeys <= w_lo || key0 >= w_hi) continue;   // the other waves' rows see it
+    if (key0 + kKeys <= w_lo || key0 >= w_hi || r0 + 32 * wv >= n_rows) continue;   // only other waves' rows see it
     const uint32_t kb = lds + buf * 2 * kTileBytes, vb = kb + kTileBytes;
     f32x16 s[2];
 #pragma unroll
@@ -265,8 +302,24 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendLaunch A) {
     }
   }
 
+  __syncthreads();   // bounds and tiles are free for the next rows
+
   l += __shfl_xor(l, 32);
-  if (r0 + 32 * wv + col >= n_rows) return;
+  const int mine = 32 * wv + col;
+  if (r0 + mine >= n_rows) return;
+  if (part) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(part + mine * kHeadDim + 32 * d + 8 * i + 4 * half) =
+            f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+    if (half == 0) {
+      part[A.slot_rows * kHeadDim + mine] = m;
+      part[A.slot_rows * (kHeadDim + 1) + mine] = l;
+    }
+    return;
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head + 4 * half;
 #pragma unroll
@@ -275,21 +328,188 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendLaunch A) {
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<u32x2*>(out + 32 * d + 8 * i) =
           u32x2{pack<kF16>(o[d][4 * i] * inv, o[d][4 * i + 1] * inv), pack<kF16>(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
-  if (a.lse && half == 0) a.lse[row * a.n_q_heads + hq] = l == 0.f ? -__builtin_inff() : m / kLog2e + logf(l);
+  if (a.lse && half == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
+}
+
+// One workgroup per row tile and KV head.
+template <bool kF16, bool kExtra>
+__global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendLaunch A) {
+  __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];   // [buffer][K, V]
+  __shared__ Bounds bounds;
+  const int h = blockIdx.x % A.p.n_kv_heads;
+  const int tile = A.n_tiles - 1 - blockIdx.x / A.p.n_kv_heads;   // a causal prompt's longest rows first
+  const int seq = __builtin_amdgcn_readfirstlane(tile_sequence(A, tile));
+  const int row0 = first_row(A.a, seq), n_q = end_row(A.a, seq) - row0, r0 = (tile - tile_start(A, seq)) * kRows;
+  if (r0 < 0 || r0 >= n_q * A.group) return;
+  attend_rows<kF16, kExtra>(A, smem, bounds, seq, row0, n_q, r0, h, 0, -1, nullptr);
+}
+
+// kShares workgroups with an equal share each of all items' key tiles, in the order (head, row tile, key tile).  Workgroup b
+// runs on XCD b % 8: it takes share (b % 8) kShares / 8 + b / 8, so that the row tiles of a head, which read the same
+// keys, meet in one L2.
+template <bool kF16, bool kExtra>
+__global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunch A) {
+  __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];
+  __shared__ Bounds bounds;
+  __shared__ int64_t sBefore[kListed + 1];   // key tiles of a head before row tile i
+  __shared__ int64_t sWave[4];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  constexpr int kPer = kListed / 256;
+  int cost[kPer];
+  int64_t sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int tile = tid * kPer + i;
+    cost[i] = 0;
+    if (tile < A.n_tiles) {
+      int lo = 0, hi = A.a.n_seqs;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (tile_start(A, mid) <= tile) lo = mid;
+        else hi = mid;
+      }
+      const int n_q = end_row(A.a, lo) - first_row(A.a, lo), r0 = (tile - tile_start(A, lo)) * kRows;
+      if (r0 >= 0 && r0 < n_q * A.group) {
+        int t0, t1;
+        tile_span(A, lo, r0, n_q, slots_of(A, lo), t0, t1);
+        cost[i] = max(1, t1 - t0);   // rows that see nothing are written too
+      }
+    }
+    sum += cost[i];
+  }
+  int64_t x = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up((long long)x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) sWave[wv] = x;
+  __syncthreads();
+  int64_t before = x - sum;
+  for (int i = 0; i < wv; ++i) before += sWave[i];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    sBefore[tid * kPer + i] = before;
+    before += cost[i];
+  }
+  if (tid == 255) sBefore[kListed] = before;
+  __syncthreads();
+  const int64_t all = sBefore[kListed], total = all * A.p.n_kv_heads;
+  const int64_t share = max((int64_t)kLeast, (total + kShares - 1) / kShares);
+  const int w = (int)(blockIdx.x % 8) * (kShares / 8) + (int)blockIdx.x / 8;
+  int64_t pos = w * share;
+  const int64_t end = min(total, pos + share);
+  int record[8] = {};   // parts, sequence's first row, first row of the tile, rows of the sequence, head
+  while (pos < end) {
+    const int h = (int)(pos / all);
+    const int64_t rem = pos - h * all;
+    int lo = 0, hi = kListed;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (sBefore[mid] <= rem) lo = mid;
+      else hi = mid;
+    }
+    const int tile = __builtin_amdgcn_readfirstlane(lo);
+    const int u0 = (int)(rem - sBefore[tile]), count = (int)(sBefore[tile + 1] - sBefore[tile]);
+    const int n = (int)min((int64_t)(count - u0), end - pos);
+    const int seq = __builtin_amdgcn_readfirstlane(tile_sequence(A, tile));
+    const int row0 = first_row(A.a, seq), n_q = end_row(A.a, seq) - row0, r0 = (tile - tile_start(A, seq)) * kRows;
+    float* part = nullptr;
+    if (n < count) {
+      part = part_slot(A, 2 * w + (u0 == 0));
+      if (u0 == 0) {
+        record[0] = (int)((pos + count - 1) / share) - w + 1;
+        record[1] = row0;
+        record[2] = r0;
+        record[3] = n_q * A.group;
+        record[4] = h;
+      }
+    }
+    attend_rows<kF16, kExtra>(A, smem, bounds, seq, row0, n_q, r0, h, u0, n, part);
+    pos += n;
+  }
+  if (tid < 8) {
+    int v = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (tid == i) v = record[i];
+    A.records[8 * w + tid] = v;
+  }
+}
+
+// Workgroup (w, y): rows 32 y .. 32 y + 31 of the item that begins in share w and ends in a later one.  32 lanes hold the 128
+// values of a row; with fewer than 32 rows, several such groups take a row's parts in turn and meet in LDS.
+constexpr int kJoinThreads = 1024;
+template <bool kF16>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A) {
+  __shared__ f32x4 sO[32][32];
+  const int* record = A.records + 8 * blockIdx.x;
+  const int parts = record[0], y0 = 32 * blockIdx.y;
+  if (parts == 0) return;
+  const int row0 = record[1], r0 = record[2], h = record[4];
+  const int rows = min(32, min(kRows, record[3] - r0) - y0);
+  if (rows <= 0) return;
+  const rkv_attend& a = A.a;
+  const int grp = threadIdx.x >> 5, c = threadIdx.x & 31;
+  const int each = 32 / rows;                       // groups of a row
+  const int i = grp / each, g = grp - i * each;     // row, and place among its groups
+  const bool in = i < rows;
+  const int w = blockIdx.x, k = y0 + (in ? i : 0);
+  auto slot = [&](int j) { return part_slot(A, j ? 2 * (w + j) : 2 * w + 1); };
+  auto stat_m = [&](int j) { return slot(j)[A.slot_rows * kHeadDim + k]; };
+  auto stat_l = [&](int j) { return slot(j)[A.slot_rows * (kHeadDim + 1) + k]; };
+  float m = -__builtin_inff();
+  for (int j = c; j < parts; j += 32) m = fmaxf(m, stat_m(j));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const float ref = m == -__builtin_inff() ? 0.f : m;
+  float l = 0.f;
+  for (int j = c; j < parts; j += 32) l += stat_l(j) * __builtin_amdgcn_exp2f(stat_m(j) - ref);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor(l, o);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int j = g; j < parts; j += each) {
+    const float f = __builtin_amdgcn_exp2f(stat_m(j) - ref);
+    const f32x4 v = *reinterpret_cast<const f32x4*>(slot(j) + k * kHeadDim + 4 * c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, v[e], acc[e]);
+  }
+  if (each > 1) {
+    sO[grp][c] = acc;
+    __syncthreads();
+    if (!in || g) return;
+    for (int x = 1; x < each; ++x) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += sO[grp + x][c][e];
+    }
+  }
+  if (!in || g) return;
+  const int r = r0 + k, t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
+  const int64_t row = row0 + t;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head + 4 * c;
+  *reinterpret_cast<u32x2*>(out) = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
+  if (a.lse && c == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
 }
 
 template <bool kF16>
 void launch_type(const AttendLaunch& A, hipStream_t st) {
+  const bool extra = A.a.softcap > 0.f || A.a.slopes;
+  if (A.parts) {
+    if (extra) attend_shares_kernel<kF16, true><<<kShares, 256, 0, st>>>(A);
+    else attend_shares_kernel<kF16, false><<<kShares, 256, 0, st>>>(A);
+    join_kernel<kF16><<<dim3(kShares, (A.slot_rows + 31) / 32), kJoinThreads, 0, st>>>(A);
+    return;
+  }
   const unsigned grid = (unsigned)(A.n_tiles * A.p.n_kv_heads);
-  if (A.a.softcap > 0.f || A.a.slopes) attend_kernel<kF16, true><<<grid, 256, 0, st>>>(A);
-  else attend_kernel<kF16, false><<<grid, 256, 0, st>>>(A);
+  if (extra) attend_tiles_kernel<kF16, true><<<grid, 256, 0, st>>>(A);
+  else attend_tiles_kernel<kF16, false><<<grid, 256, 0, st>>>(A);
 }
 
 }  // namespace
 
-int launch_attend(const AttendLaunch& A0, void* stream) {
-  AttendLaunch A = A0;
-  A.n_tiles = (int)((int64_t)A.a.n_rows * A.group / kRows) + A.a.n_seqs;
+int launch_attend(const AttendLaunch& A, void* stream) {
   if (A.p.dtype == RKV_F16) launch_type<true>(A, reinterpret_cast<hipStream_t>(stream));
   else launch_type<false>(A, reinterpret_cast<hipStream_t>(stream));
   return (int)hipGetLastError();

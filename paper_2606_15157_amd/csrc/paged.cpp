@@ -2,7 +2,9 @@
 // rkv_pages_attend.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "rkv_internal.h"
 
@@ -37,6 +39,11 @@ int check_pages(const rkv_pages* p) {
   return check_layout("v pages", p->v, {p->v_page, p->v_head, p->v_slot});
 }
 
+// Row tiles, with one part-filled tile for each sequence.
+int64_t row_tiles(const rkv_pages* p, const rkv_attend* a) {
+  return (int64_t)a->n_rows * (a->n_q_heads / p->n_kv_heads) / rkv::kAttendRows + a->n_seqs;
+}
+
 int check_attend(const rkv_pages* p, const rkv_attend* a) {
   if (int st = check_pages(p)) return st;
   if (!a) return rkv::fail(RKV_ERR_INVALID_ARG, "null attend");
@@ -51,20 +58,26 @@ int check_attend(const rkv_pages* p, const rkv_attend* a) {
   if (a->table_stride < a->max_pages) return rkv::fail(RKV_ERR_SHAPE, "table_stride is less than max_pages");
   if ((int64_t)a->max_pages * p->page_size >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "a sequence holds fewer than 2^31 slots");
   if ((int64_t)a->n_rows * a->n_q_heads >= kIntEnd / 2) return rkv::fail(RKV_ERR_UNSUPPORTED, "n_rows * n_q_heads must be below 2^30");
+  if (row_tiles(p, a) * p->n_kv_heads >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "too many sequences");
   if (int st = check_layout("q", a->q, {a->q_token, a->q_head})) return st;
   return check_layout("out", a->out, {a->out_token, a->out_head});
 }
 
 bool nothing_to_do(const rkv_attend* a) { return a->n_seqs == 0 || a->n_rows == 0; }
 
-rkv::AttendLaunch attend_launch(const rkv_pages* p, const rkv_attend* a) {
-  rkv::AttendLaunch L{};
-  L.p = *p;
-  L.a = *a;
-  L.group = a->n_q_heads / p->n_kv_heads;
-  L.by_page = rkv::fast_div(p->page_size);
-  L.by_group = rkv::fast_div(L.group);
-  return L;
+constexpr size_t kRecordBytes = sizeof(int32_t) * 8 * rkv::kAttendShares;
+
+// Rows of the largest row tile.
+int32_t tile_rows(const rkv_pages* p, const rkv_attend* a) {
+  const int64_t most = (int64_t)(a->cu_q ? a->n_rows : 1) * (a->n_q_heads / p->n_kv_heads);
+  return (int32_t)std::min<int64_t>(most, rkv::kAttendRows);
+}
+
+bool shared_out(const rkv_pages* p, const rkv_attend* a) { return row_tiles(p, a) <= rkv::kAttendListed; }
+
+size_t attend_bytes(const rkv_pages* p, const rkv_attend* a) {
+  if (nothing_to_do(a) || !shared_out(p, a)) return 0;
+  return kRecordBytes + sizeof(float) * 2 * rkv::kAttendShares * (size_t)tile_rows(p, a) * (rkv::kHeadDim + 2);
 }
 
 }  // namespace
@@ -113,7 +126,7 @@ int rkv_pages_attend_workspace_size(const rkv_pages* pages, const rkv_attend* a,
   rkv::clear_error();
   if (!bytes) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
   if (int st = check_attend(pages, a)) return st;
-  *bytes = 0;
+  *bytes = attend_bytes(pages, a);
   return RKV_OK;
 }
 
@@ -122,9 +135,23 @@ int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size
   if (int st = check_attend(pages, a)) return st;
   if (nothing_to_do(a)) return RKV_OK;
   if (!a->q || !a->out || !a->lens || (a->max_pages && !a->table)) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
-  (void)ws;
-  (void)ws_bytes;
-  return launched(rkv::launch_attend(attend_launch(pages, a), stream));
+  const size_t need = attend_bytes(pages, a);
+  if (need && !ws) return rkv::fail(RKV_ERR_WORKSPACE, "workspace is null");
+  if (need && (uintptr_t)ws % 256) return rkv::fail(RKV_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (ws_bytes < need) return rkv::fail(RKV_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
+  rkv::AttendLaunch L{};
+  L.p = *pages;
+  L.a = *a;
+  L.group = a->n_q_heads / pages->n_kv_heads;
+  L.by_page = rkv::fast_div(pages->page_size);
+  L.by_group = rkv::fast_div(L.group);
+  L.n_tiles = (int32_t)row_tiles(pages, a);
+  L.slot_rows = tile_rows(pages, a);
+  if (need) {
+    L.records = static_cast<int32_t*>(ws);
+    L.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kRecordBytes);
+  }
+  return launched(rkv::launch_attend(L, stream));
 }
 
 }  // extern "C"

@@ -212,12 +212,18 @@ struct WriteLaunch {
 };
 int launch_write(const WriteLaunch& W, void* stream);
 
+constexpr int kAttendRows = 128;       // rows (tokens x query heads of a group) of a tile
+constexpr int kAttendShares = 512;     // workgroups that share the key tiles of a short list of row tiles: two a CU
+constexpr int kAttendListed = 1024;    // row tiles such a list may have
 struct AttendLaunch {
   rkv_pages p;
   rkv_attend a;
   FastDiv by_page, by_group;
   int32_t group;       // Hq / Hkv
   int32_t n_tiles;     // row tiles of all sequences, at most
+  int32_t slot_rows;   // rows of a partial sum
+  int32_t* records;    // [kAttendShares][8], then
+  float* parts;        // [2 kAttendShares] partial sums; null: a workgroup per row tile
 };
 int launch_attend(const AttendLaunch& A, void* stream);
 

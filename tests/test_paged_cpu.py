@@ -153,3 +153,14 @@ def test_binding_refuses_what_the_library_would_misread():
                          torch.ones(1, dtype=torch.int32))
     with pytest.raises(ValueError):
         rkv.pages_resize(rkv.pages_init(1, 2, 4, 16, device="cpu"), torch.ones(1, dtype=torch.int32), 4)
+
+
+def test_workspace_is_checked():
+    L, n = _abi.lib(), C.c_size_t()
+    assert L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(attend()), C.byref(n)) == 0
+    assert n.value > 0
+    refused(5, L.rkv_pages_attend(C.byref(pages()), C.byref(attend()), None, n.value, None))
+    refused(5, L.rkv_pages_attend(C.byref(pages()), C.byref(attend()), C.c_void_p(P + 16), n.value, None))
+    refused(5, L.rkv_pages_attend(C.byref(pages()), C.byref(attend()), C.c_void_p(P), n.value - 1, None))
+    assert L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(attend(n_rows=0)), C.byref(n)) == 0 and n.value == 0
+    refused(4, L.rkv_pages_attend(C.byref(pages()), C.byref(attend(n_seqs=1 << 30)), None, 0, None))
