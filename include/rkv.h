@@ -344,7 +344,7 @@ int rkv_entropy_profile(const rkv_shape* shape, int32_t n_layers, int32_t n_q, c
  * row (page, head, slot) lies at k + page k_page + head k_head + slot k_slot elements (v likewise), so pages of
  * [n_kv_heads, page_size, d] and of [page_size, n_kv_heads, d] and views into larger buffers serve alike, and the
  * caches of rkv_decode_step are pools whose page is a sequence's whole cache.  Strides are multiples of 8 and not
- * negative, pools 16-byte aligned, n_pages * page_size < 2^31.  Slot i of a sequence lies in page
+ * negative, slots less than 2^27 elements apart, pools 16-byte aligned, n_pages * page_size < 2^31.  Slot i of a sequence lies in page
  * table[s][i / page_size] at i % page_size; a flat slot number is page * page_size + i % page_size. */
 typedef enum { RKV_BF16 = 0, RKV_F16 = 1 } rkv_dtype;
 typedef struct {

@@ -19,6 +19,8 @@
 // the workspace, and join_kernel adds them in the order of the keys.  Nothing depends on what an earlier call left there.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "lds_dma.h"
 #include "rkv_internal.h"
 
@@ -132,9 +134,9 @@ struct Bounds {
   int lo[4], hi[4];
 };
 
-// Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
+// kExtra: capped scores or a bias by distance; kPage16: page_size % 16 = 0.  Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
 // partial sums go, null: the rows are finished.
-template <bool kF16, bool kExtra>
+template <bool kF16, bool kExtra, bool kPage16>
 __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
                                             int r0, int h, int u0, int n, float* part) {
   const rkv_attend& a = A.a;
@@ -159,6 +161,10 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + row * a.q_token + hq * a.q_head;
 #pragma unroll
   for (int s = 0; s < 8; ++s) q[s] = *reinterpret_cast<const u32x4*>(qrow + 16 * s + 8 * half);
+  if (a.scale < 0.f) {
+#pragma unroll
+    for (int s = 0; s < 8; ++s) q[s] ^= 0x80008000u;
+  }
 
   const int w_lo = wave_min(lo), w_hi = wave_max(hi);      // slots some row of the wave sees
   const int all_lo = wave_max(lo), all_hi = wave_min(hi);  // and that every row sees
@@ -179,83 +185,118 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   t1 = min(t1, (b_hi + kKeys - 1) / kKeys);
 
   // The four rows this lane fetches of a tile: 16 wv + 4 j + lane / 16, 16 bytes of each.  K rows lie in LDS with chunk c at
-  // c ^ (row % 16), V rows with c at c ^ 4 (row % 4): the reads below then touch every bank alike.
+  // c ^ (row % 16), V rows with c at c ^ 4 (row % 4): the reads below then touch every bank alike.  Pages of a multiple of
+  // 16 slots hold a wave's 16 rows in one: their addresses are a scalar base and offsets that never change (150 fewer vector
+  // instructions a tile than with a page for each row, of 480).
   const uint32_t lds = lds_addr(smem);
   const int32_t* table = a.table + seq * a.table_stride;
   const char* kp = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.k) + h * p.k_head);
   const char* vp = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.v) + h * p.v_head);
   const int fr = lane >> 4;
-  int page[4], at[4];
-  auto find = [&](int tl) __attribute__((always_inline)) {   // pages of tile tl; -1: not visible, or not in the pool
+  const uint32_t k_slot = (uint32_t)p.k_slot * 2, v_slot = (uint32_t)p.v_slot * 2;   // bytes; 15 of them stay below 2^32
+  uint32_t k_off[4], v_off[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int key = tl * kKeys + 16 * wv + 4 * j + fr;
-      const bool in = key >= b_lo && key < b_hi;
+  for (int j = 0; j < 4; ++j) {
+    k_off[j] = 16 * ((lane & 15) ^ (4 * j + fr));
+    v_off[j] = 16 * ((lane & 15) ^ (4 * fr));
+    if constexpr (kPage16) {
+      k_off[j] += (4 * j + fr) * k_slot;
+      v_off[j] += (4 * j + fr) * v_slot;
+    }
+  }
+  int page[kPage16 ? 1 : 4], at[kPage16 ? 1 : 4];
+  auto find = [&](int tl) __attribute__((always_inline)) {   // pages of tile tl; -1: not visible
+    if constexpr (kPage16) {
+      const int key = tl * kKeys + 16 * wv;
+      const bool in = key + 16 > b_lo && key < b_hi;
       const int c = div_by(in ? key : 0, A.by_page);
-      at[j] = key - c * p.page_size;
-      page[j] = in ? table[c] : -1;
+      at[0] = key - c * p.page_size;
+      page[0] = in ? table[c] : -1;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = tl * kKeys + 16 * wv + 4 * j + fr;
+        const bool in = key >= b_lo && key < b_hi;
+        const int c = div_by(in ? key : 0, A.by_page);
+        at[j] = key - c * p.page_size;
+        page[j] = in ? table[c] : -1;
+      }
     }
   };
-  auto fetch = [&](int buf) __attribute__((always_inline)) {
+  const char* zeros = reinterpret_cast<const char*>(zero_row);
+  auto fetch = [&](int tl, uint32_t to) __attribute__((always_inline)) {
+    to += wv * 4096;
+    if constexpr (kPage16) {
+      const int key = tl * kKeys + 16 * wv;
+      const uint32_t pg = __builtin_amdgcn_readfirstlane(page[0]), sl = __builtin_amdgcn_readfirstlane(at[0]);
+      const bool known = pg < (uint32_t)p.n_pages;
+      const char* k = kp + (uint64_t)pg * (2 * p.k_page) + (uint64_t)sl * k_slot;
+      const char* v = vp + (uint64_t)pg * (2 * p.v_page) + (uint64_t)sl * v_slot;
+      if (known && key >= b_lo && key + 16 <= b_hi) {
+        dma16s_four(k, k_off, to);
+        dma16s_four(v, v_off, to + kTileBytes);
+      } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bool in = (uint32_t)page[j] < (uint32_t)p.n_pages;
-      const uint32_t to = lds + buf * 2 * kTileBytes + (16 * wv + 4 * j) * 256;
-      const char* k = in ? kp + 2 * (page[j] * p.k_page + at[j] * p.k_slot) : reinterpret_cast<const char*>(zero_row);
-      const char* v = in ? vp + 2 * (page[j] * p.v_page + at[j] * p.v_slot) : reinterpret_cast<const char*>(zero_row);
-      dma16(k + 16 * ((lane & 15) ^ (4 * j + fr)), to);
-      dma16(v + 16 * ((lane & 15) ^ (4 * fr)), to + kTileBytes);
+        for (int j = 0; j < 4; ++j) {
+          const bool in = known && key + 4 * j + fr >= b_lo && key + 4 * j + fr < b_hi;
+          dma16(in ? k + k_off[j] : zeros + (k_off[j] & 240), to + 1024 * j);
+          dma16(in ? v + v_off[j] : zeros + (v_off[j] & 240), to + 1024 * j + kTileBytes);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool in = (uint32_t)page[j] < (uint32_t)p.n_pages;
+        const char* k = in ? kp + (uint64_t)(uint32_t)page[j] * (uint64_t)(2 * p.k_page) + (uint64_t)(uint32_t)at[j] * k_slot : zeros;
+        const char* v = in ? vp + (uint64_t)(uint32_t)page[j] * (uint64_t)(2 * p.v_page) + (uint64_t)(uint32_t)at[j] * v_slot : zeros;
+        dma16(k + k_off[j], to + 1024 * j);
+        dma16(v + v_off[j], to + 1024 * j + kTileBytes);
+      }
     }
   };
 
   f32x16 o[4] = {};
   float m = -__builtin_inff(), l = 0.f;
-  const float sl2 = a.scale * kLog2e;
+  const float sl2 = fabsf(a.scale) * kLog2e;      // a negative scale's sign is in q
   const float slope = kExtra && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
-  const float cap = a.softcap, in_cap = kExtra && cap > 0.f ? 2.f * a.scale / cap * kLog2e : 0.f;
-  const uint32_t k_lane = col * 256 + ((col & 15) ^ half) * 16;
-  // V^T: lane reads 4 columns of key 4 half + (lane % 16) / 4 (+ 8), chunk 4 dt + 2 ((lane / 16) % 2) + (lane % 4) / 2
+  const float cap2 = 2.f * kLog2e * a.softcap, in_cap = kExtra && a.softcap > 0.f ? 2.f * sl2 / a.softcap : 0.f;
+  uint32_t k_lane[8], v_lane[4];
+#pragma unroll
+  for (int st = 0; st < 8; ++st) k_lane[st] = lds + col * 256 + (((2 * st) ^ (col & 15) ^ half) * 16);
+  // V^T: lane reads 4 columns of key 4 half + (lane % 16) / 4 (+ 8), chunk 4 d + 2 ((lane / 16) % 2) + (lane % 4) / 2
   const int v_key = 4 * half + ((lane & 15) >> 2);
-  const uint32_t v_lane = v_key * 256 + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (4 * (v_key & 3))) * 16 + (lane & 1) * 8;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+    v_lane[d] = lds + v_key * 256 + ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (4 * (v_key & 3))) * 16 + (lane & 1) * 8;
 
-  if (t0 < t1) {
-    find(t0);
-    fetch(0);
-    if (t0 + 1 < t1) find(t0 + 1);
-  }
-  for (int tl = t0; tl < t1; ++tl) {
-    const int buf = (tl - t0) & 1;
-    tile_sync();
-    if (tl + 1 < t1) {
-      fetch(buf ^ 1);
-      if (tl + 2 < t1) find(tl + 2);
-    }
+  // key of s[u][i]: key0 + 32 u + 8 (i / 4) + 4 half + i % 4
+  auto tile = [&](int tl, auto buffer) __attribute__((always_inline)) {
+    constexpr uint32_t kb = decltype(buffer)::value * 2 * kTileBytes, vb = kb + kTileBytes;
     const int key0 = tl * kKeys;
-    if (key0 + kKeys <= w_lo || key0 >= w_hi || r0 + 32 * wv >= n_rows) continue;   // only other waves' rows see it
-    const uint32_t kb = lds + buf * 2 * kTileBytes, vb = kb + kTileBytes;
+    if (key0 + kKeys <= w_lo || key0 >= w_hi || r0 + 32 * wv >= n_rows) return;   // only other waves' rows see it
     f32x16 s[2];
+    {
+      u32x4 f[4];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      s[u] = f32x16{};
-#pragma unroll
-      for (int st = 0; st < 8; ++st) s[u] = mma32<kF16>(lds_read16(kb + u * 8192 + (k_lane ^ (32 * st))), q[st], s[u]);
-    }
-    // key of s[u][i]: key0 + 32 u + 8 (i / 4) + 4 half + i % 4
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
+      for (int i = 0; i < 3; ++i) f[i] = lds_read16(k_lane[i] + kb);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float x = s[u][i];
-        if constexpr (kExtra) {
-          // cap tanh(x / cap) = cap (1 - 2 / (1 + exp(2 x / cap)))
-          if (in_cap != 0.f) x = cap * kLog2e * (1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * in_cap)));
-          else x *= sl2;
-          x -= slope * fabsf((float)(pos - (key0 + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3))));
-        } else {
-          x *= sl2;
-        }
-        s[u][i] = x;
+        if (i + 3 < 16) f[(i + 3) & 3] = lds_read16(k_lane[(i + 3) & 7] + kb + ((i + 3) >> 3) * 8192);
+        s[i >> 3] = mma32<kF16>(f[i & 3], q[i & 7], (i & 7) == 0 ? f32x16{} : s[i >> 3]);
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    if constexpr (kExtra) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          // cap tanh(x / cap) = cap - 2 cap / (1 + exp(2 x / cap)), in log2 units
+          float x = in_cap != 0.f ? 0.5f * cap2 - cap2 * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[u][i] * in_cap)) : s[u][i] * sl2;
+          x -= slope * fabsf((float)(pos - (key0 + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3))));
+          s[u][i] = x;
+        }
+    }
     if (key0 < all_lo || key0 + kKeys > all_hi) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -271,6 +312,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
     top = max_halves(top);
+    if constexpr (!kExtra) top *= sl2;
     if (__any(top > m + kGrow)) {
       const float m2 = fmaxf(m, top), f = m2 > m ? __builtin_amdgcn_exp2f(m - m2) : 1.f;
       m = m2;
@@ -285,7 +327,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[u][i] = __builtin_amdgcn_exp2f(s[u][i] - ref);
+        s[u][i] = __builtin_amdgcn_exp2f(kExtra ? s[u][i] - ref : fmaf(s[u][i], sl2, -ref));
         l += s[u][i];
       }
 #pragma unroll
@@ -295,13 +337,30 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       for (int i = 0; i < 4; ++i) pr[i] = pack<kF16>(s[ks >> 1][8 * (ks & 1) + 2 * i], s[ks >> 1][8 * (ks & 1) + 2 * i + 1]);
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        const u32x2 v0 = lds_read_tr(vb + ks * 4096 + (v_lane ^ (64 * d)));
-        const u32x2 v1 = lds_read_tr(vb + ks * 4096 + 2048 + (v_lane ^ (64 * d)));
+        const u32x2 v0 = lds_read_tr(v_lane[d] + vb + ks * 4096);
+        const u32x2 v1 = lds_read_tr(v_lane[d] + vb + ks * 4096 + 2048);
         o[d] = mma32<kF16>(u32x4{v0[0], v0[1], v1[0], v1[1]}, pr, o[d]);
       }
     }
+  };
+  auto step = [&](int tl, auto buffer) __attribute__((always_inline)) {
+    tile_sync();
+    if (tl + 1 < t1) {
+      fetch(tl + 1, lds + (1 - decltype(buffer)::value) * 2 * kTileBytes);
+      if (tl + 2 < t1) find(tl + 2);
+    }
+    tile(tl, buffer);
+  };
+  if (t0 < t1) {
+    find(t0);
+    fetch(t0, lds);
+    if (t0 + 1 < t1) find(t0 + 1);
   }
-
+#pragma unroll 1
+  for (int tl = t0; tl < t1; tl += 2) {
+    step(tl, std::integral_constant<int, 0>{});
+    if (tl + 1 < t1) step(tl + 1, std::integral_constant<int, 1>{});
+  }
   __syncthreads();   // bounds and tiles are free for the next rows
 
   l += __shfl_xor(l, 32);
@@ -332,7 +391,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 }
 
 // One workgroup per row tile and KV head.
-template <bool kF16, bool kExtra>
+template <bool kF16, bool kExtra, bool kPage16>
 __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendLaunch A) {
   __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];   // [buffer][K, V]
   __shared__ Bounds bounds;
@@ -341,13 +400,13 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendLaunch
   const int seq = __builtin_amdgcn_readfirstlane(tile_sequence(A, tile));
   const int row0 = first_row(A.a, seq), n_q = end_row(A.a, seq) - row0, r0 = (tile - tile_start(A, seq)) * kRows;
   if (r0 < 0 || r0 >= n_q * A.group) return;
-  attend_rows<kF16, kExtra>(A, smem, bounds, seq, row0, n_q, r0, h, 0, -1, nullptr);
+  attend_rows<kF16, kExtra, kPage16>(A, smem, bounds, seq, row0, n_q, r0, h, 0, -1, nullptr);
 }
 
 // kShares workgroups with an equal share each of all items' key tiles, in the order (head, row tile, key tile).  Workgroup b
 // runs on XCD b % 8: it takes share (b % 8) kShares / 8 + b / 8, so that the row tiles of a head, which read the same
 // keys, meet in one L2.
-template <bool kF16, bool kExtra>
+template <bool kF16, bool kExtra, bool kPage16>
 __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunch A) {
   __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];
   __shared__ Bounds bounds;
@@ -425,7 +484,7 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
         record[4] = h;
       }
     }
-    attend_rows<kF16, kExtra>(A, smem, bounds, seq, row0, n_q, r0, h, u0, n, part);
+    attend_rows<kF16, kExtra, kPage16>(A, smem, bounds, seq, row0, n_q, r0, h, u0, n, part);
     pos += n;
   }
   if (tid < 8) {
@@ -493,18 +552,24 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A
   if (a.lse && c == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
 }
 
+template <bool kF16, bool kExtra, bool kPage16>
+void launch_kernels(const AttendLaunch& A, hipStream_t st) {
+  if (A.parts) {
+    attend_shares_kernel<kF16, kExtra, kPage16><<<kShares, 256, 0, st>>>(A);
+    join_kernel<kF16><<<dim3(kShares, (A.slot_rows + 31) / 32), kJoinThreads, 0, st>>>(A);
+  } else {
+    attend_tiles_kernel<kF16, kExtra, kPage16><<<(unsigned)(A.n_tiles * A.p.n_kv_heads), 256, 0, st>>>(A);
+  }
+}
+template <bool kF16, bool kExtra>
+void launch_pages(const AttendLaunch& A, hipStream_t st) {
+  if (A.p.page_size % 16 == 0) launch_kernels<kF16, kExtra, true>(A, st);
+  else launch_kernels<kF16, kExtra, false>(A, st);
+}
 template <bool kF16>
 void launch_type(const AttendLaunch& A, hipStream_t st) {
-  const bool extra = A.a.softcap > 0.f || A.a.slopes;
-  if (A.parts) {
-    if (extra) attend_shares_kernel<kF16, true><<<kShares, 256, 0, st>>>(A);
-    else attend_shares_kernel<kF16, false><<<kShares, 256, 0, st>>>(A);
-    join_kernel<kF16><<<dim3(kShares, (A.slot_rows + 31) / 32), kJoinThreads, 0, st>>>(A);
-    return;
-  }
-  const unsigned grid = (unsigned)(A.n_tiles * A.p.n_kv_heads);
-  if (extra) attend_tiles_kernel<kF16, true><<<grid, 256, 0, st>>>(A);
-  else attend_tiles_kernel<kF16, false><<<grid, 256, 0, st>>>(A);
+  if (A.a.softcap > 0.f || A.a.slopes) launch_pages<kF16, true>(A, st);
+  else launch_pages<kF16, false>(A, st);
 }
 
 }  // namespace

@@ -35,6 +35,8 @@ int check_pages(const rkv_pages* p) {
   if (p->dtype != RKV_BF16 && p->dtype != RKV_F16) return rkv::fail(RKV_ERR_INVALID_ARG, "unknown dtype");
   if (p->head_dim != rkv::kHeadDim) return rkv::fail(RKV_ERR_UNSUPPORTED, "head_dim must be 128");
   if ((int64_t)p->n_pages * p->page_size >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "a pool holds fewer than 2^31 slots");
+  if (p->k_slot >= kIntEnd / 16 || p->v_slot >= kIntEnd / 16)
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "slots are fewer than 2^27 elements apart");
   if (int st = check_layout("k pages", p->k, {p->k_page, p->k_head, p->k_slot})) return st;
   return check_layout("v pages", p->v, {p->v_page, p->v_head, p->v_slot});
 }

@@ -59,7 +59,7 @@ def refused(status, call, *words):
 BAD_PAGES = [
     (1, dict(k=None)), (1, dict(v=None)), (1, dict(n_pages=0)), (1, dict(page_size=0)), (1, dict(n_kv_heads=0)), (1, dict(dtype=2)),
     (1, dict(dtype=-1)), (1, dict(k_slot=-8)), (4, dict(head_dim=64)), (4, dict(k=P + 8)), (4, dict(v=P + 2)), (4, dict(k_head=132)),
-    (4, dict(v_page=4)), (4, dict(n_pages=1 << 20, page_size=1 << 11))]
+    (4, dict(v_page=4)), (4, dict(k_slot=1 << 27)), (4, dict(v_slot=1 << 40)), (4, dict(n_pages=1 << 20, page_size=1 << 11))]
 
 
 def rows(**kw):
