@@ -44,6 +44,7 @@ constexpr int kShares = kAttendShares;
 constexpr int kListed = kAttendListed;
 constexpr int kLeast = 1;                  // key tiles of a share, at least
 constexpr int kTileBytes = kKeys * kHeadDim * 2;
+constexpr int kNone = 0x7fffffff;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGrow = 8.f;               // log2 units a maximum may outgrow the reference by
 
@@ -77,16 +78,20 @@ __device__ __forceinline__ void tile_sync() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
-__device__ __forceinline__ float max_halves(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
+__device__ __forceinline__ float max_halves(float x) {
+  const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int wave_min(int x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
-  return x;
+  return uniform(x);
 }
 __device__ __forceinline__ int wave_max(int x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
-  return x;
+  return uniform(x);
 }
 
 // First row of sequence s among all, cut to the call's rows.
@@ -142,7 +147,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   const rkv_attend& a = A.a;
   const rkv_pages& p = A.p;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int n_rows = n_q * A.group, n_kv = slots_of(A, seq);
+  const int n_rows = n_q * A.group, n_kv = uniform(slots_of(A, seq));
 
   // this lane's row (rows behind the last repeat it) and the slots it sees
   const int r = min(r0 + 32 * wv + col, n_rows - 1);
@@ -153,8 +158,8 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   if (a.causal) hi = min(n_kv, max(pos + 1, a.prefix_lens ? a.prefix_lens[seq] : 0));
   int lo = a.window ? max(0, pos - a.window + 1) : 0;
   if (a.first_keys) lo = max(lo, a.first_keys[row]);
-  if (lo >= hi) {
-    lo = 0x7fffffff;
+  if (lo >= hi) {      // nothing
+    lo = kNone;
     hi = 0;
   }
   u32x4 q[8];
@@ -173,16 +178,16 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     bounds.hi[wv] = w_hi;
   }
   __syncthreads();
-  const int b_lo = min(min(bounds.lo[0], bounds.lo[1]), min(bounds.lo[2], bounds.lo[3]));
-  const int b_hi = max(max(bounds.hi[0], bounds.hi[1]), max(bounds.hi[2], bounds.hi[3]));
+  const int b_lo = uniform(min(min(bounds.lo[0], bounds.lo[1]), min(bounds.lo[2], bounds.lo[3])));
+  const int b_hi = uniform(max(max(bounds.hi[0], bounds.hi[1]), max(bounds.hi[2], bounds.hi[3])));
   int t0, t1;
   tile_span(A, seq, r0, n_q, n_kv, t0, t1);
   if (n >= 0) {
     t0 += u0;
     t1 = min(t1, t0 + n);
   }
-  t0 = max(t0, b_lo / kKeys);
-  t1 = min(t1, (b_hi + kKeys - 1) / kKeys);
+  t0 = uniform(max(t0, b_lo / kKeys));
+  t1 = uniform(min(t1, (b_hi + kKeys - 1) / kKeys));
 
   // The four rows this lane fetches of a tile: 16 wv + 4 j + lane / 16, 16 bytes of each.  K rows lie in LDS with chunk c at
   // c ^ (row % 16), V rows with c at c ^ 4 (row % 4): the reads below then touch every bank alike.  Pages of a multiple of
@@ -204,55 +209,51 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       v_off[j] += (4 * j + fr) * v_slot;
     }
   }
-  int page[kPage16 ? 1 : 4], at[kPage16 ? 1 : 4];
-  auto find = [&](int tl) __attribute__((always_inline)) {   // pages of tile tl; -1: not visible
-    if constexpr (kPage16) {
-      const int key = tl * kKeys + 16 * wv;
-      const bool in = key + 16 > b_lo && key < b_hi;
-      const int c = div_by(in ? key : 0, A.by_page);
-      at[0] = key - c * p.page_size;
-      page[0] = in ? table[c] : -1;
-    } else {
+  struct Place {
+    int page[kPage16 ? 1 : 4], at[kPage16 ? 1 : 4];
+  };
+  auto find = [&](int tl, Place& x) __attribute__((always_inline)) {   // pages of tile tl; -1: not visible
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = tl * kKeys + 16 * wv + 4 * j + fr;
-        const bool in = key >= b_lo && key < b_hi;
-        const int c = div_by(in ? key : 0, A.by_page);
-        at[j] = key - c * p.page_size;
-        page[j] = in ? table[c] : -1;
-      }
+    for (int j = 0; j < (kPage16 ? 1 : 4); ++j) {
+      const int key = tl * kKeys + 16 * wv + (kPage16 ? 0 : 4 * j + fr);
+      const bool in = kPage16 ? key + 16 > b_lo && key < b_hi : key >= b_lo && key < b_hi;
+      const int c = div_by(in ? key : 0, A.by_page);
+      x.at[j] = key - c * p.page_size;
+      x.page[j] = in ? table[c] : -1;
     }
   };
   const char* zeros = reinterpret_cast<const char*>(zero_row);
-  auto fetch = [&](int tl, uint32_t to) __attribute__((always_inline)) {
-    to += wv * 4096;
+  auto fetch = [&](int tl, const Place& x, const char* rows, int64_t page_stride, uint32_t slot, const uint32_t (&off)[4], uint32_t to)
+      __attribute__((always_inline)) {
+    to += lds + wv * 4096;
     if constexpr (kPage16) {
       const int key = tl * kKeys + 16 * wv;
-      const uint32_t pg = __builtin_amdgcn_readfirstlane(page[0]), sl = __builtin_amdgcn_readfirstlane(at[0]);
+      const uint32_t pg = __builtin_amdgcn_readfirstlane(x.page[0]), sl = __builtin_amdgcn_readfirstlane(x.at[0]);
       const bool known = pg < (uint32_t)p.n_pages;
-      const char* k = kp + (uint64_t)pg * (2 * p.k_page) + (uint64_t)sl * k_slot;
-      const char* v = vp + (uint64_t)pg * (2 * p.v_page) + (uint64_t)sl * v_slot;
+      const char* src = rows + (uint64_t)pg * (uint64_t)(2 * page_stride) + (uint64_t)sl * slot;
       if (known && key >= b_lo && key + 16 <= b_hi) {
-        dma16s_four(k, k_off, to);
-        dma16s_four(v, v_off, to + kTileBytes);
+        dma16s_four(src, off, to);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const bool in = known && key + 4 * j + fr >= b_lo && key + 4 * j + fr < b_hi;
-          dma16(in ? k + k_off[j] : zeros + (k_off[j] & 240), to + 1024 * j);
-          dma16(in ? v + v_off[j] : zeros + (v_off[j] & 240), to + 1024 * j + kTileBytes);
+          dma16(in ? src + off[j] : zeros + (off[j] & 240), to + 1024 * j);
         }
       }
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const bool in = (uint32_t)page[j] < (uint32_t)p.n_pages;
-        const char* k = in ? kp + (uint64_t)(uint32_t)page[j] * (uint64_t)(2 * p.k_page) + (uint64_t)(uint32_t)at[j] * k_slot : zeros;
-        const char* v = in ? vp + (uint64_t)(uint32_t)page[j] * (uint64_t)(2 * p.v_page) + (uint64_t)(uint32_t)at[j] * v_slot : zeros;
-        dma16(k + k_off[j], to + 1024 * j);
-        dma16(v + v_off[j], to + 1024 * j + kTileBytes);
+        const bool in = (uint32_t)x.page[j] < (uint32_t)p.n_pages;
+        dma16((in ? rows + (uint64_t)(uint32_t)x.page[j] * (uint64_t)(2 * page_stride) + (uint64_t)(uint32_t)x.at[j] * slot : zeros) + off[j],
+              to + 1024 * j);
       }
     }
+  };
+  auto fetch_k = [&](int tl, const Place& x, int buf) __attribute__((always_inline)) {
+    fetch(tl, x, kp, p.k_page, k_slot, k_off, buf * kTileBytes);
+  };
+  auto fetch_v = [&](int tl, const Place& x, int buf) __attribute__((always_inline)) {
+    fetch(tl, x, vp, p.v_page, v_slot, v_off, (2 + buf) * kTileBytes);
   };
 
   f32x16 o[4] = {};
@@ -269,97 +270,136 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   for (int d = 0; d < 4; ++d)
     v_lane[d] = lds + v_key * 256 + ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (4 * (v_key & 3))) * 16 + (lane & 1) * 8;
 
-  // key of s[u][i]: key0 + 32 u + 8 (i / 4) + 4 half + i % 4
-  auto tile = [&](int tl, auto buffer) __attribute__((always_inline)) {
-    constexpr uint32_t kb = decltype(buffer)::value * 2 * kTileBytes, vb = kb + kTileBytes;
+  float ref = 0.f;      // the running maximum, 0 while there is none
+  f32x16 sa[2], sb[2];  // scores of a tile and the next: s.[u][i] is key 32 u + 8 (i / 4) + 4 half + i % 4
+  u32x4 pr[4];          // probabilities of a tile, 16 keys each
+
+  auto k_frag = [&](int i, uint32_t kb) __attribute__((always_inline)) { return lds_read16(k_lane[i & 7] + kb + (i >> 3) * 8192); };
+  // Scores of a tile as they stand in x: scaled and biased (kExtra), hidden where its edge is inside the tile.
+  auto finish = [&](int tl, f32x16 (&x)[2]) __attribute__((always_inline)) {
     const int key0 = tl * kKeys;
-    if (key0 + kKeys <= w_lo || key0 >= w_hi || r0 + 32 * wv >= n_rows) return;   // only other waves' rows see it
-    f32x16 s[2];
-    {
-      u32x4 f[4];
-#pragma unroll
-      for (int i = 0; i < 3; ++i) f[i] = lds_read16(k_lane[i] + kb);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (i + 3 < 16) f[(i + 3) & 3] = lds_read16(k_lane[(i + 3) & 7] + kb + ((i + 3) >> 3) * 8192);
-        s[i >> 3] = mma32<kF16>(f[i & 3], q[i & 7], (i & 7) == 0 ? f32x16{} : s[i >> 3]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
     if constexpr (kExtra) {
+      const float far = (float)(pos - key0 - 4 * half);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          // cap tanh(x / cap) = cap - 2 cap / (1 + exp(2 x / cap)), in log2 units
-          float x = in_cap != 0.f ? 0.5f * cap2 - cap2 * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s[u][i] * in_cap)) : s[u][i] * sl2;
-          x -= slope * fabsf((float)(pos - (key0 + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3))));
-          s[u][i] = x;
+          // cap tanh(y / cap) = cap - 2 cap / (1 + exp(2 y / cap)), in log2 units
+          float y = in_cap != 0.f ? 0.5f * cap2 - cap2 * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[u][i] * in_cap)) : x[u][i] * sl2;
+          x[u][i] = fmaf(-slope, fabsf(far - (float)(32 * u + 8 * (i >> 2) + (i & 3))), y);
         }
     }
     if (key0 < all_lo || key0 + kKeys > all_hi) {
+      const int from = lo - key0 - 4 * half, to = hi - key0 - 4 * half;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int key = key0 + 32 * u + 8 * (i >> 2) + 4 * half + (i & 3);
-          if (key < lo || key >= hi) s[u][i] = -__builtin_inff();
+          const int key = 32 * u + 8 * (i >> 2) + (i & 3);
+          if (key < from || key >= to) x[u][i] = -__builtin_inff();
         }
     }
-    float top = s[0][0];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+  };
+  // The maximum of a tile's scores joins the running one; what has been summed is rescaled if it grew by much.
+  auto settle = [&](float top) __attribute__((always_inline)) {
     top = max_halves(top);
     if constexpr (!kExtra) top *= sl2;
     if (__any(top > m + kGrow)) {
       const float m2 = fmaxf(m, top), f = m2 > m ? __builtin_amdgcn_exp2f(m - m2) : 1.f;
       m = m2;
+      ref = m == -__builtin_inff() ? 0.f : m;
       l *= f;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] *= f;
     }
-    const float ref = m == -__builtin_inff() ? 0.f : m;
+  };
+  // Scores of the first tile.
+  auto begin = [&](int tl, f32x16 (&x)[2], uint32_t kb) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int i = 0; i < 16; ++i) x[i >> 3] = mma32<kF16>(k_frag(i, kb), q[i & 7], (i & 7) == 0 ? f32x16{} : x[i >> 3]);
+    finish(tl, x);
+    float top = x[0][0];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
+    settle(top);
+  };
+  // Tile tl, whose scores are x, summed up, and the next one's scores y: the probabilities are computed between the products
+  // of K, the next maximum between those of V, so that both pipes have work of this wave at any time.  The last tile's
+  // "next" is whatever lies in LDS, and goes nowhere.
+  auto sum_up = [&](int tl, f32x16 (&x)[2], f32x16 (&y)[2], uint32_t kb, uint32_t vb) __attribute__((always_inline)) {
+    {
+      u32x4 f[4];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) f[i] = k_frag(i, kb);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[u][i] = __builtin_amdgcn_exp2f(kExtra ? s[u][i] - ref : fmaf(s[u][i], sl2, -ref));
-        l += s[u][i];
-      }
+        if (i + 3 < 16) f[(i + 3) & 3] = k_frag(i + 3, kb);
+        y[i >> 3] = mma32<kF16>(f[i & 3], q[i & 7], (i & 7) == 0 ? f32x16{} : y[i >> 3]);
+        float e[2];
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {   // 16 keys each
-      u32x4 pr;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) pr[i] = pack<kF16>(s[ks >> 1][8 * (ks & 1) + 2 * i], s[ks >> 1][8 * (ks & 1) + 2 * i + 1]);
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const u32x2 v0 = lds_read_tr(v_lane[d] + vb + ks * 4096);
-        const u32x2 v1 = lds_read_tr(v_lane[d] + vb + ks * 4096 + 2048);
-        o[d] = mma32<kF16>(u32x4{v0[0], v0[1], v1[0], v1[1]}, pr, o[d]);
+        for (int j = 0; j < 2; ++j) {
+          const float z = x[i >> 3][2 * (i & 7) + j];
+          e[j] = __builtin_amdgcn_exp2f(kExtra ? z - ref : fmaf(z, sl2, -ref));
+          l += e[j];
+        }
+        pr[i >> 2][i & 3] = pack<kF16>(e[0], e[1]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    finish(tl + 1, y);
+    float top = y[0][0];
+    {
+      auto v_frag = [&](int i) __attribute__((always_inline)) {   // 16 keys i / 4, columns 32 (i % 4) ..
+        const u32x2 v0 = lds_read_tr(v_lane[i & 3] + vb + (i >> 2) * 4096);
+        const u32x2 v1 = lds_read_tr(v_lane[i & 3] + vb + (i >> 2) * 4096 + 2048);
+        return u32x4{v0[0], v0[1], v1[0], v1[1]};
+      };
+      u32x4 f[4];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) f[i] = v_frag(i);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (i + 3 < 16) f[(i + 3) & 3] = v_frag(i + 3);
+        o[i & 3] = mma32<kF16>(f[i & 3], pr[i >> 2], o[i & 3]);
+        top = fmaxf(fmaxf(top, y[i >> 3][2 * (i & 7)]), y[i >> 3][2 * (i & 7) + 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (tl + 1 < t1) settle(top);
   };
-  auto step = [&](int tl, auto buffer) __attribute__((always_inline)) {
+  // Iteration tl needs tile tl of V and tile tl + 1 of K, requested in the iteration before; K's tiles are in buffers
+  // (tl - t0) % 2, V's in 2 + (tl - t0) % 2.
+  Place here, next;
+  auto advance = [&](int tl, int b) __attribute__((always_inline)) {   // b = (tl + 1 - t0) % 2
     tile_sync();
-    if (tl + 1 < t1) {
-      fetch(tl + 1, lds + (1 - decltype(buffer)::value) * 2 * kTileBytes);
-      if (tl + 2 < t1) find(tl + 2);
-    }
-    tile(tl, buffer);
+    if (tl + 2 < t1) fetch_k(tl + 2, next, 1 - b);
+    if (tl + 1 < t1 && tl >= t0) fetch_v(tl + 1, here, b);
+    here = next;
+    if (tl + 3 < t1) find(tl + 3, next);
   };
   if (t0 < t1) {
-    find(t0);
-    fetch(t0, lds);
-    if (t0 + 1 < t1) find(t0 + 1);
-  }
+    find(t0, here);
+    if (t0 + 1 < t1) find(t0 + 1, next);
+    fetch_k(t0, here, 0);
+    fetch_v(t0, here, 0);
+    if (r0 + 32 * wv < n_rows) {
+      advance(t0 - 1, 0);
+      begin(t0, sa, 0);
 #pragma unroll 1
-  for (int tl = t0; tl < t1; tl += 2) {
-    step(tl, std::integral_constant<int, 0>{});
-    if (tl + 1 < t1) step(tl + 1, std::integral_constant<int, 1>{});
+      for (int tl = t0;; tl += 2) {
+        advance(tl, 1);
+        sum_up(tl, sa, sb, kTileBytes, 2 * kTileBytes);
+        if (tl + 1 >= t1) break;
+        advance(tl + 1, 0);
+        sum_up(tl + 1, sb, sa, 0, 3 * kTileBytes);
+        if (tl + 2 >= t1) break;
+      }
+    } else {      // no rows: this wave fetches for the others
+#pragma unroll 1
+      for (int tl = t0 - 1; tl < t1; ++tl) advance(tl, (tl + 1 - t0) & 1);
+    }
   }
   __syncthreads();   // bounds and tiles are free for the next rows
 
@@ -398,7 +438,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendLaunch
   const int h = blockIdx.x % A.p.n_kv_heads;
   const int tile = A.n_tiles - 1 - blockIdx.x / A.p.n_kv_heads;   // a causal prompt's longest rows first
   const int seq = __builtin_amdgcn_readfirstlane(tile_sequence(A, tile));
-  const int row0 = first_row(A.a, seq), n_q = end_row(A.a, seq) - row0, r0 = (tile - tile_start(A, seq)) * kRows;
+  const int row0 = uniform(first_row(A.a, seq)), n_q = uniform(end_row(A.a, seq)) - row0, r0 = uniform(tile - tile_start(A, seq)) * kRows;
   if (r0 < 0 || r0 >= n_q * A.group) return;
   attend_rows<kF16, kExtra, kPage16>(A, smem, bounds, seq, row0, n_q, r0, h, 0, -1, nullptr);
 }
@@ -469,10 +509,10 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
       else hi = mid;
     }
     const int tile = __builtin_amdgcn_readfirstlane(lo);
-    const int u0 = (int)(rem - sBefore[tile]), count = (int)(sBefore[tile + 1] - sBefore[tile]);
+    const int u0 = uniform((int)(rem - sBefore[tile])), count = uniform((int)(sBefore[tile + 1] - sBefore[tile]));
     const int n = (int)min((int64_t)(count - u0), end - pos);
     const int seq = __builtin_amdgcn_readfirstlane(tile_sequence(A, tile));
-    const int row0 = first_row(A.a, seq), n_q = end_row(A.a, seq) - row0, r0 = (tile - tile_start(A, seq)) * kRows;
+    const int row0 = uniform(first_row(A.a, seq)), n_q = uniform(end_row(A.a, seq)) - row0, r0 = uniform(tile - tile_start(A, seq)) * kRows;
     float* part = nullptr;
     if (n < count) {
       part = part_slot(A, 2 * w + (u0 == 0));
