@@ -42,9 +42,11 @@ constexpr int kRows = kAttendRows;         // rows of a workgroup, 32 a wave
 constexpr int kKeys = 64;                  // keys of a streamed tile
 constexpr int kShares = kAttendShares;
 constexpr int kListed = kAttendListed;
+constexpr int kAhead = 11;                 // of a tile's 16 pairs of probabilities, those computed between the products of K
 constexpr int kLeast = 1;                  // key tiles of a share, at least
 constexpr int kTileBytes = kKeys * kHeadDim * 2;
 constexpr int kNone = 0x7fffffff;
+constexpr int64_t kStrideEnd = int64_t(1) << 31;   // page strides (elements) whose bytes 32 bits hold
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGrow = 8.f;               // log2 units a maximum may outgrow the reference by
 
@@ -139,7 +141,8 @@ struct Bounds {
   int lo[4], hi[4];
 };
 
-// kExtra: capped scores or a bias by distance; kPage16: page_size % 16 = 0.  Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
+// kExtra: capped scores or a bias by distance; kPage16: page_size % 16 = 0, pages less than 4 GiB and slots at least a
+// row apart.  Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
 // partial sums go, null: the rows are finished.
 template <bool kF16, bool kExtra, bool kPage16>
 __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
@@ -195,6 +198,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   // instructions a tile than with a page for each row, of 480).
   const uint32_t lds = lds_addr(smem);
   const int32_t* table = a.table + seq * a.table_stride;
+  const auto* known = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)table;   // scalar loads
   const char* kp = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.k) + h * p.k_head);
   const char* vp = reinterpret_cast<const char*>(static_cast<const uint16_t*>(p.v) + h * p.v_head);
   const int fr = lane >> 4;
@@ -204,22 +208,30 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   for (int j = 0; j < 4; ++j) {
     k_off[j] = 16 * ((lane & 15) ^ (4 * j + fr));
     v_off[j] = 16 * ((lane & 15) ^ (4 * fr));
-    if constexpr (kPage16) {
-      k_off[j] += (4 * j + fr) * k_slot;
-      v_off[j] += (4 * j + fr) * v_slot;
+    if constexpr (kPage16) {   // not negative: slots are at least 256 bytes apart
+      k_off[j] += (4 * j + fr) * k_slot - 1024 * j;
+      v_off[j] += (4 * j + fr) * v_slot - 1024 * j;
     }
   }
   struct Place {
     int page[kPage16 ? 1 : 4], at[kPage16 ? 1 : 4];
   };
   auto find = [&](int tl, Place& x) __attribute__((always_inline)) {   // pages of tile tl; -1: not visible
-#pragma unroll
-    for (int j = 0; j < (kPage16 ? 1 : 4); ++j) {
-      const int key = tl * kKeys + 16 * wv + (kPage16 ? 0 : 4 * j + fr);
-      const bool in = kPage16 ? key + 16 > b_lo && key < b_hi : key >= b_lo && key < b_hi;
+    if constexpr (kPage16) {
+      const int key = tl * kKeys + 16 * wv;
+      const bool in = key + 16 > b_lo && key < b_hi;
       const int c = div_by(in ? key : 0, A.by_page);
-      x.at[j] = key - c * p.page_size;
-      x.page[j] = in ? table[c] : -1;
+      x.at[0] = key - c * p.page_size;
+      x.page[0] = in ? known[c] : -1;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = tl * kKeys + 16 * wv + 4 * j + fr;
+        const bool in = key >= b_lo && key < b_hi;
+        const int c = div_by(in ? key : 0, A.by_page);
+        x.at[j] = key - c * p.page_size;
+        x.page[j] = in ? table[c] : -1;
+      }
     }
   };
   const char* zeros = reinterpret_cast<const char*>(zero_row);
@@ -228,16 +240,16 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     to += lds + wv * 4096;
     if constexpr (kPage16) {
       const int key = tl * kKeys + 16 * wv;
-      const uint32_t pg = __builtin_amdgcn_readfirstlane(x.page[0]), sl = __builtin_amdgcn_readfirstlane(x.at[0]);
-      const bool known = pg < (uint32_t)p.n_pages;
-      const char* src = rows + (uint64_t)pg * (uint64_t)(2 * page_stride) + (uint64_t)sl * slot;
-      if (known && key >= b_lo && key + 16 <= b_hi) {
+      const uint32_t pg = x.page[0];
+      const bool held = pg < (uint32_t)p.n_pages;
+      const char* src = rows + (uint64_t)pg * (uint32_t)(2 * page_stride) + (uint64_t)(uint32_t)x.at[0] * slot;
+      if (held && key >= b_lo && key + 16 <= b_hi) {
         dma16s_four(src, off, to);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bool in = known && key + 4 * j + fr >= b_lo && key + 4 * j + fr < b_hi;
-          dma16(in ? src + off[j] : zeros + (off[j] & 240), to + 1024 * j);
+          const bool in = held && key + 4 * j + fr >= b_lo && key + 4 * j + fr < b_hi;
+          dma16(in ? src + (off[j] + 1024 * j) : zeros + (off[j] & 240), to + 1024 * j);
         }
       }
     } else {
@@ -325,6 +337,17 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
     settle(top);
   };
+  // Probabilities 2 i and 2 i + 1 of a tile.
+  auto pair = [&](const f32x16 (&x)[2], int i) __attribute__((always_inline)) {
+    float e[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float z = x[i >> 3][2 * (i & 7) + j];
+      e[j] = __builtin_amdgcn_exp2f(kExtra ? z - ref : fmaf(z, sl2, -ref));
+      l += e[j];
+    }
+    pr[i >> 2][i & 3] = pack<kF16>(e[0], e[1]);
+  };
   // Tile tl, whose scores are x, summed up, and the next one's scores y: the probabilities are computed between the products
   // of K, the next maximum between those of V, so that both pipes have work of this wave at any time.  The last tile's
   // "next" is whatever lies in LDS, and goes nowhere.
@@ -337,14 +360,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       for (int i = 0; i < 16; ++i) {
         if (i + 3 < 16) f[(i + 3) & 3] = k_frag(i + 3, kb);
         y[i >> 3] = mma32<kF16>(f[i & 3], q[i & 7], (i & 7) == 0 ? f32x16{} : y[i >> 3]);
-        float e[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float z = x[i >> 3][2 * (i & 7) + j];
-          e[j] = __builtin_amdgcn_exp2f(kExtra ? z - ref : fmaf(z, sl2, -ref));
-          l += e[j];
-        }
-        pr[i >> 2][i & 3] = pack<kF16>(e[0], e[1]);
+        if (i * kAhead / 16 != (i + 1) * kAhead / 16) pair(x, i * kAhead / 16);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -363,6 +379,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       for (int i = 0; i < 16; ++i) {
         if (i + 3 < 16) f[(i + 3) & 3] = v_frag(i + 3);
         o[i & 3] = mma32<kF16>(f[i & 3], pr[i >> 2], o[i & 3]);
+        if (kAhead + i < 16) pair(x, kAhead + i);
         top = fmaxf(fmaxf(top, y[i >> 3][2 * (i & 7)]), y[i >> 3][2 * (i & 7) + 1]);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -603,7 +620,9 @@ void launch_kernels(const AttendLaunch& A, hipStream_t st) {
 }
 template <bool kF16, bool kExtra>
 void launch_pages(const AttendLaunch& A, hipStream_t st) {
-  if (A.p.page_size % 16 == 0) launch_kernels<kF16, kExtra, true>(A, st);
+  const rkv_pages& p = A.p;
+  const bool near = p.k_page < kStrideEnd && p.v_page < kStrideEnd && p.k_slot >= kHeadDim && p.v_slot >= kHeadDim;
+  if (p.page_size % 16 == 0 && near) launch_kernels<kF16, kExtra, true>(A, st);
   else launch_kernels<kF16, kExtra, false>(A, st);
 }
 template <bool kF16>
