@@ -43,9 +43,7 @@ constexpr int kKeys = 64;                  // keys of a streamed tile
 constexpr int kShares = kAttendShares;
 constexpr int kListed = kAttendListed;
 constexpr int kAhead = 11;                 // of a tile's 16 pairs of probabilities, those computed between the products of K
-constexpr int kLeast = 1;                  // key tiles of a share, at least
 constexpr int kTileBytes = kKeys * kHeadDim * 2;
-constexpr int kNone = 0x7fffffff;
 constexpr int64_t kStrideEnd = int64_t(1) << 31;   // page strides (elements) whose bytes 32 bits hold
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGrow = 8.f;               // log2 units a maximum may outgrow the reference by
@@ -104,12 +102,12 @@ __device__ __forceinline__ int first_row(const rkv_attend& a, int s) {
 // Row tiles are numbered with room for a part-filled one per sequence: sequence s starts at floor(first_row G / 128) + s, which
 // ascends and leaves each sequence ceil(rows / 128) numbers, so no list of tiles has to be built.  The sequence of a
 // tile: 64-way bisection by one wave.
-__device__ __forceinline__ int tile_start(const AttendLaunch& A, int s) { return first_row(A.a, s) * A.group / kRows + s; }
+__device__ __forceinline__ int tile_start(const AttendLaunch& A, int row0, int s) { return row0 * A.group / kRows + s; }
 __device__ __forceinline__ int tile_sequence(const AttendLaunch& A, int tile) {
   int lo = 0, n = A.a.n_seqs;
   while (n > 1) {
     const int step = (n + 63) / 64, at = (int)(threadIdx.x & 63) * step;
-    const uint64_t in = __ballot(at < n && tile_start(A, lo + at) <= tile);
+    const uint64_t in = __ballot(at < n && tile_start(A, first_row(A.a, lo + at), lo + at) <= tile);
     const int k = max(0, (int)__popcll(in) - 1) * step;
     lo += k;
     n = min(step, n - k);
@@ -138,59 +136,49 @@ __device__ __forceinline__ float* part_slot(const AttendLaunch& A, int slot) {
 }
 
 struct Bounds {
-  int lo[4], hi[4];
+  int lo[4];   // of the waves
 };
 
-// kExtra: capped scores or a bias by distance; kPage16: page_size % 16 = 0, pages less than 4 GiB and slots at least a
+// kCap: capped scores, kBias: less a slope times the distance; kPage16: page_size % 16 = 0, pages less than 4 GiB and slots at least a
 // row apart.  Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
 // partial sums go, null: the rows are finished.
-template <bool kF16, bool kExtra, bool kPage16>
+template <bool kF16, bool kCap, bool kBias, bool kPage16>
 __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
-                                            int r0, int h, int u0, int n, float* part) {
+                                            int n_kv, int r0, int h, int u0, int n, float* part) {
   const rkv_attend& a = A.a;
   const rkv_pages& p = A.p;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
-  const int n_rows = n_q * A.group, n_kv = uniform(slots_of(A, seq));
+  const int n_rows = n_q * A.group;
 
-  // this lane's row (rows behind the last repeat it) and the slots it sees
+  // The slots a position sees, and a row's position.  Both bounds ascend with the row, so that those of the tile and of the
+  // wave follow from their first and last rows, without a word from the other lanes: the first keys are requested at once.
+  const int prefix = a.prefix_lens ? uniform(a.prefix_lens[seq]) : 0;
+  auto hi_of = [&](int at) { return a.causal ? min(n_kv, max(at + 1, prefix)) : n_kv; };
+  auto lo_of = [&](int at) { return a.window ? max(0, at - a.window + 1) : 0; };
+  auto position = [&](int r) { return n_kv - n_q + div_by(min(r, n_rows - 1), A.by_group); };   // rows behind the last repeat it
+  int b_lo = lo_of(position(r0)), b_hi = hi_of(position(r0 + kRows - 1));                       // slots some row sees
+  int all_lo = lo_of(position(r0 + 32 * wv + 31)), all_hi = hi_of(position(r0 + 32 * wv));      // that every row of the wave sees
   const int r = min(r0 + 32 * wv + col, n_rows - 1);
   const int t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
   const int64_t row = row0 + t;
   const int pos = n_kv - n_q + t;
-  int hi = n_kv;
-  if (a.causal) hi = min(n_kv, max(pos + 1, a.prefix_lens ? a.prefix_lens[seq] : 0));
-  int lo = a.window ? max(0, pos - a.window + 1) : 0;
-  if (a.first_keys) lo = max(lo, a.first_keys[row]);
-  if (lo >= hi) {      // nothing
-    lo = kNone;
-    hi = 0;
+  int lo = lo_of(pos), hi = hi_of(pos);
+  if (a.first_keys) {   // these need not ascend
+    lo = max(lo, a.first_keys[row]);
+    all_lo = wave_max(lo);
+    const int least = wave_min(lo);
+    if (lane == 0) bounds.lo[wv] = least;
+    __syncthreads();
+    b_lo = uniform(min(min(bounds.lo[0], bounds.lo[1]), min(bounds.lo[2], bounds.lo[3])));
   }
-  u32x4 q[8];
-  const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + row * a.q_token + hq * a.q_head;
-#pragma unroll
-  for (int s = 0; s < 8; ++s) q[s] = *reinterpret_cast<const u32x4*>(qrow + 16 * s + 8 * half);
-  if (a.scale < 0.f) {
-#pragma unroll
-    for (int s = 0; s < 8; ++s) q[s] ^= 0x80008000u;
-  }
-
-  const int w_lo = wave_min(lo), w_hi = wave_max(hi);      // slots some row of the wave sees
-  const int all_lo = wave_max(lo), all_hi = wave_min(hi);  // and that every row sees
-  if (lane == 0) {
-    bounds.lo[wv] = w_lo;
-    bounds.hi[wv] = w_hi;
-  }
-  __syncthreads();
-  const int b_lo = uniform(min(min(bounds.lo[0], bounds.lo[1]), min(bounds.lo[2], bounds.lo[3])));
-  const int b_hi = uniform(max(max(bounds.hi[0], bounds.hi[1]), max(bounds.hi[2], bounds.hi[3])));
   int t0, t1;
   tile_span(A, seq, r0, n_q, n_kv, t0, t1);
   if (n >= 0) {
     t0 += u0;
     t1 = min(t1, t0 + n);
   }
-  t0 = uniform(max(t0, b_lo / kKeys));
-  t1 = uniform(min(t1, (b_hi + kKeys - 1) / kKeys));
+  t0 = max(t0, b_lo / kKeys);
+  t1 = min(t1, (b_hi + kKeys - 1) / kKeys);
 
   // The four rows this lane fetches of a tile: 16 wv + 4 j + lane / 16, 16 bytes of each.  K rows lie in LDS with chunk c at
   // c ^ (row % 16), V rows with c at c ^ 4 (row % 4): the reads below then touch every bank alike.  Pages of a multiple of
@@ -268,124 +256,6 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     fetch(tl, x, vp, p.v_page, v_slot, v_off, (2 + buf) * kTileBytes);
   };
 
-  f32x16 o[4] = {};
-  float m = -__builtin_inff(), l = 0.f;
-  const float sl2 = fabsf(a.scale) * kLog2e;      // a negative scale's sign is in q
-  const float slope = kExtra && a.slopes ? a.slopes[hq] * kLog2e : 0.f;
-  const float cap2 = 2.f * kLog2e * a.softcap, in_cap = kExtra && a.softcap > 0.f ? 2.f * sl2 / a.softcap : 0.f;
-  uint32_t k_lane[8], v_lane[4];
-#pragma unroll
-  for (int st = 0; st < 8; ++st) k_lane[st] = lds + col * 256 + (((2 * st) ^ (col & 15) ^ half) * 16);
-  // V^T: lane reads 4 columns of key 4 half + (lane % 16) / 4 (+ 8), chunk 4 d + 2 ((lane / 16) % 2) + (lane % 4) / 2
-  const int v_key = 4 * half + ((lane & 15) >> 2);
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-    v_lane[d] = lds + v_key * 256 + ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (4 * (v_key & 3))) * 16 + (lane & 1) * 8;
-
-  float ref = 0.f;      // the running maximum, 0 while there is none
-  f32x16 sa[2], sb[2];  // scores of a tile and the next: s.[u][i] is key 32 u + 8 (i / 4) + 4 half + i % 4
-  u32x4 pr[4];          // probabilities of a tile, 16 keys each
-
-  auto k_frag = [&](int i, uint32_t kb) __attribute__((always_inline)) { return lds_read16(k_lane[i & 7] + kb + (i >> 3) * 8192); };
-  // Scores of a tile as they stand in x: scaled and biased (kExtra), hidden where its edge is inside the tile.
-  auto finish = [&](int tl, f32x16 (&x)[2]) __attribute__((always_inline)) {
-    const int key0 = tl * kKeys;
-    if constexpr (kExtra) {
-      const float far = (float)(pos - key0 - 4 * half);
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          // cap tanh(y / cap) = cap - 2 cap / (1 + exp(2 y / cap)), in log2 units
-          float y = in_cap != 0.f ? 0.5f * cap2 - cap2 * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[u][i] * in_cap)) : x[u][i] * sl2;
-          x[u][i] = fmaf(-slope, fabsf(far - (float)(32 * u + 8 * (i >> 2) + (i & 3))), y);
-        }
-    }
-    if (key0 < all_lo || key0 + kKeys > all_hi) {
-      const int from = lo - key0 - 4 * half, to = hi - key0 - 4 * half;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = 32 * u + 8 * (i >> 2) + (i & 3);
-          if (key < from || key >= to) x[u][i] = -__builtin_inff();
-        }
-    }
-  };
-  // The maximum of a tile's scores joins the running one; what has been summed is rescaled if it grew by much.
-  auto settle = [&](float top) __attribute__((always_inline)) {
-    top = max_halves(top);
-    if constexpr (!kExtra) top *= sl2;
-    if (__any(top > m + kGrow)) {
-      const float m2 = fmaxf(m, top), f = m2 > m ? __builtin_amdgcn_exp2f(m - m2) : 1.f;
-      m = m2;
-      ref = m == -__builtin_inff() ? 0.f : m;
-      l *= f;
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= f;
-    }
-  };
-  // Scores of the first tile.
-  auto begin = [&](int tl, f32x16 (&x)[2], uint32_t kb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i >> 3] = mma32<kF16>(k_frag(i, kb), q[i & 7], (i & 7) == 0 ? f32x16{} : x[i >> 3]);
-    finish(tl, x);
-    float top = x[0][0];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
-    settle(top);
-  };
-  // Probabilities 2 i and 2 i + 1 of a tile.
-  auto pair = [&](const f32x16 (&x)[2], int i) __attribute__((always_inline)) {
-    float e[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float z = x[i >> 3][2 * (i & 7) + j];
-      e[j] = __builtin_amdgcn_exp2f(kExtra ? z - ref : fmaf(z, sl2, -ref));
-      l += e[j];
-    }
-    pr[i >> 2][i & 3] = pack<kF16>(e[0], e[1]);
-  };
-  // Tile tl, whose scores are x, summed up, and the next one's scores y: the probabilities are computed between the products
-  // of K, the next maximum between those of V, so that both pipes have work of this wave at any time.  The last tile's
-  // "next" is whatever lies in LDS, and goes nowhere.
-  auto sum_up = [&](int tl, f32x16 (&x)[2], f32x16 (&y)[2], uint32_t kb, uint32_t vb) __attribute__((always_inline)) {
-    {
-      u32x4 f[4];
-#pragma unroll
-      for (int i = 0; i < 3; ++i) f[i] = k_frag(i, kb);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (i + 3 < 16) f[(i + 3) & 3] = k_frag(i + 3, kb);
-        y[i >> 3] = mma32<kF16>(f[i & 3], q[i & 7], (i & 7) == 0 ? f32x16{} : y[i >> 3]);
-        if (i * kAhead / 16 != (i + 1) * kAhead / 16) pair(x, i * kAhead / 16);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    finish(tl + 1, y);
-    float top = y[0][0];
-    {
-      auto v_frag = [&](int i) __attribute__((always_inline)) {   // 16 keys i / 4, columns 32 (i % 4) ..
-        const u32x2 v0 = lds_read_tr(v_lane[i & 3] + vb + (i >> 2) * 4096);
-        const u32x2 v1 = lds_read_tr(v_lane[i & 3] + vb + (i >> 2) * 4096 + 2048);
-        return u32x4{v0[0], v0[1], v1[0], v1[1]};
-      };
-      u32x4 f[4];
-#pragma unroll
-      for (int i = 0; i < 3; ++i) f[i] = v_frag(i);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (i + 3 < 16) f[(i + 3) & 3] = v_frag(i + 3);
-        o[i & 3] = mma32<kF16>(f[i & 3], pr[i >> 2], o[i & 3]);
-        if (kAhead + i < 16) pair(x, kAhead + i);
-        top = fmaxf(fmaxf(top, y[i >> 3][2 * (i & 7)]), y[i >> 3][2 * (i & 7) + 1]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    if (tl + 1 < t1) settle(top);
-  };
   // Iteration tl needs tile tl of V and tile tl + 1 of K, requested in the iteration before; K's tiles are in buffers
   // (tl - t0) % 2, V's in 2 + (tl - t0) % 2.
   Place here, next;
@@ -401,6 +271,148 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     if (t0 + 1 < t1) find(t0 + 1, next);
     fetch_k(t0, here, 0);
     fetch_v(t0, here, 0);
+  }
+  u32x4 q[8];
+  const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + row * a.q_token + hq * a.q_head;
+#pragma unroll
+  for (int s = 0; s < 8; ++s) q[s] = *reinterpret_cast<const u32x4*>(qrow + 16 * s + 8 * half);
+  if (a.scale < 0.f) {
+#pragma unroll
+    for (int s = 0; s < 8; ++s) q[s] ^= 0x80008000u;
+  }
+
+  f32x16 o[4] = {};
+  float m = -__builtin_inff(), l = 0.f;
+  const float sl2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);   // a negative scale's sign is in q; above 0, so that hidden stays hidden
+  const float slope = kBias ? a.slopes[hq] * kLog2e : 0.f;
+  const float cap2 = 2.f * kLog2e * a.softcap, in_cap = kCap ? 2.f * sl2 / a.softcap : 0.f;
+  uint32_t k_lane[8], v_lane[4];
+#pragma unroll
+  for (int st = 0; st < 8; ++st) k_lane[st] = lds + col * 256 + (((2 * st) ^ (col & 15) ^ half) * 16);
+  // V^T: lane reads 4 columns of key 4 half + (lane % 16) / 4 (+ 8), chunk 4 d + 2 ((lane / 16) % 2) + (lane % 4) / 2
+  const int v_key = 4 * half + ((lane & 15) >> 2);
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+    v_lane[d] = lds + v_key * 256 + ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (4 * (v_key & 3))) * 16 + (lane & 1) * 8;
+
+  float ref = 0.f;      // the running maximum, 0 while there is none
+  f32x16 sa[2], sb[2];  // scores of a tile and the next: s.[u][i] is key 32 u + 8 (i / 4) + 4 half + i % 4
+  u32x4 pr[4];          // probabilities of a tile, 16 keys each
+
+  auto k_frag = [&](int i, uint32_t kb) __attribute__((always_inline)) { return lds_read16(k_lane[i & 7] + kb + (i >> 3) * 8192); };
+  // A product becomes what is compared and exponentiated: the score is grow x + base, in log2 units, with grow >= 0.
+  //   neither: x = the product, the scale in grow;
+  //   capped:  c tanh(y / c) = c - 2 c / (1 + exp(2 y / c)): x = -1 / (1 + exp(2 y / c)), grow = 2 c, base = c;
+  //   biased (after the cap): x = the score.
+  auto score = [&](f32x16 (&x)[2], int u, int i, float far) __attribute__((always_inline)) {
+    float y = x[u][i];
+    if constexpr (kCap) y = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(y * in_cap));
+    if constexpr (kBias) {
+      y = kCap ? fmaf(y, cap2, 0.5f * cap2) : y * sl2;
+      y = fmaf(-slope, fabsf(far - (float)(32 * u + 8 * (i >> 2) + (i & 3))), y);
+    }
+    x[u][i] = y;
+  };
+  const float grow = kBias ? 1.f : kCap ? cap2 : sl2, base = !kBias && kCap ? 0.5f * cap2 : 0.f;
+  auto distance = [&](int tl) __attribute__((always_inline)) { return (float)(pos - tl * kKeys - 4 * half); };   // of key 4 half
+  // A tile that a row sees part of: the scores of the others, and the maximum again.
+  auto hide = [&](int tl, f32x16 (&x)[2], float& top) __attribute__((always_inline)) {
+    const int key0 = tl * kKeys;
+    if (key0 >= all_lo && key0 + kKeys <= all_hi) return;
+    const int from = lo - key0 - 4 * half, to = hi - key0 - 4 * half;
+    top = -__builtin_inff();
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = 32 * u + 8 * (i >> 2) + (i & 3);
+        if (key < from || key >= to) x[u][i] = -__builtin_inff();
+        top = fmaxf(top, x[u][i]);
+      }
+  };
+  // The maximum of a tile's scores joins the running one; what has been summed is rescaled if it grew by much.
+  auto settle = [&](float top) __attribute__((always_inline)) {
+    top = fmaf(max_halves(top), grow, base);
+    if (__any(top > m + kGrow)) {
+      const float m2 = fmaxf(m, top), f = m2 > m ? __builtin_amdgcn_exp2f(m - m2) : 1.f;
+      m = m2;
+      ref = m == -__builtin_inff() ? 0.f : m;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= f;
+    }
+  };
+  // Scores of the first tile.
+  auto begin = [&](int tl, f32x16 (&x)[2], uint32_t kb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i >> 3] = mma32<kF16>(k_frag(i, kb), q[i & 7], (i & 7) == 0 ? f32x16{} : x[i >> 3]);
+    const float far = distance(tl);
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      score(x, i >> 4, i & 15, far);
+      top = fmaxf(top, x[i >> 4][i & 15]);
+    }
+    hide(tl, x, top);
+    settle(top);
+  };
+  // Probabilities 2 i and 2 i + 1 of a tile.
+  auto pair = [&](const f32x16 (&x)[2], int i) __attribute__((always_inline)) {
+    float e[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float z = x[i >> 3][2 * (i & 7) + j];
+      e[j] = __builtin_amdgcn_exp2f(fmaf(z, grow, base - ref));
+      l += e[j];
+    }
+    pr[i >> 2][i & 3] = pack<kF16>(e[0], e[1]);
+  };
+  // Tile tl, whose scores are x, summed up, and the next one's scores y: the probabilities are computed between the products
+  // of K and V, the next maximum between those of V, so that both pipes have work of this wave at any time.  The last tile's
+  // "next" is whatever lies in LDS, and goes nowhere.
+  auto sum_up = [&](int tl, f32x16 (&x)[2], f32x16 (&y)[2], uint32_t kb, uint32_t vb) __attribute__((always_inline)) {
+    {
+      u32x4 f[4];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) f[i] = k_frag(i, kb);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (i + 3 < 16) f[(i + 3) & 3] = k_frag(i + 3, kb);
+        y[i >> 3] = mma32<kF16>(f[i & 3], q[i & 7], (i & 7) == 0 ? f32x16{} : y[i >> 3]);
+        if (i * kAhead / 16 != (i + 1) * kAhead / 16) pair(x, i * kAhead / 16);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    const float far = distance(tl + 1);
+    float top = -__builtin_inff();
+    {
+      auto v_frag = [&](int i) __attribute__((always_inline)) {   // 16 keys i / 4, columns 32 (i % 4) ..
+        const u32x2 v0 = lds_read_tr(v_lane[i & 3] + vb + (i >> 2) * 4096);
+        const u32x2 v1 = lds_read_tr(v_lane[i & 3] + vb + (i >> 2) * 4096 + 2048);
+        return u32x4{v0[0], v0[1], v1[0], v1[1]};
+      };
+      u32x4 f[4];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) f[i] = v_frag(i);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (i + 3 < 16) f[(i + 3) & 3] = v_frag(i + 3);
+        o[i & 3] = mma32<kF16>(f[i & 3], pr[i >> 2], o[i & 3]);
+        if (kAhead + i < 16) pair(x, kAhead + i);
+        score(y, i >> 3, 2 * (i & 7), far);
+        score(y, i >> 3, 2 * (i & 7) + 1, far);
+        top = fmaxf(fmaxf(top, y[i >> 3][2 * (i & 7)]), y[i >> 3][2 * (i & 7) + 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    if (tl + 1 < t1) {
+      hide(tl + 1, y, top);
+      settle(top);
+    }
+  };
+  if (t0 < t1) {
     if (r0 + 32 * wv < n_rows) {
       advance(t0 - 1, 0);
       begin(t0, sa, 0);
@@ -448,29 +460,34 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 }
 
 // One workgroup per row tile and KV head.
-template <bool kF16, bool kExtra, bool kPage16>
+template <bool kF16, bool kCap, bool kBias, bool kPage16>
 __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendLaunch A) {
   __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];   // [buffer][K, V]
   __shared__ Bounds bounds;
   const int h = blockIdx.x % A.p.n_kv_heads;
   const int tile = A.n_tiles - 1 - blockIdx.x / A.p.n_kv_heads;   // a causal prompt's longest rows first
   const int seq = __builtin_amdgcn_readfirstlane(tile_sequence(A, tile));
-  const int row0 = uniform(first_row(A.a, seq)), n_q = uniform(end_row(A.a, seq)) - row0, r0 = uniform(tile - tile_start(A, seq)) * kRows;
+  const int row0 = uniform(first_row(A.a, seq)), n_q = uniform(end_row(A.a, seq)) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
   if (r0 < 0 || r0 >= n_q * A.group) return;
-  attend_rows<kF16, kExtra, kPage16>(A, smem, bounds, seq, row0, n_q, r0, h, 0, -1, nullptr);
+  attend_rows<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(slots_of(A, seq)), r0, h, 0, -1, nullptr);
 }
 
-// kShares workgroups with an equal share each of all items' key tiles, in the order (head, row tile, key tile).  Workgroup b
-// runs on XCD b % 8: it takes share (b % 8) kShares / 8 + b / 8, so that the row tiles of a head, which read the same
-// keys, meet in one L2.
-template <bool kF16, bool kExtra, bool kPage16>
-__global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunch A) {
-  __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];
-  __shared__ Bounds bounds;
-  __shared__ int64_t sBefore[kListed + 1];   // key tiles of a head before row tile i
-  __shared__ int64_t sWave[4];
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  constexpr int kPer = kListed / 256;
+// The list of row tiles that every workgroup of attend_shares_kernel makes.
+struct List {
+  int32_t row0[kListed + 1];     // first row of each sequence
+  int32_t slots[kListed];        // of each sequence
+  int32_t before[kListed + 1];   // key tiles of a head before row tile i
+  uint16_t seq[kListed];         // sequence of row tile i
+  int64_t wave[4];
+};
+constexpr int kPer = kListed / 256;   // row tiles of a thread
+
+// Fills the list; the key tiles of a head, which 32 bits may not hold.
+__device__ __forceinline__ int64_t make_list(const AttendLaunch& A, List& L) {
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = A.a.n_seqs;
+  for (int s = tid; s <= n; s += 256) L.row0[s] = s < n ? first_row(A.a, s) : end_row(A.a, n - 1);
+  for (int s = tid; s < n; s += 256) L.slots[s] = slots_of(A, s);
+  __syncthreads();
   int cost[kPer];
   int64_t sum = 0;
 #pragma unroll
@@ -478,16 +495,17 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
     const int tile = tid * kPer + i;
     cost[i] = 0;
     if (tile < A.n_tiles) {
-      int lo = 0, hi = A.a.n_seqs;
+      int lo = 0, hi = n;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (tile_start(A, mid) <= tile) lo = mid;
+        if (tile_start(A, L.row0[mid], mid) <= tile) lo = mid;
         else hi = mid;
       }
-      const int n_q = end_row(A.a, lo) - first_row(A.a, lo), r0 = (tile - tile_start(A, lo)) * kRows;
+      L.seq[tile] = (uint16_t)lo;
+      const int n_q = L.row0[lo + 1] - L.row0[lo], r0 = (tile - tile_start(A, L.row0[lo], lo)) * kRows;
       if (r0 >= 0 && r0 < n_q * A.group) {
         int t0, t1;
-        tile_span(A, lo, r0, n_q, slots_of(A, lo), t0, t1);
+        tile_span(A, lo, r0, n_q, L.slots[lo], t0, t1);
         cost[i] = max(1, t1 - t0);   // rows that see nothing are written too
       }
     }
@@ -499,50 +517,71 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
     const int64_t y = __shfl_up((long long)x, o);
     if (lane >= o) x += y;
   }
-  if (lane == 63) sWave[wv] = x;
+  if (lane == 63) L.wave[wv] = x;
   __syncthreads();
   int64_t before = x - sum;
-  for (int i = 0; i < wv; ++i) before += sWave[i];
+  for (int i = 0; i < wv; ++i) before += L.wave[i];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    sBefore[tid * kPer + i] = before;
+    L.before[tid * kPer + i] = (int32_t)before;
     before += cost[i];
   }
-  if (tid == 255) sBefore[kListed] = before;
+  if (tid == 255) L.before[kListed] = (int32_t)before;
+  const int64_t all = L.wave[0] + L.wave[1] + L.wave[2] + L.wave[3];
   __syncthreads();
-  const int64_t all = sBefore[kListed], total = all * A.p.n_kv_heads;
-  const int64_t share = max((int64_t)kLeast, (total + kShares - 1) / kShares);
+  return all;
+}
+
+// kShares workgroups with an equal share each of all items' key tiles, in the order (head, row tile, key tile).  Workgroup b
+// runs on XCD b % 8: it takes share (b % 8) kShares / 8 + b / 8, so that the row tiles of a head, which read the same
+// keys, meet in one L2.
+template <bool kF16, bool kCap, bool kBias, bool kPage16>
+__global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunch A) {
+  __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];
+  __shared__ Bounds bounds;
+  __shared__ List L;
+  const int tid = threadIdx.x;
+  const int64_t all = make_list(A, L);
   const int w = (int)(blockIdx.x % 8) * (kShares / 8) + (int)blockIdx.x / 8;
-  int64_t pos = w * share;
-  const int64_t end = min(total, pos + share);
   int record[8] = {};   // parts, sequence's first row, first row of the tile, rows of the sequence, head
-  while (pos < end) {
-    const int h = (int)(pos / all);
-    const int64_t rem = pos - h * all;
-    int lo = 0, hi = kListed;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (sBefore[mid] <= rem) lo = mid;
-      else hi = mid;
-    }
-    const int tile = __builtin_amdgcn_readfirstlane(lo);
-    const int u0 = uniform((int)(rem - sBefore[tile])), count = uniform((int)(sBefore[tile + 1] - sBefore[tile]));
-    const int n = (int)min((int64_t)(count - u0), end - pos);
-    const int seq = __builtin_amdgcn_readfirstlane(tile_sequence(A, tile));
-    const int row0 = uniform(first_row(A.a, seq)), n_q = uniform(end_row(A.a, seq)) - row0, r0 = uniform(tile - tile_start(A, seq)) * kRows;
-    float* part = nullptr;
-    if (n < count) {
-      part = part_slot(A, 2 * w + (u0 == 0));
-      if (u0 == 0) {
-        record[0] = (int)((pos + count - 1) / share) - w + 1;
-        record[1] = row0;
-        record[2] = r0;
-        record[3] = n_q * A.group;
-        record[4] = h;
+  if (all < (int64_t(1) << 31)) {
+    const int64_t total = all * A.p.n_kv_heads;
+    const int64_t share = max((int64_t)A.least, (total + kShares - 1) / kShares);
+    int64_t pos = w * share;
+    const int64_t end = min(total, pos + share);
+    while (pos < end) {
+      const int h = uniform((int)(pos / all)), rem = uniform((int)(pos - h * all));
+      int lo = 0, hi = kListed;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (L.before[mid] <= rem) lo = mid;
+        else hi = mid;
       }
+      const int tile = uniform(lo), seq = uniform(L.seq[tile]);
+      const int u0 = rem - uniform(L.before[tile]), count = uniform(L.before[tile + 1]) - uniform(L.before[tile]);
+      const int n = (int)min((int64_t)(count - u0), end - pos);
+      const int row0 = uniform(L.row0[seq]), n_q = uniform(L.row0[seq + 1]) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
+      float* part = nullptr;
+      if (n < count) {
+        part = part_slot(A, 2 * w + (u0 == 0));
+        if (u0 == 0) {
+          record[0] = (int)((pos + count - 1) / share) - w + 1;
+          record[1] = row0;
+          record[2] = r0;
+          record[3] = n_q * A.group;
+          record[4] = h;
+        }
+      }
+      attend_rows<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, u0, n, part);
+      pos += n;
     }
-    attend_rows<kF16, kExtra, kPage16>(A, smem, bounds, seq, row0, n_q, r0, h, u0, n, part);
-    pos += n;
+  } else {   // more key tiles than the list counts: whole row tiles in turn
+    for (int i = w; i < A.n_tiles * A.p.n_kv_heads; i += kShares) {
+      const int tile = i / A.p.n_kv_heads, h = i - tile * A.p.n_kv_heads, seq = uniform(L.seq[tile]);
+      const int row0 = uniform(L.row0[seq]), n_q = uniform(L.row0[seq + 1]) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
+      if (r0 < 0 || r0 >= n_q * A.group) continue;
+      attend_rows<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, 0, -1, nullptr);
+    }
   }
   if (tid < 8) {
     int v = 0;
@@ -609,26 +648,31 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A
   if (a.lse && c == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
 }
 
-template <bool kF16, bool kExtra, bool kPage16>
+template <bool kF16, bool kCap, bool kBias, bool kPage16>
 void launch_kernels(const AttendLaunch& A, hipStream_t st) {
   if (A.parts) {
-    attend_shares_kernel<kF16, kExtra, kPage16><<<kShares, 256, 0, st>>>(A);
+    attend_shares_kernel<kF16, kCap, kBias, kPage16><<<kShares, 256, 0, st>>>(A);
     join_kernel<kF16><<<dim3(kShares, (A.slot_rows + 31) / 32), kJoinThreads, 0, st>>>(A);
   } else {
-    attend_tiles_kernel<kF16, kExtra, kPage16><<<(unsigned)(A.n_tiles * A.p.n_kv_heads), 256, 0, st>>>(A);
+    attend_tiles_kernel<kF16, kCap, kBias, kPage16><<<(unsigned)(A.n_tiles * A.p.n_kv_heads), 256, 0, st>>>(A);
   }
 }
-template <bool kF16, bool kExtra>
+template <bool kF16, bool kCap, bool kBias>
 void launch_pages(const AttendLaunch& A, hipStream_t st) {
   const rkv_pages& p = A.p;
   const bool near = p.k_page < kStrideEnd && p.v_page < kStrideEnd && p.k_slot >= kHeadDim && p.v_slot >= kHeadDim;
-  if (p.page_size % 16 == 0 && near) launch_kernels<kF16, kExtra, true>(A, st);
-  else launch_kernels<kF16, kExtra, false>(A, st);
+  if (p.page_size % 16 == 0 && near) launch_kernels<kF16, kCap, kBias, true>(A, st);
+  else launch_kernels<kF16, kCap, kBias, false>(A, st);
 }
 template <bool kF16>
 void launch_type(const AttendLaunch& A, hipStream_t st) {
-  if (A.a.softcap > 0.f || A.a.slopes) launch_pages<kF16, true>(A, st);
-  else launch_pages<kF16, false>(A, st);
+  if (A.a.softcap > 0.f) {
+    if (A.a.slopes) launch_pages<kF16, true, true>(A, st);
+    else launch_pages<kF16, true, false>(A, st);
+  } else {
+    if (A.a.slopes) launch_pages<kF16, false, true>(A, st);
+    else launch_pages<kF16, false, false>(A, st);
+  }
 }
 
 }  // namespace

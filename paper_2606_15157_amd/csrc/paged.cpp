@@ -149,6 +149,7 @@ int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size
   L.by_group = rkv::fast_div(L.group);
   L.n_tiles = (int32_t)row_tiles(pages, a);
   L.slot_rows = tile_rows(pages, a);
+  L.least = 2;
   if (need) {
     L.records = static_cast<int32_t*>(ws);
     L.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kRecordBytes);

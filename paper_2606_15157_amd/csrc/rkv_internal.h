@@ -222,6 +222,7 @@ struct AttendLaunch {
   int32_t group;       // Hq / Hkv
   int32_t n_tiles;     // row tiles of all sequences, at most
   int32_t slot_rows;   // rows of a partial sum
+  int32_t least;       // key tiles of a share, at least
   int32_t* records;    // [kAttendShares][8], then
   float* parts;        // [2 kAttendShares] partial sums; null: a workgroup per row tile
 };

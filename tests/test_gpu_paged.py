@@ -240,7 +240,8 @@ def test_attention_over_head_layouts(hq, hkv):
 @pytest.mark.parametrize("lens", [ONE, MANY], ids=["one", "many"])
 @pytest.mark.parametrize("kw", [
     dict(causal=False), dict(window=1), dict(window=64), dict(window=50), dict(softcap=2.0), dict(softcap=50.0), dict(scale=0.5),
-    dict(scale=-0.2), dict(prefix_lens=1000), dict(prefix_lens=37), dict(prefix_lens=37, window=20), dict(slopes=True),
+    dict(scale=-0.2), dict(scale=0.0), dict(softcap=3.0, window=50), dict(softcap=3.0, slopes=True, window=50),
+    dict(prefix_lens=1000), dict(prefix_lens=37), dict(prefix_lens=37, window=20), dict(slopes=True),
     dict(slopes=True, softcap=5.0, prefix_lens=64), dict(first_keys="half"), dict(first_keys="beyond"), dict(causal=False, window=33)],
     ids=lambda d: "-".join(f"{k}{v}" for k, v in d.items()))
 def test_attention_masks_and_scores(lens, kw):
