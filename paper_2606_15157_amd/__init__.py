@@ -385,23 +385,18 @@ def decode_step(plan: Plan, state, q, k, v, position: int, *, victim_out=None, s
 
 # ---- paged caches
 
-def _same_device(dev, *tensors):
-    for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError("tensors must be on one device")
-
-
-def _int32(name, t, shape):
-    """Checks an int32 tensor of `shape` (None: any size), dense but for a table's row stride."""
-    if t.dtype is not _torch().int32 or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{name} must be int32 {list(shape)}")
-    if t.numel() and t.stride(-1) != 1 and t.shape[-1] != 1:
-        raise ValueError(f"{name} must be dense in its last dimension")
-
-
 def _torch():
     import torch
     return torch
+
+
+def _check_int32(name, t, shape, dev):
+    """An int32 tensor on `dev`, dense in its last dimension; shape: its sizes, -1 for any."""
+    if t.dtype is not _torch().int32 or t.device != dev:
+        raise ValueError(f"{name} must be int32 on the pool's device")
+    have = t.shape
+    if len(have) != len(shape) or (have[0] != shape[0] and shape[0] != -1) or (t.stride(-1) != 1 and have[-1] > 1):
+        raise ValueError(f"{name} must have shape {list(shape)} and a dense last dimension, not {list(have)}")
 
 
 def _elsewhere(dev, stream):
@@ -418,7 +413,10 @@ def _elsewhere(dev, stream):
 
 
 def _raw_stream(dev):
-    return _torch().cuda.current_stream(dev).cuda_stream
+    """The current stream's handle (torch's own accessor for generated code: a Stream object costs ten times as much)."""
+    torch = _torch()
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(dev.index) if get else torch.cuda.current_stream(dev).cuda_stream
 
 
 class PagedCache:
@@ -434,13 +432,14 @@ class PagedCache:
             raise ValueError("pages must be bf16 or fp16")
         if k_pages.stride(3) != 1 or v_pages.stride(3) != 1:
             raise ValueError("pages must be dense in their last dimension")
-        _same_device(k_pages.device, v_pages)
+        if k_pages.device != v_pages.device:
+            raise ValueError("pages must be on one device")
         self.k_pages, self.v_pages = k_pages, v_pages
         self.device, self.dtype = k_pages.device, k_pages.dtype
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k_pages.shape
-        self._c = _abi.Pages(k_pages.data_ptr(), v_pages.data_ptr(), *k_pages.stride()[:3], *v_pages.stride()[:3], self.n_pages,
-                             self.page_size, self.n_kv_heads, self.head_dim, _abi.BF16 if self.dtype == torch.bfloat16 else _abi.F16)
-        self._ref = C.byref(self._c)
+        self._pack = _abi.Pages.pack(k_pages.data_ptr(), v_pages.data_ptr(), *k_pages.stride()[:3], *v_pages.stride()[:3], self.n_pages,
+                                     self.page_size, self.n_kv_heads, self.head_dim, _abi.BF16 if self.dtype == torch.bfloat16 else _abi.F16)
+        self._bytes = {}     # workspace sizes by what they depend on
 
 
 def pages_init(n_seqs: int, max_pages: int, n_pages: int, page_size: int, device="cuda"):
@@ -459,7 +458,6 @@ def pages_resize(pages, new_lens, max_new: int, *, in_place=True, stream=None):
     tokens, -1 behind the last, "cu_new" int32 [n_seqs + 1], "status" int32 [1] (0, or PAGES_EXHAUSTED / PAGES_INVALID: nothing
     changed), "lens", "cursor"}.  in_place: lens and cursor of `pages` become the new ones; else they stay, and the new ones
     are only returned (the table's entries past the old lengths and the ring's behind the free ones are written all the same)."""
-    torch = _torch()
     table, lens, ring, cursor = pages["table"], pages["lens"], pages["ring"], pages["cursor"]
     dev = table.device
     ctx = _elsewhere(dev, stream)
@@ -467,21 +465,24 @@ def pages_resize(pages, new_lens, max_new: int, *, in_place=True, stream=None):
         with ctx:
             return pages_resize(pages, new_lens, max_new, in_place=in_place)
     n = lens.shape[0]
-    _same_device(dev, lens, ring, cursor, new_lens)
-    _int32("table", table, (n, None))
-    _int32("lens", lens, (n,))
-    _int32("new_lens", new_lens, (n,))
-    _int32("ring", ring, (None,))
-    _int32("cursor", cursor, (2,))
-    lens_out, cursor_out = (lens, cursor) if in_place else (torch.empty_like(lens), torch.empty_like(cursor))
-    slots = torch.empty(max_new, dtype=torch.int32, device=dev)
-    cu_new = torch.empty(n + 1, dtype=torch.int32, device=dev)
-    status = torch.empty(1, dtype=torch.int32, device=dev)
-    r = _abi.Resize(lens.data_ptr(), new_lens.data_ptr(), lens_out.data_ptr(), table.data_ptr(), table.stride(0), ring.data_ptr(),
-                    cursor.data_ptr(), cursor_out.data_ptr(), slots.data_ptr(), cu_new.data_ptr(), status.data_ptr(), n, table.shape[1],
-                    ring.shape[0], pages["page_size"], max_new)
-    check(_abi.lib().rkv_pages_resize(C.byref(r), _raw_stream(dev)))
-    return {"slots": slots, "cu_new": cu_new, "status": status, "lens": lens_out, "cursor": cursor_out}
+    _check_int32("table", table, (n, -1), dev)
+    _check_int32("lens", lens, (n,), dev)
+    _check_int32("new_lens", new_lens, (n,), dev)
+    _check_int32("ring", ring, (-1,), dev)
+    _check_int32("cursor", cursor, (2,), dev)
+    if max_new < 0:
+        raise ValueError("max_new must be >= 0")
+    torch = _torch()
+    if in_place:
+        slots, cu_new, status = torch.empty(max_new + n + 2, dtype=torch.int32, device=dev).split_with_sizes((max_new, n + 1, 1))
+    else:
+        slots, cu_new, status, lens, cursor = torch.empty(max_new + 2 * n + 4, dtype=torch.int32, device=dev).split_with_sizes(
+            (max_new, n + 1, 1, n, 2))
+    r = _abi.Resize.pack(pages["lens"].data_ptr(), new_lens.data_ptr(), lens.data_ptr(), table.data_ptr(), table.stride(0), ring.data_ptr(),
+                         pages["cursor"].data_ptr(), cursor.data_ptr(), slots.data_ptr(), cu_new.data_ptr(), status.data_ptr(), n,
+                         table.shape[1], ring.shape[0], pages["page_size"], max_new)
+    check(_abi.lib().rkv_pages_resize(r, _raw_stream(dev)))
+    return {"slots": slots, "cu_new": cu_new, "status": status, "lens": lens, "cursor": cursor}
 
 
 def pages_write(cache: PagedCache, k, v, slots, *, stream=None):
@@ -492,18 +493,18 @@ def pages_write(cache: PagedCache, k, v, slots, *, stream=None):
     if ctx is not None:
         with ctx:
             return pages_write(cache, k, v, slots)
-    if k.shape != v.shape or k.dim() not in (3, 4) or k.shape[-2:] != (cache.n_kv_heads, cache.head_dim):
+    shape, ks, vs = k.shape, k.stride(), v.stride()
+    if shape != v.shape or len(shape) not in (3, 4) or shape[-2] != cache.n_kv_heads or shape[-1] != cache.head_dim:
         raise ValueError("k and v must have shape [T, Hkv, d] or [B, n, Hkv, d]")
-    if k.dtype != cache.dtype or v.dtype != cache.dtype or k.stride(-1) != 1 or v.stride(-1) != 1:
-        raise ValueError("k and v must be of the pool's type and dense in their last dimension")
-    _same_device(dev, k, v, slots)
-    outer, n = (1, k.shape[0]) if k.dim() == 3 else k.shape[:2]
-    _int32("slots", slots, (outer * n,))
-    ks, vs = k.stride(), v.stride()
-    if k.dim() == 3:
-        ks, vs = (0, *ks), (0, *vs)
-    rows = _abi.Rows(k.data_ptr(), v.data_ptr(), *ks[:3], *vs[:3], slots.data_ptr(), outer, n)
-    check(_abi.lib().rkv_pages_write(cache._ref, C.byref(rows), _raw_stream(dev)))
+    if k.dtype != cache.dtype or v.dtype != cache.dtype or ks[-1] != 1 or vs[-1] != 1 or k.device != dev or v.device != dev:
+        raise ValueError("k and v must be of the pool's type, on its device and dense in their last dimension")
+    if len(shape) == 3:
+        outer, n, ks, vs = 1, shape[0], (0, *ks), (0, *vs)
+    else:
+        outer, n = shape[0], shape[1]
+    _check_int32("slots", slots, (outer * n,), dev)
+    rows = _abi.Rows.pack(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], slots.data_ptr(), outer, n)
+    check(_abi.lib().rkv_pages_write(cache._pack, rows, _raw_stream(dev)))
 
 
 def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_kv=0, scale=None, causal=True, window=0, softcap=0.0,
@@ -518,7 +519,6 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
     every row of the sequence sees; first_keys int32 [T]: the first slot a row sees.  Returns out [T, Hq, d] (`out` if given: rows
     behind the last sequence stay as they are; a row that sees nothing is 0), and with return_lse or lse_out also fp32
     [T, Hq], the logarithm of the sum of exponentials (-inf for a row that sees nothing)."""
-    torch = _torch()
     dev = cache.device
     ctx = _elsewhere(dev, stream)
     if ctx is not None:
@@ -526,37 +526,55 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
             return pages_attend(cache, q, table, lens, cu_q, max_q=max_q, max_kv=max_kv, scale=scale, causal=causal, window=window,
                                 softcap=softcap, slopes=slopes, prefix_lens=prefix_lens, first_keys=first_keys, out=out, lse_out=lse_out,
                                 return_lse=return_lse)
-    if q.dim() != 3 or q.shape[2] != cache.head_dim or q.dtype != cache.dtype or q.stride(2) != 1:
-        raise ValueError("q must have shape [T, Hq, d], the pool's type and a dense last dimension")
-    T, Hq, d = q.shape
+    torch = _torch()
+    shape, qs = q.shape, q.stride()
+    if len(shape) != 3 or shape[2] != cache.head_dim or q.dtype != cache.dtype or qs[2] != 1 or q.device != dev:
+        raise ValueError("q must have shape [T, Hq, d], the pool's type and device and a dense last dimension")
+    T, Hq, d = shape
     n = lens.shape[0]
-    _same_device(dev, q, table, lens, cu_q, slopes, prefix_lens, first_keys, out, lse_out)
-    _int32("table", table, (n, None))
-    _int32("lens", lens, (n,))
-    for name, t, size in (("cu_q", cu_q, n + 1), ("prefix_lens", prefix_lens, n), ("first_keys", first_keys, T)):
-        if t is not None:
-            _int32(name, t, (size,))
-    if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (Hq,) or not slopes.is_contiguous()):
-        raise ValueError("slopes must be contiguous fp32 [Hq]")
+    _check_int32("table", table, (n, -1), dev)
+    _check_int32("lens", lens, (n,), dev)
+    cu = prefix = first = slope = lse_ptr = 0
+    if cu_q is not None:
+        _check_int32("cu_q", cu_q, (n + 1,), dev)
+        cu = cu_q.data_ptr()
+    if prefix_lens is not None:
+        _check_int32("prefix_lens", prefix_lens, (n,), dev)
+        prefix = prefix_lens.data_ptr()
+    if first_keys is not None:
+        _check_int32("first_keys", first_keys, (T,), dev)
+        first = first_keys.data_ptr()
+    if slopes is not None:
+        if slopes.dtype != torch.float32 or slopes.shape != (Hq,) or not slopes.is_contiguous() or slopes.device != dev:
+            raise ValueError("slopes must be contiguous fp32 [Hq] on the pool's device")
+        slope = slopes.data_ptr()
     if out is None:
-        out = torch.empty((T, Hq, d), dtype=q.dtype, device=dev)
-    elif out.shape != q.shape or out.dtype != q.dtype or out.stride(2) != 1:
-        raise ValueError("out must have q's shape and type and a dense last dimension")
-    if lse_out is None:
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev) if return_lse else None
-    elif lse_out.shape != (T, Hq) or lse_out.dtype != torch.float32 or not lse_out.is_contiguous():
-        raise ValueError("lse_out must be contiguous fp32 [T, Hq]")
-    else:
-        lse = lse_out
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    a = _abi.Attend(q.data_ptr(), out.data_ptr(), ptr(lse), q.stride(0), q.stride(1), out.stride(0), out.stride(1), table.data_ptr(),
-                    table.stride(0), lens.data_ptr(), ptr(cu_q), ptr(prefix_lens), ptr(first_keys), ptr(slopes), n, T, Hq, table.shape[1],
-                    max_q, max_kv, bool(causal), window, d ** -0.5 if scale is None else scale, softcap)
+        out = torch.empty(shape, dtype=q.dtype, device=dev)
+    elif out.shape != shape or out.dtype != q.dtype or out.stride(2) != 1 or out.device != dev:
+        raise ValueError("out must have q's shape, type and device and a dense last dimension")
+    lse = lse_out
+    if lse is None:
+        if return_lse:
+            lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+    elif lse.shape != (T, Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev:
+        raise ValueError("lse_out must be contiguous fp32 [T, Hq] on the pool's device")
+    if lse is not None:
+        lse_ptr = lse.data_ptr()
+    os, width = out.stride(), table.shape[1]
+    a = _abi.Attend.pack(q.data_ptr(), out.data_ptr(), lse_ptr, qs[0], qs[1], os[0], os[1], table.data_ptr(), table.stride(0),
+                         lens.data_ptr(), cu, prefix, first, slope, n, T, Hq, width, max_q, max_kv, bool(causal), window,
+                         d ** -0.5 if scale is None else scale, softcap)
     L = _abi.lib()
-    nbytes = C.c_size_t()
-    check(L.rkv_pages_attend_workspace_size(cache._ref, C.byref(a), C.byref(nbytes)))
-    ws = torch.empty(nbytes.value, dtype=torch.uint8, device=dev) if nbytes.value else None
-    check(L.rkv_pages_attend(cache._ref, C.byref(a), ptr(ws), nbytes.value, _raw_stream(dev)))
+    key = (T, Hq, n, width, max_q, max_kv, cu != 0)
+    nbytes = cache._bytes.get(key)
+    if nbytes is None:
+        size = C.c_size_t()
+        check(L.rkv_pages_attend_workspace_size(cache._pack, a, C.byref(size)))
+        if len(cache._bytes) >= 1024:
+            cache._bytes.clear()
+        nbytes = cache._bytes[key] = size.value
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    check(L.rkv_pages_attend(cache._pack, a, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev)))
     return out if lse is None else (out, lse)
 
 

@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "librkv.so")
@@ -65,32 +66,53 @@ class DecodeInput(C.Structure):
                 ("victim_out", C.POINTER(C.c_void_p))]
 
 
-def _fields(*groups):
-    return [(name, kind) for kind, names in groups for name in names.split()]
+# The paged caches' structs are passed packed (struct.pack with native alignment is the C layout): a call then costs no
+# ctypes object with a setter per field.
+def _layout(*groups):
+    """(ctypes fields, struct format) of groups ("P" pointer, "q" int64, "i" int32, "f" float; names)."""
+    kinds = {"P": C.c_void_p, "q": C.c_int64, "i": C.c_int32, "f": C.c_float}
+    return ([(name, kinds[k]) for k, names in groups for name in names.split()],
+            "".join(k * len(names.split()) for k, names in groups))
+
+
+def _packer(layout):
+    pack = struct.Struct(layout[1] + "0P").pack
+
+    def packed(*values):
+        try:
+            return pack(*values)
+        except (struct.error, OverflowError) as e:
+            raise ValueError(f"an argument is out of its range: {e}") from None
+    return staticmethod(packed)
+
+
+_PAGES = _layout(("P", "k v"), ("q", "k_page k_head k_slot v_page v_head v_slot"), ("i", "n_pages page_size n_kv_heads head_dim dtype"))
+_RESIZE = _layout(("P", "lens new_lens lens_out table"), ("q", "table_stride"), ("P", "ring cursor cursor_out slots cu_new status"),
+                  ("i", "n_seqs max_pages n_pages page_size max_new"))
+_ROWS = _layout(("P", "k v"), ("q", "k_outer k_token k_head v_outer v_token v_head"), ("P", "slots"), ("i", "n_outer n_tokens"))
+_ATTEND = _layout(("P", "q out lse"), ("q", "q_token q_head out_token out_head"), ("P", "table"), ("q", "table_stride"),
+                  ("P", "lens cu_q prefix_lens first_keys slopes"),
+                  ("i", "n_seqs n_rows n_q_heads max_pages max_q max_kv causal window"), ("f", "scale softcap"))
 
 
 class Pages(C.Structure):
-    _fields_ = _fields((C.c_void_p, "k v"), (C.c_int64, "k_page k_head k_slot v_page v_head v_slot"),
-                       (C.c_int32, "n_pages page_size n_kv_heads head_dim dtype"))
+    _fields_ = _PAGES[0]
+    pack = _packer(_PAGES)
 
 
 class Resize(C.Structure):
-    _fields_ = _fields((C.c_void_p, "lens new_lens lens_out table"), (C.c_int64, "table_stride"),
-                       (C.c_void_p, "ring cursor cursor_out slots cu_new status"),
-                       (C.c_int32, "n_seqs max_pages n_pages page_size max_new"))
+    _fields_ = _RESIZE[0]
+    pack = _packer(_RESIZE)
 
 
 class Rows(C.Structure):
-    _fields_ = _fields((C.c_void_p, "k v"), (C.c_int64, "k_outer k_token k_head v_outer v_token v_head"),
-                       (C.c_void_p, "slots"), (C.c_int32, "n_outer n_tokens"))
+    _fields_ = _ROWS[0]
+    pack = _packer(_ROWS)
 
 
 class Attend(C.Structure):
-    _fields_ = _fields((C.c_void_p, "q out lse"), (C.c_int64, "q_token q_head out_token out_head"),
-                       (C.c_void_p, "table"), (C.c_int64, "table_stride"),
-                       (C.c_void_p, "lens cu_q prefix_lens first_keys slopes"),
-                       (C.c_int32, "n_seqs n_rows n_q_heads max_pages max_q max_kv causal window"),
-                       (C.c_float, "scale softcap"))
+    _fields_ = _ATTEND[0]
+    pack = _packer(_ATTEND)
 
 
 _lib = None
@@ -128,10 +150,10 @@ def lib():
         L.rkv_entropy_profile.argtypes = [C.POINTER(Shape), C.c_int32, C.c_int32, C.POINTER(C.c_void_p),
                                           C.POINTER(C.c_void_p), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                           C.c_size_t, C.c_void_p]
-        L.rkv_pages_resize.argtypes = [C.POINTER(Resize), C.c_void_p]
-        L.rkv_pages_write.argtypes = [C.POINTER(Pages), C.POINTER(Rows), C.c_void_p]
-        L.rkv_pages_attend_workspace_size.argtypes = [C.POINTER(Pages), C.POINTER(Attend), C.POINTER(C.c_size_t)]
-        L.rkv_pages_attend.argtypes = [C.POINTER(Pages), C.POINTER(Attend), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.rkv_pages_resize.argtypes = [C.c_void_p, C.c_void_p]      # structs: byref, or packed bytes
+        L.rkv_pages_write.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
+        L.rkv_pages_attend_workspace_size.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]
+        L.rkv_pages_attend.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.rkv_profile_enable.argtypes = [C.c_int32]
         L.rkv_profile_read.argtypes = [C.POINTER(C.c_int32), C.POINTER(C.c_double)]
         L.rkv_last_error.restype = C.c_char_p

@@ -592,21 +592,21 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
   }
 }
 
-// Workgroup (w, y): rows 32 y .. 32 y + 31 of the item that begins in share w and ends in a later one.  32 lanes hold the 128
-// values of a row; with fewer than 32 rows, several such groups take a row's parts in turn and meet in LDS.
-constexpr int kJoinThreads = 1024;
+// Workgroup (w, y): rows 8 y .. 8 y + 7 of the item that begins in share w and ends in a later one.  32 lanes hold the 128
+// values of a row; with fewer than 8 rows, several such groups take a row's parts in turn and meet in LDS.
+constexpr int kJoinRows = 8;
 template <bool kF16>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A) {
-  __shared__ f32x4 sO[32][32];
+__global__ __launch_bounds__(32 * kJoinRows) void join_kernel(const AttendLaunch A) {
+  __shared__ f32x4 sO[kJoinRows][32];
   const int* record = A.records + 8 * blockIdx.x;
-  const int parts = record[0], y0 = 32 * blockIdx.y;
+  const int parts = record[0], y0 = kJoinRows * blockIdx.y;
   if (parts == 0) return;
   const int row0 = record[1], r0 = record[2], h = record[4];
-  const int rows = min(32, min(kRows, record[3] - r0) - y0);
+  const int rows = min(kJoinRows, min(kRows, record[3] - r0) - y0);
   if (rows <= 0) return;
   const rkv_attend& a = A.a;
   const int grp = threadIdx.x >> 5, c = threadIdx.x & 31;
-  const int each = 32 / rows;                       // groups of a row
+  const int each = kJoinRows / rows;                 // groups of a row
   const int i = grp / each, g = grp - i * each;     // row, and place among its groups
   const bool in = i < rows;
   const int w = blockIdx.x, k = y0 + (in ? i : 0);
@@ -652,7 +652,7 @@ template <bool kF16, bool kCap, bool kBias, bool kPage16>
 void launch_kernels(const AttendLaunch& A, hipStream_t st) {
   if (A.parts) {
     attend_shares_kernel<kF16, kCap, kBias, kPage16><<<kShares, 256, 0, st>>>(A);
-    join_kernel<kF16><<<dim3(kShares, (A.slot_rows + 31) / 32), kJoinThreads, 0, st>>>(A);
+    join_kernel<kF16><<<dim3(kShares, (A.slot_rows + kJoinRows - 1) / kJoinRows), 32 * kJoinRows, 0, st>>>(A);
   } else {
     attend_tiles_kernel<kF16, kCap, kBias, kPage16><<<(unsigned)(A.n_tiles * A.p.n_kv_heads), 256, 0, st>>>(A);
   }

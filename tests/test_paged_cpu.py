@@ -157,10 +157,21 @@ def test_binding_refuses_what_the_library_would_misread():
 
 def test_workspace_is_checked():
     L, n = _abi.lib(), C.c_size_t()
-    assert L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(attend()), C.byref(n)) == 0
+    assert L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(attend(max_pages=100, table_stride=100)), C.byref(n)) == 0
     assert n.value > 0
-    refused(5, L.rkv_pages_attend(C.byref(pages()), C.byref(attend()), None, n.value, None))
-    refused(5, L.rkv_pages_attend(C.byref(pages()), C.byref(attend()), C.c_void_p(P + 16), n.value, None))
-    refused(5, L.rkv_pages_attend(C.byref(pages()), C.byref(attend()), C.c_void_p(P), n.value - 1, None))
-    assert L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(attend(n_rows=0)), C.byref(n)) == 0 and n.value == 0
+    refused(5, L.rkv_pages_attend(C.byref(pages()), C.byref(attend(max_pages=100, table_stride=100)), None, n.value, None))
+    refused(5, L.rkv_pages_attend(C.byref(pages()), C.byref(attend(max_pages=100, table_stride=100)), C.c_void_p(P + 16), n.value, None))
+    refused(5, L.rkv_pages_attend(C.byref(pages()), C.byref(attend(max_pages=100, table_stride=100)), C.c_void_p(P), n.value - 1, None))
+    assert L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(attend(n_rows=0, max_pages=100, table_stride=100)), C.byref(n)) == 0 and n.value == 0
     refused(4, L.rkv_pages_attend(C.byref(pages()), C.byref(attend(n_seqs=1 << 30)), None, 0, None))
+    # short sequences are not split: nothing to keep
+    assert L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(attend()), C.byref(n)) == 0 and n.value == 0
+
+
+def test_packed_structs_are_the_c_ones():
+    for cls, kinds in ((_abi.Pages, _abi._PAGES[1]), (_abi.Resize, _abi._RESIZE[1]), (_abi.Rows, _abi._ROWS[1]), (_abi.Attend, _abi._ATTEND[1])):
+        values = [float(i) if k == "f" else i + 1 for i, k in enumerate(kinds)]
+        got = cls.from_buffer_copy(cls.pack(*values))
+        assert [getattr(got, name) for name, _ in cls._fields_] == values
+        with pytest.raises(ValueError):
+            cls.pack(*([1 << 70] * len(kinds)))
