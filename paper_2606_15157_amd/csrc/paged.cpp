@@ -60,7 +60,7 @@ int check_attend(const rkv_pages* p, const rkv_attend* a) {
   if (a->table_stride < a->max_pages) return rkv::fail(RKV_ERR_SHAPE, "table_stride is less than max_pages");
   if ((int64_t)a->max_pages * p->page_size >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "a sequence holds fewer than 2^31 slots");
   if ((int64_t)a->n_rows * a->n_q_heads >= kIntEnd / 2) return rkv::fail(RKV_ERR_UNSUPPORTED, "n_rows * n_q_heads must be below 2^30");
-  if (row_tiles(p, a) * p->n_kv_heads >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "too many sequences");
+  if ((row_tiles(p, a) + a->n_seqs) * p->n_kv_heads >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "too many sequences");
   if (int st = check_layout("q", a->q, {a->q_token, a->q_head})) return st;
   return check_layout("out", a->out, {a->out_token, a->out_head});
 }
@@ -163,6 +163,9 @@ int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size
   L.by_page = rkv::fast_div(pages->page_size);
   L.by_group = rkv::fast_div(L.group);
   L.n_tiles = (int32_t)row_tiles(pages, a);
+  const int64_t full = (int64_t)a->n_rows * L.group / rkv::kAttendRows;
+  L.few_long = 2 * full < L.n_tiles;
+  L.n_places = a->n_seqs + (int32_t)std::min<int64_t>(2 * full, L.n_tiles);
   L.slot_rows = tile_rows(pages, a);
   // a part of 128 rows is written and read again, as many bytes as four key tiles: not for less than eight
   L.least = L.slot_rows > 32 ? 8 : 2;

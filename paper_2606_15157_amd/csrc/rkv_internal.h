@@ -221,6 +221,8 @@ struct AttendLaunch {
   FastDiv by_page, by_group;
   int32_t group;       // Hq / Hkv
   int32_t n_tiles;     // row tiles of all sequences, at most
+  int32_t n_places;    // places of attend_tiles_kernel: n_seqs, then numbers of long sequences' tiles
+  int32_t few_long;    // how those are numbered
   int32_t slot_rows;   // rows of a partial sum
   int32_t least;       // key tiles of a share, at least
   int32_t* records;    // [kAttendShares][8], then

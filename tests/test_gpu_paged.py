@@ -159,13 +159,13 @@ def test_write_and_attend_past_32_bit_offsets():
 class Case:
     """Pools whose every slot outside the sequences holds NaN, tables, and queries."""
 
-    def __init__(self, lens, hq=4, hkv=2, page=16, dtype=torch.bfloat16, seed=0, pad=0, spread=1.0, nhd=False):
+    def __init__(self, lens, hq=4, hkv=2, page=16, dtype=torch.bfloat16, seed=0, pad=0, spread=1.0, nhd=False, width=0):
         rng = np.random.default_rng(seed)
         self.lens, self.page, self.dtype = lens, page, dtype
         counts = [-(-n // page) for _, n in lens]
         n_pages = sum(counts) + 2
         ids = rng.permutation(n_pages)
-        self.table = np.full((len(lens), max(counts + [1]) + 1), -1, dtype=np.int32)
+        self.table = np.full((len(lens), max(counts + [width]) + 1), -1, dtype=np.int32)
         shape = (n_pages, page, hkv, 128) if nhd else (n_pages, hkv, page, 128)
         self.k, self.v = (torch.full(shape, NAN, dtype=dtype, device="cuda") for _ in range(2))
         if nhd:
@@ -258,6 +258,30 @@ def test_attention_masks_and_scores(lens, kw):
     out, lse = c.check(**kw)
     if kw.get("first_keys") and kw["first_keys"][0] > 0:
         assert (out[0] == 0).all() and torch.isneginf(lse[0]).all()
+
+
+@pytest.mark.parametrize("lens", [MANY, [(300, 4000)], [(1, 2000), (200, 260), (1, 1), (70, 3000), (0, 9), (129, 129), (1, 700)]], ids=["many", "chunk", "mixed"])
+@pytest.mark.parametrize("kw", [dict(), dict(window=70), dict(prefix_lens=50), dict(first_keys="half"), dict(softcap=4.0, slopes=True)],
+                         ids=lambda d: "-".join(f"{k}{v}" for k, v in d.items()) or "plain")
+@pytest.mark.parametrize("page", [16, 30])
+def test_row_tiles_that_share_the_chip(lens, kw, page):
+    """Tables wide enough for sequences of 16K slots: the tiles' keys are shared out, and split rows joined."""
+    kw = dict(kw)
+    c = Case(lens, hq=4, hkv=1, page=page, seed=21, width=16384 // page)
+    if "slopes" in kw:
+        kw["slopes"] = np.array([0.5, 0.1, 0.02, 0.003], dtype=np.float32)
+    if "prefix_lens" in kw:
+        kw["prefix_lens"] = [kw["prefix_lens"]] * len(lens)
+    if "first_keys" in kw:
+        kw["first_keys"] = [(n - m + i) // 2 for m, n in lens for i in range(m)]
+    c.check(**kw)
+
+
+def test_more_row_tiles_than_are_listed():
+    """1100 sequences: a workgroup per tile, decoding sequences before chunks, in either numbering of the tiles."""
+    lens = [(1, 1 + 7 * s % 90) for s in range(1098)]
+    Case(lens + [(100, 300), (65, 65)], hq=2, hkv=1, seed=22).check()
+    Case([(130, 140)] * 40 + [(1, 33)] * 3, hq=2, hkv=1, seed=23).check()
 
 
 def test_queries_before_the_first_slot_see_nothing():
