@@ -123,9 +123,115 @@ __device__ __forceinline__ float* part_slot(const AttendLaunch& A, int slot) {
   return A.parts + (size_t)slot * A.slot_rows * (kHeadDim + 2);
 }
 
-struct Bounds {
-  int lo[4];   // of the waves
+struct Bounds {   // of the waves
+  int lo[4], all_lo[4], bad[4];
 };
+// The workgroup's LDS operations are done; vector memory operations stay in flight.
+__device__ __forceinline__ void lds_sync() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt 0
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// Whether some wave of the workgroup says so.
+__device__ __forceinline__ bool any_wave(Bounds& bounds, bool here) {
+  const bool any = __any(here);
+  if ((threadIdx.x & 63) == 0) bounds.bad[threadIdx.x >> 6] = any;
+  lds_sync();
+  const bool all = uniform(bounds.bad[0] | bounds.bad[1] | bounds.bad[2] | bounds.bad[3]);
+  lds_sync();
+  return all;
+}
+// Two 16-bit values.
+template <bool kF16>
+__device__ __forceinline__ f32x2 widen(uint32_t v) {
+  if constexpr (kF16) return __builtin_convertvector(__builtin_bit_cast(f16x2, v), f32x2);
+  else return f32x2{__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)};
+}
+
+// Probability 0 times what a hidden slot holds is no 0 if that is infinite or NaN.  A tile whose rows see different slots and
+// some of whose sums are not finite comes here (screening every tile of V instead cost packed documents 63 -> 80 us): if
+// no slot that only some of its rows see is to blame, the sums stand; else its rows are summed up one by one, a wave
+// each, two columns a lane, over the slots that they see and no others, and written: true.
+template <bool kF16, bool kCap, bool kBias>
+__device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds& bounds, int seq, int row0, int n_q, int n_kv, int r0,
+                                                  int h, int from, int to, int b_lo, int every_lo, int every_hi, int b_hi, float* part) {
+  const rkv_attend& a = A.a;
+  const rkv_pages& p = A.p;
+  const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+  const int32_t* table = a.table + seq * a.table_stride;
+  const uint16_t* kp = static_cast<const uint16_t*>(p.k) + h * p.k_head + 2 * lane;
+  const uint16_t* vp = static_cast<const uint16_t*>(p.v) + h * p.v_head + 2 * lane;
+  auto place = [&](int key, int& page, int& at) {
+    const int c = div_by(key, A.by_page);
+    page = uniform(table[c]);
+    at = key - c * p.page_size;
+    return (uint32_t)page < (uint32_t)p.n_pages;
+  };
+  auto pair_at = [&](const uint16_t* x, int page, int at, int64_t page_stride, int64_t slot) {
+    return widen<kF16>(*reinterpret_cast<const uint32_t*>(x + page * page_stride + at * slot));
+  };
+  bool blame = false;
+  for (int part_of = 0; part_of < 2; ++part_of) {
+    const int k0 = max(from, part_of ? max(b_lo, every_hi) : b_lo), k1 = min(to, part_of ? b_hi : min(b_hi, every_lo));
+    for (int key = k0 + wv; key < k1; key += 4) {
+      int page, at;
+      if (!place(key, page, at)) continue;
+      const f32x2 v = pair_at(vp, page, at, p.v_page, p.v_slot);
+      blame |= v[0] * 0.f + v[1] * 0.f != 0.f;
+    }
+  }
+  if (!any_wave(bounds, blame)) return false;
+  const int n_rows = n_q * A.group, prefix = a.prefix_lens ? uniform(a.prefix_lens[seq]) : 0;
+  const float cap2 = 2.f * kLog2e * a.softcap;
+#pragma unroll 1
+  for (int i = 0; i < 32; ++i) {
+    const int mine = 32 * wv + i, r = r0 + mine;
+    if (r >= n_rows) break;
+    const int t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group, pos = n_kv - n_q + t;
+    const int64_t row = row0 + t;
+    int hi = a.causal ? min(n_kv, max(pos + 1, prefix)) : n_kv, lo = a.window ? max(0, pos - a.window + 1) : 0;
+    if (a.first_keys) lo = max(lo, uniform(a.first_keys[row]));
+    lo = max(lo, from);
+    hi = min(hi, to);
+    const f32x2 q = widen<kF16>(*reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(a.q) + row * a.q_token + hq * a.q_head + 2 * lane));
+    const float slope = kBias ? a.slopes[hq] * kLog2e : 0.f;
+    float m = -__builtin_inff(), l = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll 1
+    for (int key = lo; key < hi; ++key) {
+      int page, at;
+      f32x2 k = {0.f, 0.f}, v = {0.f, 0.f};
+      if (place(key, page, at)) {
+        k = pair_at(kp, page, at, p.k_page, p.k_slot);
+        v = pair_at(vp, page, at, p.v_page, p.v_slot);
+      }
+      float x = fmaf(q[0], k[0], q[1] * k[1]);
+#pragma unroll
+      for (int s = 32; s > 0; s >>= 1) x += __shfl_xor(x, s);
+      x *= a.scale;
+      if constexpr (kCap) x = 0.5f * cap2 - cap2 / (1.f + __builtin_amdgcn_exp2f(2.f * kLog2e / a.softcap * x));
+      else x *= kLog2e;
+      if constexpr (kBias) x -= slope * fabsf((float)(pos - key));
+      const float m2 = fmaxf(m, x), ref = m2 == -__builtin_inff() ? 0.f : m2;
+      const float f = __builtin_amdgcn_exp2f(m - ref), e = __builtin_amdgcn_exp2f(x - ref);
+      m = m2;
+      l = fmaf(l, f, e);
+      o0 = fmaf(o0, f, e * v[0]);
+      o1 = fmaf(o1, f, e * v[1]);
+    }
+    if (part) {
+      part[mine * kHeadDim + 2 * lane] = o0;
+      part[mine * kHeadDim + 2 * lane + 1] = o1;
+      part[A.slot_rows * kHeadDim + mine] = m;
+      part[A.slot_rows * (kHeadDim + 1) + mine] = l;
+    } else {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head)[lane] = pack<kF16>(o0 * inv, o1 * inv);
+      if (a.lse) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
+    }
+  }
+  return true;
+}
 
 // kCap: capped scores, kBias: less a slope times the distance; kPage16: page_size % 16 = 0, pages less than 4 GiB and slots at least a
 // row apart.  Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
@@ -145,7 +251,8 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   auto lo_of = [&](int at) { return a.window ? max(0, at - a.window + 1) : 0; };
   auto position = [&](int r) { return n_kv - n_q + div_by(min(r, n_rows - 1), A.by_group); };   // rows behind the last repeat it
   int b_lo = lo_of(position(r0)), b_hi = hi_of(position(r0 + kRows - 1));                       // slots some row sees
-  int all_lo = lo_of(position(r0 + 32 * wv + 31)), all_hi = hi_of(position(r0 + 32 * wv));      // that every row of the wave sees
+  int all_lo = lo_of(position(r0 + 32 * wv + 31)), all_hi = hi_of(position(r0 + 32 * wv));      // every row of the wave
+  int every_lo = lo_of(position(r0 + kRows - 1)), every_hi = hi_of(position(r0));               // every row of the tile
   const int r = min(r0 + 32 * wv + col, n_rows - 1);
   const int t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
   const int64_t row = row0 + t;
@@ -155,8 +262,12 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     lo = max(lo, a.first_keys[row]);
     all_lo = wave_max(lo);
     const int least = wave_min(lo);
-    if (lane == 0) bounds.lo[wv] = least;
+    if (lane == 0) {
+      bounds.lo[wv] = least;
+      bounds.all_lo[wv] = all_lo;
+    }
     __syncthreads();
+    every_lo = uniform(max(max(bounds.all_lo[0], bounds.all_lo[1]), max(bounds.all_lo[2], bounds.all_lo[3])));
     b_lo = uniform(min(min(bounds.lo[0], bounds.lo[1]), min(bounds.lo[2], bounds.lo[3])));
   }
   int t0, t1;
@@ -419,6 +530,16 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     }
   }
   __syncthreads();   // bounds and tiles are free for the next rows
+  if (b_lo != every_lo || b_hi != every_hi) {
+    float finite = 0.f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) finite = fmaf(o[d][i], 0.f, finite);
+    if (any_wave(bounds, finite != 0.f) &&   // NaN
+        attend_row_by_row<kF16, kCap, kBias>(A, bounds, seq, row0, n_q, n_kv, r0, h, t0 * kKeys, t1 * kKeys, b_lo, every_lo, every_hi, b_hi, part))
+      return;
+  }
 
   l += __shfl_xor(l, 32);
   const int mine = 32 * wv + col;
@@ -537,7 +658,8 @@ __device__ __forceinline__ int64_t make_list(const AttendLaunch& A, List& L) {
     before += cost[i];
   }
   if (tid == 255) L.before[kListed] = (int32_t)before;
-  const int64_t all = L.wave[0] + L.wave[1] + L.wave[2] + L.wave[3];
+  int64_t all = L.wave[0] + L.wave[1] + L.wave[2] + L.wave[3];
+  all = (int64_t)((uint64_t)(uint32_t)uniform((int)(all >> 32)) << 32 | (uint32_t)uniform((int)all));
   __syncthreads();
   return all;
 }

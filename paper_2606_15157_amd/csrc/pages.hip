@@ -31,41 +31,29 @@ __device__ __forceinline__ uint32_t wrap(uint32_t a, uint32_t j, uint32_t n) {
   return x >= n ? x - n : x;
 }
 
-constexpr int kAtOnce = 4;      // elements of a thread that are looked up side by side
-
-// Last s of [0, n) with start[s] <= j (start ascending, start[0] <= j), for several j.
-__device__ __forceinline__ void owners(const int32_t* start, int n, const int (&j)[kAtOnce], int (&s)[kAtOnce]) {
-#pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) s[i] = 0;
-  int step = 1;
-  while (2 * step < n) step *= 2;
-  for (; step > 0; step >>= 1) {
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i)
-      if (s[i] + step < n && start[s[i] + step] <= j[i]) s[i] += step;
+// Last s of [0, n) with start[s] <= j (start ascending, start[0] <= j).
+__device__ __forceinline__ int owner(const int32_t* start, int n, int j) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (start[mid] <= j) lo = mid;
+    else hi = mid;
   }
+  return lo;
 }
 
-// The flat slots of new tokens j, with `start` the sequences' first new tokens (-1 from start[n_seqs] on); -1 for a page
-// outside the pool.  new_lens: of the sequences.
-__device__ __forceinline__ void slots_of(const ResizeLaunch& R, const int32_t* start, const int32_t* new_lens, const int (&j)[kAtOnce],
-                                         int (&slot)[kAtOnce]) {
+// The flat slot of new token j, with `start` the sequences' first new tokens; -1 for a page outside the pool.
+__device__ __forceinline__ int slot_of(const ResizeLaunch& R, const int32_t* start, int j) {
   const rkv_resize& r = R.r;
-  int s[kAtOnce], at[kAtOnce], col[kAtOnce], page[kAtOnce];
-  const int end = start[r.n_seqs];
-  owners(start, r.n_seqs, j, s);
-#pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) {
-    at[i] = j[i] < end ? new_lens[s[i]] - (start[s[i] + 1] - j[i]) : 0;
-    col[i] = div_by(at[i], R.by_page);
-    page[i] = j[i] < end ? r.table[s[i] * r.table_stride + col[i]] : -1;
-  }
-#pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) slot[i] = (uint32_t)page[i] < (uint32_t)r.n_pages ? page[i] * r.page_size + at[i] - col[i] * r.page_size : -1;
+  const int s = owner(start, r.n_seqs, j);
+  const int at = r.new_lens[s] - (start[s + 1] - j);
+  const int col = div_by(at, R.by_page);
+  const int page = r.table[s * r.table_stride + col];
+  return (uint32_t)page < (uint32_t)r.n_pages ? page * r.page_size + at - col * r.page_size : -1;
 }
 
 __global__ __launch_bounds__(kResizeThreads) void resize_kernel(const ResizeLaunch R, const bool fill) {
-  __shared__ int32_t sTake[kResizeMaxSeqs + 1], sGive[kResizeMaxSeqs + 1], sAdd[kResizeMaxSeqs + 1], sNew[kResizeMaxSeqs];
+  __shared__ int32_t sTake[kResizeMaxSeqs + 1], sGive[kResizeMaxSeqs + 1], sAdd[kResizeMaxSeqs + 1];
   __shared__ int64_t sWave[3][kResizeThreads / 64];
   const rkv_resize& r = R.r;
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
@@ -132,7 +120,6 @@ __global__ __launch_bounds__(kResizeThreads) void resize_kernel(const ResizeLaun
     sTake[s] = take;
     sGive[s] = give;
     sAdd[s] = add;
-    sNew[s] = b;
     r.cu_new[s] = add;
     r.lens_out[s] = b;
     take += max(0, want - have);
@@ -146,60 +133,28 @@ __global__ __launch_bounds__(kResizeThreads) void resize_kernel(const ResizeLaun
     r.cu_new[n] = (int)total[2];
   }
   __syncthreads();
-  for (int64_t j0 = tid; j0 < total[0]; j0 += kAtOnce * kResizeThreads) {
-    int j[kAtOnce], s[kAtOnce], id[kAtOnce];
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      j[i] = (int)min(j0 + i * kResizeThreads, total[0] - 1);   // the last one again
-      id[i] = r.ring[wrap(head, j[i], cap)];
-    }
-    owners(sTake, n, j, s);
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i)
-      r.table[s[i] * r.table_stride + pages_of(sNew[s[i]], R.by_page, page) - (sTake[s[i] + 1] - j[i])] = id[i];
+  for (int64_t i = tid; i < total[0]; i += kResizeThreads) {
+    const int j = (int)i, s = owner(sTake, n, j), b = r.new_lens[s];
+    const int want = pages_of(b, R.by_page, page);
+    r.table[s * r.table_stride + want - (sTake[s + 1] - j)] = r.ring[wrap(head, j, cap)];
   }
   __syncthreads();   // pages given back may reach round to ring entries just taken
   const uint32_t tail = wrap(head, count, cap);   // total[1] <= cap: it leaves at most cap pages free
-  for (int64_t j0 = tid; j0 < total[1]; j0 += kAtOnce * kResizeThreads) {
-    int j[kAtOnce], s[kAtOnce], id[kAtOnce];
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) j[i] = (int)min(j0 + i * kResizeThreads, total[1] - 1);
-    owners(sGive, n, j, s);
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) id[i] = r.table[s[i] * r.table_stride + pages_of(sNew[s[i]], R.by_page, page) + j[i] - sGive[s[i]]];
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) r.ring[wrap(tail, j[i], cap)] = id[i];
+  for (int64_t i = tid; i < total[1]; i += kResizeThreads) {
+    const int j = (int)i, s = owner(sGive, n, j), b = r.new_lens[s];
+    const int want = pages_of(b, R.by_page, page);
+    r.ring[wrap(tail, j, cap)] = r.table[s * r.table_stride + want + j - sGive[s]];
   }
-  if (fill) {
-    for (int j0 = tid; j0 < r.max_new; j0 += kAtOnce * kResizeThreads) {
-      int j[kAtOnce], slot[kAtOnce];
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) j[i] = j0 + i * kResizeThreads;
-      slots_of(R, sAdd, sNew, j, slot);
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i)
-        if (j[i] < r.max_new) r.slots[j[i]] = slot[i];
-    }
-  }
+  if (fill)
+    for (int j = tid; j < r.max_new; j += kResizeThreads) r.slots[j] = j < (int)total[2] ? slot_of(R, sAdd, j) : -1;
 }
 
-// kStarts: the sequences' starts fit into LDS.
-constexpr int kStartsInLds = 4096;
-template <bool kStarts>
 __global__ __launch_bounds__(256) void slots_kernel(const ResizeLaunch R) {
-  __shared__ int32_t sStart[kStarts ? kStartsInLds + 1 : 1];
   const rkv_resize& r = R.r;
-  if constexpr (kStarts) {
-    for (int s = threadIdx.x; s <= r.n_seqs; s += 256) sStart[s] = r.cu_new[s];
-    __syncthreads();
-  }
-  const int64_t j0 = (int64_t)blockIdx.x * 256 * kAtOnce + threadIdx.x;
-  int j[kAtOnce], slot[kAtOnce];
-#pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) j[i] = (int)min(j0 + 256 * i, (int64_t)r.max_new - 1);   // the last one again
-  slots_of(R, kStarts ? sStart : r.cu_new, r.new_lens, j, slot);
-#pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) r.slots[j[i]] = slot[i];
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= r.max_new) return;
+  const int j = (int)i;
+  r.slots[j] = j < r.cu_new[r.n_seqs] ? slot_of(R, r.cu_new, j) : -1;
 }
 
 // blockIdx.x: 16 (token, head) rows, 16 lanes each.
@@ -225,9 +180,7 @@ int launch_resize(const ResizeLaunch& R, void* stream) {
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const bool fill = R.r.max_new <= kResizeSlots;
   resize_kernel<<<1, kResizeThreads, 0, st>>>(R, fill);
-  const unsigned grid = (unsigned)(((int64_t)R.r.max_new + 256 * kAtOnce - 1) / (256 * kAtOnce));
-  if (!fill && R.r.n_seqs <= kStartsInLds) slots_kernel<true><<<grid, 256, 0, st>>>(R);
-  else if (!fill) slots_kernel<false><<<grid, 256, 0, st>>>(R);
+  if (!fill) slots_kernel<<<(unsigned)(((int64_t)R.r.max_new + 255) / 256), 256, 0, st>>>(R);
   return (int)hipGetLastError();
 }
 

@@ -337,6 +337,36 @@ def test_nan_and_infinity_where_no_row_looks():
     assert not torch.isnan(got).any() and torch.equal(got, want)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("kw", [dict(), dict(first_keys=True), dict(window=30), dict(prefix_lens=[20, 40, 0])], ids=["causal", "documents", "window", "prefix"])
+@pytest.mark.parametrize("wide", [0, 16384])
+def test_nan_and_infinity_reach_only_the_rows_that_see_them(kw, dtype, wide):
+    """V of a few slots is not finite: columns of rows that do not see those slots are as without them, though others of the
+    same tiles do; rows that see them are not finite where V is not."""
+    kw = dict(kw)
+    lens = [(150, 150), (40, 200), (1, 70)]
+    c = Case(lens, hq=4, hkv=2, page=16, seed=31, dtype=dtype, width=wide // 16)
+    if "first_keys" in kw:
+        kw["first_keys"] = [(n - m + i) // 50 * 50 for m, n in lens for i in range(m)]
+    want, log, weight, reach = OG.attend(f64(c.k), f64(c.v), f64(c.q), c.table, [n for _, n in lens], c.cu, **kw)
+    bad = [(0, 70, NAN, 5), (0, 70, math.inf, 9), (0, 140, -math.inf, 127), (1, 180, NAN, 64), (1, 10, math.inf, 0), (2, 3, NAN, 1)]
+    for s, j, x, d in bad:
+        c.v[int(c.table[s, j // 16]), :, j % 16, d] = x
+    dev = {k: ints(x) if isinstance(x, list) else x for k, x in kw.items()}
+    got, lse = rkv.pages_attend(c.cache, c.q, ints(c.table.tolist()), ints([n for _, n in lens]), ints(c.cu), return_lse=True, **dev)
+    filled, row = got.clone(), 0
+    for s, (m, n) in enumerate(lens):
+        for i in range(m):
+            p = n - m + i
+            lo = max(0, p - kw["window"] + 1 if "window" in kw else 0, kw["first_keys"][row] if "first_keys" in kw else 0)
+            hi = max(p + 1, min(n, kw["prefix_lens"][s])) if "prefix_lens" in kw else p + 1
+            hit = [d for t, j, _, d in bad if t == s and lo <= j < hi]
+            assert not torch.isfinite(got[row][:, hit]).any()
+            filled[row][:, hit] = torch.from_numpy(want[row][:, hit]).to("cuda", dtype)
+            row += 1
+    compare(filled, lse, want, log, weight, reach, dtype, most=200)
+
+
 def test_pages_outside_the_pool_read_as_zeros():
     """Page ids that are no page: rows of zeros, and no fault; the other sequence's results are its own."""
     c = Case([(2, 64), (2, 64)], seed=12)
