@@ -419,6 +419,11 @@ def _raw_stream(dev):
     return get(dev.index) if get else torch.cuda.current_stream(dev).cuda_stream
 
 
+def _strides(t):
+    """Strides, 0 where a dimension has one entry: what stands there is arbitrary."""
+    return [0 if n == 1 else s for n, s in zip(t.shape, t.stride())]
+
+
 class PagedCache:
     """A pool of K and V pages (rkv_pages): k_pages, v_pages bf16 or fp16 [n_pages, Hkv, page_size, 128], any strides that are
     multiples of 8 with the last dimension dense.  Make one and keep it: its calls then marshal no pool again.  The decode
@@ -437,7 +442,7 @@ class PagedCache:
         self.k_pages, self.v_pages = k_pages, v_pages
         self.device, self.dtype = k_pages.device, k_pages.dtype
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k_pages.shape
-        self._pack = _abi.Pages.pack(k_pages.data_ptr(), v_pages.data_ptr(), *k_pages.stride()[:3], *v_pages.stride()[:3], self.n_pages,
+        self._pack = _abi.Pages.pack(k_pages.data_ptr(), v_pages.data_ptr(), *_strides(k_pages)[:3], *_strides(v_pages)[:3], self.n_pages,
                                      self.page_size, self.n_kv_heads, self.head_dim, _abi.BF16 if self.dtype == torch.bfloat16 else _abi.F16)
         self._bytes = {}     # workspace sizes by what they depend on
 
@@ -478,7 +483,7 @@ def pages_resize(pages, new_lens, max_new: int, *, in_place=True, stream=None):
     else:
         slots, cu_new, status, lens, cursor = torch.empty(max_new + 2 * n + 4, dtype=torch.int32, device=dev).split_with_sizes(
             (max_new, n + 1, 1, n, 2))
-    r = _abi.Resize.pack(pages["lens"].data_ptr(), new_lens.data_ptr(), lens.data_ptr(), table.data_ptr(), table.stride(0), ring.data_ptr(),
+    r = _abi.Resize.pack(pages["lens"].data_ptr(), new_lens.data_ptr(), lens.data_ptr(), table.data_ptr(), table.stride(0) if n > 1 else table.shape[1], ring.data_ptr(),
                          pages["cursor"].data_ptr(), cursor.data_ptr(), slots.data_ptr(), cu_new.data_ptr(), status.data_ptr(), n,
                          table.shape[1], ring.shape[0], pages["page_size"], max_new)
     check(_abi.lib().rkv_pages_resize(r, _raw_stream(dev)))
@@ -493,7 +498,7 @@ def pages_write(cache: PagedCache, k, v, slots, *, stream=None):
     if ctx is not None:
         with ctx:
             return pages_write(cache, k, v, slots)
-    shape, ks, vs = k.shape, k.stride(), v.stride()
+    shape, ks, vs = k.shape, _strides(k), _strides(v)
     if shape != v.shape or len(shape) not in (3, 4) or shape[-2] != cache.n_kv_heads or shape[-1] != cache.head_dim:
         raise ValueError("k and v must have shape [T, Hkv, d] or [B, n, Hkv, d]")
     if k.dtype != cache.dtype or v.dtype != cache.dtype or ks[-1] != 1 or vs[-1] != 1 or k.device != dev or v.device != dev:
@@ -527,7 +532,7 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
                                 softcap=softcap, slopes=slopes, prefix_lens=prefix_lens, first_keys=first_keys, out=out, lse_out=lse_out,
                                 return_lse=return_lse)
     torch = _torch()
-    shape, qs = q.shape, q.stride()
+    shape, qs = q.shape, _strides(q)
     if len(shape) != 3 or shape[2] != cache.head_dim or q.dtype != cache.dtype or qs[2] != 1 or q.device != dev:
         raise ValueError("q must have shape [T, Hq, d], the pool's type and device and a dense last dimension")
     T, Hq, d = shape
@@ -560,8 +565,8 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
         raise ValueError("lse_out must be contiguous fp32 [T, Hq] on the pool's device")
     if lse is not None:
         lse_ptr = lse.data_ptr()
-    os, width = out.stride(), table.shape[1]
-    a = _abi.Attend.pack(q.data_ptr(), out.data_ptr(), lse_ptr, qs[0], qs[1], os[0], os[1], table.data_ptr(), table.stride(0),
+    os, width = _strides(out), table.shape[1]
+    a = _abi.Attend.pack(q.data_ptr(), out.data_ptr(), lse_ptr, qs[0], qs[1], os[0], os[1], table.data_ptr(), table.stride(0) if n > 1 else width,
                          lens.data_ptr(), cu, prefix, first, slope, n, T, Hq, width, max_q, max_kv, bool(causal), window,
                          d ** -0.5 if scale is None else scale, softcap)
     L = _abi.lib()

@@ -103,13 +103,16 @@ __device__ __forceinline__ int first_row(const rkv_attend& a, int s) {
 // ascends and leaves each sequence ceil(rows / 128) numbers, so no list of tiles has to be built.
 __device__ __forceinline__ int tile_start(const AttendLaunch& A, int row0, int s) { return row0 * A.group / kRows + s; }
 
+// The first slot that position `at` (which may be negative) sees.
+__device__ __forceinline__ int window_start(const rkv_attend& a, int at) { return a.window && at >= a.window ? at - a.window + 1 : 0; }
+
 // The key tiles [t0, t1) that rows r0 .. r0 + 127 of a sequence of n_q tokens and n_kv slots may see (first_keys aside).
 __device__ __forceinline__ void tile_span(const AttendLaunch& A, int seq, int r0, int n_q, int n_kv, int& t0, int& t1) {
   const rkv_attend& a = A.a;
   const int first = n_kv - n_q + div_by(r0, A.by_group), last = n_kv - n_q + min(n_q - 1, div_by(r0 + kRows - 1, A.by_group));
   int hi = n_kv;
   if (a.causal) hi = min(n_kv, max(last + 1, a.prefix_lens ? a.prefix_lens[seq] : 0));
-  const int lo = a.window ? max(0, first - a.window + 1) : 0;
+  const int lo = window_start(a, first);
   t0 = lo / kKeys;
   t1 = max(t0, (hi + kKeys - 1) / kKeys);
 }
@@ -190,7 +193,7 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
     if (r >= n_rows) break;
     const int t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group, pos = n_kv - n_q + t;
     const int64_t row = row0 + t;
-    int hi = a.causal ? min(n_kv, max(pos + 1, prefix)) : n_kv, lo = a.window ? max(0, pos - a.window + 1) : 0;
+    int hi = a.causal ? min(n_kv, max(pos + 1, prefix)) : n_kv, lo = window_start(a, pos);
     if (a.first_keys) lo = max(lo, uniform(a.first_keys[row]));
     lo = max(lo, from);
     hi = min(hi, to);
@@ -248,7 +251,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   // wave follow from their first and last rows, without a word from the other lanes: the first keys are requested at once.
   const int prefix = a.prefix_lens ? uniform(a.prefix_lens[seq]) : 0;
   auto hi_of = [&](int at) { return a.causal ? min(n_kv, max(at + 1, prefix)) : n_kv; };
-  auto lo_of = [&](int at) { return a.window ? max(0, at - a.window + 1) : 0; };
+  auto lo_of = [&](int at) { return window_start(a, at); };
   auto position = [&](int r) { return n_kv - n_q + div_by(min(r, n_rows - 1), A.by_group); };   // rows behind the last repeat it
   int b_lo = lo_of(position(r0)), b_hi = hi_of(position(r0 + kRows - 1));                       // slots some row sees
   int all_lo = lo_of(position(r0 + 32 * wv + 31)), all_hi = hi_of(position(r0 + 32 * wv));      // every row of the wave

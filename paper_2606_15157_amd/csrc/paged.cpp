@@ -52,13 +52,16 @@ int check_attend(const rkv_pages* p, const rkv_attend* a) {
   if (a->n_seqs < 0 || a->n_rows < 0 || a->max_pages < 0 || a->max_q < 0 || a->max_kv < 0 || a->window < 0 || a->table_stride < 0)
     return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
   if (a->causal != 0 && a->causal != 1) return rkv::fail(RKV_ERR_INVALID_ARG, "causal must be 0 or 1");
-  if (!std::isfinite(a->scale) || !std::isfinite(a->softcap) || a->softcap < 0.f)
-    return rkv::fail(RKV_ERR_INVALID_ARG, "scale and softcap must be finite, softcap >= 0");
+  if (!std::isfinite(a->scale) || !std::isfinite(a->softcap) || a->softcap < 0.f ||
+      (a->softcap > 0.f && std::fabs(a->scale) / a->softcap > 1e30f))
+    return rkv::fail(RKV_ERR_INVALID_ARG, "scale and softcap must be finite, softcap >= 0 and not below 1e-30 of the scale");
+  if (a->softcap > 512.f) return rkv::fail(RKV_ERR_UNSUPPORTED, "softcap above 512");
   if (a->n_q_heads < 1 || a->n_q_heads % p->n_kv_heads)
     return rkv::fail(RKV_ERR_SHAPE, "n_q_heads must be a positive multiple of n_kv_heads");
   if (!a->cu_q && a->n_rows != a->n_seqs) return rkv::fail(RKV_ERR_SHAPE, "without cu_q every sequence has one row");
   if (a->table_stride < a->max_pages) return rkv::fail(RKV_ERR_SHAPE, "table_stride is less than max_pages");
-  if ((int64_t)a->max_pages * p->page_size >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "a sequence holds fewer than 2^31 slots");
+  if ((int64_t)a->max_pages * p->page_size >= kIntEnd - 1024)   // key tiles past the end stay below 2^31
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "a sequence holds fewer than 2^31 - 1024 slots");
   if ((int64_t)a->n_rows * a->n_q_heads >= kIntEnd / 2) return rkv::fail(RKV_ERR_UNSUPPORTED, "n_rows * n_q_heads must be below 2^30");
   if ((row_tiles(p, a) + a->n_seqs) * p->n_kv_heads >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "too many sequences");
   if (int st = check_layout("q", a->q, {a->q_token, a->q_head})) return st;

@@ -325,6 +325,21 @@ def test_strided_tensors(nhd):
     assert (held[:, 0] == 7).all() and (held[:, 5:] == 7).all() and (held[..., :128] == 7).all()
 
 
+def test_dimensions_of_one_have_no_stride():
+    """Pools of one page, head or slot and calls of one row, whose strides there say nothing; the widest window."""
+    pool = torch.randn((2, 40, 1, 1, 128), device="cuda").to(torch.bfloat16)
+    odd = pool.as_strided((2, 40, 1, 1, 128), (40 * 128, 128, 3, 1 << 40, 1))
+    q = torch.randn((1, 2, 128), device="cuda").to(torch.bfloat16)
+    odd_q = q.as_strided((1, 2, 128), (5, 128, 1))
+    table = torch.arange(40, dtype=torch.int32, device="cuda").view(1, 40)
+    odd_table = table.as_strided((1, 40), (0, 1))
+    want = rkv.pages_attend(rkv.PagedCache(*pool), q, table, ints([40]))
+    assert torch.equal(rkv.pages_attend(rkv.PagedCache(*odd), odd_q, odd_table, ints([40]), window=2 ** 31 - 1), want)
+    rkv.pages_write(rkv.PagedCache(*odd), pool[0, :1, 0].as_strided((1, 1, 128), (7, 9, 1)), pool[1, :1, 0], ints([3]))
+    assert torch.equal(pool[0, 3], pool[0, 0]) and torch.equal(pool[1, 3], pool[1, 0])
+    Case([(9, 4), (3, 3)], seed=32).check(causal=False, window=2 ** 31 - 1)
+
+
 def test_nan_and_infinity_where_no_row_looks():
     """Slots before the window and behind the row's own hold NaN and infinities."""
     c = Case([(1, 300), (1, 77)], seed=10)
