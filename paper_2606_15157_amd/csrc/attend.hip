@@ -32,6 +32,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -121,7 +122,7 @@ __device__ __forceinline__ int slots_of(const AttendLaunch& A, int seq) {
 }
 __device__ __forceinline__ int end_row(const rkv_attend& a, int seq) { return a.cu_q ? first_row(a, seq + 1) : min(seq + 1, a.n_rows); }
 
-// A partial sum in the workspace: slot_rows rows of 128 floats (not divided by l), then their m and l.
+// A partial sum in the workspace: slot_rows rows of 128 floats (not divided by l), then their m and l in pairs.
 __device__ __forceinline__ float* part_slot(const AttendLaunch& A, int slot) {
   return A.parts + (size_t)slot * A.slot_rows * (kHeadDim + 2);
 }
@@ -225,8 +226,8 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
     if (part) {
       part[mine * kHeadDim + 2 * lane] = o0;
       part[mine * kHeadDim + 2 * lane + 1] = o1;
-      part[A.slot_rows * kHeadDim + mine] = m;
-      part[A.slot_rows * (kHeadDim + 1) + mine] = l;
+      part[A.slot_rows * kHeadDim + 2 * mine] = m;
+      part[A.slot_rows * kHeadDim + 2 * mine + 1] = l;
     } else {
       const float inv = l == 0.f ? 0.f : 1.f / l;
       reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head)[lane] = pack<kF16>(o0 * inv, o1 * inv);
@@ -545,30 +546,44 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   }
 
   l += __shfl_xor(l, 32);
-  const int mine = 32 * wv + col;
-  if (r0 + mine >= n_rows) return;
+  // The wave's rows by way of its quarter of the tiles' memory, chunks of 16 bytes at c ^ row: whole rows leave it.
+  const int rows = min(32, n_rows - r0 - 32 * wv);
+  if (rows <= 0) return;
+  uint32_t ln = lane;
+  asm volatile("" : "+v"(ln));   // addresses of this end are not kept from one item to the next
+  const uint32_t mem = lds + wv * 16384, cl = ln & 31, hf = ln >> 5;
   if (part) {
+    const uint32_t to = mem + cl * 512;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(part + mine * kHeadDim + 32 * d + 8 * i + 4 * half) =
+        *(__attribute__((address_space(3))) f32x4*)(uintptr_t)(to + ((8 * d + 2 * i + hf) ^ cl) * 16) =
             f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-    if (half == 0) {
-      part[A.slot_rows * kHeadDim + mine] = m;
-      part[A.slot_rows * (kHeadDim + 1) + mine] = l;
-    }
+#pragma unroll 2
+    for (uint32_t x = hf; x < (uint32_t)rows; x += 2)
+      *reinterpret_cast<u32x4*>(part + (32 * wv + x) * kHeadDim + 4 * cl) = lds_read16(mem + x * 512 + (cl ^ x) * 16);
+    if (hf == 0 && cl < (uint32_t)rows) *reinterpret_cast<f32x2*>(part + A.slot_rows * kHeadDim + 2 * (32 * wv + cl)) = f32x2{m, l};
     return;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head + 4 * half;
+  const uint32_t to = mem + cl * 256 + hf * 8;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<u32x2*>(out + 32 * d + 8 * i) =
+      *(__attribute__((address_space(3))) u32x2*)(uintptr_t)(to + ((4 * d + i) ^ (cl & 15)) * 16) =
           u32x2{pack<kF16>(o[d][4 * i] * inv, o[d][4 * i + 1] * inv), pack<kF16>(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
-  if (a.lse && half == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
+#pragma unroll 2
+  for (uint32_t x = ln >> 4; x < (uint32_t)rows; x += 4) {
+    const int at = r0 + 32 * wv + (int)x, token = div_by(at, A.by_group), head = h * A.group + at - token * A.group;
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.out) + (row0 + token) * a.out_token + head * a.out_head + 8 * (ln & 15)) =
+        lds_read16(mem + x * 256 + ((ln & 15) ^ (x & 15)) * 16);
+  }
+  if (a.lse && hf == 0 && cl < (uint32_t)rows) {
+    const int at = r0 + 32 * wv + (int)cl, token = div_by(at, A.by_group), head = h * A.group + at - token * A.group;
+    a.lse[(int64_t)(row0 + token) * a.n_q_heads + head] = row_lse(m, l);
+  }
 }
 
 // The same for sequences of more than one tile alone, when those are few: floor(rows / 128) >= 1 then, and twice that is room
@@ -708,6 +723,7 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
         }
       }
       attend_rows<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, u0, n, part);
+      lds_sync();   // the memory that rows left by is the next tiles'
       pos += n;
     }
   } else {   // more key tiles than the list counts: whole row tiles in turn
@@ -716,6 +732,7 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
       const int row0 = uniform(L.row0[seq]), n_q = uniform(L.row0[seq + 1]) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
       if (r0 < 0 || r0 >= n_q * A.group) continue;
       attend_rows<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, 0, -1, nullptr);
+      lds_sync();
     }
   }
   if (tid < 8) {
@@ -727,67 +744,96 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
   }
 }
 
-// Workgroup (w, y): rows 8 y .. 8 y + 7 of the item that begins in share w and ends in a later one.  32 lanes hold the 128
-// values of a row; with fewer than 8 rows, several such groups take a row's parts in turn and meet in LDS.
-constexpr int kJoinRows = 8;
+// The parts of the items that begin in one share and end in a later one.  Which these are is in the records; the workgroups
+// share out their rows, 8 at a time or fewer where items are few.  32 lanes hold the 128 values of a row; with fewer than 8
+// rows, several such groups take a row's parts in turn and meet in LDS.
+constexpr int kJoinThreads = 256, kJoinGrid = 1024;
 template <bool kF16>
-__global__ __launch_bounds__(32 * kJoinRows) void join_kernel(const AttendLaunch A) {
-  __shared__ f32x4 sO[kJoinRows][32];
-  const int* record = A.records + 8 * blockIdx.x;
-  const int parts = record[0], y0 = kJoinRows * blockIdx.y;
-  if (parts == 0) return;
-  const int row0 = record[1], r0 = record[2], h = record[4];
-  const int rows = min(kJoinRows, min(kRows, record[3] - r0) - y0);
-  if (rows <= 0) return;
-  const rkv_attend& a = A.a;
-  const int grp = threadIdx.x >> 5, c = threadIdx.x & 31;
-  const int each = kJoinRows / rows;                 // groups of a row
-  const int i = grp / each, g = grp - i * each;     // row, and place among its groups
-  const bool in = i < rows;
-  const int w = blockIdx.x, k = y0 + (in ? i : 0);
-  auto slot = [&](int j) { return part_slot(A, j ? 2 * (w + j) : 2 * w + 1); };
-  auto stat_m = [&](int j) { return slot(j)[A.slot_rows * kHeadDim + k]; };
-  auto stat_l = [&](int j) { return slot(j)[A.slot_rows * (kHeadDim + 1) + k]; };
-  float m = -__builtin_inff();
-  for (int j = c; j < parts; j += 32) m = fmaxf(m, stat_m(j));
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  const float ref = m == -__builtin_inff() ? 0.f : m;
-  float l = 0.f;
-  for (int j = c; j < parts; j += 32) l += stat_l(j) * __builtin_amdgcn_exp2f(stat_m(j) - ref);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor(l, o);
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int j = g; j < parts; j += each) {
-    const float f = __builtin_amdgcn_exp2f(stat_m(j) - ref);
-    const f32x4 v = *reinterpret_cast<const f32x4*>(slot(j) + k * kHeadDim + 4 * c);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, v[e], acc[e]);
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A) {
+  __shared__ f32x4 sO[8][32];
+  __shared__ int sItem[kShares], sCount[4], sRows[4];
+  static_assert(kShares == 2 * kJoinThreads, "two records a thread");
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const i32x4 first = *reinterpret_cast<const i32x4*>(A.records + 16 * tid), second = *reinterpret_cast<const i32x4*>(A.records + 16 * tid + 8);
+  const bool one = first[0] != 0, two = second[0] != 0;
+  const int widest = wave_max(max(one ? min(kRows, first[3] - first[2]) : 0, two ? min(kRows, second[3] - second[2]) : 0));
+  const uint64_t ones = __ballot(one), twos = __ballot(two), below = (uint64_t(1) << lane) - 1;
+  if (lane == 0) {
+    sCount[wv] = (int)(__popcll(ones) + __popcll(twos));
+    sRows[wv] = widest;
   }
-  if (each > 1) {
+  __syncthreads();
+  int at = 0, items = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i == wv) at = items;
+    items += sCount[i];
+  }
+  at += (int)(__popcll(ones & below) + __popcll(twos & below));
+  if (one) sItem[at++] = 2 * tid;
+  if (two) sItem[at] = 2 * tid + 1;
+  items = uniform(items);
+  const int rows_most = uniform(max(max(sRows[0], sRows[1]), max(sRows[2], sRows[3])));
+  int most = 8, chunks = (rows_most + 7) / 8;   // rows of a workgroup at once
+  while (most > 1 && items * chunks < kJoinGrid) {
+    most >>= 1;
+    chunks = (rows_most + most - 1) / most;
+  }
+  const rkv_attend& a = A.a;
+  const int grp = tid >> 5, c = tid & 31;
+  for (int task = blockIdx.x; task < items * chunks; task += kJoinGrid) {
+    __syncthreads();   // the list is whole; sO is free
+    const int w = uniform(sItem[task / chunks]), y0 = task % chunks * most;
+    const int* record = A.records + 8 * w;
+    const int parts = record[0], row0 = record[1], r0 = record[2], h = record[4];
+    const int rows = min(most, min(kRows, record[3] - r0) - y0);
+    if (rows <= 0) continue;
+    const int each = 8 / rows;                        // groups of a row
+    const int i = grp / each, g = grp - i * each;     // row, and place among its groups
+    const bool in = i < rows;
+    const int k = y0 + (in ? i : 0);
+    auto slot = [&](int j) { return part_slot(A, j ? 2 * (w + j) : 2 * w + 1); };
+    auto stats = [&](int j) { return *reinterpret_cast<const f32x2*>(slot(j) + A.slot_rows * kHeadDim + 2 * k); };   // m, l
+    float m = -__builtin_inff();
+    for (int j = c; j < parts; j += 32) m = fmaxf(m, stats(j)[0]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    const float ref = m == -__builtin_inff() ? 0.f : m;
+    float l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int j = g; j < parts; j += each) {
+      const f32x2 ml = stats(j);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(slot(j) + k * kHeadDim + 4 * c);
+      const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
+      l = fmaf(f, ml[1], l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, v[e], acc[e]);
+    }
+    __shared__ float sL[8];
     sO[grp][c] = acc;
+    if (c == 0) sL[grp] = l;
     __syncthreads();
-    if (!in || g) return;
+    if (!in || g) continue;
     for (int x = 1; x < each; ++x) {
+      l += sL[grp + x];
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] += sO[grp + x][c][e];
     }
+    const int r = r0 + k, t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
+    const int64_t row = row0 + t;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head + 4 * c;
+    *reinterpret_cast<u32x2*>(out) = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
+    if (a.lse && c == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
   }
-  if (!in || g) return;
-  const int r = r0 + k, t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
-  const int64_t row = row0 + t;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head + 4 * c;
-  *reinterpret_cast<u32x2*>(out) = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
-  if (a.lse && c == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
 }
 
 template <bool kF16, bool kCap, bool kBias, bool kPage16>
 void launch_kernels(const AttendLaunch& A, hipStream_t st) {
   if (A.parts) {
     attend_shares_kernel<kF16, kCap, kBias, kPage16><<<kShares, 256, 0, st>>>(A);
-    join_kernel<kF16><<<dim3(kShares, (A.slot_rows + kJoinRows - 1) / kJoinRows), 32 * kJoinRows, 0, st>>>(A);
+    join_kernel<kF16><<<kJoinGrid, kJoinThreads, 0, st>>>(A);
   } else {
     attend_tiles_kernel<kF16, kCap, kBias, kPage16><<<(unsigned)(A.n_places * A.p.n_kv_heads), 256, 0, st>>>(A);
   }

@@ -78,20 +78,24 @@ int32_t tile_rows(const rkv_pages* p, const rkv_attend* a) {
   return (int32_t)std::min<int64_t>(most, rkv::kAttendRows);
 }
 
+// Rows of the longest sequence, if max_q says so, else of the average one.
+int64_t usual_rows(const rkv_pages* p, const rkv_attend* a) {
+  return (int64_t)(a->max_q ? a->max_q : (a->n_rows + a->n_seqs - 1) / a->n_seqs) * (a->n_q_heads / p->n_kv_heads);
+}
+
 // Whether the row tiles' keys are shared out (attend_shares_kernel and a join) or every tile has a workgroup of its own.
 // Shared out, a call pays some 8 us for the list and the join, and rows that are split go through memory; not shared out,
 // it lasts as long as its longest tile (about 1 us for 64 keys) and leaves CUs idle below 512 tiles.  Measured on 32 query
 // and 8 KV heads, us, not shared against shared:
-//   one token a sequence: 64 of 1024 keys 43 / 52, of 2048 94 / 101, ragged to 8192 158 / 105; 16 of 2048 39 / 35; one of 200
-//   15 / 19, of 1024 21 / 15, of 32768 547 / 39;
-//   prompts: 512 tokens 17 / 35, 1024 27 / 55, 2048 54 / 95, 16384 1994 / 2250; 512 after 32768 562 / 295, 256 each of four
-//   after 7936 198 / 162, 512 each of eight after 3584 262 / 290.
+//   one token a sequence: 64 of 1024 keys 43 / 51, of 2048 95 / 102, ragged to 8192 155 / 109; 16 of 2048 39 / 34; one of 200
+//   12 / 16, of 1024 21 / 15, of 32768 547 / 33;
+//   prompts: 512 tokens 16 / 34, 1024 27 / 53, 2048 53 / 99, 16384 1997 / 2282; 512 after 32768 568 / 292, 64 after 16320
+//   292 / 41, 256 each of four after 7936 200 / 160, 512 each of eight after 3584 258 / 287.
 bool shared_out(const rkv_pages* p, const rkv_attend* a) {
   const int64_t tiles = row_tiles(p, a), items = tiles * p->n_kv_heads;
   if (tiles > rkv::kAttendListed) return false;
-  const int64_t rows = (int64_t)(a->max_q ? a->max_q : (a->n_rows + a->n_seqs - 1) / a->n_seqs) * (a->n_q_heads / p->n_kv_heads);
   const int64_t most = (int64_t)a->max_pages * p->page_size, kv = a->max_kv ? std::min<int64_t>(a->max_kv, most) : most;
-  if (rows > rkv::kAttendRows) return items < 512 && kv > 2048;
+  if (usual_rows(p, a) > rkv::kAttendRows) return items < 512 && kv > 2048;
   return kv > (items >= 256 ? 1024 : 512);
 }
 
@@ -170,8 +174,9 @@ int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size
   L.few_long = 2 * full < L.n_tiles;
   L.n_places = a->n_seqs + (int32_t)std::min<int64_t>(2 * full, L.n_tiles);
   L.slot_rows = tile_rows(pages, a);
-  // a part of 128 rows is written and read again, as many bytes as four key tiles: not for less than eight
-  L.least = L.slot_rows > 32 ? 8 : 2;
+  // A part of 128 rows is written and read again, as many bytes as four key tiles: not for less than eight.  Few rows
+  // cost nothing beside a tile (one token after 1K: 15 us with shares of one, 17 of four, 21 of eight).
+  L.least = usual_rows(pages, a) > 32 ? 8 : 1;
   if (need) {
     L.records = static_cast<int32_t*>(ws);
     L.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kRecordBytes);
