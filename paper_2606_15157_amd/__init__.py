@@ -498,7 +498,8 @@ def pages_write(cache: PagedCache, k, v, slots, *, stream=None):
     if ctx is not None:
         with ctx:
             return pages_write(cache, k, v, slots)
-    shape, ks, vs = k.shape, _strides(k), _strides(v)
+    shape = k.shape
+    ks, vs = (_strides(k), _strides(v)) if 1 in shape else (k.stride(), v.stride())
     if shape != v.shape or len(shape) not in (3, 4) or shape[-2] != cache.n_kv_heads or shape[-1] != cache.head_dim:
         raise ValueError("k and v must have shape [T, Hkv, d] or [B, n, Hkv, d]")
     if k.dtype != cache.dtype or v.dtype != cache.dtype or ks[-1] != 1 or vs[-1] != 1 or k.device != dev or v.device != dev:
@@ -532,7 +533,8 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
                                 softcap=softcap, slopes=slopes, prefix_lens=prefix_lens, first_keys=first_keys, out=out, lse_out=lse_out,
                                 return_lse=return_lse)
     torch = _torch()
-    shape, qs = q.shape, _strides(q)
+    shape = q.shape
+    qs = _strides(q) if 1 in shape else q.stride()
     if len(shape) != 3 or shape[2] != cache.head_dim or q.dtype != cache.dtype or qs[2] != 1 or q.device != dev:
         raise ValueError("q must have shape [T, Hq, d], the pool's type and device and a dense last dimension")
     T, Hq, d = shape
@@ -565,7 +567,7 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
         raise ValueError("lse_out must be contiguous fp32 [T, Hq] on the pool's device")
     if lse is not None:
         lse_ptr = lse.data_ptr()
-    os, width = _strides(out), table.shape[1]
+    os, width = _strides(out) if 1 in shape else out.stride(), table.shape[1]
     a = _abi.Attend.pack(q.data_ptr(), out.data_ptr(), lse_ptr, qs[0], qs[1], os[0], os[1], table.data_ptr(), table.stride(0) if n > 1 else width,
                          lens.data_ptr(), cu, prefix, first, slope, n, T, Hq, width, max_q, max_kv, bool(causal), window,
                          d ** -0.5 if scale is None else scale, softcap)

@@ -638,7 +638,7 @@ __device__ __forceinline__ int64_t make_list(const AttendLaunch& A, List& L) {
   for (int s = tid; s < n; s += 256) L.slots[s] = slots_of(A, s);
   __syncthreads();
   int cost[kPer];
-  int64_t sum = 0;
+  uint32_t sum = 0;   // 256 tiles of a wave, below 2^23 key tiles each
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int tile = tid * kPer + i;
@@ -660,10 +660,10 @@ __device__ __forceinline__ int64_t make_list(const AttendLaunch& A, List& L) {
     }
     sum += cost[i];
   }
-  int64_t x = sum;
+  uint32_t x = sum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up((long long)x, o);
+    const uint32_t y = __shfl_up(x, o);
     if (lane >= o) x += y;
   }
   if (lane == 63) L.wave[wv] = x;
@@ -693,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
   const int tid = threadIdx.x;
   const int64_t all = make_list(A, L);
   const int w = (int)(blockIdx.x % 8) * (kShares / 8) + (int)blockIdx.x / 8;
-  int record[8] = {};   // parts, sequence's first row, first row of the tile, rows of the sequence, head
+  i32x4 record = {0, 0, 0, 0};   // parts + 1024 head, sequence's first row, first row of the tile, rows of the sequence
   if (all < (int64_t(1) << 31)) {
     const int64_t total = all * A.p.n_kv_heads;
     const int64_t share = max((int64_t)A.least, (total + kShares - 1) / kShares);
@@ -715,11 +715,7 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
       if (n < count) {
         part = part_slot(A, 2 * w + (u0 == 0));
         if (u0 == 0) {
-          record[0] = (int)((pos + count - 1) / share) - w + 1;
-          record[1] = row0;
-          record[2] = r0;
-          record[3] = n_q * A.group;
-          record[4] = h;
+          record = i32x4{(int)((pos + count - 1) / share) - w + 1 + 1024 * h, row0, r0, n_q * A.group};
         }
       }
       attend_rows<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, u0, n, part);
@@ -735,13 +731,7 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
       lds_sync();
     }
   }
-  if (tid < 8) {
-    int v = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (tid == i) v = record[i];
-    A.records[8 * w + tid] = v;
-  }
+  if (tid == 0) reinterpret_cast<i32x4*>(A.records)[w] = record;
 }
 
 // The parts of the items that begin in one share and end in a later one.  Which these are is in the records; the workgroups
@@ -751,10 +741,12 @@ constexpr int kJoinThreads = 256, kJoinGrid = 1024;
 template <bool kF16>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A) {
   __shared__ f32x4 sO[8][32];
+  __shared__ float sM[8], sL[8];
+  __shared__ i32x4 sRecord[kShares];
   __shared__ int sItem[kShares], sCount[4], sRows[4];
   static_assert(kShares == 2 * kJoinThreads, "two records a thread");
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const i32x4 first = *reinterpret_cast<const i32x4*>(A.records + 16 * tid), second = *reinterpret_cast<const i32x4*>(A.records + 16 * tid + 8);
+  const i32x4 first = reinterpret_cast<const i32x4*>(A.records)[2 * tid], second = reinterpret_cast<const i32x4*>(A.records)[2 * tid + 1];
   const bool one = first[0] != 0, two = second[0] != 0;
   const int widest = wave_max(max(one ? min(kRows, first[3] - first[2]) : 0, two ? min(kRows, second[3] - second[2]) : 0));
   const uint64_t ones = __ballot(one), twos = __ballot(two), below = (uint64_t(1) << lane) - 1;
@@ -770,8 +762,14 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A
     items += sCount[i];
   }
   at += (int)(__popcll(ones & below) + __popcll(twos & below));
-  if (one) sItem[at++] = 2 * tid;
-  if (two) sItem[at] = 2 * tid + 1;
+  if (one) {
+    sRecord[at] = first;
+    sItem[at++] = 2 * tid;
+  }
+  if (two) {
+    sRecord[at] = second;
+    sItem[at] = 2 * tid + 1;
+  }
   items = uniform(items);
   const int rows_most = uniform(max(max(sRows[0], sRows[1]), max(sRows[2], sRows[3])));
   int most = 8, chunks = (rows_most + 7) / 8;   // rows of a workgroup at once
@@ -784,42 +782,46 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A
   for (int task = blockIdx.x; task < items * chunks; task += kJoinGrid) {
     __syncthreads();   // the list is whole; sO is free
     const int w = uniform(sItem[task / chunks]), y0 = task % chunks * most;
-    const int* record = A.records + 8 * w;
-    const int parts = record[0], row0 = record[1], r0 = record[2], h = record[4];
-    const int rows = min(most, min(kRows, record[3] - r0) - y0);
+    const i32x4 record = sRecord[task / chunks];
+    const int parts = uniform(record[0] & 1023), h = uniform(record[0] >> 10), row0 = uniform(record[1]), r0 = uniform(record[2]);
+    const int rows = min(most, min(kRows, uniform(record[3]) - r0) - y0);
     if (rows <= 0) continue;
     const int each = 8 / rows;                        // groups of a row
     const int i = grp / each, g = grp - i * each;     // row, and place among its groups
     const bool in = i < rows;
     const int k = y0 + (in ? i : 0);
-    auto slot = [&](int j) { return part_slot(A, j ? 2 * (w + j) : 2 * w + 1); };
-    auto stats = [&](int j) { return *reinterpret_cast<const f32x2*>(slot(j) + A.slot_rows * kHeadDim + 2 * k); };   // m, l
-    float m = -__builtin_inff();
-    for (int j = c; j < parts; j += 32) m = fmaxf(m, stats(j)[0]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-    const float ref = m == -__builtin_inff() ? 0.f : m;
-    float l = 0.f;
+    float m = -__builtin_inff(), l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int j = g; j < parts; j += each) {
-      const f32x2 ml = stats(j);
-      const f32x4 v = *reinterpret_cast<const f32x4*>(slot(j) + k * kHeadDim + 4 * c);
-      const float f = __builtin_amdgcn_exp2f(ml[0] - ref);
-      l = fmaf(f, ml[1], l);
+    auto add = [&](float m2, float l2, f32x4 v) {
+      const float top = fmaxf(m, m2), ref = top == -__builtin_inff() ? 0.f : top;
+      const float f = __builtin_amdgcn_exp2f(m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+      m = top;
+      l = l * f + l2 * f2;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, v[e], acc[e]);
+      for (int e = 0; e < 4; ++e) acc[e] = acc[e] * f + v[e] * f2;
+    };
+    for (int j0 = g; j0 < parts; j0 += 4 * each) {   // four parts in flight
+      f32x2 ml[4];
+      f32x4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int jj = min(j0 + j * each, parts - 1);
+        const float* from = part_slot(A, jj ? 2 * (w + jj) : 2 * w + 1);
+        ml[j] = *reinterpret_cast<const f32x2*>(from + A.slot_rows * kHeadDim + 2 * k);   // m, l
+        v[j] = *reinterpret_cast<const f32x4*>(from + k * kHeadDim + 4 * c);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j0 + j * each < parts) add(ml[j][0], ml[j][1], v[j]);
     }
-    __shared__ float sL[8];
     sO[grp][c] = acc;
-    if (c == 0) sL[grp] = l;
+    if (c == 0) {
+      sM[grp] = m;
+      sL[grp] = l;
+    }
     __syncthreads();
     if (!in || g) continue;
-    for (int x = 1; x < each; ++x) {
-      l += sL[grp + x];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += sO[grp + x][c][e];
-    }
+    for (int x = 1; x < each; ++x) add(sM[grp + x], sL[grp + x], sO[grp + x][c]);
     const int r = r0 + k, t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
     const int64_t row = row0 + t;
     const float inv = l == 0.f ? 0.f : 1.f / l;

@@ -70,7 +70,7 @@ int check_attend(const rkv_pages* p, const rkv_attend* a) {
 
 bool nothing_to_do(const rkv_attend* a) { return a->n_seqs == 0 || a->n_rows == 0; }
 
-constexpr size_t kRecordBytes = sizeof(int32_t) * 8 * rkv::kAttendShares;
+constexpr size_t kRecordBytes = sizeof(int32_t) * 4 * rkv::kAttendShares;
 
 // Rows of the largest row tile.
 int32_t tile_rows(const rkv_pages* p, const rkv_attend* a) {
@@ -93,8 +93,9 @@ int64_t usual_rows(const rkv_pages* p, const rkv_attend* a) {
 //   292 / 41, 256 each of four after 7936 200 / 160, 512 each of eight after 3584 258 / 287.
 bool shared_out(const rkv_pages* p, const rkv_attend* a) {
   const int64_t tiles = row_tiles(p, a), items = tiles * p->n_kv_heads;
-  if (tiles > rkv::kAttendListed) return false;
-  const int64_t most = (int64_t)a->max_pages * p->page_size, kv = a->max_kv ? std::min<int64_t>(a->max_kv, most) : most;
+  const int64_t most = (int64_t)a->max_pages * p->page_size;
+  if (tiles > rkv::kAttendListed || most > (1 << 29) || p->n_kv_heads >= (1 << 20)) return false;   // what the list and its records hold
+  const int64_t kv = a->max_kv ? std::min<int64_t>(a->max_kv, most) : most;
   if (usual_rows(p, a) > rkv::kAttendRows) return items < 512 && kv > 2048;
   return kv > (items >= 256 ? 1024 : 512);
 }

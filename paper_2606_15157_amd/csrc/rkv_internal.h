@@ -225,7 +225,7 @@ struct AttendLaunch {
   int32_t few_long;    // how those are numbered
   int32_t slot_rows;   // rows of a partial sum
   int32_t least;       // key tiles of a share, at least
-  int32_t* records;    // [kAttendShares][8], then
+  int32_t* records;    // [kAttendShares][4], then
   float* parts;        // [2 kAttendShares] partial sums; null: a workgroup per row tile
 };
 int launch_attend(const AttendLaunch& A, void* stream);
