@@ -385,24 +385,35 @@ def decode_step(plan: Plan, state, q, k, v, position: int, *, victim_out=None, s
 
 # ---- paged caches
 
+_T = None     # torch, imported by the first call that needs it
+_I32 = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _T, _I32
+    if _T is None:
+        import torch
+        _T, _I32 = torch, torch.int32
+    return _T
 
 
 def _check_int32(name, t, shape, dev):
     """An int32 tensor on `dev`, dense in its last dimension; shape: its sizes, -1 for any."""
-    if t.dtype is not _torch().int32 or t.device != dev:
+    if t.dtype is _I32 and t.shape == shape and t.is_contiguous() and t.device == dev:
+        return
+    if t.dtype is not _I32 or t.device != dev:
         raise ValueError(f"{name} must be int32 on the pool's device")
     have = t.shape
-    if len(have) != len(shape) or (have[0] != shape[0] and shape[0] != -1) or (t.stride(-1) != 1 and have[-1] > 1):
-        raise ValueError(f"{name} must have shape {list(shape)} and a dense last dimension, not {list(have)}")
+    if have != shape and (len(have) != len(shape) or any(n != m and m != -1 for n, m in zip(have, shape))):
+        raise ValueError(f"{name} must have shape {list(shape)}, not {list(have)}")
+    if t.stride(-1) != 1 and have[-1] > 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
 
 
 def _elsewhere(dev, stream):
     """A context in which `dev` and `stream` are the current ones, or None where they are: what a call allocates then
     belongs to the stream that uses it."""
-    torch = _torch()
+    torch = _T or _torch()
     if dev.type != "cuda":
         raise ValueError("tensors must be on the GPU")
     if stream is None:
@@ -414,9 +425,8 @@ def _elsewhere(dev, stream):
 
 def _raw_stream(dev):
     """The current stream's handle (torch's own accessor for generated code: a Stream object costs ten times as much)."""
-    torch = _torch()
-    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return get(dev.index) if get else torch.cuda.current_stream(dev).cuda_stream
+    get = getattr(_T._C, "_cuda_getCurrentRawStream", None)
+    return get(dev.index) if get else _T.cuda.current_stream(dev).cuda_stream
 
 
 def _strides(t):
@@ -470,22 +480,22 @@ def pages_resize(pages, new_lens, max_new: int, *, in_place=True, stream=None):
         with ctx:
             return pages_resize(pages, new_lens, max_new, in_place=in_place)
     n = lens.shape[0]
-    _check_int32("table", table, (n, -1), dev)
+    width = table.shape[-1]
+    _check_int32("table", table, (n, width), dev)
     _check_int32("lens", lens, (n,), dev)
     _check_int32("new_lens", new_lens, (n,), dev)
-    _check_int32("ring", ring, (-1,), dev)
+    _check_int32("ring", ring, (ring.shape[0],), dev)
     _check_int32("cursor", cursor, (2,), dev)
     if max_new < 0:
         raise ValueError("max_new must be >= 0")
-    torch = _torch()
     if in_place:
-        slots, cu_new, status = torch.empty(max_new + n + 2, dtype=torch.int32, device=dev).split_with_sizes((max_new, n + 1, 1))
+        slots, cu_new, status = new_lens.new_empty(max_new + n + 2).split_with_sizes((max_new, n + 1, 1))
     else:
-        slots, cu_new, status, lens, cursor = torch.empty(max_new + 2 * n + 4, dtype=torch.int32, device=dev).split_with_sizes(
+        slots, cu_new, status, lens, cursor = new_lens.new_empty(max_new + 2 * n + 4).split_with_sizes(
             (max_new, n + 1, 1, n, 2))
-    r = _abi.Resize.pack(pages["lens"].data_ptr(), new_lens.data_ptr(), lens.data_ptr(), table.data_ptr(), table.stride(0) if n > 1 else table.shape[1], ring.data_ptr(),
-                         pages["cursor"].data_ptr(), cursor.data_ptr(), slots.data_ptr(), cu_new.data_ptr(), status.data_ptr(), n,
-                         table.shape[1], ring.shape[0], pages["page_size"], max_new)
+    r = _abi.Resize.pack(pages["lens"].data_ptr(), new_lens.data_ptr(), lens.data_ptr(), table.data_ptr(),
+                         table.stride(0) if n > 1 else width, ring.data_ptr(), pages["cursor"].data_ptr(), cursor.data_ptr(), slots.data_ptr(), cu_new.data_ptr(), status.data_ptr(), n,
+                         width, ring.shape[0], pages["page_size"], max_new)
     check(_abi.lib().rkv_pages_resize(r, _raw_stream(dev)))
     return {"slots": slots, "cu_new": cu_new, "status": status, "lens": lens, "cursor": cursor}
 
@@ -532,14 +542,15 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
             return pages_attend(cache, q, table, lens, cu_q, max_q=max_q, max_kv=max_kv, scale=scale, causal=causal, window=window,
                                 softcap=softcap, slopes=slopes, prefix_lens=prefix_lens, first_keys=first_keys, out=out, lse_out=lse_out,
                                 return_lse=return_lse)
-    torch = _torch()
+    torch = _T
     shape = q.shape
-    qs = _strides(q) if 1 in shape else q.stride()
-    if len(shape) != 3 or shape[2] != cache.head_dim or q.dtype != cache.dtype or qs[2] != 1 or q.device != dev:
+    if len(shape) != 3 or shape[2] != cache.head_dim or q.dtype != cache.dtype or q.stride(2) != 1 or q.device != dev:
         raise ValueError("q must have shape [T, Hq, d], the pool's type and device and a dense last dimension")
     T, Hq, d = shape
+    q_token, q_head, _ = q.stride()
     n = lens.shape[0]
-    _check_int32("table", table, (n, -1), dev)
+    width = table.shape[-1]
+    _check_int32("table", table, (n, width), dev)
     _check_int32("lens", lens, (n,), dev)
     cu = prefix = first = slope = lse_ptr = 0
     if cu_q is not None:
@@ -556,7 +567,7 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
             raise ValueError("slopes must be contiguous fp32 [Hq] on the pool's device")
         slope = slopes.data_ptr()
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=dev)
+        out = torch.empty_like(q) if q.is_contiguous() else torch.empty(shape, dtype=q.dtype, device=dev)
     elif out.shape != shape or out.dtype != q.dtype or out.stride(2) != 1 or out.device != dev:
         raise ValueError("out must have q's shape, type and device and a dense last dimension")
     lse = lse_out
@@ -567,8 +578,12 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
         raise ValueError("lse_out must be contiguous fp32 [T, Hq] on the pool's device")
     if lse is not None:
         lse_ptr = lse.data_ptr()
-    os, width = _strides(out) if 1 in shape else out.stride(), table.shape[1]
-    a = _abi.Attend.pack(q.data_ptr(), out.data_ptr(), lse_ptr, qs[0], qs[1], os[0], os[1], table.data_ptr(), table.stride(0) if n > 1 else width,
+    out_token, out_head, _ = out.stride()
+    if T == 1:      # what stands there says nothing
+        q_token = out_token = 0
+    if Hq == 1:
+        q_head = out_head = 0
+    a = _abi.Attend.pack(q.data_ptr(), out.data_ptr(), lse_ptr, q_token, q_head, out_token, out_head, table.data_ptr(), table.stride(0) if n > 1 else width,
                          lens.data_ptr(), cu, prefix, first, slope, n, T, Hq, width, max_q, max_kv, bool(causal), window,
                          d ** -0.5 if scale is None else scale, softcap)
     L = _abi.lib()
@@ -580,7 +595,7 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
         if len(cache._bytes) >= 1024:
             cache._bytes.clear()
         nbytes = cache._bytes[key] = size.value
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    ws = lens.new_empty(nbytes // 4) if nbytes else None
     check(L.rkv_pages_attend(cache._pack, a, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev)))
     return out if lse is None else (out, lse)
 
