@@ -37,6 +37,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kRows = kAttendRows;         // rows of a workgroup, 32 a wave
@@ -57,6 +58,17 @@ template <bool kF16>
 __device__ __forceinline__ f32x16 mma32(u32x4 a, u32x4 b, f32x16 c) {
   if constexpr (kF16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// 16 x 16, 32 and 16 deep.
+template <bool kF16>
+__device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (kF16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <bool kF16>
+__device__ __forceinline__ f32x4 mma16s(u32x2 a, u32x2 b, f32x4 c) {
+  if constexpr (kF16) return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, a), __builtin_bit_cast(f16x4, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), c, 0, 0, 0);
 }
 // Two values rounded to nearest even.
 template <bool kF16>
@@ -240,12 +252,14 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
 // kCap: capped scores, kBias: less a slope times the distance; kPage16: page_size % 16 = 0, pages less than 4 GiB and slots at least a
 // row apart.  Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
 // partial sums go, null: the rows are finished.
-template <bool kF16, bool kCap, bool kBias, bool kPage16>
+template <bool kF16, bool kCap, bool kBias, bool kPage16, bool kNarrow>
 __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
                                             int n_kv, int r0, int h, int u0, int n, float* part) {
   const rkv_attend& a = A.a;
   const rkv_pages& p = A.p;
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  int lane = threadIdx.x & 63;
+  if constexpr (kNarrow) asm volatile("" : "+v"(lane));   // its addresses are not kept from one item to the next
+  const int wv = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int n_rows = n_q * A.group;
 
   // The slots a position sees, and a row's position.  Both bounds ascend with the row, so that those of the tile and of the
@@ -255,9 +269,10 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   auto lo_of = [&](int at) { return window_start(a, at); };
   auto position = [&](int r) { return n_kv - n_q + div_by(min(r, n_rows - 1), A.by_group); };   // rows behind the last repeat it
   int b_lo = lo_of(position(r0)), b_hi = hi_of(position(r0 + kRows - 1));                       // slots some row sees
-  int all_lo = lo_of(position(r0 + 32 * wv + 31)), all_hi = hi_of(position(r0 + 32 * wv));      // every row of the wave
+  const int w_first = kNarrow ? r0 : r0 + 32 * wv, w_last = kNarrow ? r0 + 15 : r0 + 32 * wv + 31;   // the wave's rows
+  int all_lo = lo_of(position(w_last)), all_hi = hi_of(position(w_first));                      // every row of the wave
   int every_lo = lo_of(position(r0 + kRows - 1)), every_hi = hi_of(position(r0));               // every row of the tile
-  const int r = min(r0 + 32 * wv + col, n_rows - 1);
+  const int r = min(w_first + (kNarrow ? lane & 15 : col), n_rows - 1);
   const int t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
   const int64_t row = row0 + t;
   const int pos = n_kv - n_q + t;
@@ -265,14 +280,17 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   if (a.first_keys) {   // these need not ascend
     lo = max(lo, a.first_keys[row]);
     all_lo = wave_max(lo);
-    const int least = wave_min(lo);
-    if (lane == 0) {
-      bounds.lo[wv] = least;
-      bounds.all_lo[wv] = all_lo;
+    b_lo = wave_min(lo);
+    every_lo = all_lo;
+    if constexpr (!kNarrow) {
+      if (lane == 0) {
+        bounds.lo[wv] = b_lo;
+        bounds.all_lo[wv] = all_lo;
+      }
+      __syncthreads();
+      every_lo = uniform(max(max(bounds.all_lo[0], bounds.all_lo[1]), max(bounds.all_lo[2], bounds.all_lo[3])));
+      b_lo = uniform(min(min(bounds.lo[0], bounds.lo[1]), min(bounds.lo[2], bounds.lo[3])));
     }
-    __syncthreads();
-    every_lo = uniform(max(max(bounds.all_lo[0], bounds.all_lo[1]), max(bounds.all_lo[2], bounds.all_lo[3])));
-    b_lo = uniform(min(min(bounds.lo[0], bounds.lo[1]), min(bounds.lo[2], bounds.lo[3])));
   }
   int t0, t1;
   tile_span(A, seq, r0, n_q, n_kv, t0, t1);
@@ -359,6 +377,154 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     fetch(tl, x, vp, p.v_page, v_slot, v_off, (2 + buf) * kTileBytes);
   };
 
+  const float sl2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);   // a negative scale's sign is in q; above 0, so that hidden stays hidden
+  const float slope = kBias ? a.slopes[hq] * kLog2e : 0.f;
+  const float cap2 = 2.f * kLog2e * a.softcap, in_cap = kCap ? 2.f * sl2 / a.softcap : 0.f;
+  // A product becomes what is compared and exponentiated: the score is grow x + base, in log2 units, with grow >= 0.
+  //   neither: x = the product, the scale in grow;
+  //   capped:  c tanh(y / c) = c - 2 c / (1 + exp(2 y / c)): x = -1 / (1 + exp(2 y / c)), grow = 2 c, base = c;
+  //   biased (after the cap): x = the score.  far: the distance of the row from the lane's first key, key: from there.
+  auto score = [&](float y, int key, float far) __attribute__((always_inline)) {
+    if constexpr (kCap) y = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(y * in_cap));
+    if constexpr (kBias) {
+      y = kCap ? fmaf(y, cap2, 0.5f * cap2) : y * sl2;
+      y = fmaf(-slope, fabsf(far - (float)key), y);
+    }
+    return y;
+  };
+  const float grow = kBias ? 1.f : kCap ? cap2 : sl2, base = !kBias && kCap ? 0.5f * cap2 : 0.f;
+  const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + row * a.q_token + hq * a.q_head;
+  float m = -__builtin_inff(), l = 0.f, ref = 0.f;   // ref: the running maximum, 0 while there is none
+
+  if constexpr (kNarrow) {
+    // At most 16 rows, all of them in every wave; a wave takes the 16 keys of each tile that it fetched itself, two tiles
+    // ahead, and waits for no other: 16x16x32 and 16x16x16 MFMA, a lane holds keys 4 (lane / 16) + 0..3 of row lane % 16.
+    const int l16 = lane & 15, lg = lane >> 4;
+    Place next;
+    auto fetch_both = [&](int tl, int buf) __attribute__((always_inline)) {
+      fetch_k(tl, next, buf);
+      fetch_v(tl, next, buf);
+    };
+    if (t0 < t1) {
+      find(t0, next);
+      fetch_both(t0, 0);
+      if (t0 + 1 < t1) {
+        find(t0 + 1, next);
+        fetch_both(t0 + 1, 1);
+      }
+      if (t0 + 2 < t1) find(t0 + 2, next);
+    }
+    u32x4 q[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      q[s] = *reinterpret_cast<const u32x4*>(qrow + 32 * s + 8 * lg);
+      if (a.scale < 0.f) q[s] ^= 0x80008000u;
+    }
+    const uint32_t k_at = lds + wv * 4096 + l16 * 256;
+    const uint32_t v_at = lds + 2 * kTileBytes + wv * 4096 + (4 * lg + (l16 >> 2)) * 256 + (l16 & 1) * 8;
+    f32x4 o[8] = {};
+#pragma unroll 1
+    for (int tl = t0; tl < t1; ++tl) {
+      const uint32_t buf = ((tl - t0) & 1) * kTileBytes;
+      if (tl + 1 < t1) wait_vmcnt<8>();   // the next tile may be in flight
+      else wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 4; ++s) x = mma16<kF16>(lds_read16(k_at + buf + ((4 * s + lg) ^ l16) * 16), q[s], x);
+      const int key0 = tl * kKeys + 16 * wv;
+      const float far = (float)(pos - key0 - 4 * lg);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = score(x[i], i, far);
+      if (key0 < all_lo || key0 + 16 > all_hi) {
+        const int from = lo - key0 - 4 * lg, to = hi - key0 - 4 * lg;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i < from || i >= to) x[i] = -__builtin_inff();
+      }
+      float top = fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), grow, base);
+      if (__any(top > m + kGrow)) {   // the row's, over its four lanes
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m2 = fmaxf(m, top), f = m2 > m ? __builtin_amdgcn_exp2f(m - m2) : 1.f;
+        m = m2;
+        ref = m == -__builtin_inff() ? 0.f : m;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < 8; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[d][i] *= f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], grow, base - ref));
+        l += x[i];
+      }
+      const u32x2 pr = {pack<kF16>(x[0], x[1]), pack<kF16>(x[2], x[3])};
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+        o[d] = mma16s<kF16>(lds_read_tr(v_at + buf + ((2 * d + ((l16 & 3) >> 1)) ^ (4 * (l16 >> 2))) * 16), pr, o[d]);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt 0: this wave's reads of the tile are done
+      if (tl + 2 < t1) {
+        fetch_both(tl + 2, (tl - t0) & 1);
+        if (tl + 3 < t1) find(tl + 3, next);
+      }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    // The four waves' sums meet by way of the memory each fetched into: columns below 64 in its part of K's first tile, the
+    // others in the second's, chunks of 16 bytes at c ^ row; m and l in V's first.
+#pragma unroll
+    for (int d = 0; d < 8; ++d)
+      *(__attribute__((address_space(3))) f32x4*)(uintptr_t)(k_at + (d >> 2) * kTileBytes + ((4 * (d & 3) + lg) ^ l16) * 16) = o[d];
+    if (lg == 0) *(__attribute__((address_space(3))) f32x2*)(uintptr_t)(lds + 2 * kTileBytes + wv * 4096 + l16 * 8) = f32x2{m, l};
+    lds_sync();
+    const int x = 4 * wv + lg, c = l16;      // this thread's row and eight columns
+    f32x2 ml[4];
+    float mm = -__builtin_inff(), ll = 0.f, sum[8] = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      ml[w] = *(const __attribute__((address_space(3))) f32x2*)(uintptr_t)(lds + 2 * kTileBytes + w * 4096 + x * 8);
+      mm = fmaxf(mm, ml[w][0]);
+    }
+    const float mr = mm == -__builtin_inff() ? 0.f : mm;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml[w][0] - mr);
+      ll = fmaf(ml[w][1], f, ll);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const f32x4 v = *(const __attribute__((address_space(3))) f32x4*)(uintptr_t)(lds + (c >> 3) * kTileBytes + w * 4096 + x * 256 +
+                                                                                     ((2 * (c & 7) + u) ^ x) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[4 * u + i] = fmaf(v[i], f, sum[4 * u + i]);
+      }
+    }
+    if (b_lo != every_lo || b_hi != every_hi) {
+      float finite = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) finite = fmaf(sum[i], 0.f, finite);
+      if (any_wave(bounds, finite != 0.f) &&   // NaN
+          attend_row_by_row<kF16, kCap, kBias>(A, bounds, seq, row0, n_q, n_kv, r0, h, t0 * kKeys, t1 * kKeys, b_lo, every_lo, every_hi, b_hi, part))
+        return;
+    }
+    if (r0 + x >= n_rows) return;
+    if (part) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        *reinterpret_cast<f32x4*>(part + x * kHeadDim + 8 * c + 4 * u) = f32x4{sum[4 * u], sum[4 * u + 1], sum[4 * u + 2], sum[4 * u + 3]};
+      if (c == 0) *reinterpret_cast<f32x2*>(part + A.slot_rows * kHeadDim + 2 * x) = f32x2{mm, ll};
+      return;
+    }
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+    const int token = div_by(r0 + x, A.by_group), head = h * A.group + r0 + x - token * A.group;
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.out) + (row0 + token) * a.out_token + head * a.out_head + 8 * c) =
+        u32x4{pack<kF16>(sum[0] * inv, sum[1] * inv), pack<kF16>(sum[2] * inv, sum[3] * inv), pack<kF16>(sum[4] * inv, sum[5] * inv),
+              pack<kF16>(sum[6] * inv, sum[7] * inv)};
+    if (a.lse && c == 0) a.lse[(int64_t)(row0 + token) * a.n_q_heads + head] = row_lse(mm, ll);
+  } else {
+
   // Iteration tl needs tile tl of V and tile tl + 1 of K, requested in the iteration before; K's tiles are in buffers
   // (tl - t0) % 2, V's in 2 + (tl - t0) % 2.
   Place here, next;
@@ -376,7 +542,6 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     fetch_v(t0, here, 0);
   }
   u32x4 q[8];
-  const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + row * a.q_token + hq * a.q_head;
 #pragma unroll
   for (int s = 0; s < 8; ++s) q[s] = *reinterpret_cast<const u32x4*>(qrow + 16 * s + 8 * half);
   if (a.scale < 0.f) {
@@ -385,10 +550,6 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   }
 
   f32x16 o[4] = {};
-  float m = -__builtin_inff(), l = 0.f;
-  const float sl2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);   // a negative scale's sign is in q; above 0, so that hidden stays hidden
-  const float slope = kBias ? a.slopes[hq] * kLog2e : 0.f;
-  const float cap2 = 2.f * kLog2e * a.softcap, in_cap = kCap ? 2.f * sl2 / a.softcap : 0.f;
   uint32_t k_lane[8], v_lane[4];
 #pragma unroll
   for (int st = 0; st < 8; ++st) k_lane[st] = lds + col * 256 + (((2 * st) ^ (col & 15) ^ half) * 16);
@@ -398,25 +559,11 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   for (int d = 0; d < 4; ++d)
     v_lane[d] = lds + v_key * 256 + ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (4 * (v_key & 3))) * 16 + (lane & 1) * 8;
 
-  float ref = 0.f;      // the running maximum, 0 while there is none
   f32x16 sa[2], sb[2];  // scores of a tile and the next: s.[u][i] is key 32 u + 8 (i / 4) + 4 half + i % 4
   u32x4 pr[4];          // probabilities of a tile, 16 keys each
 
   auto k_frag = [&](int i, uint32_t kb) __attribute__((always_inline)) { return lds_read16(k_lane[i & 7] + kb + (i >> 3) * 8192); };
-  // A product becomes what is compared and exponentiated: the score is grow x + base, in log2 units, with grow >= 0.
-  //   neither: x = the product, the scale in grow;
-  //   capped:  c tanh(y / c) = c - 2 c / (1 + exp(2 y / c)): x = -1 / (1 + exp(2 y / c)), grow = 2 c, base = c;
-  //   biased (after the cap): x = the score.
-  auto score = [&](f32x16 (&x)[2], int u, int i, float far) __attribute__((always_inline)) {
-    float y = x[u][i];
-    if constexpr (kCap) y = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(y * in_cap));
-    if constexpr (kBias) {
-      y = kCap ? fmaf(y, cap2, 0.5f * cap2) : y * sl2;
-      y = fmaf(-slope, fabsf(far - (float)(32 * u + 8 * (i >> 2) + (i & 3))), y);
-    }
-    x[u][i] = y;
-  };
-  const float grow = kBias ? 1.f : kCap ? cap2 : sl2, base = !kBias && kCap ? 0.5f * cap2 : 0.f;
+  auto key_of = [](int i) { return 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3); };   // of score i of 32, from 4 half
   auto distance = [&](int tl) __attribute__((always_inline)) { return (float)(pos - tl * kKeys - 4 * half); };   // of key 4 half
   // A tile that a row sees part of: the scores of the others, and the maximum again.
   auto hide = [&](int tl, f32x16 (&x)[2], float& top) __attribute__((always_inline)) {
@@ -455,7 +602,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     float top = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      score(x, i >> 4, i & 15, far);
+      x[i >> 4][i & 15] = score(x[i >> 4][i & 15], key_of(i), far);
       top = fmaxf(top, x[i >> 4][i & 15]);
     }
     hide(tl, x, top);
@@ -504,8 +651,8 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
         if (i + 3 < 16) f[(i + 3) & 3] = v_frag(i + 3);
         o[i & 3] = mma32<kF16>(f[i & 3], pr[i >> 2], o[i & 3]);
         if (kAhead + i < 16) pair(x, kAhead + i);
-        score(y, i >> 3, 2 * (i & 7), far);
-        score(y, i >> 3, 2 * (i & 7) + 1, far);
+        y[i >> 3][2 * (i & 7)] = score(y[i >> 3][2 * (i & 7)], key_of(2 * i), far);
+        y[i >> 3][2 * (i & 7) + 1] = score(y[i >> 3][2 * (i & 7) + 1], key_of(2 * i + 1), far);
         top = fmaxf(fmaxf(top, y[i >> 3][2 * (i & 7)]), y[i >> 3][2 * (i & 7) + 1]);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -584,6 +731,15 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     const int at = r0 + 32 * wv + (int)cl, token = div_by(at, A.by_group), head = h * A.group + at - token * A.group;
     a.lse[(int64_t)(row0 + token) * a.n_q_heads + head] = row_lse(m, l);
   }
+  }   // !kNarrow
+}
+
+// At most 16 rows go the narrow way.
+template <bool kF16, bool kCap, bool kBias, bool kPage16>
+__device__ __forceinline__ void attend_tile(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
+                                            int n_kv, int r0, int h, int u0, int n, float* part) {
+  if (n_q * A.group - r0 <= 16) attend_rows<kF16, kCap, kBias, kPage16, true>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part);
+  else attend_rows<kF16, kCap, kBias, kPage16, false>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part);
 }
 
 // The same for sequences of more than one tile alone, when those are few: floor(rows / 128) >= 1 then, and twice that is room
@@ -618,7 +774,7 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendLaunch
   const int row0 = uniform(first_row(A.a, seq)), n_q = uniform(end_row(A.a, seq)) - row0, n_rows = n_q * A.group;
   const int r0 = brief ? 0 : (tile - long_start(A, row0, seq)) * kRows;
   if ((n_rows <= kRows) != brief || r0 < 0 || r0 >= n_rows) return;
-  attend_rows<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(slots_of(A, seq)), r0, h, 0, -1, nullptr);
+  attend_tile<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(slots_of(A, seq)), r0, h, 0, -1, nullptr);
 }
 
 // The list of row tiles that every workgroup of attend_shares_kernel makes.
@@ -718,7 +874,7 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
           record = i32x4{(int)((pos + count - 1) / share) - w + 1 + 1024 * h, row0, r0, n_q * A.group};
         }
       }
-      attend_rows<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, u0, n, part);
+      attend_tile<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, u0, n, part);
       lds_sync();   // the memory that rows left by is the next tiles'
       pos += n;
     }
@@ -727,7 +883,7 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
       const int tile = i / A.p.n_kv_heads, h = i - tile * A.p.n_kv_heads, seq = uniform(L.seq[tile]);
       const int row0 = uniform(L.row0[seq]), n_q = uniform(L.row0[seq + 1]) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
       if (r0 < 0 || r0 >= n_q * A.group) continue;
-      attend_rows<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, 0, -1, nullptr);
+      attend_tile<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, 0, -1, nullptr);
       lds_sync();
     }
   }

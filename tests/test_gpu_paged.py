@@ -220,6 +220,7 @@ def compare(out, lse, want, log, weight, reach, dtype, softcap=0.0, slopes=None,
     assert (bad <= 0).all(), (bad.max(), np.argwhere(bad > 0)[:4])
 
 
+FEW = [(4, 4), (2, 300), (3, 64), (1, 900), (4, 1030), (2, 1)]
 ONE = [(1, 1), (1, 2), (1, 63), (1, 64), (1, 65), (1, 500), (1, 1025), (1, 16)]
 MANY = [(5, 5), (1, 130), (70, 200), (33, 33), (0, 40), (129, 300), (2, 2), (0, 0)]
 
@@ -237,7 +238,7 @@ def test_attention_over_head_layouts(hq, hkv):
     Case([(1, 300), (3, 70), (40, 200), (0, 3)], hq=hq, hkv=hkv, seed=hq + 1).check()
 
 
-@pytest.mark.parametrize("lens", [ONE, MANY], ids=["one", "many"])
+@pytest.mark.parametrize("lens", [ONE, MANY, FEW], ids=["one", "many", "few"])
 @pytest.mark.parametrize("kw", [
     dict(causal=False), dict(window=1), dict(window=64), dict(window=50), dict(softcap=2.0), dict(softcap=50.0), dict(scale=0.5),
     dict(scale=-0.2), dict(scale=0.0), dict(softcap=3.0, window=50), dict(softcap=3.0, slopes=True, window=50),
@@ -353,18 +354,18 @@ def test_nan_and_infinity_where_no_row_looks():
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("kw", [dict(), dict(first_keys=True), dict(window=30), dict(prefix_lens=[20, 40, 0])], ids=["causal", "documents", "window", "prefix"])
+@pytest.mark.parametrize("kw", [dict(), dict(first_keys=True), dict(window=30), dict(prefix_lens=[20, 40, 0, 89])], ids=["causal", "documents", "window", "prefix"])
 @pytest.mark.parametrize("wide", [0, 16384])
 def test_nan_and_infinity_reach_only_the_rows_that_see_them(kw, dtype, wide):
     """V of a few slots is not finite: columns of rows that do not see those slots are as without them, though others of the
     same tiles do; rows that see them are not finite where V is not."""
     kw = dict(kw)
-    lens = [(150, 150), (40, 200), (1, 70)]
+    lens = [(150, 150), (40, 200), (1, 70), (3, 90)]
     c = Case(lens, hq=4, hkv=2, page=16, seed=31, dtype=dtype, width=wide // 16)
     if "first_keys" in kw:
         kw["first_keys"] = [(n - m + i) // 50 * 50 for m, n in lens for i in range(m)]
     want, log, weight, reach = OG.attend(f64(c.k), f64(c.v), f64(c.q), c.table, [n for _, n in lens], c.cu, **kw)
-    bad = [(0, 70, NAN, 5), (0, 70, math.inf, 9), (0, 140, -math.inf, 127), (1, 180, NAN, 64), (1, 10, math.inf, 0), (2, 3, NAN, 1)]
+    bad = [(0, 70, NAN, 5), (0, 70, math.inf, 9), (0, 140, -math.inf, 127), (1, 180, NAN, 64), (1, 10, math.inf, 0), (2, 3, NAN, 1), (3, 88, NAN, 33), (3, 55, -math.inf, 34)]
     for s, j, x, d in bad:
         c.v[int(c.table[s, j // 16]), :, j % 16, d] = x
     dev = {k: ints(x) if isinstance(x, list) else x for k, x in kw.items()}
