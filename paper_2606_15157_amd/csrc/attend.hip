@@ -141,6 +141,7 @@ __device__ __forceinline__ float* part_slot(const AttendLaunch& A, int slot) {
 
 struct Bounds {   // of the waves
   int lo[4], all_lo[4], bad[4];
+  int32_t ahead[4][64];   // page ids on their way
 };
 // The workgroup's LDS operations are done; vector memory operations stay in flight.
 __device__ __forceinline__ void lds_sync() {
@@ -322,36 +323,43 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       v_off[j] += (4 * j + fr) * v_slot - 1024 * j;
     }
   }
+  // Pages of a multiple of 16 slots: the page of the wave's rows of a tile (-1: not visible) and the slot in it.
   struct Place {
-    int page[kPage16 ? 1 : 4], at[kPage16 ? 1 : 4];
+    int page, at;
   };
-  auto find = [&](int tl, Place& x) __attribute__((always_inline)) {   // pages of tile tl; -1: not visible
+  // Others: lane i looks up row i % 16 of tile i / 16 of four, the next four ahead, and the addresses go round by permutes
+  // (looking up every row of a tile by itself took 512 tokens after 32K from 286 to 340 us).
+  int page4 = -1;
+  const char *k4 = nullptr, *v4 = nullptr;
+  const uint32_t ahead = lds_addr(bounds.ahead[wv]);
+  auto key4 = [&](int tl) { return (tl + fr) * kKeys + 16 * wv + (lane & 15); };
+  auto look = [&](int tl) __attribute__((always_inline)) {
+    dma4(table + div_by(min(max(key4(tl), b_lo), b_hi - 1), A.by_page), ahead);   // no register waits for it
+  };
+  const char* zeros = reinterpret_cast<const char*>(zero_row);
+  auto row4 = [&](int tl, const char* rows, int64_t page_stride, uint32_t slot) __attribute__((always_inline)) {
+    const int key = key4(tl);
+    const bool in = key >= b_lo && key < b_hi && (uint32_t)page4 < (uint32_t)p.n_pages;
+    const int at = key - div_by(in ? key : 0, A.by_page) * p.page_size;
+    return in ? rows + (uint64_t)(uint32_t)page4 * (uint64_t)(2 * page_stride) + (uint64_t)(uint32_t)at * slot : zeros;
+  };
+  auto find = [&](int tl, Place& x) __attribute__((always_inline)) {
     if constexpr (kPage16) {
       const int key = tl * kKeys + 16 * wv;
       const bool in = key + 16 > b_lo && key < b_hi;
       const int c = div_by(in ? key : 0, A.by_page);
-      x.at[0] = key - c * p.page_size;
-      x.page[0] = in ? known[c] : -1;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = tl * kKeys + 16 * wv + 4 * j + fr;
-        const bool in = key >= b_lo && key < b_hi;
-        const int c = div_by(in ? key : 0, A.by_page);
-        x.at[j] = key - c * p.page_size;
-        x.page[j] = in ? table[c] : -1;
-      }
+      x.at = key - c * p.page_size;
+      x.page = in ? known[c] : -1;
     }
   };
-  const char* zeros = reinterpret_cast<const char*>(zero_row);
-  auto fetch = [&](int tl, const Place& x, const char* rows, int64_t page_stride, uint32_t slot, const uint32_t (&off)[4], uint32_t to)
-      __attribute__((always_inline)) {
+  auto fetch = [&](int tl, const Place& x, const char* rows, const char* rows4, int64_t page_stride, uint32_t slot, const uint32_t (&off)[4],
+                   uint32_t to) __attribute__((always_inline)) {
     to += lds + wv * 4096;
     if constexpr (kPage16) {
       const int key = tl * kKeys + 16 * wv;
-      const uint32_t pg = x.page[0];
+      const uint32_t pg = x.page;
       const bool held = pg < (uint32_t)p.n_pages;
-      const char* src = rows + (uint64_t)pg * (uint32_t)(2 * page_stride) + (uint64_t)(uint32_t)x.at[0] * slot;
+      const char* src = rows + (uint64_t)pg * (uint32_t)(2 * page_stride) + (uint64_t)(uint32_t)x.at * slot;
       if (held && key >= b_lo && key + 16 <= b_hi) {
         dma16s_four(src, off, to);
       } else {
@@ -362,20 +370,41 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
         }
       }
     } else {
+      const int from = 4 * (16 * ((tl - t0) & 3) + fr);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const bool in = (uint32_t)x.page[j] < (uint32_t)p.n_pages;
-        dma16((in ? rows + (uint64_t)(uint32_t)x.page[j] * (uint64_t)(2 * page_stride) + (uint64_t)(uint32_t)x.at[j] * slot : zeros) + off[j],
-              to + 1024 * j);
+        const uint32_t x0 = __builtin_amdgcn_ds_bpermute(from + 16 * j, (int)(uint32_t)(uintptr_t)rows4);
+        const uint32_t x1 = __builtin_amdgcn_ds_bpermute(from + 16 * j, (int)(uint32_t)((uintptr_t)rows4 >> 32));
+        dma16(reinterpret_cast<const char*>((uintptr_t)x1 << 32 | x0) + off[j], to + 1024 * j);
       }
     }
   };
+  // Of each four tiles from t0, K's first is requested before V's, and V's before K's fifth.
   auto fetch_k = [&](int tl, const Place& x, int buf) __attribute__((always_inline)) {
-    fetch(tl, x, kp, p.k_page, k_slot, k_off, buf * kTileBytes);
+    if constexpr (!kPage16) {
+      if (((tl - t0) & 3) == 0) {
+        page4 = bounds.ahead[wv][lane];   // requested four tiles ago
+        asm volatile("" : "+v"(page4));
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // read before the next ones may arrive
+        k4 = row4(tl, kp, p.k_page, k_slot);
+        if (tl + 4 < t1) look(tl + 4);
+      }
+    }
+    fetch(tl, x, kp, k4, p.k_page, k_slot, k_off, buf * kTileBytes);
   };
   auto fetch_v = [&](int tl, const Place& x, int buf) __attribute__((always_inline)) {
-    fetch(tl, x, vp, p.v_page, v_slot, v_off, (2 + buf) * kTileBytes);
+    if constexpr (!kPage16) {
+      if (((tl - t0) & 3) == 0) v4 = row4(tl, vp, p.v_page, v_slot);
+    }
+    fetch(tl, x, vp, v4, p.v_page, v_slot, v_off, (2 + buf) * kTileBytes);
   };
+  if constexpr (!kPage16) {
+    if (t0 < t1) {
+      look(t0);
+      wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
+    }
+  }
 
   const float sl2 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);   // a negative scale's sign is in q; above 0, so that hidden stays hidden
   const float slope = kBias ? a.slopes[hq] * kLog2e : 0.f;
