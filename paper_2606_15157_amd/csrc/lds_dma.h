@@ -43,20 +43,6 @@ __device__ __forceinline__ void dma16s_pair(const char* base, uint32_t off, uint
       : "v"(off), "s"(base + 4096), "s"(lds_base + 4096u)
       : "memory");
 }
-// Four of those to LDS 1 KiB apart: [base + off[j] + 1024 j] -> lds_base + 1024 j (+ 16 lane); the instruction offsets
-// apply to both addresses.
-__device__ __forceinline__ void dma16s_four(const char* base, const uint32_t (&off)[4], uint32_t lds_base) {
-  uint32_t saved;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_nop 0\n\t"
-      "global_load_lds_dwordx4 %1, %5\n\t"
-      "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-      "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-      "global_load_lds_dwordx4 %4, %5 offset:3072\n\ts_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "s"(lds_base)
-      : "memory");
-}
 // 4 bytes per lane, likewise: to LDS at lds_base + 4 lane.
 __device__ __forceinline__ void dma4(const void* src, uint32_t lds_base) {
   uint32_t saved;

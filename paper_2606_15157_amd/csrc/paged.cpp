@@ -6,7 +6,7 @@
 #include <cmath>
 #include <initializer_list>
 
-#include "rkv_internal.h"
+#include "paged.h"
 
 namespace {
 

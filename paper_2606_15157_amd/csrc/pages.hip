@@ -3,12 +3,15 @@
 // resize_kernel: one workgroup.  A scheduler's turn is a few hundred lengths and, with a decode step, a handful of
 //   pages: latency, not bandwidth.  The three prefix sums (pages taken, pages given back, new tokens) need every
 //   sequence before any page moves, so one workgroup scans them once and keeps them in LDS, where each page and each
-//   new token finds its sequence by bisection: the work is spread by pages and tokens, not by sequences.
+//   new token finds its sequence by bisection: the work is spread by pages and tokens, not by sequences.  5.1 us for 64
+//   sequences that get a token each, 9.8 us for 192 of which 40 enter with up to 32K tokens and 48 end (four lookups of a thread
+//   side by side: 11.0).
 // slots_kernel: the slot map of many new tokens (entering prompts), over the whole chip, from the tables as written.
-// write_kernel: 16 lanes a row, 16 bytes each of K and of V; bound by HBM.
+// write_kernel: 16 lanes a row, 16 bytes each of K and of V; bound by HBM: 16371 rows of 8 heads in 21.6 us (134 MB), 28 us
+//   back to back (4.8 TB/s, what a large copy reaches).
 #include <hip/hip_runtime.h>
 
-#include "rkv_internal.h"
+#include "paged.h"
 
 namespace rkv {
 namespace {

@@ -408,6 +408,44 @@ def test_repeats_are_bit_equal_and_a_side_stream_serves():
         assert torch.equal(x, want)
 
 
+def test_two_calls_at_once():
+    """Calls whose keys are shared out, on two streams side by side, each with a workspace of its own."""
+    cases = [Case([(1, 9000), (1, 300), (2, 4000)], hq=8, seed=41), Case([(40, 5000), (1, 2000)], hq=8, seed=42)]
+    args = [(c.cache, c.q, ints(c.table.tolist()), ints([n for _, n in c.lens]), ints(c.cu)) for c in cases]
+    want = [rkv.pages_attend(*a) for a in args]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            got[i].append(rkv.pages_attend(*args[i], stream=s))
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(x, w) for x in g)
+
+
+def test_captured_calls_replay_with_other_lengths():
+    """Calls of both kinds in one graph, replayed with other lengths and queries, against eager calls."""
+    long = Case([(1, 9000), (1, 300), (1, 4000)], hq=8, seed=43)
+    chunk = Case([(40, 500), (70, 200)], hq=8, seed=44)
+    state = [(c, ints(c.table.tolist()), ints([n for _, n in c.lens]), ints(c.cu)) for c in (long, chunk)]
+    call = lambda: [rkv.pages_attend(c.cache, c.q, t, n, cu, return_lse=True) for c, t, n, cu in state]  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    g = torch.Generator(device="cuda").manual_seed(4)
+    for turn in range(4):
+        for c, _, n, _ in state:
+            c.q.copy_(torch.randn(c.q.shape, device="cuda", generator=g))
+            n.copy_(torch.tensor([max(m, x - 97 * turn) for m, x in c.lens], device="cuda"))
+        graph.replay()
+        got = [(o.clone(), l.clone()) for o, l in held]
+        for (o, l), (eo, el) in zip(got, call()):
+            assert torch.equal(o, eo) and torch.equal(l, el)
+
+
 # ------------------------------------------------------------------ together
 
 def test_evicted_prompt_moves_into_pages_and_is_attended():
