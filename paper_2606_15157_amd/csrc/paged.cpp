@@ -58,6 +58,8 @@ int check_attend(const rkv_pages* p, const rkv_attend* a) {
   if (a->softcap > 512.f) return rkv::fail(RKV_ERR_UNSUPPORTED, "softcap above 512");
   if (a->n_q_heads < 1 || a->n_q_heads % p->n_kv_heads)
     return rkv::fail(RKV_ERR_SHAPE, "n_q_heads must be a positive multiple of n_kv_heads");
+  if ((a->n_rows > 1 && a->out_token < rkv::kHeadDim) || (a->n_q_heads > 1 && a->out_head < rkv::kHeadDim))
+    return rkv::fail(RKV_ERR_INVALID_ARG, "out's rows overlap");
   if (!a->cu_q && a->n_rows != a->n_seqs) return rkv::fail(RKV_ERR_SHAPE, "without cu_q every sequence has one row");
   if (a->table_stride < a->max_pages) return rkv::fail(RKV_ERR_SHAPE, "table_stride is less than max_pages");
   if ((int64_t)a->max_pages * p->page_size >= kIntEnd - 1024)   // key tiles past the end stay below 2^31
@@ -136,6 +138,10 @@ int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream) 
   if (rows->n_outer < 0 || rows->n_tokens < 0) return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
   if (rows->n_outer == 0 || rows->n_tokens == 0) return RKV_OK;
   if (!rows->k || !rows->v || !rows->slots) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  const rkv_pages& p = *pages;
+  if ((p.n_pages > 1 && std::min(p.k_page, p.v_page) < rkv::kHeadDim) || (p.n_kv_heads > 1 && std::min(p.k_head, p.v_head) < rkv::kHeadDim) ||
+      (p.page_size > 1 && std::min(p.k_slot, p.v_slot) < rkv::kHeadDim))
+    return rkv::fail(RKV_ERR_INVALID_ARG, "the pool's rows overlap: it can be read, not written");
   if ((int64_t)rows->n_outer * rows->n_tokens >= kIntEnd / pages->n_kv_heads)
     return rkv::fail(RKV_ERR_UNSUPPORTED, "fewer than 2^31 rows a call");
   if (int st = check_layout("k rows", rows->k, {rows->k_outer, rows->k_token, rows->k_head})) return st;

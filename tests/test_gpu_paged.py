@@ -232,7 +232,7 @@ def test_attention_over_any_page_size(page, dtype):
     Case(MANY, page=page, dtype=dtype, seed=page + 1).check()
 
 
-@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (6, 2), (10, 2), (8, 1), (16, 2), (24, 1), (40, 1), (33, 1)])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (6, 2), (10, 2), (8, 1), (16, 2), (24, 1), (40, 1), (33, 1), (200, 1)])
 def test_attention_over_head_layouts(hq, hkv):
     Case(ONE, hq=hq, hkv=hkv, seed=hq).check()
     Case([(1, 300), (3, 70), (40, 200), (0, 3)], hq=hq, hkv=hkv, seed=hq + 1).check()
@@ -283,6 +283,27 @@ def test_more_row_tiles_than_are_listed():
     lens = [(1, 1 + 7 * s % 90) for s in range(1098)]
     Case(lens + [(100, 300), (65, 65)], hq=2, hkv=1, seed=22).check()
     Case([(130, 140)] * 40 + [(1, 33)] * 3, hq=2, hkv=1, seed=23).check()
+
+
+def test_calls_of_nothing():
+    c = Case([(1, 4)], seed=45)
+    none = torch.empty((0, 4, 128), dtype=torch.bfloat16, device="cuda")
+    out, lse = rkv.pages_attend(c.cache, none, ints([]).view(0, 5), ints([]), ints([0]), return_lse=True)
+    assert out.shape == (0, 4, 128) and lse.shape == (0, 4)
+    held = torch.full((3, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    rkv.pages_attend(c.cache, held.clone(), ints([]).view(0, 5), ints([]), ints([0]), out=held)
+    assert (held == 7).all()
+    out, lse = rkv.pages_attend(c.cache, c.q, ints([]).view(1, 0), ints([4]), return_lse=True)      # a table of no pages
+    assert (out == 0).all() and torch.isneginf(lse).all()
+    rkv.pages_write(c.cache, none[:, :2], none[:, :2], ints([]))
+
+
+def test_pages_that_a_window_has_left_behind():
+    """Ids of pages below every window are no longer pages."""
+    c = Case([(1, 700), (5, 300)], seed=46)
+    c.table[0, :700 // 16 - 4] = -1
+    c.table[1, :300 // 16 - 5] = 1 << 20
+    c.check(window=50)
 
 
 def test_queries_before_the_first_slot_see_nothing():

@@ -84,6 +84,11 @@ def test_bad_rows_are_refused(status, bad):
     refused(status, _abi.lib().rkv_pages_write(C.byref(pages()), C.byref(rows(**bad)), None))
 
 
+@pytest.mark.parametrize("bad", [dict(k_slot=0), dict(v_slot=64), dict(k_head=0), dict(v_page=120)])
+def test_overlapping_pools_are_not_written(bad):
+    refused(1, _abi.lib().rkv_pages_write(C.byref(pages(**bad)), C.byref(rows()), None), "overlap")
+
+
 def test_no_rows_need_no_gpu():
     L = _abi.lib()
     assert L.rkv_pages_write(C.byref(pages()), C.byref(rows(n_tokens=0, k=None, v=None, slots=None)), None) == 0
@@ -103,7 +108,7 @@ def attend(**kw):
     (1, dict(q=None)), (1, dict(out=None)), (1, dict(lens=None)), (1, dict(table=None)), (1, dict(n_seqs=-1)), (1, dict(n_rows=-1)),
     (1, dict(max_pages=-1)), (1, dict(max_q=-1)), (1, dict(max_kv=-2)), (1, dict(window=-1)), (1, dict(causal=2)),
     (1, dict(scale=float("nan"))), (1, dict(scale=float("inf"))), (1, dict(softcap=-1.0)), (1, dict(softcap=float("inf"))), (1, dict(softcap=1e-35)), (4, dict(softcap=600.0)),
-    (1, dict(q_token=-8)), (2, dict(n_q_heads=3)), (2, dict(n_q_heads=0)), (2, dict(cu_q=None)), (2, dict(table_stride=3)),
+    (1, dict(q_token=-8)), (1, dict(out_token=0)), (1, dict(out_head=64)), (2, dict(n_q_heads=3)), (2, dict(n_q_heads=0)), (2, dict(cu_q=None)), (2, dict(table_stride=3)),
     (4, dict(q=P + 8)), (4, dict(out=P + 4)), (4, dict(q_head=130)), (4, dict(out_token=513)),
     (4, dict(max_pages=1 << 27, table_stride=1 << 27)), (4, dict(n_rows=1 << 29))])
 def test_bad_attention_calls_are_refused(status, bad):
