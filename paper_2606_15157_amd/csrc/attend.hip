@@ -22,7 +22,7 @@
 // Measured with 32 query and 8 KV heads, bf16, pages of 16: a prompt of 16384 1.95 ms (1.13 PFLOP/s; the matrix pipes are busy
 // 59 % of the cycles, and the power limit sets the clock: fewer LDS reads or instructions count, not more overlap); 512
 // tokens after 32768 287 us (0.97 PFLOP/s); 64 evicted caches of 1024 rows 41 us (6.5 TB/s of keys and values), 64 ragged
-// sequences of 512 to 8192 159 us (5.1 TB/s), one token after 1024 13.4 us (16 key tiles one after another).
+// sequences of 512 to 8192 159 us (5.1 TB/s), one token after 1024 12.0 us (16 key tiles one after another).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -479,9 +479,23 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       if (tl + 1 < t1) wait_vmcnt<8>();   // the next tile may be in flight
       else wait_vmcnt<0>();
       asm volatile("" ::: "memory");
+      u32x4 kf[4];
+      u32x2 vf[8];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) kf[s] = lds_read16(k_at + buf + ((4 * s + lg) ^ l16) * 16);
+#pragma unroll
+      for (int d = 0; d < 8; ++d) vf[d] = lds_read_tr(v_at + buf + ((2 * d + ((l16 & 3) >> 1)) ^ (4 * (l16 >> 2))) * 16);
+      // The whole tile is in registers before the first product, and its memory free for the tile after the next, whose
+      // fetch then runs under the softmax: one token after 4096 in one workgroup a head 41 -> 35 us.
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt 0
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < 4; ++s) x = mma16<kF16>(lds_read16(k_at + buf + ((4 * s + lg) ^ l16) * 16), q[s], x);
+      for (int s = 0; s < 4; ++s) x = mma16<kF16>(kf[s], q[s], x);
+      if (tl + 2 < t1) {
+        fetch_both(tl + 2, (tl - t0) & 1);
+        if (tl + 3 < t1) find(tl + 3, next);
+      }
       const int key0 = tl * kKeys + 16 * wv;
       const float far = (float)(pos - key0 - 4 * lg);
 #pragma unroll
@@ -513,13 +527,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       const u32x2 pr = {pack<kF16>(x[0], x[1]), pack<kF16>(x[2], x[3])};
 #pragma unroll
       for (int d = 0; d < 8; ++d)
-        o[d] = mma16s<kF16>(lds_read_tr(v_at + buf + ((2 * d + ((l16 & 3) >> 1)) ^ (4 * (l16 >> 2))) * 16), pr, o[d]);
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt 0: this wave's reads of the tile are done
-      if (tl + 2 < t1) {
-        fetch_both(tl + 2, (tl - t0) & 1);
-        if (tl + 3 < t1) find(tl + 3, next);
-      }
+        o[d] = mma16s<kF16>(vf[d], pr, o[d]);
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);

@@ -87,11 +87,11 @@ int64_t usual_rows(const rkv_pages* p, const rkv_attend* a) {
 
 // Whether the row tiles' keys are shared out (attend_shares_kernel and a join) or every tile has a workgroup of its own.
 // Shared out, a call pays some 8 us for the list and the join, and rows that are split go through memory; not shared out,
-// it lasts as long as its longest tile and leaves CUs idle below 512 tiles.  64 keys take about 0.6 us with at most 16 rows,
+// it lasts as long as its longest tile and leaves CUs idle below 512 tiles.  64 keys take about 0.5 us with at most 16 rows,
 // 1 us with more, and at 5.5 TB/s 0.006 us of the whole chip's time.  Measured on 32 query and 8 KV heads, us, not shared
 // against shared:
-//   one token a sequence: one of 200 keys 9 / 14, of 1024 14 / 15, of 4096 41 / 16, of 32768 317 / 32; 16 of 2048 25 / 33, four
-//   of 8192 83 / 32; 64 of 1024 42 / 50, of 2048 93 / 101, of 64 to 8192 130 / 103, of 512 to 8192 189 / 159;
+//   one token a sequence: one of 200 keys 9 / 14, of 1024 12 / 15, of 4096 35 / 16, of 32768 250 / 32; 16 of 2048 23 / 33, four
+//   of 8192 67 / 33; 64 of 1024 42 / 50, of 2048 92 / 101, of 64 to 8192 127 / 103, of 512 to 8192 187 / 159;
 //   prompts: 512 tokens 16 / 34, 1024 27 / 53, 2048 53 / 99, 16384 1997 / 2282; 512 after 32768 568 / 292, 64 after 16320
 //   292 / 41, 256 each of four after 7936 200 / 160, 512 each of eight after 3584 258 / 287, 8 each of 16 after 4088 75 / 55.
 bool shared_out(const rkv_pages* p, const rkv_attend* a) {
@@ -101,9 +101,9 @@ bool shared_out(const rkv_pages* p, const rkv_attend* a) {
   const int64_t kv = a->max_kv ? std::min<int64_t>(a->max_kv, most) : most;
   if (rows > rkv::kAttendRows) return items < 512 && kv > 2048;
   if (rows > 16) return kv > (items >= 256 ? 1024 : 512);
-  // 3 + 0.6 t us for t tiles of keys against 13 + 0.4 * 0.006 items t where lengths differ as above
+  // 3 + 0.5 t us for t tiles of keys against 13 + 0.4 * 0.006 items t where lengths differ as above
   const int64_t t = (kv + 63) / 64;
-  return t > 32 || t * (250 - std::min<int64_t>(items, 250)) > 4200;
+  return t > 32 || t * (208 - std::min<int64_t>(items, 208)) > 4200;
 }
 
 size_t attend_bytes(const rkv_pages* p, const rkv_attend* a) {
