@@ -155,7 +155,8 @@ __device__ __forceinline__ int slots_of(const AttendLaunch& A, int seq) {
 }
 __device__ __forceinline__ int end_row(const rkv_attend& a, int seq) { return a.cu_q ? first_row(a, seq + 1) : min(seq + 1, a.n_rows); }
 
-// A partial sum in the workspace: slot_rows rows of 128 floats (not divided by l), then their m and l in pairs.
+// A partial sum in the workspace: slot_rows rows of 128 floats (not divided by l), then their m and l in pairs; 16-byte aligned,
+// slot_rows being even.
 __device__ __forceinline__ float* part_slot(const AttendLaunch& A, int slot) {
   return A.parts + (size_t)slot * A.slot_rows * (kHeadDim + 2);
 }

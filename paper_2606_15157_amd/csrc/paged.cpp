@@ -74,10 +74,11 @@ bool nothing_to_do(const rkv_attend* a) { return a->n_seqs == 0 || a->n_rows == 
 
 constexpr size_t kRecordBytes = sizeof(int32_t) * 4 * rkv::kAttendShares;
 
-// Rows of the largest row tile.
-int32_t tile_rows(const rkv_pages* p, const rkv_attend* a) {
+// Rows of a partial sum: those of the largest row tile, made even so that every partial sum (130 floats a row) is 16-byte
+// aligned, as its rows are written and read.
+int32_t part_rows(const rkv_pages* p, const rkv_attend* a) {
   const int64_t most = (int64_t)(a->cu_q ? a->n_rows : 1) * (a->n_q_heads / p->n_kv_heads);
-  return (int32_t)std::min<int64_t>(most, rkv::kAttendRows);
+  return (int32_t)std::min<int64_t>((most + 1) & ~int64_t(1), rkv::kAttendRows);
 }
 
 // Rows of the longest sequence, if max_q says so, else of the average one.
@@ -108,7 +109,7 @@ bool shared_out(const rkv_pages* p, const rkv_attend* a) {
 
 size_t attend_bytes(const rkv_pages* p, const rkv_attend* a) {
   if (nothing_to_do(a) || !shared_out(p, a)) return 0;
-  return kRecordBytes + sizeof(float) * 2 * rkv::kAttendShares * (size_t)tile_rows(p, a) * (rkv::kHeadDim + 2);
+  return kRecordBytes + sizeof(float) * 2 * rkv::kAttendShares * (size_t)part_rows(p, a) * (rkv::kHeadDim + 2);
 }
 
 }  // namespace
@@ -184,7 +185,7 @@ int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size
   const int64_t full = (int64_t)a->n_rows * L.group / rkv::kAttendRows;
   L.few_long = 2 * full < L.n_tiles;
   L.n_places = a->n_seqs + (int32_t)std::min<int64_t>(2 * full, L.n_tiles);
-  L.slot_rows = tile_rows(pages, a);
+  L.slot_rows = part_rows(pages, a);
   // A part of 128 rows is written and read again, as many bytes as four key tiles: not for less than eight.  Few rows
   // cost nothing beside a tile (one token after 1K: 15 us with shares of one, 17 of four, 21 of eight).
   L.least = usual_rows(pages, a) > 32 ? 8 : 1;

@@ -43,7 +43,7 @@ struct AttendLaunch {
   int32_t n_tiles;     // row tiles of all sequences, at most
   int32_t n_places;    // places of attend_tiles_kernel: n_seqs, then numbers of long sequences' tiles
   int32_t few_long;    // how those are numbered
-  int32_t slot_rows;   // rows of a partial sum
+  int32_t slot_rows;   // rows of a partial sum, an even number
   int32_t least;       // key tiles of a share, at least
   int32_t* records;    // [kAttendShares][4], then
   float* parts;        // [2 kAttendShares] partial sums; null: a workgroup per row tile

@@ -572,3 +572,15 @@ def test_refusals_reach_python():
         kw = {"table": table, "lens": lens, **bad}
         with pytest.raises(ValueError):
             rkv.pages_attend(c.cache, c.q, kw.pop("table"), kw.pop("lens"), **kw)
+
+
+@pytest.mark.parametrize("hq,hkv,lens,each", [(1, 1, [(1, 9000)], True), (3, 1, [(1, 9000)], True), (3, 1, [(1, 9000)], False),
+                                              (6, 2, [(1, 5000), (1, 9001)], True), (1, 1, [(17, 9000)], False), (3, 3, [(19, 4001), (2, 6000)], False),
+                                              (5, 1, [(5, 9000)], False), (1, 1, [(127, 3001)], False)])
+def test_split_rows_of_odd_numbers(hq, hkv, lens, each):
+    """Calls whose keys are shared out and whose tiles have an odd number of rows, with cu_q and (each) without."""
+    c = Case(lens, hq=hq, hkv=hkv, seed=51)
+    out, lse = c.check()
+    if each:
+        got = rkv.pages_attend(c.cache, c.q, ints(c.table.tolist()), ints([n for _, n in lens]), return_lse=True)
+        assert torch.equal(got[0], out) and torch.equal(got[1], lse)

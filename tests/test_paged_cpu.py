@@ -180,3 +180,14 @@ def test_packed_structs_are_the_c_ones():
         assert [getattr(got, name) for name, _ in cls._fields_] == values
         with pytest.raises(ValueError):
             cls.pack(*([1 << 70] * len(kinds)))
+
+
+@pytest.mark.parametrize("group,rows,cu_q", [(1, 1, None), (1, 1, P), (3, 1, None), (3, 3, P), (5, 5, P), (1, 129, P), (2, 4, P)])
+def test_partial_sums_are_16_byte_aligned(group, rows, cu_q):
+    """512 records of 16 bytes, then 1024 partial sums of one size, which are written and read 16 bytes at a time."""
+    L, n = _abi.lib(), C.c_size_t()
+    seqs = 1 if cu_q else rows
+    a = attend(n_seqs=seqs, n_rows=rows, n_q_heads=2 * group, cu_q=cu_q, out_token=256 * group, max_pages=400, table_stride=400)
+    assert L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(a), C.byref(n)) == 0
+    parts = n.value - 512 * 16
+    assert parts >= 1024 * min(128, (rows if cu_q else 1) * group) * 130 * 4 and parts % (1024 * 16) == 0
