@@ -3,6 +3,7 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <initializer_list>
 
@@ -25,6 +26,23 @@ int check_layout(const char* what, const void* ptr, std::initializer_list<int64_
   for (int64_t s : strides)
     if (s % 8) return rkv::fail(RKV_ERR_UNSUPPORTED, std::string(what) + ": strides must be multiples of 8 elements");
   return RKV_OK;
+}
+
+// Whether rows of 128 elements, at sum_i index_i stride_i for index_i < count_i, are told apart by their dimensions: taken by
+// stride, each is at least the extent of the smaller ones.  So are those of every slice and permutation of a dense tensor.
+struct Dim {
+  int64_t stride, count;
+};
+template <size_t kDims>
+bool rows_nest(std::array<Dim, kDims> dims) {
+  std::sort(dims.begin(), dims.end(), [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  __int128 extent = rkv::kHeadDim;
+  for (const Dim& d : dims) {
+    if (d.count <= 1) continue;
+    if (d.stride < extent) return false;
+    extent += (__int128)d.stride * (d.count - 1);
+  }
+  return true;
 }
 
 int check_pages(const rkv_pages* p) {
@@ -58,8 +76,8 @@ int check_attend(const rkv_pages* p, const rkv_attend* a) {
   if (a->softcap > 512.f) return rkv::fail(RKV_ERR_UNSUPPORTED, "softcap above 512");
   if (a->n_q_heads < 1 || a->n_q_heads % p->n_kv_heads)
     return rkv::fail(RKV_ERR_SHAPE, "n_q_heads must be a positive multiple of n_kv_heads");
-  if ((a->n_rows > 1 && a->out_token < rkv::kHeadDim) || (a->n_q_heads > 1 && a->out_head < rkv::kHeadDim))
-    return rkv::fail(RKV_ERR_INVALID_ARG, "out's rows overlap");
+  if (!rows_nest<2>({{{a->out_token, a->n_rows}, {a->out_head, a->n_q_heads}}}))
+    return rkv::fail(RKV_ERR_INVALID_ARG, "out's rows overlap (no stride may be less than the extent of the smaller ones)");
   if (!a->cu_q && a->n_rows != a->n_seqs) return rkv::fail(RKV_ERR_SHAPE, "without cu_q every sequence has one row");
   if (a->table_stride < a->max_pages) return rkv::fail(RKV_ERR_SHAPE, "table_stride is less than max_pages");
   if ((int64_t)a->max_pages * p->page_size >= kIntEnd - 1024)   // key tiles past the end stay below 2^31
@@ -139,14 +157,14 @@ int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream) 
   if (rows->n_outer < 0 || rows->n_tokens < 0) return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
   if (rows->n_outer == 0 || rows->n_tokens == 0) return RKV_OK;
   if (!rows->k || !rows->v || !rows->slots) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
-  const rkv_pages& p = *pages;
-  if ((p.n_pages > 1 && std::min(p.k_page, p.v_page) < rkv::kHeadDim) || (p.n_kv_heads > 1 && std::min(p.k_head, p.v_head) < rkv::kHeadDim) ||
-      (p.page_size > 1 && std::min(p.k_slot, p.v_slot) < rkv::kHeadDim))
-    return rkv::fail(RKV_ERR_INVALID_ARG, "the pool's rows overlap: it can be read, not written");
   if ((int64_t)rows->n_outer * rows->n_tokens >= kIntEnd / pages->n_kv_heads)
     return rkv::fail(RKV_ERR_UNSUPPORTED, "fewer than 2^31 rows a call");
   if (int st = check_layout("k rows", rows->k, {rows->k_outer, rows->k_token, rows->k_head})) return st;
   if (int st = check_layout("v rows", rows->v, {rows->v_outer, rows->v_token, rows->v_head})) return st;
+  const rkv_pages& p = *pages;
+  if (!rows_nest<3>({{{p.k_page, p.n_pages}, {p.k_head, p.n_kv_heads}, {p.k_slot, p.page_size}}}) ||
+      !rows_nest<3>({{{p.v_page, p.n_pages}, {p.v_head, p.n_kv_heads}, {p.v_slot, p.page_size}}}))
+    return rkv::fail(RKV_ERR_INVALID_ARG, "the pool's rows overlap (no stride may be less than the extent of the smaller ones): it can be read, not written");
   rkv::WriteLaunch W{};
   W.p = *pages;
   W.r = *rows;

@@ -191,3 +191,30 @@ def test_partial_sums_are_16_byte_aligned(group, rows, cu_q):
     assert L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(a), C.byref(n)) == 0
     parts = n.value - 512 * 16
     assert parts >= 1024 * min(128, (rows if cu_q else 1) * group) * 130 * 4 and parts % (1024 * 16) == 0
+
+
+@pytest.mark.parametrize("bad", [
+    dict(k_page=128, k_head=128, k_slot=128), dict(v_page=128, v_head=128, v_slot=128), dict(k_slot=128, k_head=128), dict(v_head=1920, v_slot=128),
+    dict(k_page=128, k_head=384, k_slot=1024), dict(k_page=1920, n_kv_heads=1), dict(v_page=4080, v_head=2048), dict(k_slot=120, n_pages=1, n_kv_heads=1)])
+def test_pools_whose_dimensions_run_into_each_other_are_not_written(bad):
+    refused(1, _abi.lib().rkv_pages_write(C.byref(pages(**{**NESTED, **bad})), C.byref(rows()), None), "overlap")
+
+
+NESTED = dict(k_page=4096, k_head=2048, k_slot=128, v_page=4096, v_head=2048, v_slot=128)
+
+
+@pytest.mark.parametrize("bad", [dict(out_token=128, out_head=128), dict(out_token=384, out_head=128), dict(out_token=128, out_head=640),
+                                 dict(out_token=504), dict(out_token=1 << 62, out_head=120)])
+def test_out_rows_that_run_into_each_other_are_refused(bad):
+    n = C.c_size_t()
+    refused(1, _abi.lib().rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(attend(**bad)), C.byref(n)), "overlap")
+    refused(1, _abi.lib().rkv_pages_attend(C.byref(pages()), C.byref(attend(**bad)), None, 0, None), "overlap")
+
+
+@pytest.mark.parametrize("good", [dict(out_token=128, out_head=768), dict(out_token=512, out_head=128), dict(out_token=1 << 62, out_head=1 << 58),
+                                  dict(out_token=0, n_rows=1), dict(out_head=0, n_q_heads=1, out_token=128)])
+def test_out_rows_of_either_order_are_taken(good):
+    n = C.c_size_t()
+    pool = pages(n_kv_heads=1) if "n_q_heads" in good else pages()
+    a = attend(**good)
+    assert _abi.lib().rkv_pages_attend_workspace_size(C.byref(pool), C.byref(a), C.byref(n)) == 0
