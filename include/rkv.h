@@ -410,7 +410,8 @@ typedef struct {
  * The pool's rows may not overlap: its dimensions of more than one entry taken by stride, no stride is less than the extent of
  * the smaller ones (128 elements for the smallest).  An overlapping pool can be attended.
  * Errors: RKV_ERR_INVALID_ARG (null pointers, negative sizes or strides, unknown dtype, a pool whose rows overlap), RKV_ERR_UNSUPPORTED (head_dim
- * != 128, pointers not 16-byte aligned, strides not multiples of 8, 2^31 rows or slots), RKV_ERR_HIP. */
+ * != 128, pointers not 16-byte aligned, strides not multiples of 8, n_outer * n_tokens * n_kv_heads above 2^28 - 16, 2^31 slots),
+ * RKV_ERR_HIP. */
 int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream);
 
 /* One rkv_pages_attend call.  Device pointers:
@@ -456,7 +457,8 @@ typedef struct {
  * Errors: RKV_ERR_INVALID_ARG (null pointers, negative sizes or strides, unknown dtype, scale or softcap not finite,
  * softcap < 0 or below 1e-30 of the scale, out rows that overlap, by the rule of rkv_pages_write's pool), RKV_ERR_SHAPE (Hq not a multiple of Hkv, n_rows != n_seqs without cu_q, table_stride < max_pages),
  * RKV_ERR_UNSUPPORTED (head_dim != 128, q or out not 16-byte aligned, strides not multiples of 8, softcap above 512
- * (its scores lose 2^-24 of the cap), max_pages * page_size from 2^31 - 1024, n_rows * n_q_heads from 2^30),
+ * (its scores lose 2^-24 of the cap), max_pages * page_size from 2^31 - 1024, n_rows * n_q_heads from 2^30, more row tiles
+ * than a launch takes: never while (n_seqs + n_rows * (Hq / Hkv) / 64) * Hkv is below 2^24),
  * RKV_ERR_WORKSPACE, RKV_ERR_HIP.  Validation ends before the first launch. */
 int rkv_pages_attend_workspace_size(const rkv_pages* pages, const rkv_attend* a, size_t* bytes);
 int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size_t ws_bytes, void* stream);

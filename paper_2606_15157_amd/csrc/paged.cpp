@@ -12,6 +12,7 @@
 namespace {
 
 constexpr int64_t kIntEnd = int64_t(1) << 31;
+constexpr int64_t kGridEnd = int64_t(1) << 24;   // workgroups of 256 threads: HIP takes fewer than 2^32 threads in x
 
 int launched(int err) {
   if (err) return rkv::fail(RKV_ERR_HIP, std::string("kernel launch failed: ") + hipGetErrorString((hipError_t)err));
@@ -60,9 +61,13 @@ int check_pages(const rkv_pages* p) {
 }
 
 // Row tiles, with one part-filled tile for each sequence.
-int64_t row_tiles(const rkv_pages* p, const rkv_attend* a) {
-  return (int64_t)a->n_rows * (a->n_q_heads / p->n_kv_heads) / rkv::kAttendRows + a->n_seqs;
-}
+int64_t full_tiles(const rkv_pages* p, const rkv_attend* a) { return (int64_t)a->n_rows * (a->n_q_heads / p->n_kv_heads) / rkv::kAttendRows; }
+int64_t row_tiles(const rkv_pages* p, const rkv_attend* a) { return full_tiles(p, a) + a->n_seqs; }
+
+// Places of attend_tiles_kernel: the sequences, then the numbers of long sequences' tiles.
+int64_t places(const rkv_pages* p, const rkv_attend* a) { return a->n_seqs + std::min(2 * full_tiles(p, a), row_tiles(p, a)); }
+bool nothing_to_do(const rkv_attend* a) { return a->n_seqs == 0 || a->n_rows == 0; }
+bool shared_out(const rkv_pages* p, const rkv_attend* a);
 
 int check_attend(const rkv_pages* p, const rkv_attend* a) {
   if (int st = check_pages(p)) return st;
@@ -83,12 +88,11 @@ int check_attend(const rkv_pages* p, const rkv_attend* a) {
   if ((int64_t)a->max_pages * p->page_size >= kIntEnd - 1024)   // key tiles past the end stay below 2^31
     return rkv::fail(RKV_ERR_UNSUPPORTED, "a sequence holds fewer than 2^31 - 1024 slots");
   if ((int64_t)a->n_rows * a->n_q_heads >= kIntEnd / 2) return rkv::fail(RKV_ERR_UNSUPPORTED, "n_rows * n_q_heads must be below 2^30");
-  if ((row_tiles(p, a) + a->n_seqs) * p->n_kv_heads >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "too many sequences");
+  if (!nothing_to_do(a) && !shared_out(p, a) && places(p, a) * p->n_kv_heads >= kGridEnd)   // n_tiles then is below 2^31, too
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "too many sequences for one launch");
   if (int st = check_layout("q", a->q, {a->q_token, a->q_head})) return st;
   return check_layout("out", a->out, {a->out_token, a->out_head});
 }
-
-bool nothing_to_do(const rkv_attend* a) { return a->n_seqs == 0 || a->n_rows == 0; }
 
 constexpr size_t kRecordBytes = sizeof(int32_t) * 4 * rkv::kAttendShares;
 
@@ -157,8 +161,8 @@ int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream) 
   if (rows->n_outer < 0 || rows->n_tokens < 0) return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
   if (rows->n_outer == 0 || rows->n_tokens == 0) return RKV_OK;
   if (!rows->k || !rows->v || !rows->slots) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
-  if ((int64_t)rows->n_outer * rows->n_tokens >= kIntEnd / pages->n_kv_heads)
-    return rkv::fail(RKV_ERR_UNSUPPORTED, "fewer than 2^31 rows a call");
+  if ((int64_t)rows->n_outer * rows->n_tokens > 16 * (kGridEnd - 1) / pages->n_kv_heads)
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "at most 2^28 - 16 rows a call, each head's counted");
   if (int st = check_layout("k rows", rows->k, {rows->k_outer, rows->k_token, rows->k_head})) return st;
   if (int st = check_layout("v rows", rows->v, {rows->v_outer, rows->v_token, rows->v_head})) return st;
   const rkv_pages& p = *pages;
@@ -200,9 +204,8 @@ int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size
   L.by_page = rkv::fast_div(pages->page_size);
   L.by_group = rkv::fast_div(L.group);
   L.n_tiles = (int32_t)row_tiles(pages, a);
-  const int64_t full = (int64_t)a->n_rows * L.group / rkv::kAttendRows;
-  L.few_long = 2 * full < L.n_tiles;
-  L.n_places = a->n_seqs + (int32_t)std::min<int64_t>(2 * full, L.n_tiles);
+  L.few_long = 2 * full_tiles(pages, a) < L.n_tiles;
+  L.n_places = (int32_t)places(pages, a);
   L.slot_rows = part_rows(pages, a);
   // A part of 128 rows is written and read again, as many bytes as four key tiles: not for less than eight.  Few rows
   // cost nothing beside a tile (one token after 1K: 15 us with shares of one, 17 of four, 21 of eight).

@@ -218,3 +218,21 @@ def test_out_rows_of_either_order_are_taken(good):
     pool = pages(n_kv_heads=1) if "n_q_heads" in good else pages()
     a = attend(**good)
     assert _abi.lib().rkv_pages_attend_workspace_size(C.byref(pool), C.byref(a), C.byref(n)) == 0
+
+
+@pytest.mark.parametrize("bad", [dict(n_tokens=1 << 27), dict(n_tokens=(1 << 27) - 7), dict(n_outer=1 << 13, n_tokens=1 << 14), dict(n_outer=1 << 15, n_tokens=1 << 13)])
+def test_more_rows_than_a_launch_takes_are_refused(bad):
+    """16 rows a workgroup of 256 threads, fewer than 2^32 threads; two heads a row here."""
+    refused(4, _abi.lib().rkv_pages_write(C.byref(pages(**NESTED)), C.byref(rows(**bad)), None), "rows")
+
+
+@pytest.mark.parametrize("status,kw", [
+    (0, dict(n_seqs=(1 << 23) - 1)), (4, dict(n_seqs=1 << 23)), (4, dict(n_seqs=1 << 24)), (4, dict(n_seqs=1 << 23, n_rows=1 << 23, cu_q=None)),
+    (0, dict(n_seqs=1, n_rows=(1 << 28) - 1)), (4, dict(n_seqs=1 << 22, n_rows=(1 << 28) - 1)), (0, dict(n_seqs=0, n_rows=(1 << 28) - 1))])
+def test_more_row_tiles_than_a_launch_takes_are_refused(status, kw):
+    """A workgroup of 256 threads per place and KV head, two of which are here."""
+    L, n = _abi.lib(), C.c_size_t()
+    got = L.rkv_pages_attend_workspace_size(C.byref(pages()), C.byref(attend(**kw)), C.byref(n))
+    assert got == status
+    if status:
+        refused(status, L.rkv_pages_attend(C.byref(pages()), C.byref(attend(**kw)), None, 0, None), "sequences")
