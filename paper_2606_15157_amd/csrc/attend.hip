@@ -842,18 +842,18 @@ struct List {
   int32_t slots[kListed];        // of each sequence
   int32_t before[kListed + 1];   // key tiles of a head before row tile i
   uint16_t seq[kListed];         // sequence of row tile i
-  int64_t wave[4];
+  int32_t wave[4];
 };
 constexpr int kPer = kListed / 256;   // row tiles of a thread
 
-// Fills the list; the key tiles of a head, which 32 bits may not hold.
-__device__ __forceinline__ int64_t make_list(const AttendLaunch& A, List& L) {
+// Fills the list; the key tiles of a head, fewer than 2^31 (the host lets no other call here).
+__device__ __forceinline__ int make_list(const AttendLaunch& A, List& L) {
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = A.a.n_seqs;
   for (int s = tid; s <= n; s += 256) L.row0[s] = s < n ? first_row(A.a, s) : end_row(A.a, n - 1);
   for (int s = tid; s < n; s += 256) L.slots[s] = slots_of(A, s);
   __syncthreads();
   int cost[kPer];
-  uint32_t sum = 0;   // 256 tiles of a wave, below 2^23 key tiles each
+  int sum = 0;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int tile = tid * kPer + i;
@@ -875,24 +875,23 @@ __device__ __forceinline__ int64_t make_list(const AttendLaunch& A, List& L) {
     }
     sum += cost[i];
   }
-  uint32_t x = sum;
+  int x = sum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t y = __shfl_up(x, o);
+    const int y = __shfl_up(x, o);
     if (lane >= o) x += y;
   }
   if (lane == 63) L.wave[wv] = x;
   __syncthreads();
-  int64_t before = x - sum;
+  int before = x - sum;
   for (int i = 0; i < wv; ++i) before += L.wave[i];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    L.before[tid * kPer + i] = (int32_t)before;
+    L.before[tid * kPer + i] = before;
     before += cost[i];
   }
-  if (tid == 255) L.before[kListed] = (int32_t)before;
-  int64_t all = L.wave[0] + L.wave[1] + L.wave[2] + L.wave[3];
-  all = (int64_t)((uint64_t)(uint32_t)uniform((int)(all >> 32)) << 32 | (uint32_t)uniform((int)all));
+  if (tid == 255) L.before[kListed] = before;
+  const int all = uniform(L.wave[0] + L.wave[1] + L.wave[2] + L.wave[3]);
   __syncthreads();
   return all;
 }
@@ -906,45 +905,35 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
   __shared__ Bounds bounds;
   __shared__ List L;
   const int tid = threadIdx.x;
-  const int64_t all = make_list(A, L);
+  const int all = make_list(A, L);
   const int w = (int)(blockIdx.x % 8) * (kShares / 8) + (int)blockIdx.x / 8;
   i32x4 record = {0, 0, 0, 0};   // parts + 1024 head, sequence's first row, first row of the tile, rows of the sequence
-  if (all < (int64_t(1) << 31)) {
-    const int64_t total = all * A.p.n_kv_heads;
-    const int64_t share = max((int64_t)A.least, (total + kShares - 1) / kShares);
-    int64_t pos = w * share;
-    const int64_t end = min(total, pos + share);
-    while (pos < end) {
-      const int h = uniform((int)(pos / all)), rem = uniform((int)(pos - h * all));
-      int lo = 0, hi = kListed;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (L.before[mid] <= rem) lo = mid;
-        else hi = mid;
-      }
-      const int tile = uniform(lo), seq = uniform(L.seq[tile]);
-      const int u0 = rem - uniform(L.before[tile]), count = uniform(L.before[tile + 1]) - uniform(L.before[tile]);
-      const int n = (int)min((int64_t)(count - u0), end - pos);
-      const int row0 = uniform(L.row0[seq]), n_q = uniform(L.row0[seq + 1]) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
-      float* part = nullptr;
-      if (n < count) {
-        part = part_slot(A, 2 * w + (u0 == 0));
-        if (u0 == 0) {
-          record = i32x4{(int)((pos + count - 1) / share) - w + 1 + 1024 * h, row0, r0, n_q * A.group};
-        }
-      }
-      attend_tile<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, u0, n, part);
-      lds_sync();   // the memory that rows left by is the next tiles'
-      pos += n;
+  const int64_t total = (int64_t)all * A.p.n_kv_heads;
+  const int64_t share = max((int64_t)A.least, (total + kShares - 1) / kShares);
+  int64_t pos = w * share;
+  const int64_t end = min(total, pos + share);
+  while (pos < end) {
+    const int h = uniform((int)(pos / all)), rem = uniform((int)(pos - (int64_t)h * all));
+    int lo = 0, hi = kListed;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (L.before[mid] <= rem) lo = mid;
+      else hi = mid;
     }
-  } else {   // more key tiles than the list counts: whole row tiles in turn
-    for (int i = w; i < A.n_tiles * A.p.n_kv_heads; i += kShares) {
-      const int tile = i / A.p.n_kv_heads, h = i - tile * A.p.n_kv_heads, seq = uniform(L.seq[tile]);
-      const int row0 = uniform(L.row0[seq]), n_q = uniform(L.row0[seq + 1]) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
-      if (r0 < 0 || r0 >= n_q * A.group) continue;
-      attend_tile<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, 0, -1, nullptr);
-      lds_sync();
+    const int tile = uniform(lo), seq = uniform(L.seq[tile]);
+    const int u0 = rem - uniform(L.before[tile]), count = uniform(L.before[tile + 1]) - uniform(L.before[tile]);
+    const int n = (int)min((int64_t)(count - u0), end - pos);
+    const int row0 = uniform(L.row0[seq]), n_q = uniform(L.row0[seq + 1]) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
+    float* part = nullptr;
+    if (n < count) {
+      part = part_slot(A, 2 * w + (u0 == 0));
+      if (u0 == 0) {
+        record = i32x4{(int)((pos + count - 1) / share) - w + 1 + 1024 * h, row0, r0, n_q * A.group};
+      }
     }
+    attend_tile<kF16, kCap, kBias, kPage16>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, u0, n, part);
+    lds_sync();   // the memory that rows left by is the next tiles'
+    pos += n;
   }
   if (tid == 0) reinterpret_cast<i32x4*>(A.records)[w] = record;
 }

@@ -120,7 +120,8 @@ int64_t usual_rows(const rkv_pages* p, const rkv_attend* a) {
 bool shared_out(const rkv_pages* p, const rkv_attend* a) {
   const int64_t tiles = row_tiles(p, a), items = tiles * p->n_kv_heads, rows = usual_rows(p, a);
   const int64_t most = (int64_t)a->max_pages * p->page_size;
-  if (tiles > rkv::kAttendListed || most > (1 << 29) || p->n_kv_heads >= (1 << 20)) return false;   // what the list and its records hold
+  if (tiles > rkv::kAttendListed || tiles * std::max<int64_t>(1, (most + 63) / 64) >= kIntEnd || p->n_kv_heads >= (1 << 20))
+    return false;   // what the list and its records hold
   const int64_t kv = a->max_kv ? std::min<int64_t>(a->max_kv, most) : most;
   if (rows > rkv::kAttendRows) return items < 512 && kv > 2048;
   if (rows > 16) return kv > (items >= 256 ? 1024 : 512);

@@ -236,3 +236,12 @@ def test_more_row_tiles_than_a_launch_takes_are_refused(status, kw):
     assert got == status
     if status:
         refused(status, L.rkv_pages_attend(C.byref(pages()), C.byref(attend(**kw)), None, 0, None), "sequences")
+
+
+@pytest.mark.parametrize("seqs,split", [(1, True), (100, True), (252, True), (256, False), (512, False), (1000, False)])
+def test_lists_whose_key_tiles_32_bits_may_not_hold_are_not_split(seqs, split):
+    """Tables of 2^29 slots a sequence, 2^23 key tiles: up to 255 row tiles (three here are the long sequences' room)."""
+    a = attend(n_seqs=seqs, n_rows=192, max_pages=1 << 16, table_stride=1 << 16)
+    n = C.c_size_t()
+    assert _abi.lib().rkv_pages_attend_workspace_size(C.byref(pages(page_size=1 << 13)), C.byref(a), C.byref(n)) == 0
+    assert (n.value > 0) == split
