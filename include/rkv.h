@@ -449,7 +449,8 @@ typedef struct {
  *   out = sum_j softmax_j(x) v_j,  lse = log sum_j exp(x_j); a row that sees nothing: out 0, lse -infinity.
  * Slots are the cache's: in a cache that an eviction compacted, windows, documents and distances count kept rows.
  * Products on bf16 / fp16 MFMA with 32-bit accumulation; softmax statistics and sums in 32 bits; probabilities are
- * rounded to the pool's dtype for the product with V, once, before they are divided by their unrounded sum.
+ * rounded to the pool's dtype for the product with V, once, before they are divided by their unrounded sum (fp16 ones below
+ * 2^-21 of the row's largest to a multiple of 2^-31 of it or less).
  * Page ids are checked: a slot whose page is outside [0, n_pages) reads as a row of zeros.  Slots outside a sequence's
  * visible ones are never read into a result, whatever they hold; lens are cut to [0, max_pages * page_size].
  * ws: device workspace of rkv_pages_attend_workspace_size bytes, 256-byte aligned, one for each call in flight, and for

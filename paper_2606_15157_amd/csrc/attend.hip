@@ -11,7 +11,8 @@
 //                 8 + 4 half + 0..3 of each 16.  V^T in that order is two transposing LDS reads.  P never leaves registers.
 //
 // One pass with a running maximum m (log2 units), sum l and output O^T per row, rescaled only when a maximum outgrows the
-// reference by more than 8 (factors of exp2(8) at most in P, which has the exponent range for it).
+// reference by more than 8 (factors of exp2(8) at most in P, which has the exponent range for it: in fp16 the reference lies
+// 2^7 below the maximum).
 //
 // Prompts are a workgroup per row tile and head.  Up to kListed tiles of long sequences (decode steps, chunks) are dealt out by
 // key tiles: every workgroup adds up the same list of tiles' costs from cu_q and lens, which the host does not know, and
@@ -55,6 +56,11 @@ constexpr int kTileBytes = kKeys * kHeadDim * 2;
 constexpr int64_t kStrideEnd = int64_t(1) << 31;   // page strides (elements) whose bytes 32 bits hold
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGrow = 8.f;               // log2 units a maximum may outgrow the reference by
+// Log2 units of the reference below the maximum it was set at.  Probabilities then reach 2^(kGrow + kUnder): fp16 holds 65504, and
+// with 2^7 a row's small ones keep half a step of 2^-32 of its largest.  With none, keys 17 nats below an attention sink
+// were 0 in the output and not in its divisor.  bf16 has the range of the sums.
+template <bool kF16>
+constexpr float kUnder = kF16 ? 7.f : 0.f;
 
 __device__ __align__(256) uint32_t zero_row[kHeadDim / 2];   // what a slot outside the visible ones reads as
 
@@ -102,7 +108,7 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t at) { return *(const __attr
 __device__ __forceinline__ u32x2 lds_read_tr(uint32_t at) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at));
 }
-// log sum exp of a row from its running maximum (log2 units) and sum.
+// log sum exp of a row from its sum and what that is relative to (log2 units).
 __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -__builtin_inff() : m / kLog2e + logf(l); }
 // All of this wave's DMA is in and its LDS reads are done, then the workgroup's.
 __device__ __forceinline__ void tile_sync() {
@@ -155,8 +161,8 @@ __device__ __forceinline__ int slots_of(const AttendLaunch& A, int seq) {
 }
 __device__ __forceinline__ int end_row(const rkv_attend& a, int seq) { return a.cu_q ? first_row(a, seq + 1) : min(seq + 1, a.n_rows); }
 
-// A partial sum in the workspace: slot_rows rows of 128 floats (not divided by l), then their m and l in pairs; 16-byte aligned,
-// slot_rows being even.
+// A partial sum in the workspace: slot_rows rows of 128 floats (not divided by l), then pairs of what they and l are relative to
+// (log2) and l; 16-byte aligned, slot_rows being even.
 __device__ __forceinline__ float* part_slot(const AttendLaunch& A, int slot) {
   return A.parts + (size_t)slot * A.slot_rows * (kHeadDim + 2);
 }
@@ -445,7 +451,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   };
   const float grow = kBias ? 1.f : kCap ? cap2 : sl2, base = !kBias && kCap ? 0.5f * cap2 : 0.f;
   const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + row * a.q_token + hq * a.q_head;
-  float m = -__builtin_inff(), l = 0.f, ref = 0.f;   // ref: the running maximum, 0 while there is none
+  float m = -__builtin_inff(), l = 0.f, ref = 0.f;   // ref: the running maximum less kUnder, 0 while there is none
 
   if constexpr (kNarrow) {
     // At most 16 rows, all of them in every wave; a wave takes the 16 keys of each tile that it fetched itself, two tiles
@@ -513,7 +519,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
         top = fmaxf(top, __shfl_xor(top, 32));
         const float m2 = fmaxf(m, top), f = m2 > m ? __builtin_amdgcn_exp2f(m - m2) : 1.f;
         m = m2;
-        ref = m == -__builtin_inff() ? 0.f : m;
+        ref = m == -__builtin_inff() ? 0.f : m - kUnder<kF16>;
         l *= f;
 #pragma unroll
         for (int d = 0; d < 8; ++d)
@@ -560,6 +566,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
         for (int i = 0; i < 4; ++i) sum[4 * u + i] = fmaf(v[i], f, sum[4 * u + i]);
       }
     }
+    mm -= kUnder<kF16>;   // what the sums are relative to
     if (b_lo != every_lo || b_hi != every_hi) {
       float finite = 0.f;
 #pragma unroll
@@ -645,7 +652,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     if (__any(top > m + kGrow)) {
       const float m2 = fmaxf(m, top), f = m2 > m ? __builtin_amdgcn_exp2f(m - m2) : 1.f;
       m = m2;
-      ref = m == -__builtin_inff() ? 0.f : m;
+      ref = m == -__builtin_inff() ? 0.f : m - kUnder<kF16>;
       l *= f;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -752,6 +759,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   }
 
   l += __shfl_xor(l, 32);
+  m -= kUnder<kF16>;   // what the sums are relative to
   // The wave's rows by way of its quarter of the tiles' memory, chunks of 16 bytes at c ^ row: whole rows leave it.
   const int rows = min(32, n_rows - r0 - 32 * wv);
   if (rows <= 0) return;

@@ -584,3 +584,40 @@ def test_split_rows_of_odd_numbers(hq, hkv, lens, each):
     if each:
         got = rkv.pages_attend(c.cache, c.q, ints(c.table.tolist()), ints([n for _, n in lens]), return_lse=True)
         assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+
+
+@pytest.mark.parametrize("lens,width,page", [([(1, 40000)], 0, 64), ([(1, 900), (2, 700)], 0, 16), ([(40, 3000)], 16384, 16), ([(150, 3001)], 0, 30),
+                                             ([(150, 3001)], 16384, 48)], ids=["split", "few", "chunk", "pages-of-30", "split-chunk"])
+@pytest.mark.parametrize("kw", [dict(), dict(softcap=40.0), dict(softcap=40.0, slopes=True)], ids=["plain", "cap", "cap-slopes"])
+@pytest.mark.parametrize("gap,sink", [(17.5, 0), (13.0, 0), (17.5, 600), (13.0, 600), (5.5, 600)])
+def test_fp16_keeps_the_mass_behind_a_sink(lens, width, page, kw, gap, sink):
+    """Every key but one lies `gap` below it, and that one's value is 0: the output is what the others' small probabilities hold.
+    A row's largest probability is held at 2^7 or more, where half a step of fp16's smallest values is 2^-25: each key is off by
+    at most 2^-32 of the largest or 2^-11 of itself, the output by half a step (2^-25 below the normal range) again."""
+    kw = dict(kw)
+    c = Case(lens, hq=4, hkv=2, page=page, dtype=torch.float16, seed=61, width=width // page)
+    rng = np.random.default_rng(62)
+    c.q.zero_()
+    c.q[..., 0] = 8.0
+    for s, (_, n) in enumerate(lens):
+        for j in range(-(-n // page)):
+            m, at = min(page, n - j * page), int(c.table[s, j])
+            c.k[at, :, :m] = 0
+            c.v[at, :, :m] = torch.from_numpy(rng.uniform(0.5, 1.5, (2, m, 128))).to("cuda", torch.float16)
+        c.k[int(c.table[s, sink // page]), :, sink % page, 0] = 2.0      # a score of 16 times the scale
+        c.v[int(c.table[s, sink // page]), :, sink % page] = 0
+    top = gap if not kw else 40.0 * math.atanh(gap / 40.0)
+    kw["scale"] = top / 16.0
+    if "slopes" in kw:
+        kw["slopes"] = np.array([0.0, 2.0 ** -16, 0.0, 2.0 ** -15], dtype=np.float32)
+    dev = {k: torch.tensor(x, device="cuda") if k == "slopes" else x for k, x in kw.items()}
+    n_kv = [n for _, n in lens]
+    out, lse = rkv.pages_attend(c.cache, c.q, ints(c.table.tolist()), ints(n_kv), ints(c.cu), return_lse=True, **dev)
+    want, log, weight, reach = OG.attend(f64(c.k), f64(c.v), f64(c.q), c.table, n_kv, c.cu, **kw)
+    # scores as in compare(): products are exact here, the cap's steps are of 40
+    score = 2.0 ** -24 * (140 * reach + 8 * (reach + 2) + 16 * kw.get("softcap", 0.0) + 8)
+    mass = 1.5 * max(n_kv)
+    bound = 2.0 ** -32 * mass + 2.0 ** -11 * 1.01 * (weight + np.abs(want)) + (2 * score[..., None] + 2.0 ** -15) * weight + 2.0 ** -25
+    bad = np.abs(f64(out) - want) - bound
+    assert (bad <= 0).all(), (bad.max(), np.argwhere(bad > 0)[:4])
+    assert (np.abs(f64(lse) - log) <= score + 2.0 ** -13 * 0.01 + 2.0 ** -22 * np.abs(log)).all()
