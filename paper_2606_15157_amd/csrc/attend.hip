@@ -228,7 +228,7 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
   }
   if (!any_wave(bounds, blame)) return false;
   const int n_rows = n_q * A.group, prefix = a.prefix_lens ? uniform(a.prefix_lens[seq]) : 0;
-  const float cap2 = 2.f * kLog2e * a.softcap;
+  const float cap2 = 2.f * kLog2e * a.softcap, in_cap = kCap ? 2.f * kLog2e * (a.scale / a.softcap) : 0.f;   // 1 / softcap may overflow
 #pragma unroll 1
   for (int i = 0; i < 32; ++i) {
     const int mine = 32 * wv + i, r = r0 + mine;
@@ -253,9 +253,8 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
       float x = fmaf(q[0], k[0], q[1] * k[1]);
 #pragma unroll
       for (int s = 32; s > 0; s >>= 1) x += __shfl_xor(x, s);
-      x *= a.scale;
-      if constexpr (kCap) x = 0.5f * cap2 - cap2 / (1.f + __builtin_amdgcn_exp2f(2.f * kLog2e / a.softcap * x));
-      else x *= kLog2e;
+      if constexpr (kCap) x = 0.5f * cap2 - cap2 / (1.f + __builtin_amdgcn_exp2f(in_cap * x));
+      else x *= a.scale * kLog2e;
       if constexpr (kBias) x -= slope * fabsf((float)(pos - key));
       const float m2 = fmaxf(m, x), ref = m2 == -__builtin_inff() ? 0.f : m2;
       const float f = __builtin_amdgcn_exp2f(m - ref), e = __builtin_amdgcn_exp2f(x - ref);

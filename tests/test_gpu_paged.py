@@ -621,3 +621,18 @@ def test_fp16_keeps_the_mass_behind_a_sink(lens, width, page, kw, gap, sink):
     bad = np.abs(f64(out) - want) - bound
     assert (bad <= 0).all(), (bad.max(), np.argwhere(bad > 0)[:4])
     assert (np.abs(f64(lse) - log) <= score + 2.0 ** -13 * 0.01 + 2.0 ** -22 * np.abs(log)).all()
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-12])
+@pytest.mark.parametrize("slopes", [None, np.array([0.0, 0.5, 0.0, 0.1], dtype=np.float32)], ids=["cap", "cap-slopes"])
+def test_the_smallest_caps_beside_hidden_nan(scale, slopes):
+    """A cap whose reciprocal is past fp32: scores are 0, also for rows summed up by themselves beside a NaN that they do not see."""
+    c = Case([(40, 60), (1, 30)], hq=4, hkv=2, seed=71)
+    c.v[int(c.table[0, 3]), :, 2] = NAN      # slot 50
+    kw = dict(scale=scale, softcap=1e-39)
+    dev = {**kw, "slopes": None if slopes is None else torch.tensor(slopes, device="cuda")}
+    out, lse = rkv.pages_attend(c.cache, c.q, ints(c.table.tolist()), ints([60, 30]), ints(c.cu), return_lse=True, **dev)
+    want, log, weight, reach = OG.attend(f64(c.k), f64(c.v), f64(c.q), c.table, [60, 30], c.cu, slopes=slopes, **kw)
+    rows = [*range(30), 40]
+    assert torch.isnan(out[30:40]).all()
+    compare(out[rows], lse[rows], want[rows], log[rows], weight[rows], reach[rows], c.dtype, 1e-39, slopes, 60)
