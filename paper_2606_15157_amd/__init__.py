@@ -434,6 +434,13 @@ def _strides(t):
     return [0 if n == 1 else s for n, s in zip(t.shape, t.stride())]
 
 
+def _refuse_gradients(name, *tensors):
+    """No backward pass: a result that silently ended the graph would train on wrong gradients."""
+    for t in tensors:
+        if t is not None and t.requires_grad and _torch().is_grad_enabled():
+            raise ValueError(f"{name} has no backward pass: call it under torch.no_grad(), or with detached tensors")
+
+
 class PagedCache:
     """A pool of K and V pages (rkv_pages): k_pages, v_pages bf16 or fp16 [n_pages, Hkv, page_size, 128], any strides that are
     multiples of 8 with the last dimension dense.  Make one and keep it: its calls then marshal no pool again.  The decode
@@ -502,8 +509,10 @@ def pages_resize(pages, new_lens, max_new: int, *, in_place=True, stream=None):
 
 def pages_write(cache: PagedCache, k, v, slots, *, stream=None):
     """Copies new rows to their slots (rkv_pages_write): k, v [T, Hkv, d], or [B, n, Hkv, d] with T = B n, of the pool's type and any
-    strides that are multiples of 8; slots int32 [T], distinct; rows with a slot outside the pool (-1) are skipped."""
+    strides that are multiples of 8; slots int32 [T], distinct; rows with a slot outside the pool (-1) are skipped.  No backward
+    pass: tensors that require gradients are refused unless gradients are off."""
     dev = cache.device
+    _refuse_gradients("pages_write", k, v, cache.k_pages, cache.v_pages)
     ctx = _elsewhere(dev, stream)
     if ctx is not None:
         with ctx:
@@ -534,8 +543,10 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
     softcap c: scores c tanh(x / c); slopes fp32 [Hq]: scores less slope times distance; prefix_lens int32 [n_seqs]: slots
     every row of the sequence sees; first_keys int32 [T]: the first slot a row sees.  Returns out [T, Hq, d] (`out` if given: rows
     behind the last sequence stay as they are; a row that sees nothing is 0), and with return_lse or lse_out also fp32
-    [T, Hq], the logarithm of the sum of exponentials (-inf for a row that sees nothing)."""
+    [T, Hq], the logarithm of the sum of exponentials (-inf for a row that sees nothing).  No backward pass: tensors that
+    require gradients are refused unless gradients are off."""
     dev = cache.device
+    _refuse_gradients("pages_attend", q, cache.k_pages, cache.v_pages, slopes, out, lse_out)
     ctx = _elsewhere(dev, stream)
     if ctx is not None:
         with ctx:

@@ -245,3 +245,22 @@ def test_lists_whose_key_tiles_32_bits_may_not_hold_are_not_split(seqs, split):
     n = C.c_size_t()
     assert _abi.lib().rkv_pages_attend_workspace_size(C.byref(pages(page_size=1 << 13)), C.byref(a), C.byref(n)) == 0
     assert (n.value > 0) == split
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "pool", "slopes", "out"])
+def test_calls_that_would_drop_gradients_are_refused(which):
+    """Before anything else is looked at; with gradients off the call goes on (here to the refusal of tensors off the GPU)."""
+    def make(name, *shape):
+        return torch.zeros(shape, dtype=torch.float32 if name == "slopes" else torch.bfloat16, requires_grad=which == name)
+    cache = rkv.PagedCache(make("pool", 2, 3, 16, 128), torch.zeros(2, 3, 16, 128, dtype=torch.bfloat16))
+    one = torch.ones(1, dtype=torch.int32)
+    calls = []
+    if which in ("k", "v", "pool"):
+        calls.append(lambda: rkv.pages_write(cache, make("k", 1, 3, 128), make("v", 1, 3, 128), one))
+    if which not in ("k", "v"):
+        calls.append(lambda: rkv.pages_attend(cache, make("q", 1, 3, 128), one.view(1, 1), one, slopes=make("slopes", 3), out=make("out", 1, 3, 128)))
+    for call in calls:
+        with pytest.raises(ValueError, match="no backward pass"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="on the GPU"):
+            call()
