@@ -615,6 +615,8 @@ def pages_init_from_prefill(plan: Plan, prefill_out, *, page_size=16, extra=0, s
     """Prefill -> paged caches: the compacted prompt cache of every layer of an evict_prefill result moves into pages, of which a
     layer takes as many as its retained rows need, and `extra` more slots' worth per sequence stay free for new tokens.
     Returns, per layer, (cache, pages): a PagedCache and its tables (pages_init) with lens at the layer's retained count."""
+    if page_size < 1 or extra < 0:
+        raise ValueError("page_size must be >= 1 and extra >= 0")
     torch = _torch()
     got = []
     dev = prefill_out["k_out"][0].device

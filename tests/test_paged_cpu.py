@@ -264,3 +264,11 @@ def test_calls_that_would_drop_gradients_are_refused(which):
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="on the GPU"):
             call()
+
+
+@pytest.mark.parametrize("kw", [dict(extra=-1), dict(extra=-16), dict(page_size=0), dict(page_size=-16)])
+def test_a_hand_over_without_room_is_refused(kw):
+    """Fewer pages than the retained rows need would leave every layer's cache empty."""
+    x = [torch.zeros(1, 2, 20, 128, dtype=torch.bfloat16)]
+    with pytest.raises(ValueError, match="extra"):
+        rkv.pages_init_from_prefill(None, {"k_out": x, "v_out": x}, **kw)
