@@ -636,3 +636,29 @@ def test_the_smallest_caps_beside_hidden_nan(scale, slopes):
     rows = [*range(30), 40]
     assert torch.isnan(out[30:40]).all()
     compare(out[rows], lse[rows], want[rows], log[rows], weight[rows], reach[rows], c.dtype, 1e-39, slopes, 60)
+
+
+@pytest.mark.parametrize("shape,strides", [((2, 2, 32, 128), (1 << 31, 32 * 128, 128, 1)), ((2, 1, 20, 128), ((1 << 31) + 8, 0, 128, 1)),
+                                           ((1, 1, 16, 128), (0, 0, (1 << 27) - 8, 1)), ((1, 1, 48, 128), (0, 0, 1 << 26, 1)),
+                                           ((2, 2, 16, 128), (128, 1 << 31, 256, 1))], ids=["pages", "odd-pages", "slots", "more-slots", "heads"])
+def test_strides_whose_bytes_pass_32_bits(shape, strides):
+    """Rows written to and read from pools of 4 to 9 GB whose pages, slots or heads lie 2 to 4 GB apart, against a dense pool."""
+    need = sum((n - 1) * s for n, s in zip(shape, strides)) + 1
+    far = [torch.empty(need, dtype=torch.bfloat16, device="cuda").as_strided(shape, strides) for _ in range(2)]
+    near = [torch.empty(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    n_pages, hkv, page, _ = shape
+    T = n_pages * page
+    g = torch.Generator(device="cuda").manual_seed(81)
+    k, v, q = (torch.randn((T, h, 128), device="cuda", generator=g).to(torch.bfloat16) for h in (hkv, hkv, 2 * hkv))
+    slots = torch.randperm(T, device="cuda", generator=g).to(torch.int32)
+    got = []
+    for pool in (far, near):
+        cache = rkv.PagedCache(*pool)
+        rkv.pages_write(cache, k, v, slots)
+        got.append([rkv.pages_attend(cache, x, torch.arange(n_pages, dtype=torch.int32, device="cuda").view(1, -1), ints([T]), ints([0, x.shape[0]]))
+                    for x in (q, q[:1])])
+    for a, b in zip(far, near):
+        assert torch.equal(a, b)
+    for a, b in zip(*got):
+        # both within half a step for P and half a step for the output, of the largest value at most
+        assert (a.float() - b.float()).abs().max() <= 4 * 2.0 ** -8 * v.float().abs().max()
