@@ -10,6 +10,9 @@
 //                 keys runs in the order the lane holds them: slots 0-3 of a half are keys 4 half + 0..3, slots 4-7 keys
 //                 8 + 4 half + 0..3 of each 16.  V^T in that order is two transposing LDS reads.  P never leaves registers.
 //
+// P in 16 bits is what the matrix instructions take at this rate; it takes the outputs' error against 64 bits from 1.6e-3 (an
+// output's own rounding to bf16) to at most 1.9e-3, in fp16 from 2.1e-4 to 2.4e-4.
+//
 // One pass with a running maximum m (log2 units), sum l and output O^T per row, rescaled only when a maximum outgrows the
 // reference by more than 8 (factors of exp2(8) at most in P, which has the exponent range for it: in fp16 the reference lies
 // 2^7 below the maximum).

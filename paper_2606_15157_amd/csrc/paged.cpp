@@ -117,6 +117,8 @@ int64_t usual_rows(const rkv_pages* p, const rkv_attend* a) {
 //   of 8192 67 / 33; 64 of 1024 42 / 50, of 2048 92 / 101, of 64 to 8192 127 / 103, of 512 to 8192 187 / 159;
 //   prompts: 512 tokens 16 / 34, 1024 27 / 53, 2048 53 / 99, 16384 1997 / 2282; 512 after 32768 568 / 292, 64 after 16320
 //   292 / 41, 256 each of four after 7936 200 / 160, 512 each of eight after 3584 258 / 287, 8 each of 16 after 4088 75 / 55.
+// Other head layouts go by their items alone.  A call is decided as a whole: one decoding sequence of 131072 keys beside a prompt of 2048
+// tokens stays with one workgroup a head (1136 us), and 2304 or 2560 tokens after 32768 take two rounds of tiles (1477, 1502).
 bool shared_out(const rkv_pages* p, const rkv_attend* a) {
   const int64_t tiles = row_tiles(p, a), items = tiles * p->n_kv_heads, rows = usual_rows(p, a);
   const int64_t most = (int64_t)a->max_pages * p->page_size;
