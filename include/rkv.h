@@ -414,6 +414,34 @@ typedef struct {
  * RKV_ERR_HIP. */
 int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream);
 
+/* The way back: row (o, t, h) of `rows` (whose k and v are written) becomes what lies in slot slots[o n_tokens + t], zeros for a slot outside
+ * [0, n_pages * page_size).  Slots may repeat.  Errors: as rkv_pages_write, with the rows' own dimensions in the place of the pool's: they may not
+ * run into each other, while an overlapping pool can be read. */
+int rkv_pages_read(const rkv_pages* pages, const rkv_rows* rows, void* stream);
+
+/* A pool held in 8 bits: rows of 128 codes in OCP e4m3 (no infinities, NaN 0x7f and 0xff), one byte each, and for each row of K
+ * and of V one byte b, its scale 2^(b - 127): a value is code times scale.  Codes of row (page, head, slot) lie at k + page k_page + head k_head +
+ * slot k_slot bytes, its scale at k_scale + page ks_page + head ks_head + slot ks_slot (v likewise).  Code strides are
+ * multiples of 16, k and v 16-byte aligned; scales lie anywhere.  dtype is that of the rows written, read and of queries. */
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
+  int64_t ks_page, ks_head, ks_slot, vs_page, vs_head, vs_slot;
+  int32_t n_pages, page_size, n_kv_heads, head_dim, dtype;
+} rkv_qpages;
+
+/* rkv_pages_write into 8 bits.  A row x gets the exponent e, the least with max |x_i| <= 448 2^e (over finite x_i; all zeros: the least there
+ * is), cut to [-117, 120] for bf16 and [-15, 8] for fp16, the byte e + 127, and codes x_i 2^-e rounded to nearest even (at the largest e
+ * cut to 240 2^e first), NaN for what is not finite.  An x_i is so off by at most 2^-4 of it, or 2^(e - 10) where that is more, and every value
+ * is exact in dtype.  Any other bytes stand for what they say, rounded to dtype where they are read.
+ * rkv_qpages_read gives the values back.  Errors: as rkv_pages_write and rkv_pages_read; null scales, negative scale strides or
+ * scales that overlap are RKV_ERR_INVALID_ARG. */
+int rkv_qpages_write(const rkv_qpages* pages, const rkv_rows* rows, void* stream);
+int rkv_qpages_read(const rkv_qpages* pages, const rkv_rows* rows, void* stream);
+
 /* One rkv_pages_attend call.  Device pointers:
  *  q, out   [n_rows, Hq, d] of the pool's dtype, row (t, hq) at q + t q_token + hq q_head elements (out likewise);
  *  lse      NULL, or fp32 [n_rows, Hq], dense;
@@ -463,6 +491,34 @@ typedef struct {
  * RKV_ERR_WORKSPACE, RKV_ERR_HIP.  Validation ends before the first launch. */
 int rkv_pages_attend_workspace_size(const rkv_pages* pages, const rkv_attend* a, size_t* bytes);
 int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size_t ws_bytes, void* stream);
+
+/* The same over 8-bit pools: k_j and v_j are code times scale, exact in dtype, and all else is as above. */
+int rkv_qpages_attend_workspace_size(const rkv_qpages* pages, const rkv_attend* a, size_t* bytes);
+int rkv_qpages_attend(const rkv_qpages* pages, const rkv_attend* a, void* ws, size_t ws_bytes, void* stream);
+
+/* Prefixes that sequences share.  Sequences cu_seqs[g] .. cu_seqs[g + 1] - 1 of a call form group g (cu_seqs int32 [n_groups + 1], not
+ * descending) and begin with the same lens[g] slots, which lie in pages table[g] [max_pages], rows table_stride apart, of the same pool;
+ * the call's own table and lens hold what follows them, new tokens among it.  Sequences before cu_seqs[0] and from cu_seqs[n_groups] on have no
+ * prefix.  max_len: the most slots of a prefix, or 0 (as max_kv: it chooses kernels, never results). */
+typedef struct {
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* lens;
+  const int32_t* cu_seqs;
+  int32_t n_groups, max_pages, max_len;
+} rkv_shared;
+
+/* rkv_pages_attend of sequences that share prefixes: the result is that of caches in which each sequence's own slots follow its
+ * group's prefix (positions, windows and distances count from the prefix's first slot; causal governs the own slots, while a prefix lies
+ * before every row), with each prefix read once for the rows of all its sequences instead of once for each.  A
+ * row's sums over its prefix are held in 32 bits between the two.  A group of one sequence is allowed, as is a prefix of no slots.
+ * ws: as rkv_pages_attend; it holds 520 bytes for each row and query head besides.
+ * Errors: as rkv_pages_attend; RKV_ERR_UNSUPPORTED also for prefix_lens or first_keys, and where a prefix and a sequence
+ * could hold 2^31 - 1024 slots together; RKV_ERR_SHAPE for a shared table whose stride is less than max_pages. */
+int rkv_pages_attend_shared_workspace_size(const rkv_pages* pages, const rkv_attend* a, const rkv_shared* shared, size_t* bytes);
+int rkv_pages_attend_shared(const rkv_pages* pages, const rkv_attend* a, const rkv_shared* shared, void* ws, size_t ws_bytes, void* stream);
+int rkv_qpages_attend_shared_workspace_size(const rkv_qpages* pages, const rkv_attend* a, const rkv_shared* shared, size_t* bytes);
+int rkv_qpages_attend_shared(const rkv_qpages* pages, const rkv_attend* a, const rkv_shared* shared, void* ws, size_t ws_bytes, void* stream);
 
 /* Implementation calls (measurement, no paper passage): kernel timing for benchmarks and tests.
  * rkv_profile_enable(stage) makes every following

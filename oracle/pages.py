@@ -1,4 +1,5 @@
-"""Paged caches in float64 NumPy: block tables from request lengths, rows to slots, attention over pages.
+"""Paged caches in float64 NumPy: block tables from request lengths, rows to slots, rows in 8 bits, attention over pages, and
+of sequences that share prefixes.
 
 Written from the definitions in include/rkv.h; parity unpinned by the paper, which has no paged cache.
 """
@@ -81,3 +82,58 @@ def attend(k_pages, v_pages, q, table, lens, cu_q=None, *, scale=None, causal=Tr
                     total = w.sum()
                     out[t, e], weight[t, e], lse[t, e] = (w / total) @ v, (w / total) @ np.abs(v), top + math.log(total)
     return out, lse, weight, reach
+
+
+# exponents of a row's scale, for bf16 and fp16 rows
+EXPONENTS = {"bf16": (-117, 120), "fp16": (-15, 8)}
+
+
+def e4m3_values():
+    """The values of the 256 codes: sign, four bits of exponent (bias 7), three of mantissa; 0x7f and 0xff are NaN."""
+    v = [m / 8 * 2.0 ** -6 if e == 0 else (1 + m / 8) * 2.0 ** (e - 7) for e in range(16) for m in range(8)]
+    v[127] = math.nan
+    return np.array(v + [-x for x in v])
+
+
+def encode(x, kind):
+    """(codes uint8, scale bytes uint8) of rows x [..., d]; the code of what is not finite is 0x7f here (either NaN will do)."""
+    lo, hi = EXPONENTS[kind]
+    x = np.asarray(x, dtype=np.float64)
+    fine = np.isfinite(x)
+    size = np.where(fine, np.abs(x), 0.0)
+    top = size.max(-1)
+    e = np.full(top.shape, lo, dtype=np.int64)
+    while True:
+        grow = (top > np.ldexp(448.0, e)) & (e < hi)
+        if not grow.any():
+            break
+        e = e + grow
+    y = np.minimum(size, np.ldexp(240.0, hi)) * np.exp2(-e.astype(np.float64))[..., None]
+    step = np.exp2(np.maximum(np.floor(np.log2(np.where(y > 0, y, 1.0))), -6.0) - 3.0)
+    y = np.rint(y / step) * step
+    code = np.searchsorted(e4m3_values()[:127], y)
+    code = np.where(fine, code + 128 * np.signbit(x), 127)
+    return code.astype(np.uint8), (e + 127).astype(np.uint8)
+
+
+def decode(codes, scales):
+    return e4m3_values()[codes] * np.exp2(scales.astype(np.float64) - 127)[..., None]
+
+
+def attend_shared(k_pages, v_pages, q, shared_table, shared_lens, cu_seqs, table, lens, cu_q=None, **kw):
+    """`attend` of sequences whose own slots follow their group's prefix: each slot a page of its own, in one table."""
+    page_size = k_pages.shape[2]
+    k, v = (x.transpose(0, 2, 1, 3).reshape(-1, x.shape[1], 1, x.shape[3]) for x in (k_pages, v_pages))
+
+    def slots(row, n):
+        return [int(row[j // page_size]) * page_size + j % page_size if 0 <= int(row[j // page_size]) < k_pages.shape[0] else -1 for j in range(n)]
+
+    rows, most = [], []
+    for s, n in enumerate(int(x) for x in lens):
+        own = slots(table[s], n)
+        for g in range(len(shared_lens)):
+            if cu_seqs[g] <= s < cu_seqs[g + 1]:
+                own = slots(shared_table[g], int(shared_lens[g])) + own
+        rows.append(own)
+        most.append(len(own))
+    return attend(k, v, q, rows, most, cu_q, **kw)

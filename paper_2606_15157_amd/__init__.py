@@ -21,7 +21,8 @@ from ._abi import RkvError, check
 
 __all__ = ["Plan", "allocate_budgets", "evict_prefill", "decode_step", "decode_init_from_prefill", "prefill_check",
            "rule_phases", "version", "entropy_profile", "entropy_budgets",
-           "PagedCache", "pages_init", "pages_resize", "pages_write", "pages_attend", "pages_init_from_prefill",
+           "PagedCache", "QuantizedCache", "pages_init", "pages_resize", "pages_write", "pages_read", "pages_attend", "pages_attend_shared",
+           "pages_init_from_prefill",
            "FULL", "STREAMING", "SNAPKV", "H2O", "TOVA", "H2O_FULL", "SCOPE_PREFILL", "SCOPE_DECODE", "SCOPE_BOTH",
            "RkvError"]
 
@@ -462,6 +463,50 @@ class PagedCache:
         self._pack = _abi.Pages.pack(k_pages.data_ptr(), v_pages.data_ptr(), *_strides(k_pages)[:3], *_strides(v_pages)[:3], self.n_pages,
                                      self.page_size, self.n_kv_heads, self.head_dim, _abi.BF16 if self.dtype == torch.bfloat16 else _abi.F16)
         self._bytes = {}     # workspace sizes by what they depend on
+        L = _abi.lib()
+        self._write, self._read, self._attend, self._attend_shared = L.rkv_pages_write, L.rkv_pages_read, L.rkv_pages_attend, L.rkv_pages_attend_shared
+        self._attend_bytes, self._attend_shared_bytes = L.rkv_pages_attend_workspace_size, L.rkv_pages_attend_shared_workspace_size
+
+
+class QuantizedCache:
+    """A pool of K and V pages held in 8 bits (rkv_qpages): k_pages, v_pages torch.float8_e4m3fn [n_pages, Hkv, page_size, 128], any strides
+    that are multiples of 16 with the last dimension dense; k_scales, v_scales uint8 [n_pages, Hkv, page_size], any strides: a row's
+    values are its codes times 2^(byte - 127).  dtype: bf16 or fp16, of the rows written and read and of queries.  Rows that
+    `pages_write` put here come back exact in dtype, each within 2^-4 of what was written."""
+
+    def __init__(self, k_pages, v_pages, k_scales, v_scales, dtype=None):
+        torch = _torch()
+        dtype = torch.bfloat16 if dtype is None else dtype
+        if k_pages.dim() != 4 or k_pages.shape != v_pages.shape:
+            raise ValueError("k_pages and v_pages must have shape [n_pages, Hkv, page_size, d]")
+        if k_pages.dtype != torch.float8_e4m3fn or v_pages.dtype != torch.float8_e4m3fn:
+            raise ValueError("pages must be float8_e4m3fn")
+        if k_scales.shape != k_pages.shape[:3] or v_scales.shape != k_pages.shape[:3] or k_scales.dtype != torch.uint8 or v_scales.dtype != torch.uint8:
+            raise ValueError("scales must be uint8 [n_pages, Hkv, page_size]")
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("dtype must be bf16 or fp16")
+        if k_pages.stride(3) != 1 or v_pages.stride(3) != 1:
+            raise ValueError("pages must be dense in their last dimension")
+        if any(x.device != k_pages.device for x in (v_pages, k_scales, v_scales)):
+            raise ValueError("pages and scales must be on one device")
+        self.k_pages, self.v_pages, self.k_scales, self.v_scales = k_pages, v_pages, k_scales, v_scales
+        self.device, self.dtype = k_pages.device, dtype
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k_pages.shape
+        self._pack = _abi.QPages.pack(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), *_strides(k_pages)[:3],
+                                      *_strides(v_pages)[:3], *_strides(k_scales), *_strides(v_scales), self.n_pages, self.page_size,
+                                      self.n_kv_heads, self.head_dim, _abi.BF16 if dtype == torch.bfloat16 else _abi.F16)
+        self._bytes = {}
+        L = _abi.lib()
+        self._write, self._read, self._attend, self._attend_shared = L.rkv_qpages_write, L.rkv_qpages_read, L.rkv_qpages_attend, L.rkv_qpages_attend_shared
+        self._attend_bytes, self._attend_shared_bytes = L.rkv_qpages_attend_workspace_size, L.rkv_qpages_attend_shared_workspace_size
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, page_size: int, dtype=None, device="cuda"):
+        """A pool of its own memory; what it holds before the first write is not defined."""
+        torch = _torch()
+        pages = torch.empty((2, n_pages, n_kv_heads, page_size, 128), dtype=torch.float8_e4m3fn, device=device)
+        scales = torch.empty((2, n_pages, n_kv_heads, page_size), dtype=torch.uint8, device=device)
+        return cls(pages[0], pages[1], scales[0], scales[1], dtype)
 
 
 def pages_init(n_seqs: int, max_pages: int, n_pages: int, page_size: int, device="cuda"):
@@ -507,34 +552,62 @@ def pages_resize(pages, new_lens, max_new: int, *, in_place=True, stream=None):
     return {"slots": slots, "cu_new": cu_new, "status": status, "lens": lens, "cursor": cursor}
 
 
-def pages_write(cache: PagedCache, k, v, slots, *, stream=None):
-    """Copies new rows to their slots (rkv_pages_write): k, v [T, Hkv, d], or [B, n, Hkv, d] with T = B n, of the pool's type and any
-    strides that are multiples of 8; slots int32 [T], distinct; rows with a slot outside the pool (-1) are skipped.  No backward
-    pass: tensors that require gradients are refused unless gradients are off."""
+def _rows_pack(cache, k, v, slots, what):
+    """rkv_rows of k and v, [T, Hkv, d] or [B, n, Hkv, d], and their slots."""
+    dev, shape = cache.device, k.shape
+    ks, vs = (_strides(k), _strides(v)) if 1 in shape else (k.stride(), v.stride())
+    if shape != v.shape or len(shape) not in (3, 4) or shape[-2] != cache.n_kv_heads or shape[-1] != cache.head_dim:
+        raise ValueError(f"{what} must have shape [T, Hkv, d] or [B, n, Hkv, d]")
+    if k.dtype != cache.dtype or v.dtype != cache.dtype or ks[-1] != 1 or vs[-1] != 1 or k.device != dev or v.device != dev:
+        raise ValueError(f"{what} must be of the pool's type, on its device and dense in their last dimension")
+    if len(shape) == 3:
+        outer, n, ks, vs = 1, shape[0], (0, *ks), (0, *vs)
+    else:
+        outer, n = shape[0], shape[1]
+    _check_int32("slots", slots, (outer * n,), dev)
+    return _abi.Rows.pack(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], slots.data_ptr(), outer, n)
+
+
+def pages_write(cache, k, v, slots, *, stream=None):
+    """Copies new rows to their slots (rkv_pages_write), or into a QuantizedCache in 8 bits (rkv_qpages_write): k, v [T, Hkv, d], or
+    [B, n, Hkv, d] with T = B n, of the pool's type and any strides that are multiples of 8; slots int32 [T], distinct; rows with a slot
+    outside the pool (-1) are skipped.  No backward pass: tensors that require gradients are refused unless gradients are off."""
     dev = cache.device
     _refuse_gradients("pages_write", k, v, cache.k_pages, cache.v_pages)
     ctx = _elsewhere(dev, stream)
     if ctx is not None:
         with ctx:
             return pages_write(cache, k, v, slots)
-    shape = k.shape
-    ks, vs = (_strides(k), _strides(v)) if 1 in shape else (k.stride(), v.stride())
-    if shape != v.shape or len(shape) not in (3, 4) or shape[-2] != cache.n_kv_heads or shape[-1] != cache.head_dim:
-        raise ValueError("k and v must have shape [T, Hkv, d] or [B, n, Hkv, d]")
-    if k.dtype != cache.dtype or v.dtype != cache.dtype or ks[-1] != 1 or vs[-1] != 1 or k.device != dev or v.device != dev:
-        raise ValueError("k and v must be of the pool's type, on its device and dense in their last dimension")
-    if len(shape) == 3:
-        outer, n, ks, vs = 1, shape[0], (0, *ks), (0, *vs)
-    else:
-        outer, n = shape[0], shape[1]
-    _check_int32("slots", slots, (outer * n,), dev)
-    rows = _abi.Rows.pack(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], slots.data_ptr(), outer, n)
-    check(_abi.lib().rkv_pages_write(cache._pack, rows, _raw_stream(dev)))
+    check(cache._write(cache._pack, _rows_pack(cache, k, v, slots, "k and v"), _raw_stream(dev)))
 
 
-def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_kv=0, scale=None, causal=True, window=0, softcap=0.0,
+def pages_read(cache, slots, *, k_out=None, v_out=None, stream=None):
+    """Rows back from their slots (rkv_pages_read, rkv_qpages_read): slots int32 [T] or [B, n], zeros for a slot outside the pool (-1); the
+    same slot may come twice.  Returns k, v [T, Hkv, d] or [B, n, Hkv, d] of the pool's type: k_out and v_out if given, of any strides that are
+    multiples of 8 (out.permute(0, 2, 1, 3) of [B, Hkv, n, d], what evict_prefill takes).  No backward pass: tensors that require
+    gradients are refused unless gradients are off."""
+    dev = cache.device
+    _refuse_gradients("pages_read", cache.k_pages, cache.v_pages, k_out, v_out)
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return pages_read(cache, slots, k_out=k_out, v_out=v_out)
+    if slots.dim() not in (1, 2):
+        raise ValueError("slots must have shape [T] or [B, n]")
+    _check_int32("slots", slots, tuple(slots.shape), dev)
+    if not slots.is_contiguous():
+        raise ValueError("slots must be contiguous")
+    shape = (*slots.shape, cache.n_kv_heads, cache.head_dim)
+    k, v = (_T.empty(shape, dtype=cache.dtype, device=dev) if x is None else x for x in (k_out, v_out))
+    if k.shape != shape:
+        raise ValueError(f"k_out and v_out must have shape {list(shape)}")
+    check(cache._read(cache._pack, _rows_pack(cache, k, v, slots.reshape(-1), "k_out and v_out"), _raw_stream(dev)))
+    return k, v
+
+
+def pages_attend(cache, q, table, lens, cu_q=None, *, max_q=0, max_kv=0, scale=None, causal=True, window=0, softcap=0.0,
                  slopes=None, prefix_lens=None, first_keys=None, out=None, lse_out=None, return_lse=False, stream=None):
-    """Attention of new tokens over a paged cache (rkv_pages_attend).
+    """Attention of new tokens over a paged cache, a PagedCache or a QuantizedCache (rkv_pages_attend, rkv_qpages_attend).
 
     q: [T, Hq, d] of the pool's type, any strides that are multiples of 8; table int32 [n_seqs, max_pages]; lens int32 [n_seqs],
     the slots of each sequence with its new tokens' own among them; cu_q int32 [n_seqs + 1]: sequence s has rows cu_q[s] ..
@@ -553,6 +626,39 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
             return pages_attend(cache, q, table, lens, cu_q, max_q=max_q, max_kv=max_kv, scale=scale, causal=causal, window=window,
                                 softcap=softcap, slopes=slopes, prefix_lens=prefix_lens, first_keys=first_keys, out=out, lse_out=lse_out,
                                 return_lse=return_lse)
+    return _attend(cache, q, table, lens, cu_q, None, max_q, max_kv, scale, causal, window, softcap, slopes, prefix_lens, first_keys, out, lse_out, return_lse)
+
+
+def pages_attend_shared(cache, q, shared_table, shared_lens, cu_seqs, table, lens, cu_q=None, *, max_shared=0, max_q=0, max_kv=0, scale=None, causal=True,
+                        window=0, softcap=0.0, slopes=None, out=None, lse_out=None, return_lse=False, stream=None):
+    """Attention of sequences that begin with shared prefixes (rkv_pages_attend_shared, rkv_qpages_attend_shared): a prefix is read once for
+    all the rows of its sequences.
+
+    shared_table int32 [n_groups, max_pages] and shared_lens int32 [n_groups]: pages and slots of each prefix (a sequence of `pages_init`'s
+    tables, or rows of its own); cu_seqs int32 [n_groups + 1]: sequences cu_seqs[g] .. cu_seqs[g + 1] - 1 begin with prefix g, others
+    with none; table, lens, cu_q and all else as in pages_attend, with only what follows the prefix in table and lens.  The result is that of
+    pages_attend on caches in which each sequence's slots follow its prefix's.  max_shared: the most slots of a prefix, if known.  No backward
+    pass: tensors that require gradients are refused unless gradients are off."""
+    dev = cache.device
+    _refuse_gradients("pages_attend_shared", q, cache.k_pages, cache.v_pages, slopes, out, lse_out)
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return pages_attend_shared(cache, q, shared_table, shared_lens, cu_seqs, table, lens, cu_q, max_shared=max_shared, max_q=max_q, max_kv=max_kv,
+                                       scale=scale, causal=causal, window=window, softcap=softcap, slopes=slopes, out=out, lse_out=lse_out,
+                                       return_lse=return_lse)
+    n = shared_lens.shape[0]
+    width = shared_table.shape[-1]
+    _check_int32("shared_table", shared_table, (n, width), dev)
+    _check_int32("shared_lens", shared_lens, (n,), dev)
+    _check_int32("cu_seqs", cu_seqs, (n + 1,), dev)
+    shared = (shared_table.data_ptr(), shared_table.stride(0) if n > 1 else width, shared_lens.data_ptr(), cu_seqs.data_ptr(), n, width, max_shared)
+    return _attend(cache, q, table, lens, cu_q, shared, max_q, max_kv, scale, causal, window, softcap, slopes, None, None, out, lse_out, return_lse)
+
+
+def _attend(cache, q, table, lens, cu_q, shared, max_q, max_kv, scale, causal, window, softcap, slopes, prefix_lens, first_keys, out, lse_out, return_lse):
+    """A call on the current stream of the pool's device; shared: rkv_shared's fields, or None."""
+    dev = cache.device
     torch = _T
     shape = q.shape
     if len(shape) != 3 or shape[2] != cache.head_dim or q.dtype != cache.dtype or q.stride(2) != 1 or q.device != dev:
@@ -597,24 +703,28 @@ def pages_attend(cache: PagedCache, q, table, lens, cu_q=None, *, max_q=0, max_k
     a = _abi.Attend.pack(q.data_ptr(), out.data_ptr(), lse_ptr, q_token, q_head, out_token, out_head, table.data_ptr(), table.stride(0) if n > 1 else width,
                          lens.data_ptr(), cu, prefix, first, slope, n, T, Hq, width, max_q, max_kv, bool(causal), window,
                          d ** -0.5 if scale is None else scale, softcap)
-    L = _abi.lib()
+    args = (cache._pack, a)
     key = (T, Hq, n, width, max_q, max_kv, cu != 0)
+    if shared is not None:
+        args = (cache._pack, a, _abi.Shared.pack(*shared))
+        key += shared[4:]
     nbytes = cache._bytes.get(key)
     if nbytes is None:
         size = C.c_size_t()
-        check(L.rkv_pages_attend_workspace_size(cache._pack, a, C.byref(size)))
+        check((cache._attend_bytes if shared is None else cache._attend_shared_bytes)(*args, C.byref(size)))
         if len(cache._bytes) >= 1024:
             cache._bytes.clear()
         nbytes = cache._bytes[key] = size.value
     ws = lens.new_empty(nbytes // 4) if nbytes else None
-    check(L.rkv_pages_attend(cache._pack, a, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev)))
+    check((cache._attend if shared is None else cache._attend_shared)(*args, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev)))
     return out if lse is None else (out, lse)
 
 
-def pages_init_from_prefill(plan: Plan, prefill_out, *, page_size=16, extra=0, stream=None):
+def pages_init_from_prefill(plan: Plan, prefill_out, *, page_size=16, extra=0, quantized=False, stream=None):
     """Prefill -> paged caches: the compacted prompt cache of every layer of an evict_prefill result moves into pages, of which a
     layer takes as many as its retained rows need, and `extra` more slots' worth per sequence stay free for new tokens.
-    Returns, per layer, (cache, pages): a PagedCache and its tables (pages_init) with lens at the layer's retained count."""
+    Returns, per layer, (cache, pages): a PagedCache, or with `quantized` a QuantizedCache, and its tables (pages_init) with lens at
+    the layer's retained count."""
     if page_size < 1 or extra < 0:
         raise ValueError("page_size must be >= 1 and extra >= 0")
     torch = _torch()
@@ -623,13 +733,16 @@ def pages_init_from_prefill(plan: Plan, prefill_out, *, page_size=16, extra=0, s
     ctx = _elsewhere(dev, stream)
     if ctx is not None:
         with ctx:
-            return pages_init_from_prefill(plan, prefill_out, page_size=page_size, extra=extra)
+            return pages_init_from_prefill(plan, prefill_out, page_size=page_size, extra=extra, quantized=quantized)
     for k, v in zip(prefill_out["k_out"], prefill_out["v_out"]):
         B, Hkv, n, d = k.shape
         per = -(-(n + extra) // page_size)
         pages = pages_init(B, max(1, per), max(1, B * per), page_size, dev)
-        pool = torch.empty((2, max(1, B * per), Hkv, page_size, d), dtype=k.dtype, device=dev)
-        cache = PagedCache(pool[0], pool[1])
+        if quantized:
+            cache = QuantizedCache.empty(max(1, B * per), Hkv, page_size, k.dtype, dev)
+        else:
+            pool = torch.empty((2, max(1, B * per), Hkv, page_size, d), dtype=k.dtype, device=dev)
+            cache = PagedCache(pool[0], pool[1])
         step = pages_resize(pages, torch.full((B,), n, dtype=torch.int32, device=dev), B * n)
         pages_write(cache, k.permute(0, 2, 1, 3), v.permute(0, 2, 1, 3), step["slots"])
         got.append((cache, pages))

@@ -26,7 +26,8 @@ EXPORTED = [
     "rkv_plan_retained_counts", "rkv_prefill_workspace_size", "rkv_prefill_evict", "rkv_prefill_evict_noalloc", "rkv_prefill_check",
     "rkv_decode_step", "rkv_decode_init_from_prefill", "rkv_entropy_workspace_size", "rkv_entropy_profile",
     "rkv_pages_resize", "rkv_pages_write", "rkv_pages_attend_workspace_size", "rkv_pages_attend", "rkv_profile_enable", "rkv_profile_read", "rkv_last_error",
-    "rkv_version",
+    "rkv_version", "rkv_pages_read", "rkv_pages_attend_shared_workspace_size", "rkv_pages_attend_shared", "rkv_qpages_write", "rkv_qpages_read",
+    "rkv_qpages_attend_workspace_size", "rkv_qpages_attend", "rkv_qpages_attend_shared_workspace_size", "rkv_qpages_attend_shared",
 ]
 
 
@@ -87,6 +88,9 @@ def _packer(layout):
 
 
 _PAGES = _layout(("P", "k v"), ("q", "k_page k_head k_slot v_page v_head v_slot"), ("i", "n_pages page_size n_kv_heads head_dim dtype"))
+_QPAGES = _layout(("P", "k v k_scale v_scale"), ("q", "k_page k_head k_slot v_page v_head v_slot ks_page ks_head ks_slot vs_page vs_head vs_slot"),
+                  ("i", "n_pages page_size n_kv_heads head_dim dtype"))
+_SHARED = _layout(("P", "table"), ("q", "table_stride"), ("P", "lens cu_seqs"), ("i", "n_groups max_pages max_len"))
 _RESIZE = _layout(("P", "lens new_lens lens_out table"), ("q", "table_stride"), ("P", "ring cursor cursor_out slots cu_new status"),
                   ("i", "n_seqs max_pages n_pages page_size max_new"))
 _ROWS = _layout(("P", "k v"), ("q", "k_outer k_token k_head v_outer v_token v_head"), ("P", "slots"), ("i", "n_outer n_tokens"))
@@ -98,6 +102,16 @@ _ATTEND = _layout(("P", "q out lse"), ("q", "q_token q_head out_token out_head")
 class Pages(C.Structure):
     _fields_ = _PAGES[0]
     pack = _packer(_PAGES)
+
+
+class QPages(C.Structure):
+    _fields_ = _QPAGES[0]
+    pack = _packer(_QPAGES)
+
+
+class Shared(C.Structure):
+    _fields_ = _SHARED[0]
+    pack = _packer(_SHARED)
 
 
 class Resize(C.Structure):
@@ -151,9 +165,13 @@ def lib():
                                           C.POINTER(C.c_void_p), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                           C.c_size_t, C.c_void_p]
         L.rkv_pages_resize.argtypes = [C.c_void_p, C.c_void_p]      # structs: byref, or packed bytes
-        L.rkv_pages_write.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
-        L.rkv_pages_attend_workspace_size.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]
-        L.rkv_pages_attend.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        for kind in ("rkv_pages", "rkv_qpages"):
+            getattr(L, kind + "_write").argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
+            getattr(L, kind + "_read").argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
+            getattr(L, kind + "_attend_workspace_size").argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]
+            getattr(L, kind + "_attend").argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+            getattr(L, kind + "_attend_shared_workspace_size").argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]
+            getattr(L, kind + "_attend_shared").argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.rkv_profile_enable.argtypes = [C.c_int32]
         L.rkv_profile_read.argtypes = [C.POINTER(C.c_int32), C.POINTER(C.c_double)]
         L.rkv_last_error.restype = C.c_char_p
@@ -165,6 +183,9 @@ def lib():
                      "rkv_rule_phases", "rkv_plan_from_route", "rkv_decode_init_from_prefill", "rkv_prefill_evict_noalloc",
                      "rkv_entropy_workspace_size", "rkv_entropy_profile",
                      "rkv_pages_resize", "rkv_pages_write", "rkv_pages_attend_workspace_size", "rkv_pages_attend",
+                     "rkv_qpages_write", "rkv_qpages_attend_workspace_size", "rkv_qpages_attend", "rkv_pages_read", "rkv_qpages_read",
+                     "rkv_pages_attend_shared_workspace_size", "rkv_pages_attend_shared", "rkv_qpages_attend_shared_workspace_size",
+                     "rkv_qpages_attend_shared",
                      "rkv_profile_enable", "rkv_profile_read", "rkv_version"):
             getattr(L, name).restype = C.c_int
         _lib = L

@@ -13,7 +13,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librkv.so")
-SOURCES = ["attend.hip", "host.cpp", "prefill.hip", "decode.hip", "entropy.hip", "fullspan.hip", "tova.hip", "handoff.hip", "noalloc.hip", "window.hip",
+SOURCES = ["attend.hip", "attend_shared.hip", "attend8.hip", "attend8_shared.hip", "host.cpp", "prefill.hip", "decode.hip", "entropy.hip", "fullspan.hip", "tova.hip", "handoff.hip", "noalloc.hip", "window.hip",
            "paged.cpp", "pages.hip"]
 
 HIPCC_FLAGS = [
@@ -51,7 +51,7 @@ def build(verbose: bool = False) -> str:
         objs = [os.path.join(work, s + ".o") for s in SOURCES]
         cmds = [[hipcc(), *HIPCC_FLAGS, "-I", os.path.join(HERE, "..", "include"), "-c", os.path.join(CSRC, s), "-o", o]
                 for s, o in zip(SOURCES, objs)]
-        with ThreadPoolExecutor(max_workers=6) as pool:
+        with ThreadPoolExecutor(max_workers=8) as pool:
             list(pool.map(run, cmds))
         run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", *objs, "-o", tmp])
     os.replace(tmp, LIB)

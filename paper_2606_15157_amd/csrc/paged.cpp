@@ -1,5 +1,4 @@
-// Host side of the paged caches: argument checks and launches of rkv_pages_resize, rkv_pages_write and
-// rkv_pages_attend.
+// Host side of the paged caches: argument checks and launches of rkv_pages_* and, for pools of 8-bit codes, rkv_qpages_*.
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
@@ -19,25 +18,25 @@ int launched(int err) {
   return RKV_OK;
 }
 
-// A 16-byte aligned pointer and strides (elements) of whole 16-byte pieces.
-int check_layout(const char* what, const void* ptr, std::initializer_list<int64_t> strides) {
+// A 16-byte aligned pointer and strides (elements) of whole 16-byte pieces, `piece` elements each.
+int check_layout(const char* what, const void* ptr, std::initializer_list<int64_t> strides, int piece = 8) {
   for (int64_t s : strides)
     if (s < 0) return rkv::fail(RKV_ERR_INVALID_ARG, std::string(what) + ": negative stride");
   if ((uintptr_t)ptr % 16) return rkv::fail(RKV_ERR_UNSUPPORTED, std::string(what) + " must be 16-byte aligned");
   for (int64_t s : strides)
-    if (s % 8) return rkv::fail(RKV_ERR_UNSUPPORTED, std::string(what) + ": strides must be multiples of 8 elements");
+    if (s % piece)
+      return rkv::fail(RKV_ERR_UNSUPPORTED, std::string(what) + ": strides must be multiples of " + std::to_string(piece) + " elements");
   return RKV_OK;
 }
 
-// Whether rows of 128 elements, at sum_i index_i stride_i for index_i < count_i, are told apart by their dimensions: taken by
+// Whether rows of `extent` elements, at sum_i index_i stride_i for index_i < count_i, are told apart by their dimensions: taken by
 // stride, each is at least the extent of the smaller ones.  So are those of every slice and permutation of a dense tensor.
 struct Dim {
   int64_t stride, count;
 };
 template <size_t kDims>
-bool rows_nest(std::array<Dim, kDims> dims) {
+bool rows_nest(std::array<Dim, kDims> dims, __int128 extent = rkv::kHeadDim) {
   std::sort(dims.begin(), dims.end(), [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
-  __int128 extent = rkv::kHeadDim;
   for (const Dim& d : dims) {
     if (d.count <= 1) continue;
     if (d.stride < extent) return false;
@@ -46,7 +45,8 @@ bool rows_nest(std::array<Dim, kDims> dims) {
   return true;
 }
 
-int check_pages(const rkv_pages* p) {
+template <class Pages>
+int check_pool(const Pages* p) {
   if (!p) return rkv::fail(RKV_ERR_INVALID_ARG, "null pages");
   if (!p->k || !p->v) return rkv::fail(RKV_ERR_INVALID_ARG, "null page pool");
   if (p->n_pages < 1 || p->page_size < 1 || p->n_kv_heads < 1)
@@ -54,10 +54,36 @@ int check_pages(const rkv_pages* p) {
   if (p->dtype != RKV_BF16 && p->dtype != RKV_F16) return rkv::fail(RKV_ERR_INVALID_ARG, "unknown dtype");
   if (p->head_dim != rkv::kHeadDim) return rkv::fail(RKV_ERR_UNSUPPORTED, "head_dim must be 128");
   if ((int64_t)p->n_pages * p->page_size >= kIntEnd) return rkv::fail(RKV_ERR_UNSUPPORTED, "a pool holds fewer than 2^31 slots");
+  return RKV_OK;
+}
+int check_pages(const rkv_pages* p) {
+  if (int st = check_pool(p)) return st;
   if (p->k_slot >= kIntEnd / 16 || p->v_slot >= kIntEnd / 16)
     return rkv::fail(RKV_ERR_UNSUPPORTED, "slots are fewer than 2^27 elements apart");
   if (int st = check_layout("k pages", p->k, {p->k_page, p->k_head, p->k_slot})) return st;
   return check_layout("v pages", p->v, {p->v_page, p->v_head, p->v_slot});
+}
+int check_pages(const rkv_qpages* p) {
+  if (int st = check_pool(p)) return st;
+  if (!p->k_scale || !p->v_scale) return rkv::fail(RKV_ERR_INVALID_ARG, "null scales");
+  for (int64_t x : {p->ks_page, p->ks_head, p->ks_slot, p->vs_page, p->vs_head, p->vs_slot})
+    if (x < 0) return rkv::fail(RKV_ERR_INVALID_ARG, "scales: negative stride");
+  if (int st = check_layout("k pages", p->k, {p->k_page, p->k_head, p->k_slot}, 16)) return st;
+  return check_layout("v pages", p->v, {p->v_page, p->v_head, p->v_slot}, 16);
+}
+
+// The pool as the launches take it.
+struct Pool {
+  rkv_pages p;
+  rkv::Scales ks, vs;
+  bool codes;
+};
+Pool pool_of(const rkv_pages* p) { return {*p, {}, {}, false}; }
+Pool pool_of(const rkv_qpages* p) {
+  return {{p->k, p->v, p->k_page, p->k_head, p->k_slot, p->v_page, p->v_head, p->v_slot, p->n_pages, p->page_size, p->n_kv_heads, p->head_dim, p->dtype},
+          {p->k_scale, p->ks_page, p->ks_head, p->ks_slot},
+          {p->v_scale, p->vs_page, p->vs_head, p->vs_slot},
+          true};
 }
 
 // Row tiles, with one part-filled tile for each sequence.
@@ -69,8 +95,8 @@ int64_t places(const rkv_pages* p, const rkv_attend* a) { return a->n_seqs + std
 bool nothing_to_do(const rkv_attend* a) { return a->n_seqs == 0 || a->n_rows == 0; }
 bool shared_out(const rkv_pages* p, const rkv_attend* a);
 
+// A call on a pool that has been checked.
 int check_attend(const rkv_pages* p, const rkv_attend* a) {
-  if (int st = check_pages(p)) return st;
   if (!a) return rkv::fail(RKV_ERR_INVALID_ARG, "null attend");
   if (a->n_seqs < 0 || a->n_rows < 0 || a->max_pages < 0 || a->max_q < 0 || a->max_kv < 0 || a->window < 0 || a->table_stride < 0)
     return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
@@ -97,9 +123,9 @@ int check_attend(const rkv_pages* p, const rkv_attend* a) {
 constexpr size_t kRecordBytes = sizeof(int32_t) * 4 * rkv::kAttendShares;
 
 // Rows of a partial sum: those of the largest row tile, made even so that every partial sum (130 floats a row) is 16-byte
-// aligned, as its rows are written and read.
-int32_t part_rows(const rkv_pages* p, const rkv_attend* a) {
-  const int64_t most = (int64_t)(a->cu_q ? a->n_rows : 1) * (a->n_q_heads / p->n_kv_heads);
+// aligned, as its rows are written and read.  groups: a's sequences are groups of sequences, which without cu_q have one row each.
+int32_t part_rows(const rkv_pages* p, const rkv_attend* a, bool groups) {
+  const int64_t most = (int64_t)(a->cu_q || groups ? a->n_rows : 1) * (a->n_q_heads / p->n_kv_heads);
   return (int32_t)std::min<int64_t>((most + 1) & ~int64_t(1), rkv::kAttendRows);
 }
 
@@ -132,9 +158,209 @@ bool shared_out(const rkv_pages* p, const rkv_attend* a) {
   return t > 32 || t * (208 - std::min<int64_t>(items, 208)) > 4200;
 }
 
-size_t attend_bytes(const rkv_pages* p, const rkv_attend* a) {
+size_t attend_bytes(const rkv_pages* p, const rkv_attend* a, bool groups = false) {
   if (nothing_to_do(a) || !shared_out(p, a)) return 0;
-  return kRecordBytes + sizeof(float) * 2 * rkv::kAttendShares * (size_t)part_rows(p, a) * (rkv::kHeadDim + 2);
+  return kRecordBytes + sizeof(float) * 2 * rkv::kAttendShares * (size_t)part_rows(p, a, groups) * (rkv::kHeadDim + 2);
+}
+
+// Rows of a call that moves them, and the launch; the rows are written by a read.
+int check_rows(const Pool& pool, const rkv_rows* rows, bool written) {
+  if (!rows) return rkv::fail(RKV_ERR_INVALID_ARG, "null rows");
+  if (rows->n_outer < 0 || rows->n_tokens < 0) return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
+  if (rows->n_outer == 0 || rows->n_tokens == 0) return RKV_OK;
+  if (!rows->k || !rows->v || !rows->slots) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  if ((int64_t)rows->n_outer * rows->n_tokens > 16 * (kGridEnd - 1) / pool.p.n_kv_heads)
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "at most 2^28 - 16 rows a call, each head's counted");
+  if (int st = check_layout("k rows", rows->k, {rows->k_outer, rows->k_token, rows->k_head})) return st;
+  if (int st = check_layout("v rows", rows->v, {rows->v_outer, rows->v_token, rows->v_head})) return st;
+  const int32_t heads = pool.p.n_kv_heads;
+  if (written && (!rows_nest<3>({{{rows->k_outer, rows->n_outer}, {rows->k_token, rows->n_tokens}, {rows->k_head, heads}}}) ||
+                  !rows_nest<3>({{{rows->v_outer, rows->n_outer}, {rows->v_token, rows->n_tokens}, {rows->v_head, heads}}})))
+    return rkv::fail(RKV_ERR_INVALID_ARG, "the rows to be read into overlap (no stride may be less than the extent of the smaller ones)");
+  return RKV_OK;
+}
+int check_written(const Pool& pool) {
+  const rkv_pages& p = pool.p;
+  bool apart = rows_nest<3>({{{p.k_page, p.n_pages}, {p.k_head, p.n_kv_heads}, {p.k_slot, p.page_size}}}) &&
+               rows_nest<3>({{{p.v_page, p.n_pages}, {p.v_head, p.n_kv_heads}, {p.v_slot, p.page_size}}});
+  for (const rkv::Scales& x : {pool.ks, pool.vs})
+    apart &= !pool.codes || rows_nest<3>({{{x.page, p.n_pages}, {x.head, p.n_kv_heads}, {x.slot, p.page_size}}}, 1);
+  if (!apart)
+    return rkv::fail(RKV_ERR_INVALID_ARG, "the pool's rows overlap (no stride may be less than the extent of the smaller ones): it can be read, not written");
+  return RKV_OK;
+}
+rkv::WriteLaunch rows_launch(const Pool& pool, const rkv_rows* rows) {
+  rkv::WriteLaunch W{};
+  W.p = pool.p;
+  W.ks = pool.ks;
+  W.vs = pool.vs;
+  W.r = *rows;
+  W.by_page = rkv::fast_div(pool.p.page_size);
+  W.by_head = rkv::fast_div(pool.p.n_kv_heads);
+  W.by_token = rkv::fast_div(rows->n_tokens);
+  W.n_items = rows->n_outer * rows->n_tokens * pool.p.n_kv_heads;
+  W.n_slots = pool.p.n_pages * pool.p.page_size;
+  return W;
+}
+template <class Pages>
+int write_rows(const Pages* pages, const rkv_rows* rows, void* stream) {
+  rkv::clear_error();
+  if (int st = check_pages(pages)) return st;
+  const Pool pool = pool_of(pages);
+  if (int st = check_rows(pool, rows, false)) return st;
+  if (rows->n_outer == 0 || rows->n_tokens == 0) return RKV_OK;
+  if (int st = check_written(pool)) return st;
+  const rkv::WriteLaunch W = rows_launch(pool, rows);
+  return launched(pool.codes ? rkv::launch_write8(W, stream) : rkv::launch_write(W, stream));
+}
+template <class Pages>
+int read_rows(const Pages* pages, const rkv_rows* rows, void* stream) {
+  rkv::clear_error();
+  if (int st = check_pages(pages)) return st;
+  const Pool pool = pool_of(pages);
+  if (int st = check_rows(pool, rows, true)) return st;
+  if (rows->n_outer == 0 || rows->n_tokens == 0) return RKV_OK;
+  const rkv::WriteLaunch W = rows_launch(pool, rows);
+  return launched(pool.codes ? rkv::launch_read8(W, stream) : rkv::launch_read(W, stream));
+}
+
+// A launch over the row tiles of a call that has been checked, but for its workspace.
+rkv::AttendLaunch attend_launch(const Pool& pool, const rkv_attend* a, bool groups = false) {
+  const rkv_pages* p = &pool.p;
+  rkv::AttendLaunch L{};
+  L.p = pool.p;
+  L.ks = pool.ks;
+  L.vs = pool.vs;
+  L.a = *a;
+  L.group = a->n_q_heads / p->n_kv_heads;
+  L.by_page = rkv::fast_div(p->page_size);
+  L.by_group = rkv::fast_div(L.group);
+  L.n_tiles = (int32_t)row_tiles(p, a);
+  L.few_long = 2 * full_tiles(p, a) < L.n_tiles;
+  L.n_places = (int32_t)places(p, a);
+  L.slot_rows = part_rows(p, a, groups);
+  // A part of 128 rows is written and read again, as many bytes as four key tiles: not for less than eight.  Few rows
+  // cost nothing beside a tile (one token after 1K: 15 us with shares of one, 17 of four, 21 of eight).
+  L.least = usual_rows(p, a) > 32 ? 8 : 1;
+  return L;
+}
+void set_parts(rkv::AttendLaunch& L, size_t need, void* ws) {
+  if (!need) return;
+  L.records = static_cast<int32_t*>(ws);
+  L.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kRecordBytes);
+}
+int check_workspace(size_t need, const void* ws, size_t ws_bytes) {
+  if (need && !ws) return rkv::fail(RKV_ERR_WORKSPACE, "workspace is null");
+  if (need && (uintptr_t)ws % 256) return rkv::fail(RKV_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (ws_bytes < need) return rkv::fail(RKV_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
+  return RKV_OK;
+}
+
+template <class Pages>
+int attend_size(const Pages* pages, const rkv_attend* a, size_t* bytes) {
+  rkv::clear_error();
+  if (!bytes) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  if (int st = check_pages(pages)) return st;
+  const Pool pool = pool_of(pages);
+  if (int st = check_attend(&pool.p, a)) return st;
+  *bytes = attend_bytes(&pool.p, a);
+  return RKV_OK;
+}
+template <class Pages>
+int attend(const Pages* pages, const rkv_attend* a, void* ws, size_t ws_bytes, void* stream) {
+  rkv::clear_error();
+  if (int st = check_pages(pages)) return st;
+  const Pool pool = pool_of(pages);
+  if (int st = check_attend(&pool.p, a)) return st;
+  if (nothing_to_do(a)) return RKV_OK;
+  if (!a->q || !a->out || !a->lens || (a->max_pages && !a->table)) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  const size_t need = attend_bytes(&pool.p, a);
+  if (int st = check_workspace(need, ws, ws_bytes)) return st;
+  rkv::AttendLaunch L = attend_launch(pool, a);
+  set_parts(L, need, ws);
+  return launched(pool.codes ? rkv::launch_attend8(L, stream) : rkv::launch_attend(L, stream));
+}
+
+// ---- shared prefixes: the groups' rows over their prefixes, then each sequence's rows over its own slots, from those sums on
+
+// The call over the prefixes.  A group's rows are those of all its sequences.
+rkv_attend over_prefixes(const rkv_attend* a, const rkv_shared* g) {
+  rkv_attend b = *a;
+  b.table = g->table;
+  b.table_stride = g->table_stride;
+  b.lens = g->lens;
+  b.prefix_lens = b.first_keys = nullptr;
+  b.n_seqs = g->n_groups;
+  b.max_pages = g->max_pages;
+  b.max_q = 0;     // the groups' rows on average
+  b.max_kv = g->max_len;
+  return b;
+}
+int check_shared(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
+  if (int st = check_attend(p, a)) return st;
+  if (!g) return rkv::fail(RKV_ERR_INVALID_ARG, "null shared");
+  if (g->n_groups < 0 || g->max_pages < 0 || g->max_len < 0 || g->table_stride < 0) return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
+  if (a->prefix_lens || a->first_keys) return rkv::fail(RKV_ERR_UNSUPPORTED, "prefix_lens and first_keys do not go with shared prefixes");
+  if (g->table_stride < g->max_pages) return rkv::fail(RKV_ERR_SHAPE, "the shared table's stride is less than its max_pages");
+  if (((int64_t)g->max_pages + a->max_pages) * p->page_size >= kIntEnd - 1024)
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "a prefix and a sequence hold fewer than 2^31 - 1024 slots together");
+  const rkv_attend b = over_prefixes(a, g);
+  if (!nothing_to_do(&b) && !shared_out(p, &b) && places(p, &b) * p->n_kv_heads >= kGridEnd)
+    return rkv::fail(RKV_ERR_UNSUPPORTED, "too many groups for one launch");
+  return RKV_OK;
+}
+// The sums of every row, rounded up to where the shares' records may begin; then the workspace of either launch.
+size_t sums_bytes(const rkv_attend* a) {
+  return (sizeof(float) * (rkv::kHeadDim + 2) * (size_t)a->n_rows * (size_t)a->n_q_heads + 255) & ~size_t(255);
+}
+size_t shared_bytes(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
+  const rkv_attend b = over_prefixes(a, g);
+  if (nothing_to_do(a) || nothing_to_do(&b)) return attend_bytes(p, a);
+  return sums_bytes(a) + std::max(attend_bytes(p, a), attend_bytes(p, &b, true));
+}
+
+template <class Pages>
+int shared_size(const Pages* pages, const rkv_attend* a, const rkv_shared* g, size_t* bytes) {
+  rkv::clear_error();
+  if (!bytes) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  if (int st = check_pages(pages)) return st;
+  const Pool pool = pool_of(pages);
+  if (int st = check_shared(&pool.p, a, g)) return st;
+  *bytes = shared_bytes(&pool.p, a, g);
+  return RKV_OK;
+}
+template <class Pages>
+int attend_shared(const Pages* pages, const rkv_attend* a, const rkv_shared* g, void* ws, size_t ws_bytes, void* stream) {
+  rkv::clear_error();
+  if (int st = check_pages(pages)) return st;
+  const Pool pool = pool_of(pages);
+  const rkv_pages* p = &pool.p;
+  if (int st = check_shared(p, a, g)) return st;
+  if (nothing_to_do(a)) return RKV_OK;
+  if (!a->q || !a->out || !a->lens || (a->max_pages && !a->table) || (g->n_groups && (!g->lens || !g->cu_seqs || (g->max_pages && !g->table))))
+    return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
+  if (int st = check_workspace(shared_bytes(p, a, g), ws, ws_bytes)) return st;
+  rkv::AttendLaunch L = attend_launch(pool, a);
+  const rkv_attend b = over_prefixes(a, g);
+  if (nothing_to_do(&b)) {
+    set_parts(L, attend_bytes(p, a), ws);
+    return launched(pool.codes ? rkv::launch_attend8(L, stream) : rkv::launch_attend(L, stream));
+  }
+  rkv::AttendLaunch G = attend_launch(pool, &b, true);
+  for (rkv::AttendLaunch* x : {&G, &L}) {
+    x->n_groups = g->n_groups;
+    x->n_members = a->n_seqs;
+    x->cu_seqs = g->cu_seqs;
+    x->own_lens = a->lens;
+    x->own_most = a->max_pages * p->page_size;
+    x->sums = static_cast<float*>(ws);
+    set_parts(*x, attend_bytes(p, &x->a, x == &G), static_cast<char*>(ws) + sums_bytes(a));
+  }
+  G.stage = rkv::kOverPrefix;
+  L.stage = rkv::kOverOwn;
+  auto* launch = pool.codes ? rkv::launch_attend8_shared : rkv::launch_attend_shared;
+  if (int st = launched(launch(G, stream))) return st;
+  return launched(launch(L, stream));
 }
 
 }  // namespace
@@ -157,67 +383,33 @@ int rkv_pages_resize(const rkv_resize* r, void* stream) {
   return launched(rkv::launch_resize({*r, rkv::fast_div(r->page_size)}, stream));
 }
 
-int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream) {
-  rkv::clear_error();
-  if (int st = check_pages(pages)) return st;
-  if (!rows) return rkv::fail(RKV_ERR_INVALID_ARG, "null rows");
-  if (rows->n_outer < 0 || rows->n_tokens < 0) return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
-  if (rows->n_outer == 0 || rows->n_tokens == 0) return RKV_OK;
-  if (!rows->k || !rows->v || !rows->slots) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
-  if ((int64_t)rows->n_outer * rows->n_tokens > 16 * (kGridEnd - 1) / pages->n_kv_heads)
-    return rkv::fail(RKV_ERR_UNSUPPORTED, "at most 2^28 - 16 rows a call, each head's counted");
-  if (int st = check_layout("k rows", rows->k, {rows->k_outer, rows->k_token, rows->k_head})) return st;
-  if (int st = check_layout("v rows", rows->v, {rows->v_outer, rows->v_token, rows->v_head})) return st;
-  const rkv_pages& p = *pages;
-  if (!rows_nest<3>({{{p.k_page, p.n_pages}, {p.k_head, p.n_kv_heads}, {p.k_slot, p.page_size}}}) ||
-      !rows_nest<3>({{{p.v_page, p.n_pages}, {p.v_head, p.n_kv_heads}, {p.v_slot, p.page_size}}}))
-    return rkv::fail(RKV_ERR_INVALID_ARG, "the pool's rows overlap (no stride may be less than the extent of the smaller ones): it can be read, not written");
-  rkv::WriteLaunch W{};
-  W.p = *pages;
-  W.r = *rows;
-  W.by_page = rkv::fast_div(pages->page_size);
-  W.by_head = rkv::fast_div(pages->n_kv_heads);
-  W.by_token = rkv::fast_div(rows->n_tokens);
-  W.n_items = rows->n_outer * rows->n_tokens * pages->n_kv_heads;
-  W.n_slots = pages->n_pages * pages->page_size;
-  return launched(rkv::launch_write(W, stream));
-}
+int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream) { return write_rows(pages, rows, stream); }
+int rkv_qpages_write(const rkv_qpages* pages, const rkv_rows* rows, void* stream) { return write_rows(pages, rows, stream); }
 
-int rkv_pages_attend_workspace_size(const rkv_pages* pages, const rkv_attend* a, size_t* bytes) {
-  rkv::clear_error();
-  if (!bytes) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
-  if (int st = check_attend(pages, a)) return st;
-  *bytes = attend_bytes(pages, a);
-  return RKV_OK;
-}
+int rkv_pages_read(const rkv_pages* pages, const rkv_rows* rows, void* stream) { return read_rows(pages, rows, stream); }
+int rkv_qpages_read(const rkv_qpages* pages, const rkv_rows* rows, void* stream) { return read_rows(pages, rows, stream); }
+
+int rkv_pages_attend_workspace_size(const rkv_pages* pages, const rkv_attend* a, size_t* bytes) { return attend_size(pages, a, bytes); }
+int rkv_qpages_attend_workspace_size(const rkv_qpages* pages, const rkv_attend* a, size_t* bytes) { return attend_size(pages, a, bytes); }
 
 int rkv_pages_attend(const rkv_pages* pages, const rkv_attend* a, void* ws, size_t ws_bytes, void* stream) {
-  rkv::clear_error();
-  if (int st = check_attend(pages, a)) return st;
-  if (nothing_to_do(a)) return RKV_OK;
-  if (!a->q || !a->out || !a->lens || (a->max_pages && !a->table)) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
-  const size_t need = attend_bytes(pages, a);
-  if (need && !ws) return rkv::fail(RKV_ERR_WORKSPACE, "workspace is null");
-  if (need && (uintptr_t)ws % 256) return rkv::fail(RKV_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (ws_bytes < need) return rkv::fail(RKV_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes");
-  rkv::AttendLaunch L{};
-  L.p = *pages;
-  L.a = *a;
-  L.group = a->n_q_heads / pages->n_kv_heads;
-  L.by_page = rkv::fast_div(pages->page_size);
-  L.by_group = rkv::fast_div(L.group);
-  L.n_tiles = (int32_t)row_tiles(pages, a);
-  L.few_long = 2 * full_tiles(pages, a) < L.n_tiles;
-  L.n_places = (int32_t)places(pages, a);
-  L.slot_rows = part_rows(pages, a);
-  // A part of 128 rows is written and read again, as many bytes as four key tiles: not for less than eight.  Few rows
-  // cost nothing beside a tile (one token after 1K: 15 us with shares of one, 17 of four, 21 of eight).
-  L.least = usual_rows(pages, a) > 32 ? 8 : 1;
-  if (need) {
-    L.records = static_cast<int32_t*>(ws);
-    L.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kRecordBytes);
-  }
-  return launched(rkv::launch_attend(L, stream));
+  return attend(pages, a, ws, ws_bytes, stream);
+}
+int rkv_qpages_attend(const rkv_qpages* pages, const rkv_attend* a, void* ws, size_t ws_bytes, void* stream) {
+  return attend(pages, a, ws, ws_bytes, stream);
+}
+
+int rkv_pages_attend_shared_workspace_size(const rkv_pages* pages, const rkv_attend* a, const rkv_shared* shared, size_t* bytes) {
+  return shared_size(pages, a, shared, bytes);
+}
+int rkv_qpages_attend_shared_workspace_size(const rkv_qpages* pages, const rkv_attend* a, const rkv_shared* shared, size_t* bytes) {
+  return shared_size(pages, a, shared, bytes);
+}
+int rkv_pages_attend_shared(const rkv_pages* pages, const rkv_attend* a, const rkv_shared* shared, void* ws, size_t ws_bytes, void* stream) {
+  return attend_shared(pages, a, shared, ws, ws_bytes, stream);
+}
+int rkv_qpages_attend_shared(const rkv_qpages* pages, const rkv_attend* a, const rkv_shared* shared, void* ws, size_t ws_bytes, void* stream) {
+  return attend_shared(pages, a, shared, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

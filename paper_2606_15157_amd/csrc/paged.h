@@ -23,20 +23,32 @@ struct ResizeLaunch {
 };
 int launch_resize(const ResizeLaunch& R, void* stream);
 
+struct Scales {      // exponent bytes of an 8-bit pool's rows
+  uint8_t* at;
+  int64_t page, head, slot;
+};
+
+// Rows to slots, and back.
 struct WriteLaunch {
-  rkv_pages p;
-  rkv_rows r;
+  rkv_pages p;         // an 8-bit pool's strides are of its codes
+  Scales ks, vs;
+  rkv_rows r;          // a read writes them
   FastDiv by_page, by_head, by_token;
   int32_t n_items;     // n_outer * n_tokens * n_kv_heads
   int32_t n_slots;
 };
 int launch_write(const WriteLaunch& W, void* stream);
+int launch_write8(const WriteLaunch& W, void* stream);
+int launch_read(const WriteLaunch& W, void* stream);
+int launch_read8(const WriteLaunch& W, void* stream);
 
 constexpr int kAttendRows = 128;       // rows (tokens x query heads of a group) of a tile
 constexpr int kAttendShares = 512;     // workgroups that share the key tiles of a short list of row tiles: two a CU
 constexpr int kAttendListed = 1024;    // row tiles such a list may have
+enum { kAlone = 0, kOverPrefix = 1, kOverOwn = 2 };   // the launches of a call whose sequences share prefixes
 struct AttendLaunch {
-  rkv_pages p;
+  rkv_pages p;         // an 8-bit pool's strides are of its codes
+  Scales ks, vs;
   rkv_attend a;
   FastDiv by_page, by_group;
   int32_t group;       // Hq / Hkv
@@ -47,7 +59,19 @@ struct AttendLaunch {
   int32_t least;       // key tiles of a share, at least
   int32_t* records;    // [kAttendShares][4], then
   float* parts;        // [2 kAttendShares] partial sums; null: a workgroup per row tile
+  // Shared prefixes: over the prefixes a's sequences are the groups, and its rows those of their members; over the members' own
+  // slots, the sums go on from there.
+  int32_t stage;
+  int32_t n_groups, n_members;
+  const int32_t* cu_seqs;     // [n_groups + 1]
+  const int32_t* own_lens;    // the members' lens, at most own_most
+  int32_t own_most;
+  float* sums;                // [n_rows][Hq] sums over the prefixes
 };
+// 16-bit and 8-bit pools, without and with shared prefixes.
 int launch_attend(const AttendLaunch& A, void* stream);
+int launch_attend8(const AttendLaunch& A, void* stream);
+int launch_attend_shared(const AttendLaunch& A, void* stream);
+int launch_attend8_shared(const AttendLaunch& A, void* stream);
 
 }  // namespace rkv

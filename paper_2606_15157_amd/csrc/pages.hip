@@ -17,6 +17,7 @@ namespace rkv {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kResizeThreads = 1024;
 constexpr int kResizeSlots = 8192;      // slots the workgroup fills itself
@@ -160,21 +161,147 @@ __global__ __launch_bounds__(256) void slots_kernel(const ResizeLaunch R) {
   r.slots[j] = j < r.cu_new[r.n_seqs] ? slot_of(R, r.cu_new, j) : -1;
 }
 
+// Where a (token, head) row of a call lies among the rows and in the pool.
+struct RowPlace {
+  int o, t, h, page, at;
+  bool there;      // whether its slot is one of the pool's
+};
+__device__ __forceinline__ RowPlace place_of(const WriteLaunch& W, int item) {
+  RowPlace x;
+  const int row = div_by(item, W.by_head), slot = W.r.slots[row];
+  x.h = item - row * W.p.n_kv_heads;
+  x.o = div_by(row, W.by_token);
+  x.t = row - x.o * W.r.n_tokens;
+  x.there = (uint32_t)slot < (uint32_t)W.n_slots;
+  x.page = div_by(x.there ? slot : 0, W.by_page);
+  x.at = slot - x.page * W.p.page_size;
+  return x;
+}
 // blockIdx.x: 16 (token, head) rows, 16 lanes each.
+__device__ __forceinline__ int item_of() { return blockIdx.x * 16 + (threadIdx.x >> 4); }
+// This lane's eight values of a row, among the rows and in a pool of 16-bit rows; its eight codes; the row's exponent.
+__device__ __forceinline__ u32x4* k_row(const WriteLaunch& W, const RowPlace& x) {
+  return reinterpret_cast<u32x4*>((uint16_t*)W.r.k + x.o * W.r.k_outer + x.t * W.r.k_token + x.h * W.r.k_head) + (threadIdx.x & 15);
+}
+__device__ __forceinline__ u32x4* v_row(const WriteLaunch& W, const RowPlace& x) {
+  return reinterpret_cast<u32x4*>((uint16_t*)W.r.v + x.o * W.r.v_outer + x.t * W.r.v_token + x.h * W.r.v_head) + (threadIdx.x & 15);
+}
+__device__ __forceinline__ u32x4* k_slot(const WriteLaunch& W, const RowPlace& x) {
+  return reinterpret_cast<u32x4*>(static_cast<uint16_t*>(W.p.k) + x.page * W.p.k_page + x.at * W.p.k_slot + x.h * W.p.k_head) + (threadIdx.x & 15);
+}
+__device__ __forceinline__ u32x4* v_slot(const WriteLaunch& W, const RowPlace& x) {
+  return reinterpret_cast<u32x4*>(static_cast<uint16_t*>(W.p.v) + x.page * W.p.v_page + x.at * W.p.v_slot + x.h * W.p.v_head) + (threadIdx.x & 15);
+}
+__device__ __forceinline__ u32x2* k_codes(const WriteLaunch& W, const RowPlace& x) {
+  return reinterpret_cast<u32x2*>(static_cast<uint8_t*>(W.p.k) + x.page * W.p.k_page + x.at * W.p.k_slot + x.h * W.p.k_head) + (threadIdx.x & 15);
+}
+__device__ __forceinline__ u32x2* v_codes(const WriteLaunch& W, const RowPlace& x) {
+  return reinterpret_cast<u32x2*>(static_cast<uint8_t*>(W.p.v) + x.page * W.p.v_page + x.at * W.p.v_slot + x.h * W.p.v_head) + (threadIdx.x & 15);
+}
+__device__ __forceinline__ uint8_t* scale_at(const Scales& s, const RowPlace& x) { return s.at + x.page * s.page + x.h * s.head + x.at * s.slot; }
+
 __global__ __launch_bounds__(256) void write_kernel(const WriteLaunch W) {
-  const int item = blockIdx.x * 16 + (threadIdx.x >> 4), c = 8 * (threadIdx.x & 15);
-  if (item >= W.n_items) return;
-  const rkv_rows& r = W.r;
-  const rkv_pages& p = W.p;
-  const int row = div_by(item, W.by_head), h = item - row * p.n_kv_heads;
-  const int slot = r.slots[row];
-  if ((uint32_t)slot >= (uint32_t)W.n_slots) return;
-  const int o = div_by(row, W.by_token), t = row - o * r.n_tokens;
-  const int page = div_by(slot, W.by_page), at = slot - page * p.page_size;
-  const u32x4 k = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(r.k) + o * r.k_outer + t * r.k_token + h * r.k_head + c);
-  const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(r.v) + o * r.v_outer + t * r.v_token + h * r.v_head + c);
-  *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.k) + page * p.k_page + at * p.k_slot + h * p.k_head + c) = k;
-  *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.v) + page * p.v_page + at * p.v_slot + h * p.v_head + c) = v;
+  if (item_of() >= W.n_items) return;
+  const RowPlace x = place_of(W, item_of());
+  if (!x.there) return;
+  const u32x4 k = *k_row(W, x), v = *v_row(W, x);
+  *k_slot(W, x) = k;
+  *v_slot(W, x) = v;
+}
+
+// A row of 128 values as e4m3 codes and a power of two 2^e, e the least with max |x| <= 448 2^e among those that leave every code
+// times 2^e a value of the row's own type (bf16 -117 .. 120, fp16 -15 .. 8, and at the largest e codes to 240): x 2^-e is exact, the
+// code its one rounding, and what is read back is exact again.  What is not finite has no part in e, and NaN for a code.
+// Returns this lane's eight codes; byte: e + 127.
+template <bool kF16>
+__device__ __forceinline__ u32x2 encode(u32x4 v, uint32_t& byte) {
+  constexpr uint32_t kLeast = kF16 ? 112 : 10, kMost = kF16 ? 135 : 247;
+  constexpr uint32_t kInf = 0x7f800000u;
+  float x[8];
+  uint32_t top = 0;     // bits of non-negative floats are in their order
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t half = i & 1 ? v[i >> 1] >> 16 : v[i >> 1] & 0xffffu;
+    if constexpr (kF16) x[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)half);
+    else x[i] = __uint_as_float(half << 16);
+    const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
+    top = max(top, a < kInf ? a : 0u);
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+  // floor(log2 top) - 8, one more if top exceeds 1.75 of its power of two: that carries into the exponent
+  const int e = (int)((top + 0x1fffffu) >> 23) - 8;
+  byte = (uint32_t)min(max(e, (int)kLeast), (int)kMost);
+  const float down = __uint_as_float((254u - byte) << 23), most = byte == kMost ? 240.f : 448.f;
+  u32x2 code;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float z = x[4 * i + j];
+      y[j] = (__float_as_uint(z) & 0x7fffffffu) < kInf ? fminf(fmaxf(z * down, -most), most) : __builtin_nanf("");
+    }
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    code[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  }
+  return code;
+}
+template <bool kF16>
+__global__ __launch_bounds__(256) void write8_kernel(const WriteLaunch W) {
+  if (item_of() >= W.n_items) return;      // by whole rows: their 16 lanes stay together
+  const RowPlace x = place_of(W, item_of());
+  if (!x.there) return;
+  const u32x4 k = *k_row(W, x), v = *v_row(W, x);
+  uint32_t k_byte, v_byte;
+  const u32x2 kc = encode<kF16>(k, k_byte), vc = encode<kF16>(v, v_byte);
+  *k_codes(W, x) = kc;
+  *v_codes(W, x) = vc;
+  if ((threadIdx.x & 15) == 0) {
+    *scale_at(W.ks, x) = (uint8_t)k_byte;
+    *scale_at(W.vs, x) = (uint8_t)v_byte;
+  }
+}
+
+__global__ __launch_bounds__(256) void read_kernel(const WriteLaunch W) {
+  if (item_of() >= W.n_items) return;
+  const RowPlace x = place_of(W, item_of());
+  u32x4 k = {0, 0, 0, 0}, v = k;
+  if (x.there) {
+    k = *k_slot(W, x);
+    v = *v_slot(W, x);
+  }
+  *k_row(W, x) = k;
+  *v_row(W, x) = v;
+}
+
+template <bool kF16>
+__device__ __forceinline__ u32x4 decode(u32x2 code, uint32_t byte) {
+  const float scale = __uint_as_float(byte << 23);
+  u32x4 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t c = code[i >> 1];
+    if constexpr (kF16)
+      x[i] = __builtin_bit_cast(uint32_t, i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, scale, false));
+    else
+      x[i] = __builtin_bit_cast(uint32_t, i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false));
+  }
+  return x;
+}
+template <bool kF16>
+__global__ __launch_bounds__(256) void read8_kernel(const WriteLaunch W) {
+  if (item_of() >= W.n_items) return;
+  const RowPlace x = place_of(W, item_of());
+  u32x4 k = {0, 0, 0, 0}, v = k;
+  if (x.there) {
+    const u32x2 kc = *k_codes(W, x), vc = *v_codes(W, x);
+    const uint32_t k_byte = *scale_at(W.ks, x), v_byte = *scale_at(W.vs, x);
+    k = decode<kF16>(kc, k_byte);
+    v = decode<kF16>(vc, v_byte);
+  }
+  *k_row(W, x) = k;
+  *v_row(W, x) = v;
 }
 
 }  // namespace
@@ -187,10 +314,21 @@ int launch_resize(const ResizeLaunch& R, void* stream) {
   return (int)hipGetLastError();
 }
 
-int launch_write(const WriteLaunch& W, void* stream) {
-  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  write_kernel<<<(unsigned)(((int64_t)W.n_items + 15) / 16), 256, 0, st>>>(W);
+namespace {
+using RowsKernel = void(const WriteLaunch);
+int launch_items(RowsKernel* kernel, const WriteLaunch& W, void* stream) {
+  kernel<<<(unsigned)(((int64_t)W.n_items + 15) / 16), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(W);
   return (int)hipGetLastError();
+}
+}  // namespace
+
+int launch_write(const WriteLaunch& W, void* stream) { return launch_items(write_kernel, W, stream); }
+int launch_write8(const WriteLaunch& W, void* stream) {
+  return launch_items(W.p.dtype == RKV_F16 ? write8_kernel<true> : write8_kernel<false>, W, stream);
+}
+int launch_read(const WriteLaunch& W, void* stream) { return launch_items(read_kernel, W, stream); }
+int launch_read8(const WriteLaunch& W, void* stream) {
+  return launch_items(W.p.dtype == RKV_F16 ? read8_kernel<true> : read8_kernel<false>, W, stream);
 }
 
 }  // namespace rkv

@@ -1,0 +1,396 @@
+"""GPU parity of caches held in 8 bits (rows written, read back and attended) against the float64 oracle."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_15157_amd as rkv
+from oracle import pages as OG
+from test_gpu_paged import Case, FEW, MANY, NAN, ONE, compare, f64, ints
+
+pytestmark = pytest.mark.gpu
+
+KIND = {torch.bfloat16: "bf16", torch.float16: "fp16"}
+E4M3 = torch.float8_e4m3fn
+
+
+def bits(t):
+    return t.view(torch.uint8).cpu().numpy()
+
+
+def pool_of(n_pages, hkv, page, dtype, layout="heads", seed=0):
+    """A pool of random bytes; heads before slots, or slots before heads, or a slice of a wider buffer with gaps."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *s: torch.randint(0, 256, s, dtype=torch.uint8, device="cuda", generator=g)  # noqa: E731
+    if layout == "heads":
+        x, s = rand(2, n_pages, hkv, page, 128), rand(2, n_pages, hkv, page)
+    elif layout == "slots":
+        x, s = rand(2, n_pages, page, hkv, 128).transpose(2, 3), rand(2, n_pages, page, hkv).transpose(2, 3)
+    else:
+        x, s = rand(2, n_pages, hkv + 1, page, 272)[:, :, 1:, :, 16:144], rand(2, n_pages, hkv, page + 3, 2)[:, :, :, 3:, 1]
+    return rkv.QuantizedCache(x[0].view(E4M3), x[1].view(E4M3), s[0], s[1], dtype)
+
+
+def values(T, hkv, dtype, g):
+    """Rows of every size: normal ones, tiny and huge ones, zeros, and some that are not finite."""
+    x = torch.randn((T, hkv, 128), device="cuda", generator=g)
+    x *= torch.exp2(torch.randint(-12, 8, (T, hkv, 1), device="cuda", generator=g).float())
+    most = torch.finfo(dtype).max
+    for t in range(0, T, 7):
+        x[t] *= 2.0 ** -140 if dtype == torch.bfloat16 and t % 2 else 2.0 ** -20
+    x[1::11, 0] = 0.0
+    x[2::11, 0, 5] = most
+    x[3::11, 0, 6:9] = torch.tensor([-most, 1.75 * 2.0 ** 10, -(1.75 + 2.0 ** -6) * 2.0 ** 10], device="cuda")
+    x[4::11, 0, 7] = 1.7578125 * 2.0 ** 12        # just above 448 of a power of two: the next exponent
+    x[5::11, 0, 7] = 448.0
+    x[6::11, 0, 3], x[6::11, 0, 9], x[6::11, 0, 100] = NAN, math.inf, -math.inf
+    x[9::11, 0] = math.inf
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,hkv,page,layout,pool", [(1, 8, 16, "rows", "heads"), (13, 1, 1, "rows", "heads"), (300, 3, 7, "fused", "slots"),
+                                                    (130, 8, 100, "heads", "gaps"), (4099, 2, 64, "fused", "heads")])
+def test_write_and_read_follow_the_oracle_bit_for_bit(T, hkv, page, layout, pool, dtype):
+    g = torch.Generator(device="cuda").manual_seed(T)
+    n_pages = -(-2 * T // page) + 2
+    cache = pool_of(n_pages, hkv, page, dtype, pool, T)
+    k, v = values(T, hkv, dtype, g), values(T, hkv, dtype, g).flip(0)
+    if layout == "heads":
+        k, v = (x.view(2, T // 2, hkv, 128).permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3) for x in (k, v))
+    elif layout == "fused":
+        x = torch.zeros((T, 2 * hkv + 4, 128), device="cuda", dtype=dtype)
+        x[:, 4:4 + hkv], x[:, 4 + hkv:] = k, v
+        k, v = x[:, 4:4 + hkv], x[:, 4 + hkv:]
+    slots = torch.randperm(n_pages * page, device="cuda", generator=g)[:T].to(torch.int32)
+    if T > 5:
+        slots[3], slots[T - 1], slots[4] = -1, n_pages * page, -7
+    pools = [cache.k_pages, cache.v_pages, cache.k_scales, cache.v_scales]
+    want = [bits(x).copy() for x in pools]
+    rkv.pages_write(cache, k, v, slots)
+    for i, src in enumerate((k, v)):
+        codes, scales = OG.encode(f64(src).reshape(T, hkv, 128), KIND[dtype])
+        for t, s in enumerate(slots.tolist()):
+            if 0 <= s < n_pages * page:
+                want[i][s // page, :, s % page] = codes[t]
+                want[2 + i][s // page, :, s % page] = scales[t]
+    for i, x in enumerate(pools):
+        got, w = bits(x), want[i]
+        if i < 2:      # one NaN is as good as the other
+            got, w = np.where(got & 127 == 127, 127, got), np.where(w & 127 == 127, 127, w)
+        assert np.array_equal(got, w)
+    # every value back, the same slot twice, zeros where there is none
+    back = torch.cat([slots, slots[:1]])
+    for got, i in zip(rkv.pages_read(cache, back), range(2)):
+        s = np.clip(back.cpu().numpy(), 0, n_pages * page - 1)
+        wide = OG.decode(want[i], want[2 + i])[s // page, :, s % page]
+        there = (back.cpu().numpy() >= 0) & (back.cpu().numpy() < n_pages * page)
+        wide[~there] = 0.0
+        assert got.shape == (T + 1, hkv, 128) and got.dtype == dtype
+        assert np.array_equal(f64(got), wide, equal_nan=True)
+    # and within a rounding of what was written
+    x = f64(k).reshape(T, hkv, 128)
+    y = f64(rkv.pages_read(cache, slots)[0])
+    ok = ((slots >= 0) & (slots < n_pages * page)).cpu().numpy()
+    fine = np.isfinite(x) & ok[:, None, None]
+    top = np.where(np.isfinite(x), np.abs(x), 0.0).max(-1, keepdims=True)
+    least = 2.0 ** (OG.EXPONENTS[KIND[dtype]][0] - 10)       # half the smallest code at the least exponent
+    # top <= 448 2^e and not 448 2^(e - 1): the smallest code's half is 2^(e - 10) <= top 2^-17 / 0.875 (2^-9 of 2^e, e < log2(top) - 7.8)
+    assert (np.abs(x - y) <= np.maximum(2.0 ** -4 * np.abs(x), np.maximum(top * 2.0 ** -17, least)))[fine].all()
+    assert np.isnan(y[~np.isfinite(x) & ok[:, None, None]]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_every_code_at_every_scale_reads_as_what_it_stands_for(dtype):
+    """All codes at all exponents that a write gives: exact in the type."""
+    lo, hi = OG.EXPONENTS[KIND[dtype]]
+    n = hi - lo + 1
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda").view(2, 128).repeat(n, 1).view(n * 2, 1, 1, 128)
+    codes[2 * n - 2:][codes[2 * n - 2:] & 127 > 119] = 0      # above 240 at the largest exponent
+    scales = torch.arange(lo + 127, hi + 128, dtype=torch.uint8, device="cuda").repeat_interleave(2).view(n * 2, 1, 1)
+    cache = rkv.QuantizedCache(codes.view(E4M3), codes.view(E4M3), scales, scales, dtype)
+    for x in rkv.pages_read(cache, torch.arange(2 * n, dtype=torch.int32, device="cuda")):
+        assert np.array_equal(f64(x), OG.decode(codes.cpu().numpy(), scales.cpu().numpy())[:, 0], equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("given", [False, True])
+def test_read_of_a_16_bit_pool_and_of_batches(dtype, given):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    pool = torch.randn((2, 9, 3, 7, 128), device="cuda", generator=g).to(dtype)
+    slots = torch.randint(-4, 67, (4, 11), device="cuda", generator=g).to(torch.int32)
+    kw = {}
+    if given:
+        held = torch.full((2, 4, 5, 12, 128), 7.0, dtype=dtype, device="cuda")
+        kw = dict(k_out=held[0, :, 1:4, 1:].permute(0, 2, 1, 3), v_out=held[1, :, 1:4, 1:].permute(0, 2, 1, 3))
+    got = rkv.pages_read(rkv.PagedCache(pool[0], pool[1]), slots, **kw)
+    s = slots.long()
+    there = ((s >= 0) & (s < 63))[..., None, None]
+    for x, src in zip(got, pool):
+        assert torch.equal(x, torch.where(there, src[s.clamp(0, 62) // 7, :, s.clamp(0, 62) % 7], 0.0))
+    if given:
+        assert (held[:, :, 0] == 7).all() and (held[:, :, 4] == 7).all() and (held[:, :, :, 0] == 7).all()
+
+
+def test_calls_of_nothing():
+    cache = pool_of(3, 2, 4, torch.bfloat16)
+    before = bits(cache.k_pages).copy()
+    none = torch.empty((0, 2, 128), dtype=torch.bfloat16, device="cuda")
+    rkv.pages_write(cache, none, none, ints([]))
+    assert rkv.pages_read(cache, ints([]))[0].shape == (0, 2, 128)
+    out, lse = rkv.pages_attend(cache, torch.empty((0, 4, 128), dtype=torch.bfloat16, device="cuda"), ints([]).view(0, 5), ints([]), ints([0]), return_lse=True)
+    assert out.shape == (0, 4, 128) and np.array_equal(before, bits(cache.k_pages))
+    out, lse = rkv.pages_attend(cache, torch.ones((1, 4, 128), dtype=torch.bfloat16, device="cuda"), ints([]).view(1, 0), ints([4]), return_lse=True)
+    assert (out == 0).all() and torch.isneginf(lse).all()
+
+
+# ------------------------------------------------------------------ attention
+
+class QCase(Case):
+    """A case whose pools are held in 8 bits; k and v are what their codes stand for.  What lies outside the sequences is NaN."""
+
+    def __init__(self, *a, nhd=False, gaps=False, **kw):
+        super().__init__(*a, nhd=nhd, **kw)
+        self.gaps = gaps
+        self.quantize()
+
+    def quantize(self):
+        parts = []
+        for x in (self.k, self.v):
+            codes, scales = OG.encode(f64(x), KIND[self.dtype])
+            scales = np.where(np.isnan(f64(x)).all(-1), 255, scales)
+            parts.append((torch.from_numpy(codes).cuda(), torch.from_numpy(scales.astype(np.uint8)).cuda()))
+        (k, ks), (v, vs) = parts
+        if self.gaps:      # slots before heads, rows and scales apart
+            k, v = (torch.nn.functional.pad(x.transpose(1, 2).contiguous(), (0, 16)).transpose(1, 2)[..., :128] for x in (k, v))
+            ks, vs = (torch.stack([x.transpose(1, 2).contiguous()] * 3, -1).transpose(1, 2)[..., 1] for x in (ks, vs))
+        self.cache = rkv.QuantizedCache(k.view(E4M3), v.view(E4M3), ks, vs, self.dtype)
+        wide = [torch.from_numpy(OG.decode(x.cpu().numpy(), s.cpu().numpy())) for x, s in parts]
+        self.k, self.v = (x.to("cuda", self.dtype) for x in wide)
+        assert all(torch.equal(torch.nan_to_num(y.double().cpu()), torch.nan_to_num(x)) for x, y in zip(wide, (self.k, self.v)))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("page", [1, 7, 8, 16, 24, 32, 48, 64, 100, 2000])
+def test_attention_over_any_page_size(page, dtype):
+    QCase(ONE, page=page, dtype=dtype, seed=page).check(max_q=1)
+    QCase(MANY, page=page, dtype=dtype, seed=page + 1, gaps=page == 7 or page == 32).check()
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (6, 2), (10, 2), (8, 1), (16, 2), (24, 1), (40, 1), (33, 1), (200, 1)])
+def test_attention_over_head_layouts(hq, hkv):
+    QCase(ONE, hq=hq, hkv=hkv, seed=hq).check()
+    QCase([(1, 300), (3, 70), (40, 200), (0, 3)], hq=hq, hkv=hkv, seed=hq + 1).check()
+
+
+@pytest.mark.parametrize("page", [16, 10])
+@pytest.mark.parametrize("lens", [ONE, MANY, FEW], ids=["one", "many", "few"])
+@pytest.mark.parametrize("kw", [
+    dict(causal=False), dict(window=1), dict(window=64), dict(window=50), dict(softcap=2.0), dict(softcap=50.0), dict(scale=0.5),
+    dict(scale=-0.2), dict(scale=0.0), dict(softcap=3.0, slopes=True, window=50), dict(prefix_lens=37), dict(prefix_lens=37, window=20),
+    dict(slopes=True), dict(first_keys="half"), dict(first_keys="beyond"), dict(causal=False, window=33)],
+    ids=lambda d: "-".join(f"{k}{v}" for k, v in d.items()))
+def test_attention_masks_and_scores(lens, kw, page):
+    kw = dict(kw)
+    c = QCase(lens, hq=6, hkv=2, page=page, seed=11)
+    if "slopes" in kw:
+        kw["slopes"] = np.array([2.0 ** -(i + 1) for i in range(6)], dtype=np.float32)
+    if "prefix_lens" in kw:
+        kw["prefix_lens"] = [kw["prefix_lens"]] * len(lens)
+    if "first_keys" in kw:
+        at = [n - m + i for m, n in lens for i in range(m)]
+        kw["first_keys"] = [p // 2 if kw["first_keys"] == "half" or t % 2 else p + 1 for t, p in enumerate(at)]
+    out, lse = c.check(**kw)
+    if kw.get("first_keys") and kw["first_keys"][0] > 0:
+        assert (out[0] == 0).all() and torch.isneginf(lse[0]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("lens", [ONE, MANY, [(300, 4000)], [(1, 2000), (200, 260), (1, 1), (70, 3000), (0, 9), (129, 129), (1, 700)]],
+                         ids=["one", "many", "chunk", "mixed"])
+@pytest.mark.parametrize("kw", [dict(), dict(window=70), dict(first_keys="half"), dict(softcap=4.0, slopes=True)],
+                         ids=lambda d: "-".join(f"{k}{v}" for k, v in d.items()) or "plain")
+@pytest.mark.parametrize("page", [16, 30])
+def test_row_tiles_that_share_the_chip(lens, kw, page, dtype):
+    kw = dict(kw)
+    c = QCase(lens, hq=4, hkv=1, page=page, seed=21, width=16384 // page, dtype=dtype)
+    if "slopes" in kw:
+        kw["slopes"] = np.array([0.5, 0.1, 0.02, 0.003], dtype=np.float32)
+    if "first_keys" in kw:
+        kw["first_keys"] = [(n - m + i) // 2 for m, n in lens for i in range(m)]
+    c.check(**kw)
+
+
+def test_more_row_tiles_than_are_listed():
+    lens = [(1, 1 + 7 * s % 90) for s in range(1098)]
+    QCase(lens + [(100, 300), (65, 65)], hq=2, hkv=1, seed=22).check()
+
+
+def test_queries_before_the_first_slot_see_nothing():
+    out, lse = QCase([(9, 4), (3, 0), (1, 20)], seed=2).check()
+    assert (out[:5] == 0).all() and torch.isneginf(lse[9:12]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_large_scores_sinks_and_scales_far_apart(dtype):
+    QCase([(1, 700), (40, 333)], seed=5, spread=4.0, dtype=dtype).check()
+    c = QCase([(1, 4000), (20, 1000), (1, 130)], seed=6, dtype=dtype)
+    for s, j in ((0, 3900), (1, 3), (1, 970)):
+        c.k[int(c.table[s, j // 16]), :, j % 16] = 20 * c.q[0, ::2]
+    for j in range(130):      # V from the smallest to the largest rows that stay finite in sums
+        c.v[int(c.table[2, j // 16]), :, j % 16] *= 2.0 ** (j % 24 - 14)
+    c.quantize()
+    c.check()
+
+
+def test_long_sequences_in_few_rows():
+    QCase([(1, 40000), (1, 17), (1, 9001)], hq=8, hkv=1, page=64, seed=7).check(max_q=1, max_kv=40000)
+    QCase([(30, 20011)], hq=4, hkv=1, page=32, seed=8).check()
+
+
+def test_strided_tensors():
+    c = QCase([(3, 50), (1, 200), (20, 20)], hq=4, hkv=2, seed=9, pad=5, gaps=True)
+    wide = torch.randn((29, 9, 128), device="cuda").to(torch.bfloat16)
+    wide[:, 2:6] = c.q
+    held = torch.full((29, 7, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((29, 4), 7.0, device="cuda")
+    c.check(q=wide[:, 2:6], out=held[:, 1:5, 128:], lse_out=lse)
+    assert (held[24:] == 7).all() and (lse[24:] == 7).all()
+    assert (held[:, 0] == 7).all() and (held[:, 5:] == 7).all() and (held[..., :128] == 7).all()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(first_keys=True), dict(window=30), dict(prefix_lens=[20, 40, 0, 89])], ids=["causal", "documents", "window", "prefix"])
+@pytest.mark.parametrize("wide", [0, 16384])
+def test_nan_reaches_only_the_rows_that_see_it(kw, wide):
+    kw = dict(kw)
+    lens = [(150, 150), (40, 200), (1, 70), (3, 90)]
+    c = QCase(lens, hq=4, hkv=2, page=16, seed=31, width=wide // 16)
+    if "first_keys" in kw:
+        kw["first_keys"] = [(n - m + i) // 50 * 50 for m, n in lens for i in range(m)]
+    want, log, weight, reach = OG.attend(f64(c.k), f64(c.v), f64(c.q), c.table, [n for _, n in lens], c.cu, **kw)
+    bad = [(0, 70, 5), (0, 70, 9), (0, 140, 127), (1, 180, 64), (1, 10, 0), (2, 3, 1), (3, 88, 33), (3, 55, 34)]
+    for s, j, d in bad:
+        c.cache.v_pages.view(torch.uint8)[int(c.table[s, j // 16]), :, j % 16, d] = 127
+    dev = {k: ints(x) if isinstance(x, list) else x for k, x in kw.items()}
+    got, lse = rkv.pages_attend(c.cache, c.q, ints(c.table.tolist()), ints([n for _, n in lens]), ints(c.cu), return_lse=True, **dev)
+    filled, row = got.clone(), 0
+    for s, (m, n) in enumerate(lens):
+        for i in range(m):
+            p = n - m + i
+            lo = max(0, p - kw["window"] + 1 if "window" in kw else 0, kw["first_keys"][row] if "first_keys" in kw else 0)
+            hi = max(p + 1, min(n, kw["prefix_lens"][s])) if "prefix_lens" in kw else p + 1
+            hit = [d for t, j, d in bad if t == s and lo <= j < hi]
+            assert not torch.isfinite(got[row][:, hit]).any()
+            filled[row][:, hit] = torch.from_numpy(want[row][:, hit]).to("cuda", torch.bfloat16)
+            row += 1
+    compare(filled, lse, want, log, weight, reach, torch.bfloat16, most=200)
+
+
+def test_pages_outside_the_pool_read_as_zeros():
+    c = QCase([(2, 64), (2, 64)], seed=12)
+    c.table[0, 1], c.table[0, 2] = 1 << 30, -5
+    c.check()
+    c = QCase([(1, 70), (1, 64)], page=10, seed=12)
+    c.table[0, 1], c.table[0, 2] = 1 << 30, -5
+    c.check()
+
+
+def test_the_same_as_attention_over_the_rows_read_back():
+    """A 16-bit pool of the values gives the same result to a rounding of the sums, whatever chose either call's kernels."""
+    lens = [(1, 500), (20, 300), (1, 64), (130, 700)]
+    c = QCase(lens, hq=8, hkv=2, seed=14)
+    args = (c.q, ints(c.table.tolist()), ints([n for _, n in lens]), ints(c.cu))
+    a = rkv.pages_attend(c.cache, *args)
+    b = rkv.pages_attend(rkv.PagedCache(c.k, c.v), *args)
+    # both round probabilities and outputs to bf16 (half a step each), of |p| |v| sums within 4 of the largest output here
+    assert (a.float() - b.float()).abs().max() <= 4 * 2.0 ** -8 * 4 * b.float().abs().max()
+
+
+def test_repeats_are_bit_equal_on_a_side_stream_and_under_a_graph():
+    c = QCase([(1, 3000), (1, 80), (7, 300)], hq=8, hkv=2, seed=15, width=1024)
+    args = (c.q, ints(c.table.tolist()), ints([3000, 80, 300]), ints(c.cu))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k = torch.randn((9, 2, 128), device="cuda", generator=g).to(torch.bfloat16)
+    slots = ints([int(c.table[0, 3000 // 16 - 1]) * 16 + i for i in range(4)] + [-1] * 5)
+
+    def step():
+        rkv.pages_write(c.cache, k, k, slots)
+        return (*rkv.pages_read(c.cache, slots), rkv.pages_attend(c.cache, *args))
+
+    want = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(4):
+        k.normal_(generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, step())), i
+
+
+def test_pools_past_32_bit_offsets():
+    """Codes of more than 2^32 bytes, scales far apart: the last page's rows."""
+    page, n_pages = 1024, (1 << 25) // 1024 + 2
+    pool = torch.empty((n_pages, 1, page, 128), dtype=torch.uint8, device="cuda")
+    scales = torch.empty((n_pages, 1, page, 128), dtype=torch.uint8, device="cuda")[..., 5]
+    cache = rkv.QuantizedCache(pool.view(E4M3), pool.view(E4M3), scales, scales)
+    k = torch.randn((70, 1, 128), device="cuda").to(torch.bfloat16)
+    slots = torch.arange(n_pages * page - 70, n_pages * page, dtype=torch.int32, device="cuda")
+    rkv.pages_write(cache, k, k, slots)
+    back = rkv.pages_read(cache, slots)[0]
+    assert np.array_equal(f64(back), OG.decode(*OG.encode(f64(k), "bf16")))
+    q = torch.randn((1, 1, 128), device="cuda").to(torch.bfloat16)
+    out = rkv.pages_attend(cache, q, ints([[n_pages - 1]]), ints([page]), window=70)
+    want, log, weight, reach = OG.attend(f64(back.view(1, 1, 70, 128)), f64(back.view(1, 1, 70, 128)), f64(q), [[0]], [70])
+    compare(out, torch.from_numpy(log).cuda(), want, log, weight, reach, torch.bfloat16, most=70)
+
+
+def test_an_evicted_prompt_is_held_in_8_bits_and_decoded():
+    """Eviction, hand-over into 8-bit pages, new tokens through resize, write and attention; and back into an eviction's matrices."""
+    B, Hq, Hkv, L, n = 3, 8, 2, 256, 64
+    g = torch.Generator(device="cuda").manual_seed(7)
+    k, v = (torch.randn((B, Hkv, L, 128), device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((B, Hq, 32, 128), device="cuda", generator=g).to(torch.bfloat16)
+    plan = rkv.Plan.from_scoped_route([rkv.SNAPKV], [rkv.SCOPE_PREFILL], [n], window=32, pool_kernel=7)
+    out = rkv.evict_prefill(plan, [q], [k], [v], check_status=True)
+    (cache, pages), = rkv.pages_init_from_prefill(plan, out, page_size=16, extra=40, quantized=True)
+    assert isinstance(cache, rkv.QuantizedCache)
+    kept = [f64(x[0]) for x in (out["k_out"], out["v_out"])]
+    kept = [OG.decode(*OG.encode(x, "bf16")) for x in kept]
+    for step in range(20):
+        kt, vt = (torch.randn((B, Hkv, 128), device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+        qt = torch.randn((B, Hq, 128), device="cuda", generator=g).to(torch.bfloat16)
+        got = rkv.pages_resize(pages, pages["lens"] + 1, max_new=B)
+        rkv.pages_write(cache, kt, vt, got["slots"])
+        y, lse = rkv.pages_attend(cache, qt, pages["table"], pages["lens"], got["cu_new"], max_q=1, return_lse=True)
+        kept = [np.concatenate([x, OG.decode(*OG.encode(f64(t), "bf16"))[:, :, None]], 2) for x, t in zip(kept, (kt, vt))]
+    m = n + 20
+    want, log, weight, reach = OG.attend(kept[0], kept[1], f64(qt), [[b] for b in range(B)], [m] * B)
+    compare(y, lse, want, log, weight, reach, torch.bfloat16, most=m)
+    j = torch.arange(m, device="cuda")
+    slots = pages["table"][:, j // 16] * 16 + (j % 16).to(torch.int32)
+    back = [torch.empty((B, Hkv, m, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    rkv.pages_read(cache, slots.contiguous(), k_out=back[0].permute(0, 2, 1, 3), v_out=back[1].permute(0, 2, 1, 3))
+    assert all(np.array_equal(f64(x), w) for x, w in zip(back, kept))
+
+
+def test_gradients_are_refused():
+    c = QCase([(1, 5)], seed=1)
+    q = c.q.clone().requires_grad_()
+    with pytest.raises(ValueError, match="backward"):
+        rkv.pages_attend(c.cache, q, ints(c.table.tolist()), ints([5]))
+    k = torch.zeros((1, 2, 128), dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    with pytest.raises(ValueError, match="backward"):
+        rkv.pages_write(c.cache, k, k, ints([0]))
+    with pytest.raises(ValueError, match="backward"):
+        rkv.pages_read(c.cache, ints([0]), k_out=k, v_out=k)
+    with torch.no_grad():
+        rkv.pages_attend(c.cache, q, ints(c.table.tolist()), ints([5]))
