@@ -66,8 +66,10 @@ template <bool kF16>
 constexpr float kUnder = kF16 ? 7.f : 0.f;
 
 // What a pool is: 16-bit rows in pages of any size; in pages whose size is a multiple of 16, less than 4 GiB and slots at least a row
-// apart; 8-bit codes and a power of two for each row.
-enum Pool { kAnyPages, kPages16, kCodes };
+// apart; 8-bit codes and a power of two for each row; those in pages whose size is a multiple of 8, with the scales of eight slots in
+// eight bytes, 8-byte aligned.
+enum Pool { kAnyPages, kPages16, kCodes, kCodes8 };
+constexpr bool in_codes(Pool pool) { return pool == kCodes || pool == kCodes8; }
 
 __device__ __align__(256) uint32_t zero_row[kHeadDim / 2];   // what a slot outside the visible ones reads as
 
@@ -292,7 +294,7 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
     return (uint32_t)page < (uint32_t)p.n_pages;
   };
   auto pair_at = [&](const void* x, int page, int at, int64_t page_stride, int64_t head, int64_t slot, const Scales& scales) {
-    if constexpr (kPool == kCodes) {
+    if constexpr (in_codes(kPool)) {
       const uint8_t byte = scales.at[page * scales.page + h * scales.head + at * scales.slot];
       const uint16_t two = reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(x) + page * page_stride + h * head + at * slot)[lane];
       return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((uint32_t)two, scale_of(byte), false));
@@ -378,8 +380,7 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
 template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared, bool kNarrow>
 __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
                                             int n_kv, int r0, int h, int u0, int n, float* part, bool early) {
-  constexpr bool kPage16 = kPool == kPages16, kQuant = kPool == kCodes;
-  static_assert(!kQuant || !kNarrow);
+  constexpr bool kPage16 = kPool == kPages16, kQuant = in_codes(kPool);
   const rkv_attend& a = A.a;
   const rkv_pages& p = A.p;
   const bool over_prefix = kShared && A.stage == kOverPrefix;
@@ -569,6 +570,235 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     // At most 16 rows, all of them in every wave; a wave takes the 16 keys of each tile that it fetched itself, two tiles
     // ahead, and waits for no other: 16x16x32 and 16x16x16 MFMA, a lane holds keys 4 (lane / 16) + 0..3 of row lane % 16.
     const int l16 = lane & 15, lg = lane >> 4;
+    f32x4 o[8] = {};
+    if constexpr (kQuant) {
+      // Codes go from memory to registers alone.  A wave takes 32 keys at a time, every fourth 32 of the item's; eight keys of a quarter are the
+      // ones whose probabilities a lane will hold, as the products with V take them.
+      //   K: lane (l16, lg) takes codes 16 lg .. and 64 + 16 lg .. of keys 8 (l16 / 4) + l16 % 4 and 4 further: of either 16 keys, one column
+      //      of 16x16x32 a lane, the sum over the row's 128 in the order that the lanes hold them, as q does.  Scores of keys 8 lg + 0..7 come out.
+      //   V: lane (l16, lg) takes codes 8 l16 + 0..7 of keys 8 lg + 0..7: a column of V^T for each of eight products once pairs of keys are
+      //      put together.  Output 32 lg + 8 i + d of row l16 is o[d][i].
+      // The next block of either is requested as soon as the registers are free: two are in flight.
+      constexpr bool kDense = kPool == kCodes8;
+      struct Block {
+        u32x4 k[4];          // [16 keys][half of the row]
+        u32x2 v[8];
+        uint32_t ks[2], vs[8];     // kDense: two words of eight bytes
+        int key0;
+        bool k_in, v_in;     // kDense: whether this lane's eight keys have a page
+      };
+      struct Pages {
+        int k[kDense ? 1 : 2], v[kDense ? 1 : 8];
+      };
+      const int kg = 8 * (l16 >> 2), k_first = kg + (l16 & 3);
+      const uint8_t* k_scales = A.ks.at + h * A.ks.head;
+      const uint8_t* v_scales = A.vs.at + h * A.vs.head;
+      const int end = t1 * kKeys;
+      auto look32 = [&](int key0, Pages& pages) __attribute__((always_inline)) {      // of 32 keys, those outside taken for the nearest inside
+        auto page_of = [&](int key) { return table[div_by(min(max(key, b_lo), b_hi - 1), A.by_page)]; };
+        if constexpr (kDense) {
+          pages.k[0] = page_of(min(key0 + kg + 7, b_hi - 1));
+          pages.v[0] = page_of(min(key0 + 8 * lg + 7, b_hi - 1));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) pages.k[i] = page_of(key0 + k_first + 4 * i);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) pages.v[i] = page_of(key0 + 8 * lg + i);
+        }
+      };
+      // Whether a key of eight from `key` on is visible to some row, and their page is one.
+      auto held8 = [&](int key, int page) { return key + 8 > b_lo && key < b_hi && key < end && (uint32_t)page < (uint32_t)p.n_pages; };
+      auto place = [&](int key, int page, bool in, const char* rows, int64_t page_stride, int64_t slot, const uint8_t* scales, const Scales& s,
+                       const char*& row, const uint8_t*& scale) __attribute__((always_inline)) {
+        const int at = in ? key - div_by(key, A.by_page) * p.page_size : 0, pg = in ? page : 0;     // else slots that there are
+        row = rows + pg * page_stride + at * slot;
+        scale = scales + pg * s.page + at * s.slot;
+      };
+      auto load_k = [&](int key0, const Pages& pages, Block& x) __attribute__((always_inline)) {
+        const char* row;
+        const uint8_t* scale;
+        if constexpr (kDense) {
+          x.k_in = held8(key0 + kg, pages.k[0]);
+          place(key0 + kg, pages.k[0], x.k_in, kp, p.k_page, p.k_slot, k_scales, A.ks, row, scale);
+          const u32x2 bytes = *reinterpret_cast<const u32x2*>(scale);
+          x.ks[0] = bytes[0];
+          x.ks[1] = bytes[1];
+          row += (l16 & 3) * p.k_slot + 16 * lg;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if constexpr (!kDense) {
+            const int key = key0 + k_first + 4 * i;
+            const bool in = key >= b_lo && key < b_hi && key < end && (uint32_t)pages.k[i] < (uint32_t)p.n_pages;
+            place(key, pages.k[i], in, kp, p.k_page, p.k_slot, k_scales, A.ks, row, scale);
+            row = (in ? row : zeros) + 16 * lg;
+            x.ks[i] = *(in ? scale : reinterpret_cast<const uint8_t*>(zeros));
+          }
+          x.k[2 * i] = *reinterpret_cast<const u32x4*>(row);
+          x.k[2 * i + 1] = *reinterpret_cast<const u32x4*>(row + 64);
+          if constexpr (kDense) row += 4 * p.k_slot;
+        }
+      };
+      auto load_v = [&](int key0, const Pages& pages, Block& x) __attribute__((always_inline)) {
+        const char* row;
+        const uint8_t* scale;
+        x.key0 = key0;
+        if constexpr (kDense) {
+          x.v_in = held8(key0 + 8 * lg, pages.v[0]);
+          place(key0 + 8 * lg, pages.v[0], x.v_in, vp, p.v_page, p.v_slot, v_scales, A.vs, row, scale);
+          const u32x2 bytes = *reinterpret_cast<const u32x2*>(scale);
+          x.vs[0] = bytes[0];
+          x.vs[1] = bytes[1];
+          row += 8 * l16;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if constexpr (!kDense) {
+            const int key = key0 + 8 * lg + i;
+            const bool in = key >= b_lo && key < b_hi && key < end && (uint32_t)pages.v[i] < (uint32_t)p.n_pages;
+            place(key, pages.v[i], in, vp, p.v_page, p.v_slot, v_scales, A.vs, row, scale);
+            row = (in ? row : zeros) + 8 * l16;
+            x.vs[i] = *(in ? scale : reinterpret_cast<const uint8_t*>(zeros));
+          }
+          x.v[i] = *reinterpret_cast<const u32x2*>(row);
+          if constexpr (kDense) row += p.v_slot;
+        }
+      };
+      const int first = t0 * kKeys + 32 * wv;
+      Block x0, x1;
+      Pages ids0, ids1;
+      u32x4 q[4];
+      if (t0 < t1) {
+        look32(first, ids0);
+        look32(first + 128, ids1);
+        load_k(first, ids0, x0);
+        load_v(first, ids0, x0);
+        look32(first + 256, ids0);
+        load_k(first + 128, ids1, x1);
+        load_v(first + 128, ids1, x1);
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        q[s] = *reinterpret_cast<const u32x4*>(qrow + 64 * (s >> 1) + 16 * lg + 8 * (s & 1));
+        if (a.scale < 0.f) q[s] ^= 0x80008000u;
+      }
+      if (kShared && go_on && wv == 0) {      // the first wave's sums begin with the prefix's
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(sums_scale(A, row, hq));
+        if (lg == 0) l = ml[1];
+        ref = ml[0] == -__builtin_inff() ? 0.f : ml[0];
+        m = ml[0] + kUnder<kF16>;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(sums_row(A, row, hq) + 32 * lg + 8 * i + 4 * u);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[4 * u + d][i] = y[d];
+          }
+      }
+      // 32 keys; ids: the pages of the block that is requested in their place, and then of the next one's.
+      auto step = [&](Block& b, Pages& ids, Pages& next) __attribute__((always_inline)) {
+        const int key0 = b.key0;
+        const bool whole = key0 >= b_lo && key0 + 32 <= b_hi && key0 + 32 <= end;
+        look32(key0 + 384, next);
+        float scale[8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) scale[i] = scale_of(kDense ? (b.ks[i] >> (8 * (l16 & 3))) & 255u : b.ks[i]);
+        if constexpr (kDense) {
+          if (!whole || __any(!b.k_in)) {      // slots outside read as zeros, codes and scales
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int key = key0 + k_first + 4 * i;
+              if (!b.k_in || key < b_lo || key >= b_hi) {
+                b.k[2 * i] = b.k[2 * i + 1] = u32x4{0, 0, 0, 0};
+                scale[i] = 0.f;
+              }
+            }
+          }
+        }
+        f32x4 s[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            s[i] = mma16<kF16>(widen8<kF16>(b.k[2 * i + (u >> 1)][2 * (u & 1)], b.k[2 * i + (u >> 1)][2 * (u & 1) + 1], scale[i]), q[u], s[i]);
+        }
+        load_k(key0 + 256, ids, b);
+        const float far = (float)(pos - key0 - 8 * lg);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = score(s[i >> 2][i & 3], i, far);
+        if (key0 < all_lo || key0 + 32 > all_hi) {
+          const int from = lo - key0 - 8 * lg, to = hi - key0 - 8 * lg;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i < from || i >= to) x[i] = -__builtin_inff();
+        }
+        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        top = fmaf(top, grow, base);
+        if (__any(top > m + kGrow)) {   // the row's, over its four lanes
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float m2 = fmaxf(m, top), f = m2 > m ? __builtin_amdgcn_exp2f(m - m2) : 1.f;
+          m = m2;
+          ref = m == -__builtin_inff() ? 0.f : m - kUnder<kF16>;
+          l *= f;
+#pragma unroll
+          for (int d = 0; d < 8; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[d][i] *= f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], grow, base - ref));
+          l += x[i];
+        }
+        const u32x4 pr = {pack<kF16>(x[0], x[1]), pack<kF16>(x[2], x[3]), pack<kF16>(x[4], x[5]), pack<kF16>(x[6], x[7])};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) scale[i] = scale_of(kDense ? (b.vs[i >> 2] >> (8 * (i & 3))) & 255u : b.vs[i]);
+        if constexpr (kDense) {
+          if (!whole || __any(!b.v_in)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int key = key0 + 8 * lg + i;
+              if (!b.v_in || key < b_lo || key >= b_hi) {
+                b.v[i] = u32x2{0, 0};
+                scale[i] = 0.f;
+              }
+            }
+          }
+        }
+        u32x4 w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = widen8<kF16>(b.v[i][0], b.v[i][1], scale[i]);
+        load_v(key0 + 256, ids, b);
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+          const uint32_t halves = d & 1 ? 0x07060302u : 0x05040100u;     // of two keys' words: the lower, or the upper, 16 bits
+          u32x4 vt;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vt[i] = __builtin_amdgcn_perm(w[2 * i + 1][d >> 1], w[2 * i][d >> 1], halves);
+          o[d] = mma16<kF16>(vt, pr, o[d]);
+        }
+      };
+      if (first < end) {
+#pragma unroll 1
+        for (int key0 = first;; key0 += 256) {
+          step(x0, ids0, ids1);
+          if (key0 + 128 >= end) break;
+          step(x1, ids1, ids0);
+          if (key0 + 256 >= end) break;
+        }
+      }
+      const uint32_t meet = lds + wv * 8192 + l16 * 512;     // the end as below, a wave's sums in one piece
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          *(__attribute__((address_space(3))) f32x4*)(uintptr_t)(meet + ((8 * lg + 2 * i + u) ^ l16) * 16) =
+              f32x4{o[4 * u][i], o[4 * u + 1][i], o[4 * u + 2][i], o[4 * u + 3][i]};
+    } else {
     Place next;
     auto fetch_both = [&](int tl, int buf) __attribute__((always_inline)) {
       fetch_k(tl, next, buf);
@@ -591,7 +821,6 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     }
     const uint32_t k_at = lds + wv * 4096 + l16 * 256;
     const uint32_t v_at = lds + 2 * kTileBytes + wv * 4096 + (4 * lg + (l16 >> 2)) * 256 + (l16 & 1) * 8;
-    f32x4 o[8] = {};
     if (kShared && go_on && wv == 0) {      // the first wave's sums begin with the prefix's
       const f32x2 ml = *reinterpret_cast<const f32x2*>(sums_scale(A, row, hq));
       if (lg == 0) l = ml[1];
@@ -656,13 +885,14 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       for (int d = 0; d < 8; ++d)
         o[d] = mma16s<kF16>(vf[d], pr, o[d]);
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
     // The four waves' sums meet by way of the memory each fetched into: columns below 64 in its part of K's first tile, the
     // others in the second's, chunks of 16 bytes at c ^ row; m and l in V's first.
 #pragma unroll
     for (int d = 0; d < 8; ++d)
       *(__attribute__((address_space(3))) f32x4*)(uintptr_t)(k_at + (d >> 2) * kTileBytes + ((4 * (d & 3) + lg) ^ l16) * 16) = o[d];
+    }   // !kQuant
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
     if (lg == 0) *(__attribute__((address_space(3))) f32x2*)(uintptr_t)(lds + 2 * kTileBytes + wv * 4096 + l16 * 8) = f32x2{m, l};
     lds_sync();
     const int x = 4 * wv + lg, c = l16;      // this thread's row and eight columns
@@ -680,8 +910,8 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       ll = fmaf(ml[w][1], f, ll);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const f32x4 v = *(const __attribute__((address_space(3))) f32x4*)(uintptr_t)(lds + (c >> 3) * kTileBytes + w * 4096 + x * 256 +
-                                                                                     ((2 * (c & 7) + u) ^ x) * 16);
+        const uint32_t at = kQuant ? w * 8192 + x * 512 + ((2 * c + u) ^ x) * 16 : (c >> 3) * kTileBytes + w * 4096 + x * 256 + ((2 * (c & 7) + u) ^ x) * 16;
+        const f32x4 v = *(const __attribute__((address_space(3))) f32x4*)(uintptr_t)(lds + at);
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[4 * u + i] = fmaf(v[i], f, sum[4 * u + i]);
       }
@@ -1015,13 +1245,8 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared>
 __device__ __forceinline__ void attend_tile(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
                                             int n_kv, int r0, int h, int u0, int n, float* part, bool early) {
-  if constexpr (kPool != kCodes) {
-    if (n_q * A.group - r0 <= 16) {
-      attend_rows<kF16, kCap, kBias, kPool, kShared, true>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part, early);
-      return;
-    }
-  }
-  attend_rows<kF16, kCap, kBias, kPool, kShared, false>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part, early);
+  if (n_q * A.group - r0 <= 16) attend_rows<kF16, kCap, kBias, kPool, kShared, true>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part, early);
+  else attend_rows<kF16, kCap, kBias, kPool, kShared, false>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part, early);
 }
 
 // The same for sequences of more than one tile alone, when those are few: floor(rows / 128) >= 1 then, and twice that is room
@@ -1316,8 +1541,15 @@ int launch_rows(const AttendLaunch& A, void* stream) {
 template <bool kShared>
 int launch_codes(const AttendLaunch& A, void* stream) {
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  if (A.p.dtype == RKV_F16) launch_scores<true, kCodes, kShared>(A, st);
-  else launch_scores<false, kCodes, kShared>(A, st);
+  bool dense = A.p.page_size % 8 == 0;
+  for (const Scales& s : {A.ks, A.vs}) dense &= s.slot == 1 && ((uintptr_t)s.at | s.page | s.head) % 8 == 0;
+  if (A.p.dtype == RKV_F16) {
+    if (dense) launch_scores<true, kCodes8, kShared>(A, st);
+    else launch_scores<true, kCodes, kShared>(A, st);
+  } else {
+    if (dense) launch_scores<false, kCodes8, kShared>(A, st);
+    else launch_scores<false, kCodes, kShared>(A, st);
+  }
   return (int)hipGetLastError();
 }
 
