@@ -66,8 +66,8 @@ template <bool kF16>
 constexpr float kUnder = kF16 ? 7.f : 0.f;
 
 // What a pool is: 16-bit rows in pages of any size; in pages whose size is a multiple of 16, less than 4 GiB and slots at least a row
-// apart; 8-bit codes and a power of two for each row; those in pages whose size is a multiple of 8, with the scales of eight slots in
-// eight bytes, 8-byte aligned.
+// apart; 8-bit codes and a power of two for each row; those in pages whose size is a multiple of 8 and which are less than 2 GiB, with
+// the scales of eight slots in eight bytes, 8-byte aligned.
 enum Pool { kAnyPages, kPages16, kCodes, kCodes8 };
 constexpr bool in_codes(Pool pool) { return pool == kCodes || pool == kCodes8; }
 
@@ -587,78 +587,80 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
         int key0;
         bool k_in, v_in;     // kDense: whether this lane's eight keys have a page
       };
-      struct Pages {
-        int k[kDense ? 1 : 2], v[kDense ? 1 : 8];
+      // Where a lane's rows of 32 keys lie: of its eight of K and of V (kDense; a page that is none: slots that there are, hidden later),
+      // or of each.
+      struct Places {
+        int k[kDense ? 1 : 2], v[kDense ? 1 : 8], k_at, v_at;
       };
       const int kg = 8 * (l16 >> 2), k_first = kg + (l16 & 3);
       const uint8_t* k_scales = A.ks.at + h * A.ks.head;
       const uint8_t* v_scales = A.vs.at + h * A.vs.head;
+      const char* k_lane = kp + (l16 & 3) * p.k_slot + 16 * lg;      // kDense
+      const char* v_lane = vp + 8 * l16;
       const int end = t1 * kKeys;
-      auto look32 = [&](int key0, Pages& pages) __attribute__((always_inline)) {      // of 32 keys, those outside taken for the nearest inside
-        auto page_of = [&](int key) { return table[div_by(min(max(key, b_lo), b_hi - 1), A.by_page)]; };
+      auto look32 = [&](int key0, Places& x) __attribute__((always_inline)) {      // keys that no row sees are taken for ones that some do
         if constexpr (kDense) {
-          pages.k[0] = page_of(min(key0 + kg + 7, b_hi - 1));
-          pages.v[0] = page_of(min(key0 + 8 * lg + 7, b_hi - 1));
+          auto place = [&](int key, int& page, int& at) {
+            const int c = div_by(min(max(key + 7, b_lo), b_hi - 1), A.by_page);
+            page = table[c];
+            at = key - c * p.page_size;
+          };
+          place(key0 + kg, x.k[0], x.k_at);
+          place(key0 + 8 * lg, x.v[0], x.v_at);
         } else {
+          auto page_of = [&](int key) { return table[div_by(min(max(key, b_lo), b_hi - 1), A.by_page)]; };
 #pragma unroll
-          for (int i = 0; i < 2; ++i) pages.k[i] = page_of(key0 + k_first + 4 * i);
+          for (int i = 0; i < 2; ++i) x.k[i] = page_of(key0 + k_first + 4 * i);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) pages.v[i] = page_of(key0 + 8 * lg + i);
+          for (int i = 0; i < 8; ++i) x.v[i] = page_of(key0 + 8 * lg + i);
         }
       };
-      // Whether a key of eight from `key` on is visible to some row, and their page is one.
-      auto held8 = [&](int key, int page) { return key + 8 > b_lo && key < b_hi && key < end && (uint32_t)page < (uint32_t)p.n_pages; };
-      auto place = [&](int key, int page, bool in, const char* rows, int64_t page_stride, int64_t slot, const uint8_t* scales, const Scales& s,
-                       const char*& row, const uint8_t*& scale) __attribute__((always_inline)) {
-        const int at = in ? key - div_by(key, A.by_page) * p.page_size : 0, pg = in ? page : 0;     // else slots that there are
-        row = rows + pg * page_stride + at * slot;
-        scale = scales + pg * s.page + at * s.slot;
-      };
-      auto load_k = [&](int key0, const Pages& pages, Block& x) __attribute__((always_inline)) {
-        const char* row;
-        const uint8_t* scale;
+      // Whether some of eight keys from `key` on is visible to some row, and their page is one.
+      auto held8 = [&](int key, int page) { return key + 8 > b_lo && key < min(b_hi, end) && (uint32_t)page < (uint32_t)p.n_pages; };
+      auto far_by = [](auto* from, int n, int64_t stride) { return from + (uint64_t)(uint32_t)n * (uint32_t)stride; };      // both below 2^31
+      auto load_k = [&](int key0, const Places& at, Block& x) __attribute__((always_inline)) {
+        const char* row = nullptr;
         if constexpr (kDense) {
-          x.k_in = held8(key0 + kg, pages.k[0]);
-          place(key0 + kg, pages.k[0], x.k_in, kp, p.k_page, p.k_slot, k_scales, A.ks, row, scale);
-          const u32x2 bytes = *reinterpret_cast<const u32x2*>(scale);
+          x.k_in = held8(key0 + kg, at.k[0]);
+          const int page = x.k_in ? at.k[0] : 0, slot = x.k_in ? at.k_at : 0;
+          const u32x2 bytes = *reinterpret_cast<const u32x2*>(far_by(k_scales, page, A.ks.page) + slot);
           x.ks[0] = bytes[0];
           x.ks[1] = bytes[1];
-          row += (l16 & 3) * p.k_slot + 16 * lg;
+          row = far_by(far_by(k_lane, page, p.k_page), slot, p.k_slot);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           if constexpr (!kDense) {
             const int key = key0 + k_first + 4 * i;
-            const bool in = key >= b_lo && key < b_hi && key < end && (uint32_t)pages.k[i] < (uint32_t)p.n_pages;
-            place(key, pages.k[i], in, kp, p.k_page, p.k_slot, k_scales, A.ks, row, scale);
-            row = (in ? row : zeros) + 16 * lg;
-            x.ks[i] = *(in ? scale : reinterpret_cast<const uint8_t*>(zeros));
+            const bool in = key >= b_lo && key < b_hi && key < end && (uint32_t)at.k[i] < (uint32_t)p.n_pages;
+            const int slot = key - div_by(in ? key : 0, A.by_page) * p.page_size;
+            row = (in ? kp + at.k[i] * p.k_page + slot * p.k_slot : zeros) + 16 * lg;
+            x.ks[i] = *(in ? k_scales + at.k[i] * A.ks.page + slot * A.ks.slot : reinterpret_cast<const uint8_t*>(zeros));
           }
           x.k[2 * i] = *reinterpret_cast<const u32x4*>(row);
           x.k[2 * i + 1] = *reinterpret_cast<const u32x4*>(row + 64);
           if constexpr (kDense) row += 4 * p.k_slot;
         }
       };
-      auto load_v = [&](int key0, const Pages& pages, Block& x) __attribute__((always_inline)) {
-        const char* row;
-        const uint8_t* scale;
+      auto load_v = [&](int key0, const Places& at, Block& x) __attribute__((always_inline)) {
+        const char* row = nullptr;
         x.key0 = key0;
         if constexpr (kDense) {
-          x.v_in = held8(key0 + 8 * lg, pages.v[0]);
-          place(key0 + 8 * lg, pages.v[0], x.v_in, vp, p.v_page, p.v_slot, v_scales, A.vs, row, scale);
-          const u32x2 bytes = *reinterpret_cast<const u32x2*>(scale);
+          x.v_in = held8(key0 + 8 * lg, at.v[0]);
+          const int page = x.v_in ? at.v[0] : 0, slot = x.v_in ? at.v_at : 0;
+          const u32x2 bytes = *reinterpret_cast<const u32x2*>(far_by(v_scales, page, A.vs.page) + slot);
           x.vs[0] = bytes[0];
           x.vs[1] = bytes[1];
-          row += 8 * l16;
+          row = far_by(far_by(v_lane, page, p.v_page), slot, p.v_slot);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if constexpr (!kDense) {
             const int key = key0 + 8 * lg + i;
-            const bool in = key >= b_lo && key < b_hi && key < end && (uint32_t)pages.v[i] < (uint32_t)p.n_pages;
-            place(key, pages.v[i], in, vp, p.v_page, p.v_slot, v_scales, A.vs, row, scale);
-            row = (in ? row : zeros) + 8 * l16;
-            x.vs[i] = *(in ? scale : reinterpret_cast<const uint8_t*>(zeros));
+            const bool in = key >= b_lo && key < b_hi && key < end && (uint32_t)at.v[i] < (uint32_t)p.n_pages;
+            const int slot = key - div_by(in ? key : 0, A.by_page) * p.page_size;
+            row = (in ? vp + at.v[i] * p.v_page + slot * p.v_slot : zeros) + 8 * l16;
+            x.vs[i] = *(in ? v_scales + at.v[i] * A.vs.page + slot * A.vs.slot : reinterpret_cast<const uint8_t*>(zeros));
           }
           x.v[i] = *reinterpret_cast<const u32x2*>(row);
           if constexpr (kDense) row += p.v_slot;
@@ -666,7 +668,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       };
       const int first = t0 * kKeys + 32 * wv;
       Block x0, x1;
-      Pages ids0, ids1;
+      Places ids0, ids1;
       u32x4 q[4];
       if (t0 < t1) {
         look32(first, ids0);
@@ -696,8 +698,8 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
             for (int d = 0; d < 4; ++d) o[4 * u + d][i] = y[d];
           }
       }
-      // 32 keys; ids: the pages of the block that is requested in their place, and then of the next one's.
-      auto step = [&](Block& b, Pages& ids, Pages& next) __attribute__((always_inline)) {
+      // 32 keys; ids: where the block lies that is requested in their place, next: the one after.
+      auto step = [&](Block& b, Places& ids, Places& next) __attribute__((always_inline)) {
         const int key0 = b.key0;
         const bool whole = key0 >= b_lo && key0 + 32 <= b_hi && key0 + 32 <= end;
         look32(key0 + 384, next);
@@ -1542,6 +1544,7 @@ template <bool kShared>
 int launch_codes(const AttendLaunch& A, void* stream) {
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   bool dense = A.p.page_size % 8 == 0;
+  for (int64_t stride : {A.p.k_page, A.p.v_page, A.p.k_slot, A.p.v_slot, A.ks.page, A.vs.page}) dense &= stride < kStrideEnd;
   for (const Scales& s : {A.ks, A.vs}) dense &= s.slot == 1 && ((uintptr_t)s.at | s.page | s.head) % 8 == 0;
   if (A.p.dtype == RKV_F16) {
     if (dense) launch_scores<true, kCodes8, kShared>(A, st);
