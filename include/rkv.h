@@ -512,7 +512,7 @@ typedef struct {
  * group's prefix (positions, windows and distances count from the prefix's first slot; causal governs the own slots, while a prefix lies
  * before every row), with each prefix read once for the rows of all its sequences instead of once for each.  A
  * row's sums over its prefix are held in 32 bits between the two.  A group of one sequence is allowed, as is a prefix of no slots.
- * ws: as rkv_pages_attend; it holds 520 bytes for each row and query head besides.
+ * ws: as rkv_pages_attend; it holds 528 or 1056 bytes for each row and query head besides.
  * Errors: as rkv_pages_attend; RKV_ERR_UNSUPPORTED also for prefix_lens or first_keys, and where a prefix and a sequence
  * could hold 2^31 - 1024 slots together; RKV_ERR_SHAPE for a shared table whose stride is less than max_pages. */
 int rkv_pages_attend_shared_workspace_size(const rkv_pages* pages, const rkv_attend* a, const rkv_shared* shared, size_t* bytes);

@@ -43,6 +43,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -57,6 +58,7 @@ constexpr int kListed = kAttendListed;
 constexpr int kAhead = 11;                 // of a tile's 16 pairs of probabilities, those computed between the products of K
 constexpr int kTileBytes = kKeys * kHeadDim * 2;
 constexpr int64_t kStrideEnd = int64_t(1) << 31;   // page strides (elements) whose bytes 32 bits hold
+constexpr int kHasPrefix = 1 << 16;                // in a record of a row's own slots
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGrow = 8.f;               // log2 units a maximum may outgrow the reference by
 // Log2 units of the reference below the maximum it was set at.  Probabilities then reach 2^(kGrow + kUnder): fp16 holds 65504, and
@@ -143,18 +145,14 @@ __device__ __forceinline__ int wave_max(int x) {
   return uniform(x);
 }
 
-// First row of sequence s among all, cut to the call's rows.  Over the prefixes, a "sequence" is a group of them.
+// First row of sequence s among all, cut to the call's rows; over the prefixes, of group s.
 template <bool kShared>
-__device__ __forceinline__ int first_row(const AttendLaunch& A, int s) {
+__device__ __forceinline__ int first_row(const AttendLaunch& A, int s, bool over) {
   const rkv_attend& a = A.a;
   if constexpr (kShared) {
-    if (A.stage == kOverPrefix) s = min(max(A.cu_seqs[s], 0), A.n_members);
+    if (over) s = min(max(A.g.cu_seqs[s], 0), a.n_seqs);
   }
   return a.cu_q ? min(max(a.cu_q[s], 0), a.n_rows) : min(s, a.n_rows);
-}
-template <bool kShared>
-__device__ __forceinline__ int end_row(const AttendLaunch& A, int s) {
-  return first_row<kShared>(A, s + 1);
 }
 
 // Row tiles are numbered with room for a part-filled one per sequence: sequence s starts at floor(row0 G / 128) + s, which
@@ -164,14 +162,25 @@ __device__ __forceinline__ int tile_start(const AttendLaunch& A, int row0, int s
 // The first slot that position `at` (which may be negative) sees.
 __device__ __forceinline__ int window_start(const rkv_attend& a, int at) { return a.window && at >= a.window ? at - a.window + 1 : 0; }
 
+__device__ __forceinline__ int slots_of(const AttendLaunch& A, int seq) {
+  return min(max(A.a.lens[seq], 0), A.a.max_pages * A.p.page_size);
+}
+template <bool kShared>
+__device__ __forceinline__ int slots_of(const AttendLaunch& A, int seq, bool over) {
+  if constexpr (kShared) {
+    if (over) return min(max(A.g.lens[seq], 0), A.g.max_pages * A.p.page_size);
+  }
+  return slots_of(A, seq);
+}
+
 // Over the prefixes: the position of a row (of all) of group g whose prefix has n_kv slots: the prefix's slots and those that the row's
 // own sequence, which a bisection finds, holds before it.
 __device__ __forceinline__ int member_position(const AttendLaunch& A, int g, int row, int n_kv) {
   const int32_t* cu = A.a.cu_q;
-  int s = min(row, A.n_members - 1), end = s + 1;
+  int s = min(row, A.a.n_seqs - 1), end = s + 1;
   if (cu) {
-    int hi = min(max(A.cu_seqs[g + 1], 0), A.n_members);
-    s = min(max(A.cu_seqs[g], 0), A.n_members - 1);
+    int hi = min(max(A.g.cu_seqs[g + 1], 0), A.a.n_seqs);
+    s = min(max(A.g.cu_seqs[g], 0), A.a.n_seqs - 1);
     while (hi - s > 1) {
       const int mid = (s + hi) >> 1;
       if (cu[mid] <= row) s = mid;
@@ -179,7 +188,7 @@ __device__ __forceinline__ int member_position(const AttendLaunch& A, int g, int
     }
     end = cu[s + 1];
   }
-  return n_kv + min(max(A.own_lens[s], 0), A.own_most) - (end - row);
+  return n_kv + slots_of(A, s) - (end - row);
 }
 
 // Whether some of sequences s0 .. s1 - 1 has rows before its last prefix slot (more rows than own slots and one): these see part of the
@@ -188,16 +197,16 @@ __device__ __forceinline__ bool early_rows(const AttendLaunch& A, int s0, int s1
   const int32_t* cu = A.a.cu_q;
   bool early = false;
   if (cu && A.a.causal)
-    for (int s = s0 + i; s < s1; s += n) early |= cu[s + 1] - cu[s] > min(max(A.own_lens[s], 0), A.own_most) + 1;
+    for (int s = s0 + i; s < s1; s += n) early |= cu[s + 1] - cu[s] > slots_of(A, s) + 1;
   return early;
 }
 
 // The key tiles [t0, t1) that rows r0 .. r0 + 127 of a sequence of n_q tokens and n_kv slots may see (first_keys aside).
 template <bool kShared>
-__device__ __forceinline__ void tile_span(const AttendLaunch& A, int seq, int r0, int n_q, int n_kv, int& t0, int& t1) {
+__device__ __forceinline__ void tile_span(const AttendLaunch& A, int seq, int r0, int n_q, int n_kv, bool over, int& t0, int& t1) {
   const rkv_attend& a = A.a;
   if constexpr (kShared) {
-    if (A.stage == kOverPrefix) {      // a window is seen to when the rows are
+    if (over) {      // a window is seen to when the rows are
       t0 = 0;
       t1 = (n_kv + kKeys - 1) / kKeys;
       return;
@@ -210,9 +219,6 @@ __device__ __forceinline__ void tile_span(const AttendLaunch& A, int seq, int r0
   t0 = lo / kKeys;
   t1 = max(t0, (hi + kKeys - 1) / kKeys);
 }
-__device__ __forceinline__ int slots_of(const AttendLaunch& A, int seq) {
-  return min(max(A.a.lens[seq], 0), A.a.max_pages * A.p.page_size);
-}
 
 // A partial sum in the workspace: slot_rows rows of 128 floats (not divided by l), then pairs of what they and l are relative to
 // (log2) and l; 16-byte aligned, slot_rows being even.
@@ -220,17 +226,19 @@ __device__ __forceinline__ float* part_slot(const AttendLaunch& A, int slot) {
   return A.parts + (size_t)slot * A.slot_rows * (kHeadDim + 2);
 }
 
-// What the rows' sums over their prefixes are, between the two launches: 128 floats a row and head (not divided by l), then pairs (m, l) as above.
-__device__ __forceinline__ float* sums_row(const AttendLaunch& A, int64_t row, int hq) { return A.sums + (row * A.a.n_q_heads + hq) * kHeadDim; }
-__device__ __forceinline__ float* sums_scale(const AttendLaunch& A, int64_t row, int hq) {
-  return A.sums + (int64_t)A.a.n_rows * A.a.n_q_heads * kHeadDim + 2 * (row * A.a.n_q_heads + hq);
+// Sums of whole rows between launches: 128 floats a row and head (not divided by l), and a record of m, l as above and two words (below).
+// Over the prefixes' first, those over the rows' own slots behind.
+__device__ __forceinline__ int64_t sums_at(const AttendLaunch& A, int64_t row, int hq, bool own) {
+  return ((own ? A.a.n_rows : 0) + row) * A.a.n_q_heads + hq;
 }
-// Whether the rows of sequence seq go on from there.
-template <bool kShared>
-__device__ __forceinline__ bool has_prefix(const AttendLaunch& A, int seq) {
-  if constexpr (kShared) return A.stage == kOverOwn && seq >= A.cu_seqs[0] && seq < A.cu_seqs[A.n_groups];
-  else return false;
+__device__ __forceinline__ float* sums_row(const AttendLaunch& A, int64_t row, int hq, bool own = false) {
+  return A.sums + sums_at(A, row, hq, own) * kHeadDim;
 }
+__device__ __forceinline__ float* sums_scale(const AttendLaunch& A, int64_t row, int hq, bool own = false) {
+  return A.sum_records + sums_at(A, row, hq, own) * 4;
+}
+// Whether sequence seq has a prefix.
+__device__ __forceinline__ bool has_prefix(const AttendLaunch& A, int seq) { return seq >= A.g.cu_seqs[0] && seq < A.g.cu_seqs[A.g.n_groups]; }
 
 struct Bounds {   // of the waves
   int lo[4], all_lo[4], bad[4];
@@ -281,12 +289,12 @@ __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_floa
 // each, two columns a lane, over the slots that they see and no others, and written: true.
 template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared>
 __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds& bounds, int seq, int row0, int n_q, int n_kv, int r0,
-                                                  int h, int from, int to, int b_lo, int every_lo, int every_hi, int b_hi, float* part, bool go_on) {
+                                                  int h, int from, int to, int b_lo, int every_lo, int every_hi, int b_hi, float* part, bool over, bool go_on) {
   const rkv_attend& a = A.a;
   const rkv_pages& p = A.p;
   const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
-  const int32_t* table = a.table + seq * a.table_stride;
-  const bool over_prefix = kShared && A.stage == kOverPrefix;
+  const int32_t* table = kShared && over ? A.g.table + seq * A.g.table_stride : a.table + seq * a.table_stride;
+  const bool to_sums = kShared && (over || A.stage == kBoth);
   auto place = [&](int key, int& page, int& at) {
     const int c = div_by(key, A.by_page);
     page = uniform(table[c]);
@@ -315,7 +323,7 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
     }
   }
   if (!any_wave(bounds, blame)) return false;
-  const int n_rows = n_q * A.group, prefix = a.prefix_lens ? uniform(a.prefix_lens[seq]) : 0;
+  const int n_rows = n_q * A.group, prefix = !kShared && a.prefix_lens ? uniform(a.prefix_lens[seq]) : 0;
   const float cap2 = 2.f * kLog2e * a.softcap, in_cap = kCap ? 2.f * kLog2e * (a.scale / a.softcap) : 0.f;   // 1 / softcap may overflow
 #pragma unroll 1
   for (int i = 0; i < 32; ++i) {
@@ -323,7 +331,7 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
     if (r >= n_rows) break;
     const int t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
     const int64_t row = row0 + t;
-    const int pos = over_prefix ? member_position(A, seq, (int)row, n_kv) : n_kv - n_q + t;
+    const int pos = kShared && over ? member_position(A, seq, (int)row, n_kv) : n_kv - n_q + t;
     int hi = a.causal ? min(n_kv, max(pos + 1, prefix)) : n_kv, lo = window_start(a, pos);
     if (a.first_keys) lo = max(lo, uniform(a.first_keys[row]));
     lo = max(lo, from);
@@ -358,9 +366,9 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
       o0 = fmaf(o0, f, e * v[0]);
       o1 = fmaf(o1, f, e * v[1]);
     }
-    if (part || over_prefix) {
-      float* to_o = part ? part + mine * kHeadDim : sums_row(A, row, hq);
-      float* to_m = part ? part + A.slot_rows * kHeadDim + 2 * mine : sums_scale(A, row, hq);
+    if (part || to_sums) {
+      float* to_o = part ? part + mine * kHeadDim : sums_row(A, row, hq, !over);
+      float* to_m = part ? part + A.slot_rows * kHeadDim + 2 * mine : sums_scale(A, row, hq, !over);
       to_o[2 * lane] = o0;
       to_o[2 * lane + 1] = o1;
       to_m[0] = m;
@@ -379,12 +387,12 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
 // partial sums go, null: the rows are finished (over the prefixes, their sums are).
 template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared, bool kNarrow>
 __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
-                                            int n_kv, int r0, int h, int u0, int n, float* part, bool early) {
+                                            int n_kv, int r0, int h, int u0, int n, float* part, bool over, bool early) {
   constexpr bool kPage16 = kPool == kPages16, kQuant = in_codes(kPool);
   const rkv_attend& a = A.a;
   const rkv_pages& p = A.p;
-  const bool over_prefix = kShared && A.stage == kOverPrefix;
-  const bool go_on = u0 == 0 && has_prefix<kShared>(A, seq);      // from the rows' sums over the prefix
+  const bool to_sums = kShared && (over || A.stage == kBoth);
+  const bool go_on = kShared && A.stage == kOverOwn && u0 == 0 && has_prefix(A, seq);      // from the rows' sums over the prefix
   int lane = threadIdx.x & 63;
   if constexpr (kNarrow) asm volatile("" : "+v"(lane));   // its addresses are not kept from one item to the next
   const int wv = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
@@ -392,7 +400,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 
   // The slots a position sees, and a row's position.  Both bounds ascend with the row, so that those of the tile and of the
   // wave follow from their first and last rows, without a word from the other lanes: the first keys are requested at once.
-  const int prefix = a.prefix_lens ? uniform(a.prefix_lens[seq]) : 0;
+  const int prefix = !kShared && a.prefix_lens ? uniform(a.prefix_lens[seq]) : 0;
   auto hi_of = [&](int at) { return a.causal ? min(n_kv, max(at + 1, prefix)) : n_kv; };
   auto lo_of = [&](int at) { return window_start(a, at); };
   auto position = [&](int r) { return n_kv - n_q + div_by(min(r, n_rows - 1), A.by_group); };   // rows behind the last repeat it
@@ -405,9 +413,9 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   const int64_t row = row0 + t;
   int pos = n_kv - n_q + t;
   int lo = lo_of(pos), hi = hi_of(pos);
-  bool by_row = a.first_keys;
+  bool by_row = !kShared && a.first_keys;
   if constexpr (kShared) {      // rows of a group: all of the prefix, or from where each one's window begins, or to where an early one lies
-    if (over_prefix) {
+    if (over) {
       by_row = a.window;
       if (by_row || kBias || early) pos = member_position(A, seq, (int)row, n_kv);
       lo = a.window ? window_start(a, pos) : 0;
@@ -419,7 +427,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     }
   }
   if (by_row) {   // these need not ascend
-    if (a.first_keys) lo = max(lo, a.first_keys[row]);
+    if (!kShared) lo = max(lo, a.first_keys[row]);
     all_lo = wave_max(lo);
     b_lo = wave_min(lo);
     every_lo = all_lo;
@@ -434,7 +442,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     }
   }
   int t0, t1;
-  tile_span<kShared>(A, seq, r0, n_q, n_kv, t0, t1);
+  tile_span<kShared>(A, seq, r0, n_q, n_kv, over, t0, t1);
   if (n >= 0) {
     t0 += u0;
     t1 = min(t1, t0 + n);
@@ -447,7 +455,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   // 16 slots hold a wave's 16 rows in one: their addresses are a scalar base and offsets that never change (150 fewer vector
   // instructions a tile than with a page for each row, of 480).
   const uint32_t lds = lds_addr(smem);
-  const int32_t* table = a.table + seq * a.table_stride;
+  const int32_t* table = kShared && over ? A.g.table + seq * A.g.table_stride : a.table + seq * a.table_stride;
   const auto* known = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)table;   // scalar loads
   constexpr int kBytes = kQuant ? 1 : 2;     // of a value
   const char* kp = static_cast<const char*>(p.k) + h * p.k_head * kBytes;
@@ -925,17 +933,17 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       for (int i = 0; i < 8; ++i) finite = fmaf(sum[i], 0.f, finite);
       if (any_wave(bounds, finite != 0.f) &&   // NaN
           attend_row_by_row<kF16, kCap, kBias, kPool, kShared>(A, bounds, seq, row0, n_q, n_kv, r0, h, t0 * kKeys, t1 * kKeys, b_lo, every_lo,
-                                                               every_hi, b_hi, part, go_on))
+                                                               every_hi, b_hi, part, over, go_on))
         return;
     }
     if (r0 + x >= n_rows) return;
     const int token = div_by(r0 + x, A.by_group), head = h * A.group + r0 + x - token * A.group;
-    if (part || over_prefix) {
-      float* to = part ? part + x * kHeadDim : sums_row(A, row0 + token, head);
+    if (part || to_sums) {
+      float* to = part ? part + x * kHeadDim : sums_row(A, row0 + token, head, !over);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
         *reinterpret_cast<f32x4*>(to + 8 * c + 4 * u) = f32x4{sum[4 * u], sum[4 * u + 1], sum[4 * u + 2], sum[4 * u + 3]};
-      if (c == 0) *reinterpret_cast<f32x2*>(part ? part + A.slot_rows * kHeadDim + 2 * x : sums_scale(A, row0 + token, head)) = f32x2{mm, ll};
+      if (c == 0) *reinterpret_cast<f32x2*>(part ? part + A.slot_rows * kHeadDim + 2 * x : sums_scale(A, row0 + token, head, !over)) = f32x2{mm, ll};
       return;
     }
     const float inv = ll == 0.f ? 0.f : 1.f / ll;
@@ -1177,7 +1185,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       for (int i = 0; i < 16; ++i) finite = fmaf(o[d][i], 0.f, finite);
     if (any_wave(bounds, finite != 0.f) &&   // NaN
         attend_row_by_row<kF16, kCap, kBias, kPool, kShared>(A, bounds, seq, row0, n_q, n_kv, r0, h, t0 * kKeys, t1 * kKeys, b_lo, every_lo, every_hi,
-                                                             b_hi, part, go_on))
+                                                             b_hi, part, over, go_on))
       return;
   }
 
@@ -1189,7 +1197,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   uint32_t ln = lane;
   asm volatile("" : "+v"(ln));   // addresses of this end are not kept from one item to the next
   const uint32_t mem = lds + wv * 16384, cl = ln & 31, hf = ln >> 5;
-  if (part || over_prefix) {
+  if (part || to_sums) {
     const uint32_t to = mem + cl * 512;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -1208,7 +1216,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       float* to_o = part + (32 * wv + x) * kHeadDim;
       if (kShared && !part) {
         const int64_t to_row = at_row(x, head);
-        to_o = sums_row(A, to_row, head);
+        to_o = sums_row(A, to_row, head, !over);
       }
       *reinterpret_cast<u32x4*>(to_o + 4 * cl) = lds_read16(mem + x * 512 + (cl ^ x) * 16);
     }
@@ -1216,7 +1224,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       float* to_m = part + A.slot_rows * kHeadDim + 2 * (32 * wv + cl);
       if (kShared && !part) {
         const int64_t to_row = at_row(cl, head);
-        to_m = sums_scale(A, to_row, head);
+        to_m = sums_scale(A, to_row, head, !over);
       }
       *reinterpret_cast<f32x2*>(to_m) = f32x2{m, l};
     }
@@ -1246,9 +1254,9 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 // At most 16 rows go the narrow way.
 template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared>
 __device__ __forceinline__ void attend_tile(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
-                                            int n_kv, int r0, int h, int u0, int n, float* part, bool early) {
-  if (n_q * A.group - r0 <= 16) attend_rows<kF16, kCap, kBias, kPool, kShared, true>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part, early);
-  else attend_rows<kF16, kCap, kBias, kPool, kShared, false>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part, early);
+                                            int n_kv, int r0, int h, int u0, int n, float* part, bool over, bool early) {
+  if (n_q * A.group - r0 <= 16) attend_rows<kF16, kCap, kBias, kPool, kShared, true>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part, over, early);
+  else attend_rows<kF16, kCap, kBias, kPool, kShared, false>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part, over, early);
 }
 
 // The same for sequences of more than one tile alone, when those are few: floor(rows / 128) >= 1 then, and twice that is room
@@ -1258,11 +1266,11 @@ __device__ __forceinline__ int long_start(const AttendLaunch& A, int row0, int s
 }
 // The sequence of a tile numbered by long_start: 64-way bisection by a wave.
 template <bool kShared>
-__device__ __forceinline__ int tile_sequence(const AttendLaunch& A, int tile) {
-  int lo = 0, n = A.a.n_seqs;
+__device__ __forceinline__ int tile_sequence(const AttendLaunch& A, int tile, int n, bool over) {
+  int lo = 0;
   while (n > 1) {
     const int step = (n + 63) / 64, at = (int)(threadIdx.x & 63) * step;
-    const uint64_t in = __ballot(at < n && long_start(A, first_row<kShared>(A, lo + at), lo + at) <= tile);
+    const uint64_t in = __ballot(at < n && long_start(A, first_row<kShared>(A, lo + at, over), lo + at) <= tile);
     const int k = max(0, (int)__popcll(in) - 1) * step;
     lo += k;
     n = min(step, n - k);
@@ -1279,38 +1287,57 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendLaunch
   __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];   // [buffer][K, V]
   __shared__ Bounds bounds;
   const int place = blockIdx.x / A.p.n_kv_heads, h = blockIdx.x - place * A.p.n_kv_heads;
-  const bool brief = place < A.a.n_seqs;
-  const int tile = A.n_places - 1 - place, seq = brief ? place : uniform(tile_sequence<kShared>(A, tile));
-  const int row0 = uniform(first_row<kShared>(A, seq)), n_q = uniform(end_row<kShared>(A, seq)) - row0, n_rows = n_q * A.group;
+  const bool over = kShared && A.stage == kOverPrefix;
+  const int n_seqs = over ? A.g.n_groups : A.a.n_seqs;
+  const bool brief = place < n_seqs;
+  const int tile = A.n_places - 1 - place, seq = brief ? place : uniform(tile_sequence<kShared>(A, tile, n_seqs, over));
+  const int row0 = uniform(first_row<kShared>(A, seq, over)), n_q = uniform(first_row<kShared>(A, seq + 1, over)) - row0, n_rows = n_q * A.group;
   const int r0 = brief ? 0 : (tile - long_start(A, row0, seq)) * kRows;
   if ((n_rows <= kRows) != brief || r0 < 0 || r0 >= n_rows) return;
   bool early = false;
   if constexpr (kShared) {
-    if (A.stage == kOverPrefix)
-      early = __any(early_rows(A, min(max(A.cu_seqs[seq], 0), A.n_members), min(max(A.cu_seqs[seq + 1], 0), A.n_members), threadIdx.x & 63, 64));
+    if (over)
+      early = __any(early_rows(A, min(max(A.g.cu_seqs[seq], 0), A.a.n_seqs), min(max(A.g.cu_seqs[seq + 1], 0), A.a.n_seqs), threadIdx.x & 63, 64));
   }
-  attend_tile<kF16, kCap, kBias, kPool, kShared>(A, smem, bounds, seq, row0, n_q, uniform(slots_of(A, seq)), r0, h, 0, -1, nullptr, early);
+  attend_tile<kF16, kCap, kBias, kPool, kShared>(A, smem, bounds, seq, row0, n_q, uniform(slots_of<kShared>(A, seq, over)), r0, h, 0, -1, nullptr, over, early);
 }
 
-// The list of row tiles that every workgroup of attend_shares_kernel makes.
+// The list of row tiles that every workgroup of attend_shares_kernel makes: those of the groups over their prefixes, then those of
+// the sequences.
 struct List {
-  int32_t row0[kListed + 1];     // first row of each sequence
-  int32_t slots[kListed];        // of each sequence
+  int32_t row0[kListed + 2];     // first row of each group and behind the last, then of each sequence
+  int32_t slots[kListed];        // of each prefix, then of each sequence
   int32_t before[kListed + 1];   // key tiles of a head before row tile i
-  uint16_t seq[kListed];         // sequence of row tile i
+  uint16_t seq[kListed];         // group or sequence of row tile i
   int32_t wave[4];
-  int32_t early;                 // over the prefixes: whether some sequence has rows before its last prefix slot
+  int32_t early;                 // whether some sequence has rows before its last prefix slot
 };
 constexpr int kPer = kListed / 256;   // row tiles of a thread
+
+// Groups and sequences of a launch.
+template <bool kShared>
+__device__ __forceinline__ int groups_of(const AttendLaunch& A) { return kShared && A.stage != kOverOwn ? A.g.n_groups : 0; }
+template <bool kShared>
+__device__ __forceinline__ int seqs_of(const AttendLaunch& A) { return kShared && A.stage == kOverPrefix ? 0 : A.a.n_seqs; }
+// Where in row0 a group or sequence stands.
+__device__ __forceinline__ int row0_at(int groups, int s, bool over) { return over || !groups ? s : groups + 1 + s; }
 
 // Fills the list; the key tiles of a head, fewer than 2^31 (the host lets no other call here).
 template <bool kShared>
 __device__ __forceinline__ int make_list(const AttendLaunch& A, List& L) {
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = A.a.n_seqs;
-  for (int s = tid; s <= n; s += 256) L.row0[s] = first_row<kShared>(A, s);
-  for (int s = tid; s < n; s += 256) L.slots[s] = slots_of(A, s);
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, groups = groups_of<kShared>(A), seqs = seqs_of<kShared>(A);
   if constexpr (kShared) {
-    const bool early = A.stage == kOverPrefix && early_rows(A, 0, A.n_members, tid, 256);
+    if (groups) {
+      for (int s = tid; s <= groups; s += 256) L.row0[s] = first_row<kShared>(A, s, true);
+      for (int s = tid; s < groups; s += 256) L.slots[s] = slots_of<kShared>(A, s, true);
+    }
+  }
+  if (!kShared || seqs) {
+    for (int s = tid; s <= seqs; s += 256) L.row0[row0_at(groups, s, false)] = first_row<kShared>(A, s, false);
+    for (int s = tid; s < seqs; s += 256) L.slots[groups + s] = slots_of(A, s);
+  }
+  if constexpr (kShared) {
+    const bool early = groups && early_rows(A, 0, A.a.n_seqs, tid, 256);
     const int any = __syncthreads_or(early);
     if (tid == 0) L.early = any;
   }
@@ -1322,17 +1349,19 @@ __device__ __forceinline__ int make_list(const AttendLaunch& A, List& L) {
     const int tile = tid * kPer + i;
     cost[i] = 0;
     if (tile < A.n_tiles) {
-      int lo = 0, hi = n;
+      const bool over = kShared && tile < A.n_group_tiles;
+      const int at = over || !kShared ? tile : tile - A.n_group_tiles;
+      int lo = 0, hi = over ? groups : seqs;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (tile_start(A, L.row0[mid], mid) <= tile) lo = mid;
+        if (tile_start(A, L.row0[row0_at(groups, mid, over)], mid) <= at) lo = mid;
         else hi = mid;
       }
       L.seq[tile] = (uint16_t)lo;
-      const int n_q = L.row0[lo + 1] - L.row0[lo], r0 = (tile - tile_start(A, L.row0[lo], lo)) * kRows;
+      const int v = row0_at(groups, lo, over), n_q = L.row0[v + 1] - L.row0[v], r0 = (at - tile_start(A, L.row0[v], lo)) * kRows;
       if (r0 >= 0 && r0 < n_q * A.group) {
         int t0, t1;
-        tile_span<kShared>(A, lo, r0, n_q, L.slots[lo], t0, t1);
+        tile_span<kShared>(A, lo, r0, n_q, L.slots[over ? lo : groups + lo], over, t0, t1);
         cost[i] = max(1, t1 - t0);   // rows that see nothing are written too
       }
     }
@@ -1384,17 +1413,31 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
       else hi = mid;
     }
     const int tile = uniform(lo), seq = uniform(L.seq[tile]);
+    const bool over = kShared && tile < A.n_group_tiles;
+    const int groups = groups_of<kShared>(A), v = row0_at(groups, seq, over), at = over || !kShared ? tile : tile - A.n_group_tiles;
     const int u0 = rem - uniform(L.before[tile]), count = uniform(L.before[tile + 1]) - uniform(L.before[tile]);
     const int n = (int)min((int64_t)(count - u0), end - pos);
-    const int row0 = uniform(L.row0[seq]), n_q = uniform(L.row0[seq + 1]) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
+    const int row0 = uniform(L.row0[v]), n_q = uniform(L.row0[v + 1]) - row0, r0 = (at - tile_start(A, row0, seq)) * kRows;
     float* part = nullptr;
+    int parts = 0;
     if (n < count) {
       part = part_slot(A, 2 * w + (u0 == 0));
       if (u0 == 0) {
-        record = i32x4{(int)((pos + count - 1) / share) - w + 1 + 1024 * h, row0, r0, n_q * A.group};
+        parts = (int)((pos + count - 1) / share) - w + 1;
+        record = i32x4{parts + 1024 * h, row0, r0, n_q * A.group};
       }
     }
-    attend_tile<kF16, kCap, kBias, kPool, kShared>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, u0, n, part, kShared && L.early);
+    if constexpr (kShared) {
+      if (A.stage == kBoth && u0 == 0) {      // where the rows' sums are: in a record's place, or in parts from share w's second on
+        const int prefix = !over && has_prefix(A, seq) ? kHasPrefix : 0;
+        for (int r = r0 + tid; r < min(n_q * A.group, r0 + kRows); r += 256) {
+          const int t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
+          reinterpret_cast<i32x2*>(sums_scale(A, row0 + t, hq, !over))[1] = i32x2{parts | prefix, w | (r - r0) << 16};
+        }
+      }
+    }
+    attend_tile<kF16, kCap, kBias, kPool, kShared>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[over ? seq : groups + seq]), r0, h, u0, n, part,
+                                                   over, kShared && L.early);
     lds_sync();   // the memory that rows left by is the next tiles'
     pos += n;
   }
@@ -1505,10 +1548,89 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A
   }
 }
 
+// Rows whose sums over prefix and own slots one launch has made (kBoth): their parts, or the whole, of either, in the order of the keys, by
+// the two records of each row and head.  As above 8 rows a workgroup, or fewer with several groups of 32 lanes each.
+template <bool kF16>
+__global__ __launch_bounds__(kJoinThreads) void join_both_kernel(const AttendLaunch A) {
+  __shared__ f32x4 sO[8][32];
+  __shared__ float sM[8], sL[8];
+  const rkv_attend& a = A.a;
+  const int tid = threadIdx.x, grp = tid >> 5, c = tid & 31;
+  const int begin = first_row<true>(A, 0, false), stop = first_row<true>(A, a.n_seqs, false);
+  const int64_t first = (int64_t)begin * a.n_q_heads, total = (int64_t)stop * a.n_q_heads;      // rows of no sequence are not touched
+  int most = 8;
+  while (most > 1 && (total - first + most - 1) / most < kJoinGrid) most >>= 1;
+  const int each = 8 / most, i = grp / each, g = grp - i * each;
+  for (int64_t task = first + (int64_t)blockIdx.x * most; task < total; task += (int64_t)kJoinGrid * most) {
+    const int64_t id = task + i;
+    const bool in = id < total;
+    const int64_t row = (in ? id : task) / a.n_q_heads;
+    const int hq = (int)((in ? id : task) - row * a.n_q_heads);
+    const f32x4 own = *reinterpret_cast<const f32x4*>(sums_scale(A, row, hq, true));
+    const int own_word = __float_as_int(own[2]), own_parts = own_word & 1023;
+    f32x4 pre = {0.f, 0.f, 0.f, 0.f};
+    if (own_word & kHasPrefix) pre = *reinterpret_cast<const f32x4*>(sums_scale(A, row, hq));
+    const int pre_parts = __float_as_int(pre[2]) & 1023;
+    const int n_pre = own_word & kHasPrefix ? max(1, pre_parts) : 0, n = n_pre + max(1, own_parts);
+    float m = -__builtin_inff(), l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float m2, float l2, f32x4 v) {
+      const float top = fmaxf(m, m2), ref = top == -__builtin_inff() ? 0.f : top;
+      const float f = __builtin_amdgcn_exp2f(m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
+      m = top;
+      l = l * f + l2 * f2;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = acc[e] * f + v[e] * f2;
+    };
+    for (int j0 = g; j0 < n; j0 += 4 * each) {   // four parts in flight
+      f32x2 ml[4];
+      f32x4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int jj = min(j0 + j * each, n - 1);
+        const bool over = jj < n_pre;
+        const f32x4 rec = over ? pre : own;
+        const int k = over ? jj : jj - n_pre, where = __float_as_int(rec[3]);
+        const float *from_o = sums_row(A, row, hq, !over) + 4 * c, *from_m = sums_scale(A, row, hq, !over);
+        if (over ? pre_parts : own_parts) {      // cut to the workspace, whatever cu_seqs holds
+          const int share = min((where & 0xffff) + k, kShares - 1), at = min(where >> 16, A.slot_rows - 1);
+          const float* from = part_slot(A, k ? 2 * share : 2 * share + 1);
+          from_o = from + at * kHeadDim + 4 * c;
+          from_m = from + A.slot_rows * kHeadDim + 2 * at;
+        }
+        ml[j] = *reinterpret_cast<const f32x2*>(from_m);
+        v[j] = *reinterpret_cast<const f32x4*>(from_o);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j0 + j * each < n) add(ml[j][0], ml[j][1], v[j]);
+    }
+    __syncthreads();   // sO is free
+    sO[grp][c] = acc;
+    if (c == 0) {
+      sM[grp] = m;
+      sL[grp] = l;
+    }
+    __syncthreads();
+    if (!in || g) continue;
+    for (int x = 1; x < each; ++x) add(sM[grp + x], sL[grp + x], sO[grp + x][c]);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head + 4 * c;
+    *reinterpret_cast<u32x2*>(out) = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
+    if (a.lse && c == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
+  }
+}
+
 template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared>
 void launch_kernels(const AttendLaunch& A, hipStream_t st) {
   if (A.parts) {
     attend_shares_kernel<kF16, kCap, kBias, kPool, kShared><<<kShares, 256, 0, st>>>(A);
+    if constexpr (kShared) {
+      if (A.stage == kBoth) {
+        join_both_kernel<kF16><<<kJoinGrid, kJoinThreads, 0, st>>>(A);
+        return;
+      }
+    }
     join_kernel<kF16, kShared><<<kJoinGrid, kJoinThreads, 0, st>>>(A);
   } else {
     attend_tiles_kernel<kF16, kCap, kBias, kPool, kShared><<<(unsigned)(A.n_places * A.p.n_kv_heads), 256, 0, st>>>(A);

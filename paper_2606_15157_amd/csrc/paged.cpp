@@ -309,14 +309,25 @@ int check_shared(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
     return rkv::fail(RKV_ERR_UNSUPPORTED, "too many groups for one launch");
   return RKV_OK;
 }
-// The sums of every row, rounded up to where the shares' records may begin; then the workspace of either launch.
-size_t sums_bytes(const rkv_attend* a) {
-  return (sizeof(float) * (rkv::kHeadDim + 2) * (size_t)a->n_rows * (size_t)a->n_q_heads + 255) & ~size_t(255);
+// Whether one launch takes both: the rows of all sequences over the prefixes and those of each over its own slots in one list.  Few rows a
+// sequence cost more in launches than in sums of whole rows that go through memory.
+bool both_at_once(const rkv_pages* p, const rkv_attend* a, const rkv_attend* b) {
+  const int64_t own = row_tiles(p, a), over = row_tiles(p, b);
+  auto tiles = [&](int64_t pages) { return std::max<int64_t>(1, (pages * p->page_size + 63) / 64); };
+  return usual_rows(p, a) <= 64 && own + over <= rkv::kAttendListed && own * tiles(a->max_pages) + over * tiles(b->max_pages) < kIntEnd &&
+         p->n_kv_heads < (1 << 20);
+}
+size_t parts_bytes(int32_t rows) { return kRecordBytes + sizeof(float) * 2 * rkv::kAttendShares * (size_t)rows * (rkv::kHeadDim + 2); }
+// The sums of every row with their records, of one kind or both, rounded up to where the shares' records may begin; then the workspace of
+// the launches.
+size_t sums_bytes(const rkv_attend* a, bool both) {
+  return (sizeof(float) * (rkv::kHeadDim + 4) * (both ? 2 : 1) * (size_t)a->n_rows * (size_t)a->n_q_heads + 255) & ~size_t(255);
 }
 size_t shared_bytes(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
   const rkv_attend b = over_prefixes(a, g);
   if (nothing_to_do(a) || nothing_to_do(&b)) return attend_bytes(p, a);
-  return sums_bytes(a) + std::max(attend_bytes(p, a), attend_bytes(p, &b, true));
+  if (both_at_once(p, a, &b)) return sums_bytes(a, true) + parts_bytes(part_rows(p, &b, true));
+  return sums_bytes(a, false) + std::max(attend_bytes(p, a), attend_bytes(p, &b, true));
 }
 
 template <class Pages>
@@ -346,19 +357,32 @@ int attend_shared(const Pages* pages, const rkv_attend* a, const rkv_shared* g, 
     set_parts(L, attend_bytes(p, a), ws);
     return launched(pool.codes ? rkv::launch_attend8(L, stream) : rkv::launch_attend(L, stream));
   }
-  rkv::AttendLaunch G = attend_launch(pool, &b, true);
-  for (rkv::AttendLaunch* x : {&G, &L}) {
-    x->n_groups = g->n_groups;
-    x->n_members = a->n_seqs;
-    x->cu_seqs = g->cu_seqs;
-    x->own_lens = a->lens;
-    x->own_most = a->max_pages * p->page_size;
-    x->sums = static_cast<float*>(ws);
-    set_parts(*x, attend_bytes(p, &x->a, x == &G), static_cast<char*>(ws) + sums_bytes(a));
+  auto* launch = pool.codes ? rkv::launch_attend8_shared : rkv::launch_attend_shared;
+  const bool both = both_at_once(p, a, &b);
+  L.g = *g;
+  L.sums = static_cast<float*>(ws);
+  L.sum_records = L.sums + (both ? 2 : 1) * (size_t)a->n_rows * a->n_q_heads * rkv::kHeadDim;
+  char* rest = static_cast<char*>(ws) + sums_bytes(a, both);
+  if (both) {
+    L.stage = rkv::kBoth;
+    L.n_group_tiles = (int32_t)row_tiles(p, &b);
+    L.n_tiles += L.n_group_tiles;
+    L.slot_rows = part_rows(p, &b, true);
+    L.least = 1;
+    set_parts(L, parts_bytes(L.slot_rows), rest);
+    return launched(launch(L, stream));
   }
+  const rkv::AttendLaunch tiles = attend_launch(pool, &b, true);
+  rkv::AttendLaunch G = L;
+  G.n_tiles = G.n_group_tiles = tiles.n_tiles;
+  G.few_long = tiles.few_long;
+  G.n_places = tiles.n_places;
+  G.slot_rows = tiles.slot_rows;
+  G.least = tiles.least;
   G.stage = rkv::kOverPrefix;
   L.stage = rkv::kOverOwn;
-  auto* launch = pool.codes ? rkv::launch_attend8_shared : rkv::launch_attend_shared;
+  set_parts(G, attend_bytes(p, &b, true), rest);
+  set_parts(L, attend_bytes(p, a), rest);
   if (int st = launched(launch(G, stream))) return st;
   return launched(launch(L, stream));
 }

@@ -45,7 +45,9 @@ int launch_read8(const WriteLaunch& W, void* stream);
 constexpr int kAttendRows = 128;       // rows (tokens x query heads of a group) of a tile
 constexpr int kAttendShares = 512;     // workgroups that share the key tiles of a short list of row tiles: two a CU
 constexpr int kAttendListed = 1024;    // row tiles such a list may have
-enum { kAlone = 0, kOverPrefix = 1, kOverOwn = 2 };   // the launches of a call whose sequences share prefixes
+// The launches of a call whose sequences share prefixes: over the prefixes, and over the own slots from the sums of the first on; or over both, whose
+// sums a join brings together.
+enum { kAlone = 0, kOverPrefix = 1, kOverOwn = 2, kBoth = 3 };
 struct AttendLaunch {
   rkv_pages p;         // an 8-bit pool's strides are of its codes
   Scales ks, vs;
@@ -59,14 +61,13 @@ struct AttendLaunch {
   int32_t least;       // key tiles of a share, at least
   int32_t* records;    // [kAttendShares][4], then
   float* parts;        // [2 kAttendShares] partial sums; null: a workgroup per row tile
-  // Shared prefixes: over the prefixes a's sequences are the groups, and its rows those of their members; over the members' own
-  // slots, the sums go on from there.
+  // Shared prefixes.  Row tiles of the groups are those of all their sequences' rows; a launch has the tiles of the groups, of the
+  // sequences, or of both (the groups' first).
   int32_t stage;
-  int32_t n_groups, n_members;
-  const int32_t* cu_seqs;     // [n_groups + 1]
-  const int32_t* own_lens;    // the members' lens, at most own_most
-  int32_t own_most;
-  float* sums;                // [n_rows][Hq] sums over the prefixes
+  int32_t n_group_tiles;      // of n_tiles
+  rkv_shared g;
+  float* sums;                // [n_rows][Hq][128] over the prefixes, with kBoth then over the own slots
+  float* sum_records;         // [n_rows][Hq][4], likewise
 };
 // 16-bit and 8-bit pools, without and with shared prefixes.
 int launch_attend(const AttendLaunch& A, void* stream);
