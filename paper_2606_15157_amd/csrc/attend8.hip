@@ -1,8 +1,15 @@
-// Attention over pages (attend_rows.h): 8-bit pools.
-#include "attend_rows.h"
+// Attention over pages (attend_dealt.h): 8-bit pools.
+#include "attend_dealt.h"
 
 namespace rkv {
 
-int launch_attend8(const AttendLaunch& A, void* stream) { return launch_codes<false>(A, stream); }
+int launch_attend8(const AttendLaunch& A, void* stream) {
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  by_scores(A, [&](auto f16, auto cap, auto bias) {
+    if (dense_codes(A)) launch_dealt<f16.value, cap.value, bias.value, kCodes8, false>(A, st);
+    else launch_dealt<f16.value, cap.value, bias.value, kCodes, false>(A, st);
+  });
+  return (int)hipGetLastError();
+}
 
 }  // namespace rkv

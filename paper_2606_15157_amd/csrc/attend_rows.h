@@ -58,7 +58,6 @@ constexpr int kListed = kAttendListed;
 constexpr int kAhead = 11;                 // of a tile's 16 pairs of probabilities, those computed between the products of K
 constexpr int kTileBytes = kKeys * kHeadDim * 2;
 constexpr int64_t kStrideEnd = int64_t(1) << 31;   // page strides (elements) whose bytes 32 bits hold
-constexpr int kHasPrefix = 1 << 16;                // in a record of a row's own slots
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGrow = 8.f;               // log2 units a maximum may outgrow the reference by
 // Log2 units of the reference below the maximum it was set at.  Probabilities then reach 2^(kGrow + kUnder): fp16 holds 65504, and
@@ -226,6 +225,11 @@ __device__ __forceinline__ float* part_slot(const AttendLaunch& A, int slot) {
   return A.parts + (size_t)slot * A.slot_rows * (kHeadDim + 2);
 }
 
+// Those of at most 16 rows by waves, likewise, few_rows a slot.
+__device__ __forceinline__ float* few_slot(const AttendLaunch& A, int slot) {
+  return A.few_parts + (size_t)slot * A.few_rows * (kHeadDim + 2);
+}
+
 // Sums of whole rows between launches: 128 floats a row and head (not divided by l), and a record of m, l as above and two words (below).
 // Over the prefixes' first, those over the rows' own slots behind.
 __device__ __forceinline__ int64_t sums_at(const AttendLaunch& A, int64_t row, int hq, bool own) {
@@ -286,13 +290,14 @@ __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_floa
 // Probability 0 times what a hidden slot holds is no 0 if that is infinite or NaN.  A tile whose rows see different slots and
 // some of whose sums are not finite comes here (screening every tile of V instead cost packed documents 63 -> 80 us): if
 // no slot that only some of its rows see is to blame, the sums stand; else its rows are summed up one by one, a wave
-// each, two columns a lane, over the slots that they see and no others, and written: true.
-template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared>
+// each, two columns a lane, over the slots that they see and no others, and written: true.  kWave: a wave by itself, at most 16 rows.
+template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared, bool kWave>
 __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds& bounds, int seq, int row0, int n_q, int n_kv, int r0,
                                                   int h, int from, int to, int b_lo, int every_lo, int every_hi, int b_hi, float* part, bool over, bool go_on) {
   const rkv_attend& a = A.a;
   const rkv_pages& p = A.p;
-  const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wv = kWave ? 0 : uniform(threadIdx.x >> 6);
+  const int slot_rows = kWave ? A.few_rows : A.slot_rows;
   const int32_t* table = kShared && over ? A.g.table + seq * A.g.table_stride : a.table + seq * a.table_stride;
   const bool to_sums = kShared && (over || A.stage == kBoth);
   auto place = [&](int key, int& page, int& at) {
@@ -315,14 +320,14 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
   bool blame = false;
   for (int part_of = 0; part_of < 2; ++part_of) {
     const int k0 = max(from, part_of ? max(b_lo, every_hi) : b_lo), k1 = min(to, part_of ? b_hi : min(b_hi, every_lo));
-    for (int key = k0 + wv; key < k1; key += 4) {
+    for (int key = k0 + wv; key < k1; key += kWave ? 1 : 4) {
       int page, at;
       if (!place(key, page, at)) continue;
       const f32x2 v = v_pair(page, at);
       blame |= v[0] * 0.f + v[1] * 0.f != 0.f;
     }
   }
-  if (!any_wave(bounds, blame)) return false;
+  if (kWave ? !__any(blame) : !any_wave(bounds, blame)) return false;
   const int n_rows = n_q * A.group, prefix = !kShared && a.prefix_lens ? uniform(a.prefix_lens[seq]) : 0;
   const float cap2 = 2.f * kLog2e * a.softcap, in_cap = kCap ? 2.f * kLog2e * (a.scale / a.softcap) : 0.f;   // 1 / softcap may overflow
 #pragma unroll 1
@@ -368,7 +373,7 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
     }
     if (part || to_sums) {
       float* to_o = part ? part + mine * kHeadDim : sums_row(A, row, hq, !over);
-      float* to_m = part ? part + A.slot_rows * kHeadDim + 2 * mine : sums_scale(A, row, hq, !over);
+      float* to_m = part ? part + slot_rows * kHeadDim + 2 * mine : sums_scale(A, row, hq, !over);
       to_o[2 * lane] = o0;
       to_o[2 * lane + 1] = o1;
       to_m[0] = m;
@@ -384,18 +389,19 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
 
 // kCap: capped scores, kBias: less a slope times the distance; kShared: one of the two launches of a call whose sequences share
 // prefixes.  Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
-// partial sums go, null: the rows are finished (over the prefixes, their sums are).
-template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared, bool kNarrow>
+// partial sums go, null: the rows are finished (over the prefixes, their sums are).  kNarrow: at most 16 rows; kWave: those by one wave, which
+// neither waits for another nor touches LDS.
+template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared, bool kNarrow, bool kWave = false>
 __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char* smem, Bounds& bounds, int seq, int row0, int n_q,
                                             int n_kv, int r0, int h, int u0, int n, float* part, bool over, bool early) {
-  constexpr bool kPage16 = kPool == kPages16, kQuant = in_codes(kPool);
+  constexpr bool kPage16 = kPool == kPages16, kQuant = in_codes(kPool), kInRegisters = kNarrow && (kQuant || kWave);
   const rkv_attend& a = A.a;
   const rkv_pages& p = A.p;
   const bool to_sums = kShared && (over || A.stage == kBoth);
   const bool go_on = kShared && A.stage == kOverOwn && u0 == 0 && has_prefix(A, seq);      // from the rows' sums over the prefix
   int lane = threadIdx.x & 63;
   if constexpr (kNarrow) asm volatile("" : "+v"(lane));   // its addresses are not kept from one item to the next
-  const int wv = uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  const int wv = kWave ? 0 : uniform(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   const int n_rows = n_q * A.group;
 
   // The slots a position sees, and a row's position.  Both bounds ascend with the row, so that those of the tile and of the
@@ -547,7 +553,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     }
     fetch(tl, x, vp, v4, p.v_page, v_slot, v_off, (2 + buf) * kTileBytes);
   };
-  if constexpr (kPool == kAnyPages) {
+  if constexpr (kPool == kAnyPages && !kInRegisters) {
     if (t0 < t1) {
       look(t0);
       wait_vmcnt<0>();
@@ -579,117 +585,129 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     // ahead, and waits for no other: 16x16x32 and 16x16x16 MFMA, a lane holds keys 4 (lane / 16) + 0..3 of row lane % 16.
     const int l16 = lane & 15, lg = lane >> 4;
     f32x4 o[8] = {};
-    if constexpr (kQuant) {
-      // Codes go from memory to registers alone.  A wave takes 32 keys at a time, every fourth 32 of the item's; eight keys of a quarter are the
-      // ones whose probabilities a lane will hold, as the products with V take them.
-      //   K: lane (l16, lg) takes codes 16 lg .. and 64 + 16 lg .. of keys 8 (l16 / 4) + l16 % 4 and 4 further: of either 16 keys, one column
-      //      of 16x16x32 a lane, the sum over the row's 128 in the order that the lanes hold them, as q does.  Scores of keys 8 lg + 0..7 come out.
-      //   V: lane (l16, lg) takes codes 8 l16 + 0..7 of keys 8 lg + 0..7: a column of V^T for each of eight products once pairs of keys are
+    if constexpr (kInRegisters) {
+      // Keys go from memory to registers alone.  A wave takes a block of 32 (16-bit rows: 16) at a time, every fourth one of the item's (kWave:
+      // all of them); the eight (four) keys of a quarter are the ones whose probabilities a lane will hold, as the products with V take them.
+      //   K: lane (l16, lg) takes 16 bytes of each 64 of keys 8 (l16 / 4) + l16 % 4 and 4 further (16-bit rows: of key l16): of either 16 keys, one
+      //      column of 16x16x32 a lane, the sum over the row's 128 in the order that the lanes hold them, as q does.  Scores of keys 8 lg + 0..7 come out.
+      //   V: lane (l16, lg) takes values 8 l16 + 0..7 of keys 8 lg + 0..7: a column of V^T for each of eight products once pairs of keys are
       //      put together.  Output 32 lg + 8 i + d of row l16 is o[d][i].
-      // The next block of either is requested as soon as the registers are free: two are in flight.
-      constexpr bool kDense = kPool == kCodes8;
+      // The next block of either is requested as soon as the registers are free: two are in flight, 16 KiB a wave.
+      constexpr bool kDense = kPool == kCodes8 || kPool == kPages16;
+      constexpr int kBlock = kQuant ? 32 : 16, kSets = kBlock / 16, kEach = kBlock / 4, kStep = kWave ? kBlock : 4 * kBlock;
       struct Block {
-        u32x4 k[4];          // [16 keys][half of the row]
-        u32x2 v[8];
-        uint32_t ks[2], vs[8];     // kDense: two words of eight bytes
+        u32x4 k[4];                   // [16 keys][64 bytes of the row]
+        u32x2 v[kEach][kBytes];
+        uint32_t ks[2], vs[8];        // kDense: two words of eight bytes
         int key0;
-        bool k_in, v_in;     // kDense: whether this lane's eight keys have a page
+        bool k_in, v_in;              // kDense: whether this lane's keys have a page
       };
-      // Where a lane's rows of 32 keys lie: of its eight of K and of V (kDense; a page that is none: slots that there are, hidden later),
+      // Where a lane's rows of a block lie: of its eight of K and of V (kDense; a page that is none: slots that there are, hidden later),
       // or of each.
       struct Places {
-        int k[kDense ? 1 : 2], v[kDense ? 1 : 8], k_at, v_at;
+        int k[kDense ? 1 : kSets], v[kDense ? 1 : kEach], k_at, v_at;
       };
-      const int kg = 8 * (l16 >> 2), k_first = kg + (l16 & 3);
+      const int kg = kEach * (l16 >> 2), k_first = kg + (l16 & 3);
       const uint8_t* k_scales = A.ks.at + h * A.ks.head;
       const uint8_t* v_scales = A.vs.at + h * A.vs.head;
-      const char* k_lane = kp + (l16 & 3) * p.k_slot + 16 * lg;      // kDense
-      const char* v_lane = vp + 8 * l16;
+      const int64_t k_slot = p.k_slot * kBytes, v_slot = p.v_slot * kBytes, k_page = p.k_page * kBytes, v_page = p.v_page * kBytes;
+      const char* k_lane = kp + (l16 & 3) * k_slot + 16 * lg;      // kDense
+      const char* v_lane = vp + 8 * kBytes * l16;
       const int end = t1 * kKeys;
-      auto look32 = [&](int key0, Places& x) __attribute__((always_inline)) {      // keys that no row sees are taken for ones that some do
+      auto look_up = [&](int key0, Places& x) __attribute__((always_inline)) {      // keys that no row sees are taken for ones that some do
         if constexpr (kDense) {
           auto place = [&](int key, int& page, int& at) {
-            const int c = div_by(min(max(key + 7, b_lo), b_hi - 1), A.by_page);
+            const int c = div_by(min(max(key + kEach - 1, b_lo), b_hi - 1), A.by_page);
             page = table[c];
             at = key - c * p.page_size;
           };
           place(key0 + kg, x.k[0], x.k_at);
-          place(key0 + 8 * lg, x.v[0], x.v_at);
+          place(key0 + kEach * lg, x.v[0], x.v_at);
         } else {
           auto page_of = [&](int key) { return table[div_by(min(max(key, b_lo), b_hi - 1), A.by_page)]; };
 #pragma unroll
-          for (int i = 0; i < 2; ++i) x.k[i] = page_of(key0 + k_first + 4 * i);
+          for (int i = 0; i < kSets; ++i) x.k[i] = page_of(key0 + k_first + 4 * i);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x.v[i] = page_of(key0 + 8 * lg + i);
+          for (int i = 0; i < kEach; ++i) x.v[i] = page_of(key0 + kEach * lg + i);
         }
       };
-      // Whether some of eight keys from `key` on is visible to some row, and their page is one.
-      auto held8 = [&](int key, int page) { return key + 8 > b_lo && key < min(b_hi, end) && (uint32_t)page < (uint32_t)p.n_pages; };
-      auto far_by = [](auto* from, int n, int64_t stride) { return from + (uint64_t)(uint32_t)n * (uint32_t)stride; };      // both below 2^31
+      // Whether some of this lane's keys from `key` on is visible to some row, and their page is one.
+      auto held = [&](int key, int page) { return key + kEach > b_lo && key < min(b_hi, end) && (uint32_t)page < (uint32_t)p.n_pages; };
+      auto far_by = [](auto* from, int n, int64_t stride) { return from + (uint64_t)(uint32_t)n * (uint32_t)stride; };      // both below 2^32
       auto load_k = [&](int key0, const Places& at, Block& x) __attribute__((always_inline)) {
         const char* row = nullptr;
         if constexpr (kDense) {
-          x.k_in = held8(key0 + kg, at.k[0]);
+          x.k_in = held(key0 + kg, at.k[0]);
           const int page = x.k_in ? at.k[0] : 0, slot = x.k_in ? at.k_at : 0;
-          const u32x2 bytes = *reinterpret_cast<const u32x2*>(far_by(k_scales, page, A.ks.page) + slot);
-          x.ks[0] = bytes[0];
-          x.ks[1] = bytes[1];
-          row = far_by(far_by(k_lane, page, p.k_page), slot, p.k_slot);
+          if constexpr (kQuant) {
+            const u32x2 bytes = *reinterpret_cast<const u32x2*>(far_by(k_scales, page, A.ks.page) + slot);
+            x.ks[0] = bytes[0];
+            x.ks[1] = bytes[1];
+          }
+          row = far_by(far_by(k_lane, page, k_page), slot, k_slot);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kSets; ++i) {
           if constexpr (!kDense) {
             const int key = key0 + k_first + 4 * i;
             const bool in = key >= b_lo && key < b_hi && key < end && (uint32_t)at.k[i] < (uint32_t)p.n_pages;
             const int slot = key - div_by(in ? key : 0, A.by_page) * p.page_size;
-            row = (in ? kp + at.k[i] * p.k_page + slot * p.k_slot : zeros) + 16 * lg;
-            x.ks[i] = *(in ? k_scales + at.k[i] * A.ks.page + slot * A.ks.slot : reinterpret_cast<const uint8_t*>(zeros));
+            row = (in ? kp + at.k[i] * k_page + slot * k_slot : zeros) + 16 * lg;
+            if constexpr (kQuant) x.ks[i] = *(in ? k_scales + at.k[i] * A.ks.page + slot * A.ks.slot : reinterpret_cast<const uint8_t*>(zeros));
           }
-          x.k[2 * i] = *reinterpret_cast<const u32x4*>(row);
-          x.k[2 * i + 1] = *reinterpret_cast<const u32x4*>(row + 64);
-          if constexpr (kDense) row += 4 * p.k_slot;
+#pragma unroll
+          for (int j = 0; j < 2 * kBytes; ++j) x.k[2 * kBytes * i + j] = *reinterpret_cast<const u32x4*>(row + 64 * j);
+          if constexpr (kDense) row += 4 * k_slot;
         }
       };
       auto load_v = [&](int key0, const Places& at, Block& x) __attribute__((always_inline)) {
         const char* row = nullptr;
         x.key0 = key0;
         if constexpr (kDense) {
-          x.v_in = held8(key0 + 8 * lg, at.v[0]);
+          x.v_in = held(key0 + kEach * lg, at.v[0]);
           const int page = x.v_in ? at.v[0] : 0, slot = x.v_in ? at.v_at : 0;
-          const u32x2 bytes = *reinterpret_cast<const u32x2*>(far_by(v_scales, page, A.vs.page) + slot);
-          x.vs[0] = bytes[0];
-          x.vs[1] = bytes[1];
-          row = far_by(far_by(v_lane, page, p.v_page), slot, p.v_slot);
+          if constexpr (kQuant) {
+            const u32x2 bytes = *reinterpret_cast<const u32x2*>(far_by(v_scales, page, A.vs.page) + slot);
+            x.vs[0] = bytes[0];
+            x.vs[1] = bytes[1];
+          }
+          row = far_by(far_by(v_lane, page, v_page), slot, v_slot);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kEach; ++i) {
           if constexpr (!kDense) {
-            const int key = key0 + 8 * lg + i;
+            const int key = key0 + kEach * lg + i;
             const bool in = key >= b_lo && key < b_hi && key < end && (uint32_t)at.v[i] < (uint32_t)p.n_pages;
             const int slot = key - div_by(in ? key : 0, A.by_page) * p.page_size;
-            row = (in ? vp + at.v[i] * p.v_page + slot * p.v_slot : zeros) + 8 * l16;
-            x.vs[i] = *(in ? v_scales + at.v[i] * A.vs.page + slot * A.vs.slot : reinterpret_cast<const uint8_t*>(zeros));
+            row = (in ? vp + at.v[i] * v_page + slot * v_slot : zeros) + 8 * kBytes * l16;
+            if constexpr (kQuant) x.vs[i] = *(in ? v_scales + at.v[i] * A.vs.page + slot * A.vs.slot : reinterpret_cast<const uint8_t*>(zeros));
           }
-          x.v[i] = *reinterpret_cast<const u32x2*>(row);
-          if constexpr (kDense) row += p.v_slot;
+          if constexpr (kQuant) {
+            x.v[i][0] = *reinterpret_cast<const u32x2*>(row);
+          } else {
+            const u32x4 y = *reinterpret_cast<const u32x4*>(row);
+            x.v[i][0] = u32x2{y[0], y[1]};
+            x.v[i][kBytes - 1] = u32x2{y[2], y[3]};
+          }
+          if constexpr (kDense) row += v_slot;
         }
       };
-      const int first = t0 * kKeys + 32 * wv;
+      const int first = t0 * kKeys + kBlock * wv;
       Block x0, x1;
       Places ids0, ids1;
       u32x4 q[4];
       if (t0 < t1) {
-        look32(first, ids0);
-        look32(first + 128, ids1);
+        look_up(first, ids0);
+        look_up(first + kStep, ids1);
         load_k(first, ids0, x0);
         load_v(first, ids0, x0);
-        look32(first + 256, ids0);
-        load_k(first + 128, ids1, x1);
-        load_v(first + 128, ids1, x1);
+        look_up(first + 2 * kStep, ids0);
+        load_k(first + kStep, ids1, x1);
+        load_v(first + kStep, ids1, x1);
       }
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        q[s] = *reinterpret_cast<const u32x4*>(qrow + 64 * (s >> 1) + 16 * lg + 8 * (s & 1));
+        q[s] = *reinterpret_cast<const u32x4*>(qrow + (kQuant ? 64 * (s >> 1) + 16 * lg + 8 * (s & 1) : 32 * s + 8 * lg));
         if (a.scale < 0.f) q[s] ^= 0x80008000u;
       }
       if (kShared && go_on && wv == 0) {      // the first wave's sums begin with the prefix's
@@ -706,46 +724,51 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
             for (int d = 0; d < 4; ++d) o[4 * u + d][i] = y[d];
           }
       }
-      // 32 keys; ids: where the block lies that is requested in their place, next: the one after.
+      // A block; ids: where the block lies that is requested in their place, next: the one after.
       auto step = [&](Block& b, Places& ids, Places& next) __attribute__((always_inline)) {
         const int key0 = b.key0;
-        const bool whole = key0 >= b_lo && key0 + 32 <= b_hi && key0 + 32 <= end;
-        look32(key0 + 384, next);
+        const bool whole = key0 >= b_lo && key0 + kBlock <= min(b_hi, end);
+        look_up(key0 + 3 * kStep, next);
         float scale[8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) scale[i] = scale_of(kDense ? (b.ks[i] >> (8 * (l16 & 3))) & 255u : b.ks[i]);
+        for (int i = 0; i < kSets; ++i) scale[i] = !kQuant ? 1.f : scale_of(kDense ? (b.ks[i] >> (8 * (l16 & 3))) & 255u : b.ks[i]);
         if constexpr (kDense) {
           if (!whole || __any(!b.k_in)) {      // slots outside read as zeros, codes and scales
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < kSets; ++i) {
               const int key = key0 + k_first + 4 * i;
               if (!b.k_in || key < b_lo || key >= b_hi) {
-                b.k[2 * i] = b.k[2 * i + 1] = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < 2 * kBytes; ++j) b.k[2 * kBytes * i + j] = u32x4{0, 0, 0, 0};
                 scale[i] = 0.f;
               }
             }
           }
         }
-        f32x4 s[2];
+        f32x4 s[kSets];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kSets; ++i) {
           s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int u = 0; u < 4; ++u)
-            s[i] = mma16<kF16>(widen8<kF16>(b.k[2 * i + (u >> 1)][2 * (u & 1)], b.k[2 * i + (u >> 1)][2 * (u & 1) + 1], scale[i]), q[u], s[i]);
+            if constexpr (kQuant)
+              s[i] = mma16<kF16>(widen8<kF16>(b.k[2 * i + (u >> 1)][2 * (u & 1)], b.k[2 * i + (u >> 1)][2 * (u & 1) + 1], scale[i]), q[u], s[i]);
+            else s[i] = mma16<kF16>(b.k[u], q[u], s[i]);
         }
-        load_k(key0 + 256, ids, b);
-        const float far = (float)(pos - key0 - 8 * lg);
-        float x[8];
+        load_k(key0 + 2 * kStep, ids, b);
+        const float far = (float)(pos - key0 - kEach * lg);
+        float x[kEach];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = score(s[i >> 2][i & 3], i, far);
-        if (key0 < all_lo || key0 + 32 > all_hi) {
-          const int from = lo - key0 - 8 * lg, to = hi - key0 - 8 * lg;
+        for (int i = 0; i < kEach; ++i) x[i] = score(s[i >> 2][i & 3], i, far);
+        if (key0 < all_lo || key0 + kBlock > all_hi) {
+          const int from = lo - key0 - kEach * lg, to = hi - key0 - kEach * lg;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < kEach; ++i)
             if (i < from || i >= to) x[i] = -__builtin_inff();
         }
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < kEach; ++i) top = fmaxf(top, x[i]);
         top = fmaf(top, grow, base);
         if (__any(top > m + kGrow)) {   // the row's, over its four lanes
           top = fmaxf(top, __shfl_xor(top, 16));
@@ -760,46 +783,88 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
             for (int i = 0; i < 4; ++i) o[d][i] *= f;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kEach; ++i) {
           x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], grow, base - ref));
           l += x[i];
         }
-        const u32x4 pr = {pack<kF16>(x[0], x[1]), pack<kF16>(x[2], x[3]), pack<kF16>(x[4], x[5]), pack<kF16>(x[6], x[7])};
+        uint32_t pr[kEach / 2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) scale[i] = scale_of(kDense ? (b.vs[i >> 2] >> (8 * (i & 3))) & 255u : b.vs[i]);
+        for (int i = 0; i < kEach / 2; ++i) pr[i] = pack<kF16>(x[2 * i], x[2 * i + 1]);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) scale[i] = !kQuant ? 1.f : scale_of(kDense ? (b.vs[i >> 2] >> (8 * (i & 3))) & 255u : b.vs[i]);
         if constexpr (kDense) {
           if (!whole || __any(!b.v_in)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int key = key0 + 8 * lg + i;
+            for (int i = 0; i < kEach; ++i) {
+              const int key = key0 + kEach * lg + i;
               if (!b.v_in || key < b_lo || key >= b_hi) {
-                b.v[i] = u32x2{0, 0};
+                b.v[i][0] = b.v[i][kBytes - 1] = u32x2{0, 0};
                 scale[i] = 0.f;
               }
             }
           }
         }
-        u32x4 w[8];
+        u32x4 w[kEach];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = widen8<kF16>(b.v[i][0], b.v[i][1], scale[i]);
-        load_v(key0 + 256, ids, b);
+        for (int i = 0; i < kEach; ++i) {
+          if constexpr (kQuant) w[i] = widen8<kF16>(b.v[i][0][0], b.v[i][0][1], scale[i]);
+          else w[i] = u32x4{b.v[i][0][0], b.v[i][0][1], b.v[i][kBytes - 1][0], b.v[i][kBytes - 1][1]};
+        }
+        load_v(key0 + 2 * kStep, ids, b);
 #pragma unroll
         for (int d = 0; d < 8; ++d) {
           const uint32_t halves = d & 1 ? 0x07060302u : 0x05040100u;     // of two keys' words: the lower, or the upper, 16 bits
-          u32x4 vt;
+          uint32_t vt[kEach / 2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) vt[i] = __builtin_amdgcn_perm(w[2 * i + 1][d >> 1], w[2 * i][d >> 1], halves);
-          o[d] = mma16<kF16>(vt, pr, o[d]);
+          for (int i = 0; i < kEach / 2; ++i) vt[i] = __builtin_amdgcn_perm(w[2 * i + 1][d >> 1], w[2 * i][d >> 1], halves);
+          if constexpr (kQuant)
+            o[d] = mma16<kF16>(u32x4{vt[0], vt[1], vt[kEach / 2 - 2], vt[kEach / 2 - 1]}, u32x4{pr[0], pr[1], pr[kEach / 2 - 2], pr[kEach / 2 - 1]}, o[d]);
+          else o[d] = mma16s<kF16>(u32x2{vt[0], vt[1]}, u32x2{pr[0], pr[1]}, o[d]);
         }
       };
       if (first < end) {
 #pragma unroll 1
-        for (int key0 = first;; key0 += 256) {
+        for (int key0 = first;; key0 += 2 * kStep) {
           step(x0, ids0, ids1);
-          if (key0 + 128 >= end) break;
+          if (key0 + kStep >= end) break;
           step(x1, ids1, ids0);
-          if (key0 + 256 >= end) break;
+          if (key0 + 2 * kStep >= end) break;
         }
+      }
+      if constexpr (kWave) {      // the rows leave from where they are, 32 columns a lane
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (b_lo != every_lo || b_hi != every_hi) {
+          float finite = 0.f;
+#pragma unroll
+          for (int d = 0; d < 8; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) finite = fmaf(o[d][i], 0.f, finite);
+          if (__any(finite != 0.f) &&   // NaN
+              attend_row_by_row<kF16, kCap, kBias, kPool, kShared, true>(A, bounds, seq, row0, n_q, n_kv, r0, h, t0 * kKeys, t1 * kKeys, b_lo, every_lo,
+                                                                         every_hi, b_hi, part, over, go_on))
+            return;
+        }
+        if (r0 + l16 >= n_rows) return;
+        m -= kUnder<kF16>;   // what the sums are relative to
+        if (part || to_sums) {
+          float* to = (part ? part + l16 * kHeadDim : sums_row(A, row, hq, !over)) + 32 * lg;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              *reinterpret_cast<f32x4*>(to + 8 * i + 4 * u) = f32x4{o[4 * u][i], o[4 * u + 1][i], o[4 * u + 2][i], o[4 * u + 3][i]};
+          if (lg == 0) *reinterpret_cast<f32x2*>(part ? part + A.few_rows * kHeadDim + 2 * l16 : sums_scale(A, row, hq, !over)) = f32x2{m, l};
+          return;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        uint16_t* to = static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head + 32 * lg;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<u32x4*>(to + 8 * i) = u32x4{pack<kF16>(o[0][i] * inv, o[1][i] * inv), pack<kF16>(o[2][i] * inv, o[3][i] * inv),
+                                                       pack<kF16>(o[4][i] * inv, o[5][i] * inv), pack<kF16>(o[6][i] * inv, o[7][i] * inv)};
+        if (a.lse && lg == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
+        return;
       }
       const uint32_t meet = lds + wv * 8192 + l16 * 512;     // the end as below, a wave's sums in one piece
 #pragma unroll
@@ -900,7 +965,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 #pragma unroll
     for (int d = 0; d < 8; ++d)
       *(__attribute__((address_space(3))) f32x4*)(uintptr_t)(k_at + (d >> 2) * kTileBytes + ((4 * (d & 3) + lg) ^ l16) * 16) = o[d];
-    }   // !kQuant
+    }   // !kInRegisters
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (lg == 0) *(__attribute__((address_space(3))) f32x2*)(uintptr_t)(lds + 2 * kTileBytes + wv * 4096 + l16 * 8) = f32x2{m, l};
@@ -920,7 +985,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       ll = fmaf(ml[w][1], f, ll);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint32_t at = kQuant ? w * 8192 + x * 512 + ((2 * c + u) ^ x) * 16 : (c >> 3) * kTileBytes + w * 4096 + x * 256 + ((2 * (c & 7) + u) ^ x) * 16;
+        const uint32_t at = kInRegisters ? w * 8192 + x * 512 + ((2 * c + u) ^ x) * 16 : (c >> 3) * kTileBytes + w * 4096 + x * 256 + ((2 * (c & 7) + u) ^ x) * 16;
         const f32x4 v = *(const __attribute__((address_space(3))) f32x4*)(uintptr_t)(lds + at);
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[4 * u + i] = fmaf(v[i], f, sum[4 * u + i]);
@@ -932,7 +997,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 #pragma unroll
       for (int i = 0; i < 8; ++i) finite = fmaf(sum[i], 0.f, finite);
       if (any_wave(bounds, finite != 0.f) &&   // NaN
-          attend_row_by_row<kF16, kCap, kBias, kPool, kShared>(A, bounds, seq, row0, n_q, n_kv, r0, h, t0 * kKeys, t1 * kKeys, b_lo, every_lo,
+          attend_row_by_row<kF16, kCap, kBias, kPool, kShared, false>(A, bounds, seq, row0, n_q, n_kv, r0, h, t0 * kKeys, t1 * kKeys, b_lo, every_lo,
                                                                every_hi, b_hi, part, over, go_on))
         return;
     }
@@ -1184,7 +1249,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 #pragma unroll
       for (int i = 0; i < 16; ++i) finite = fmaf(o[d][i], 0.f, finite);
     if (any_wave(bounds, finite != 0.f) &&   // NaN
-        attend_row_by_row<kF16, kCap, kBias, kPool, kShared>(A, bounds, seq, row0, n_q, n_kv, r0, h, t0 * kKeys, t1 * kKeys, b_lo, every_lo, every_hi,
+        attend_row_by_row<kF16, kCap, kBias, kPool, kShared, false>(A, bounds, seq, row0, n_q, n_kv, r0, h, t0 * kKeys, t1 * kKeys, b_lo, every_lo, every_hi,
                                                              b_hi, part, over, go_on))
       return;
   }
@@ -1302,45 +1367,21 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttendLaunch
   attend_tile<kF16, kCap, kBias, kPool, kShared>(A, smem, bounds, seq, row0, n_q, uniform(slots_of<kShared>(A, seq, over)), r0, h, 0, -1, nullptr, over, early);
 }
 
-// The list of row tiles that every workgroup of attend_shares_kernel makes: those of the groups over their prefixes, then those of
-// the sequences.
+// The list of row tiles that every workgroup of attend_shares_kernel makes.
 struct List {
-  int32_t row0[kListed + 2];     // first row of each group and behind the last, then of each sequence
-  int32_t slots[kListed];        // of each prefix, then of each sequence
+  int32_t row0[kListed + 1];     // first row of each sequence
+  int32_t slots[kListed];        // of each sequence
   int32_t before[kListed + 1];   // key tiles of a head before row tile i
-  uint16_t seq[kListed];         // group or sequence of row tile i
+  uint16_t seq[kListed];         // sequence of row tile i
   int32_t wave[4];
-  int32_t early;                 // whether some sequence has rows before its last prefix slot
 };
 constexpr int kPer = kListed / 256;   // row tiles of a thread
 
-// Groups and sequences of a launch.
-template <bool kShared>
-__device__ __forceinline__ int groups_of(const AttendLaunch& A) { return kShared && A.stage != kOverOwn ? A.g.n_groups : 0; }
-template <bool kShared>
-__device__ __forceinline__ int seqs_of(const AttendLaunch& A) { return kShared && A.stage == kOverPrefix ? 0 : A.a.n_seqs; }
-// Where in row0 a group or sequence stands.
-__device__ __forceinline__ int row0_at(int groups, int s, bool over) { return over || !groups ? s : groups + 1 + s; }
-
 // Fills the list; the key tiles of a head, fewer than 2^31 (the host lets no other call here).
-template <bool kShared>
 __device__ __forceinline__ int make_list(const AttendLaunch& A, List& L) {
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, groups = groups_of<kShared>(A), seqs = seqs_of<kShared>(A);
-  if constexpr (kShared) {
-    if (groups) {
-      for (int s = tid; s <= groups; s += 256) L.row0[s] = first_row<kShared>(A, s, true);
-      for (int s = tid; s < groups; s += 256) L.slots[s] = slots_of<kShared>(A, s, true);
-    }
-  }
-  if (!kShared || seqs) {
-    for (int s = tid; s <= seqs; s += 256) L.row0[row0_at(groups, s, false)] = first_row<kShared>(A, s, false);
-    for (int s = tid; s < seqs; s += 256) L.slots[groups + s] = slots_of(A, s);
-  }
-  if constexpr (kShared) {
-    const bool early = groups && early_rows(A, 0, A.a.n_seqs, tid, 256);
-    const int any = __syncthreads_or(early);
-    if (tid == 0) L.early = any;
-  }
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = A.a.n_seqs;
+  for (int s = tid; s <= n; s += 256) L.row0[s] = first_row<false>(A, s, false);
+  for (int s = tid; s < n; s += 256) L.slots[s] = slots_of(A, s);
   __syncthreads();
   int cost[kPer];
   int sum = 0;
@@ -1349,19 +1390,17 @@ __device__ __forceinline__ int make_list(const AttendLaunch& A, List& L) {
     const int tile = tid * kPer + i;
     cost[i] = 0;
     if (tile < A.n_tiles) {
-      const bool over = kShared && tile < A.n_group_tiles;
-      const int at = over || !kShared ? tile : tile - A.n_group_tiles;
-      int lo = 0, hi = over ? groups : seqs;
+      int lo = 0, hi = n;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (tile_start(A, L.row0[row0_at(groups, mid, over)], mid) <= at) lo = mid;
+        if (tile_start(A, L.row0[mid], mid) <= tile) lo = mid;
         else hi = mid;
       }
       L.seq[tile] = (uint16_t)lo;
-      const int v = row0_at(groups, lo, over), n_q = L.row0[v + 1] - L.row0[v], r0 = (at - tile_start(A, L.row0[v], lo)) * kRows;
+      const int n_q = L.row0[lo + 1] - L.row0[lo], r0 = (tile - tile_start(A, L.row0[lo], lo)) * kRows;
       if (r0 >= 0 && r0 < n_q * A.group) {
         int t0, t1;
-        tile_span<kShared>(A, lo, r0, n_q, L.slots[over ? lo : groups + lo], over, t0, t1);
+        tile_span<false>(A, lo, r0, n_q, L.slots[lo], false, t0, t1);
         cost[i] = max(1, t1 - t0);   // rows that see nothing are written too
       }
     }
@@ -1391,13 +1430,13 @@ __device__ __forceinline__ int make_list(const AttendLaunch& A, List& L) {
 // kShares workgroups with an equal share each of all items' key tiles, in the order (head, row tile, key tile).  Workgroup b
 // runs on XCD b % 8: it takes share (b % 8) kShares / 8 + b / 8, so that the row tiles of a head, which read the same
 // keys, meet in one L2.
-template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared>
+template <bool kF16, bool kCap, bool kBias, Pool kPool>
 __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunch A) {
   __shared__ __align__(1024) unsigned char smem[4 * kTileBytes];
   __shared__ Bounds bounds;
   __shared__ List L;
   const int tid = threadIdx.x;
-  const int all = make_list<kShared>(A, L);
+  const int all = make_list(A, L);
   const int w = (int)(blockIdx.x % 8) * (kShares / 8) + (int)blockIdx.x / 8;
   i32x4 record = {0, 0, 0, 0};   // parts + 1024 head, sequence's first row, first row of the tile, rows of the sequence
   const int64_t total = (int64_t)all * A.p.n_kv_heads;
@@ -1413,31 +1452,17 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
       else hi = mid;
     }
     const int tile = uniform(lo), seq = uniform(L.seq[tile]);
-    const bool over = kShared && tile < A.n_group_tiles;
-    const int groups = groups_of<kShared>(A), v = row0_at(groups, seq, over), at = over || !kShared ? tile : tile - A.n_group_tiles;
     const int u0 = rem - uniform(L.before[tile]), count = uniform(L.before[tile + 1]) - uniform(L.before[tile]);
     const int n = (int)min((int64_t)(count - u0), end - pos);
-    const int row0 = uniform(L.row0[v]), n_q = uniform(L.row0[v + 1]) - row0, r0 = (at - tile_start(A, row0, seq)) * kRows;
+    const int row0 = uniform(L.row0[seq]), n_q = uniform(L.row0[seq + 1]) - row0, r0 = (tile - tile_start(A, row0, seq)) * kRows;
     float* part = nullptr;
-    int parts = 0;
     if (n < count) {
       part = part_slot(A, 2 * w + (u0 == 0));
       if (u0 == 0) {
-        parts = (int)((pos + count - 1) / share) - w + 1;
-        record = i32x4{parts + 1024 * h, row0, r0, n_q * A.group};
+        record = i32x4{(int)((pos + count - 1) / share) - w + 1 + 1024 * h, row0, r0, n_q * A.group};
       }
     }
-    if constexpr (kShared) {
-      if (A.stage == kBoth && u0 == 0) {      // where the rows' sums are: in a record's place, or in parts from share w's second on
-        const int prefix = !over && has_prefix(A, seq) ? kHasPrefix : 0;
-        for (int r = r0 + tid; r < min(n_q * A.group, r0 + kRows); r += 256) {
-          const int t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
-          reinterpret_cast<i32x2*>(sums_scale(A, row0 + t, hq, !over))[1] = i32x2{parts | prefix, w | (r - r0) << 16};
-        }
-      }
-    }
-    attend_tile<kF16, kCap, kBias, kPool, kShared>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[over ? seq : groups + seq]), r0, h, u0, n, part,
-                                                   over, kShared && L.early);
+    attend_tile<kF16, kCap, kBias, kPool, false>(A, smem, bounds, seq, row0, n_q, uniform(L.slots[seq]), r0, h, u0, n, part, false, false);
     lds_sync();   // the memory that rows left by is the next tiles'
     pos += n;
   }
@@ -1448,7 +1473,7 @@ __global__ __launch_bounds__(256, 2) void attend_shares_kernel(const AttendLaunc
 // share out their rows, 8 at a time or fewer where items are few.  32 lanes hold the 128 values of a row; with fewer than 8
 // rows, several such groups take a row's parts in turn and meet in LDS.
 constexpr int kJoinThreads = 256, kJoinGrid = 1024;
-template <bool kF16, bool kShared>
+template <bool kF16>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A) {
   __shared__ f32x4 sO[8][32];
   __shared__ float sM[8], sL[8];
@@ -1534,13 +1559,6 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A
     for (int x = 1; x < each; ++x) add(sM[grp + x], sL[grp + x], sO[grp + x][c]);
     const int r = r0 + k, t = div_by(r, A.by_group), hq = h * A.group + r - t * A.group;
     const int64_t row = row0 + t;
-    if constexpr (kShared) {
-      if (A.stage == kOverPrefix) {
-        *reinterpret_cast<f32x4*>(sums_row(A, row, hq) + 4 * c) = acc;
-        if (c == 0) *reinterpret_cast<f32x2*>(sums_scale(A, row, hq)) = f32x2{m, l};
-        continue;
-      }
-    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head + 4 * c;
     *reinterpret_cast<u32x2*>(out) = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
@@ -1548,134 +1566,47 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendLaunch A
   }
 }
 
-// Rows whose sums over prefix and own slots one launch has made (kBoth): their parts, or the whole, of either, in the order of the keys, by
-// the two records of each row and head.  As above 8 rows a workgroup, or fewer with several groups of 32 lanes each.
-template <bool kF16>
-__global__ __launch_bounds__(kJoinThreads) void join_both_kernel(const AttendLaunch A) {
-  __shared__ f32x4 sO[8][32];
-  __shared__ float sM[8], sL[8];
-  const rkv_attend& a = A.a;
-  const int tid = threadIdx.x, grp = tid >> 5, c = tid & 31;
-  const int begin = first_row<true>(A, 0, false), stop = first_row<true>(A, a.n_seqs, false);
-  const int64_t first = (int64_t)begin * a.n_q_heads, total = (int64_t)stop * a.n_q_heads;      // rows of no sequence are not touched
-  int most = 8;
-  while (most > 1 && (total - first + most - 1) / most < kJoinGrid) most >>= 1;
-  const int each = 8 / most, i = grp / each, g = grp - i * each;
-  for (int64_t task = first + (int64_t)blockIdx.x * most; task < total; task += (int64_t)kJoinGrid * most) {
-    const int64_t id = task + i;
-    const bool in = id < total;
-    const int64_t row = (in ? id : task) / a.n_q_heads;
-    const int hq = (int)((in ? id : task) - row * a.n_q_heads);
-    const f32x4 own = *reinterpret_cast<const f32x4*>(sums_scale(A, row, hq, true));
-    const int own_word = __float_as_int(own[2]), own_parts = own_word & 1023;
-    f32x4 pre = {0.f, 0.f, 0.f, 0.f};
-    if (own_word & kHasPrefix) pre = *reinterpret_cast<const f32x4*>(sums_scale(A, row, hq));
-    const int pre_parts = __float_as_int(pre[2]) & 1023;
-    const int n_pre = own_word & kHasPrefix ? max(1, pre_parts) : 0, n = n_pre + max(1, own_parts);
-    float m = -__builtin_inff(), l = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    auto add = [&](float m2, float l2, f32x4 v) {
-      const float top = fmaxf(m, m2), ref = top == -__builtin_inff() ? 0.f : top;
-      const float f = __builtin_amdgcn_exp2f(m - ref), f2 = __builtin_amdgcn_exp2f(m2 - ref);
-      m = top;
-      l = l * f + l2 * f2;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = acc[e] * f + v[e] * f2;
-    };
-    for (int j0 = g; j0 < n; j0 += 4 * each) {   // four parts in flight
-      f32x2 ml[4];
-      f32x4 v[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int jj = min(j0 + j * each, n - 1);
-        const bool over = jj < n_pre;
-        const f32x4 rec = over ? pre : own;
-        const int k = over ? jj : jj - n_pre, where = __float_as_int(rec[3]);
-        const float *from_o = sums_row(A, row, hq, !over) + 4 * c, *from_m = sums_scale(A, row, hq, !over);
-        if (over ? pre_parts : own_parts) {      // cut to the workspace, whatever cu_seqs holds
-          const int share = min((where & 0xffff) + k, kShares - 1), at = min(where >> 16, A.slot_rows - 1);
-          const float* from = part_slot(A, k ? 2 * share : 2 * share + 1);
-          from_o = from + at * kHeadDim + 4 * c;
-          from_m = from + A.slot_rows * kHeadDim + 2 * at;
-        }
-        ml[j] = *reinterpret_cast<const f32x2*>(from_m);
-        v[j] = *reinterpret_cast<const f32x4*>(from_o);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (j0 + j * each < n) add(ml[j][0], ml[j][1], v[j]);
-    }
-    __syncthreads();   // sO is free
-    sO[grp][c] = acc;
-    if (c == 0) {
-      sM[grp] = m;
-      sL[grp] = l;
-    }
-    __syncthreads();
-    if (!in || g) continue;
-    for (int x = 1; x < each; ++x) add(sM[grp + x], sL[grp + x], sO[grp + x][c]);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint16_t* out = static_cast<uint16_t*>(a.out) + row * a.out_token + hq * a.out_head + 4 * c;
-    *reinterpret_cast<u32x2*>(out) = u32x2{pack<kF16>(acc[0] * inv, acc[1] * inv), pack<kF16>(acc[2] * inv, acc[3] * inv)};
-    if (a.lse && c == 0) a.lse[row * a.n_q_heads + hq] = row_lse(m, l);
-  }
-}
-
-template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared>
+template <bool kF16, bool kCap, bool kBias, Pool kPool>
 void launch_kernels(const AttendLaunch& A, hipStream_t st) {
   if (A.parts) {
-    attend_shares_kernel<kF16, kCap, kBias, kPool, kShared><<<kShares, 256, 0, st>>>(A);
-    if constexpr (kShared) {
-      if (A.stage == kBoth) {
-        join_both_kernel<kF16><<<kJoinGrid, kJoinThreads, 0, st>>>(A);
-        return;
-      }
-    }
-    join_kernel<kF16, kShared><<<kJoinGrid, kJoinThreads, 0, st>>>(A);
+    attend_shares_kernel<kF16, kCap, kBias, kPool><<<kShares, 256, 0, st>>>(A);
+    join_kernel<kF16><<<kJoinGrid, kJoinThreads, 0, st>>>(A);
   } else {
-    attend_tiles_kernel<kF16, kCap, kBias, kPool, kShared><<<(unsigned)(A.n_places * A.p.n_kv_heads), 256, 0, st>>>(A);
+    attend_tiles_kernel<kF16, kCap, kBias, kPool, false><<<(unsigned)(A.n_places * A.p.n_kv_heads), 256, 0, st>>>(A);
   }
 }
-template <bool kF16, Pool kPool, bool kShared>
-void launch_scores(const AttendLaunch& A, hipStream_t st) {
-  if (A.a.softcap > 0.f) {
-    if (A.a.slopes) launch_kernels<kF16, true, true, kPool, kShared>(A, st);
-    else launch_kernels<kF16, true, false, kPool, kShared>(A, st);
-  } else {
-    if (A.a.slopes) launch_kernels<kF16, false, true, kPool, kShared>(A, st);
-    else launch_kernels<kF16, false, false, kPool, kShared>(A, st);
-  }
+
+// What the instances of a launch differ by: call(type, capped, biased, pool), each a constant.
+template <bool kValue>
+struct Flag {
+  static constexpr bool value = kValue;
+};
+template <Pool kValue>
+struct PoolKind {
+  static constexpr Pool value = kValue;
+};
+template <class Call>
+void by_scores(const AttendLaunch& A, Call call) {
+  auto with = [&](auto f16, auto cap) {
+    if (A.a.slopes) call(f16, cap, Flag<true>{});
+    else call(f16, cap, Flag<false>{});
+  };
+  auto of_type = [&](auto f16) {
+    if (A.a.softcap > 0.f) with(f16, Flag<true>{});
+    else with(f16, Flag<false>{});
+  };
+  if (A.p.dtype == RKV_F16) of_type(Flag<true>{});
+  else of_type(Flag<false>{});
 }
-// 16-bit pools.
-template <bool kShared>
-int launch_rows(const AttendLaunch& A, void* stream) {
-  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+inline bool pages_of_16(const AttendLaunch& A) {
   const rkv_pages& p = A.p;
-  const bool near = p.k_page < kStrideEnd && p.v_page < kStrideEnd && p.k_slot >= kHeadDim && p.v_slot >= kHeadDim;
-  const bool by_16 = p.page_size % 16 == 0 && near;
-  if (p.dtype == RKV_F16) {
-    if (by_16) launch_scores<true, kPages16, kShared>(A, st);
-    else launch_scores<true, kAnyPages, kShared>(A, st);
-  } else {
-    if (by_16) launch_scores<false, kPages16, kShared>(A, st);
-    else launch_scores<false, kAnyPages, kShared>(A, st);
-  }
-  return (int)hipGetLastError();
+  return p.page_size % 16 == 0 && p.k_page < kStrideEnd && p.v_page < kStrideEnd && p.k_slot >= kHeadDim && p.v_slot >= kHeadDim;
 }
-template <bool kShared>
-int launch_codes(const AttendLaunch& A, void* stream) {
-  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+inline bool dense_codes(const AttendLaunch& A) {
   bool dense = A.p.page_size % 8 == 0;
   for (int64_t stride : {A.p.k_page, A.p.v_page, A.p.k_slot, A.p.v_slot, A.ks.page, A.vs.page}) dense &= stride < kStrideEnd;
   for (const Scales& s : {A.ks, A.vs}) dense &= s.slot == 1 && ((uintptr_t)s.at | s.page | s.head) % 8 == 0;
-  if (A.p.dtype == RKV_F16) {
-    if (dense) launch_scores<true, kCodes8, kShared>(A, st);
-    else launch_scores<true, kCodes, kShared>(A, st);
-  } else {
-    if (dense) launch_scores<false, kCodes8, kShared>(A, st);
-    else launch_scores<false, kCodes, kShared>(A, st);
-  }
-  return (int)hipGetLastError();
+  return dense;
 }
 
 }  // namespace

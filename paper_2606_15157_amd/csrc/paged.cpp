@@ -94,9 +94,10 @@ int64_t row_tiles(const rkv_pages* p, const rkv_attend* a) { return full_tiles(p
 int64_t places(const rkv_pages* p, const rkv_attend* a) { return a->n_seqs + std::min(2 * full_tiles(p, a), row_tiles(p, a)); }
 bool nothing_to_do(const rkv_attend* a) { return a->n_seqs == 0 || a->n_rows == 0; }
 bool shared_out(const rkv_pages* p, const rkv_attend* a);
+bool dealt(const rkv_pages* p, const rkv_attend* a);
 
-// A call on a pool that has been checked.
-int check_attend(const rkv_pages* p, const rkv_attend* a) {
+// A call on a pool that has been checked.  split: whether a list of its key tiles is dealt out.
+int check_attend(const rkv_pages* p, const rkv_attend* a, bool (*split)(const rkv_pages*, const rkv_attend*)) {
   if (!a) return rkv::fail(RKV_ERR_INVALID_ARG, "null attend");
   if (a->n_seqs < 0 || a->n_rows < 0 || a->max_pages < 0 || a->max_q < 0 || a->max_kv < 0 || a->window < 0 || a->table_stride < 0)
     return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
@@ -114,7 +115,7 @@ int check_attend(const rkv_pages* p, const rkv_attend* a) {
   if ((int64_t)a->max_pages * p->page_size >= kIntEnd - 1024)   // key tiles past the end stay below 2^31
     return rkv::fail(RKV_ERR_UNSUPPORTED, "a sequence holds fewer than 2^31 - 1024 slots");
   if ((int64_t)a->n_rows * a->n_q_heads >= kIntEnd / 2) return rkv::fail(RKV_ERR_UNSUPPORTED, "n_rows * n_q_heads must be below 2^30");
-  if (!nothing_to_do(a) && !shared_out(p, a) && places(p, a) * p->n_kv_heads >= kGridEnd)   // n_tiles then is below 2^31, too
+  if (!nothing_to_do(a) && !split(p, a) && places(p, a) * p->n_kv_heads >= kGridEnd)   // n_tiles then is below 2^31, too
     return rkv::fail(RKV_ERR_UNSUPPORTED, "too many sequences for one launch");
   if (int st = check_layout("q", a->q, {a->q_token, a->q_head})) return st;
   return check_layout("out", a->out, {a->out_token, a->out_head});
@@ -158,9 +159,28 @@ bool shared_out(const rkv_pages* p, const rkv_attend* a) {
   return t > 32 || t * (208 - std::min<int64_t>(items, 208)) > 4200;
 }
 
-size_t attend_bytes(const rkv_pages* p, const rkv_attend* a, bool groups = false) {
+size_t attend_bytes(const rkv_pages* p, const rkv_attend* a) {
   if (nothing_to_do(a) || !shared_out(p, a)) return 0;
-  return kRecordBytes + sizeof(float) * 2 * rkv::kAttendShares * (size_t)part_rows(p, a, groups) * (rkv::kHeadDim + 2);
+  return kRecordBytes + sizeof(float) * 2 * rkv::kAttendShares * (size_t)part_rows(p, a, false) * (rkv::kHeadDim + 2);
+}
+
+// 8-bit pools and shared prefixes: whether a launch's key tiles are dealt out (attend_dealt_kernel and a join).
+bool dealt(const rkv_pages* p, const rkv_attend* a) {
+  const int64_t tiles = row_tiles(p, a), most = ((int64_t)a->max_pages * p->page_size + 63) / 64;
+  if (tiles > rkv::kAttendDealt || tiles * std::max<int64_t>(1, most) >= kIntEnd || p->n_kv_heads >= (1 << 20)) return false;
+  return shared_out(p, a);
+}
+// Partial sums of workgroups and of waves: of `rows` rows, the most that a row tile has.
+size_t parts_bytes(int32_t rows) {
+  return sizeof(float) * (rkv::kHeadDim + 2) * rkv::kAttendShares * (2 * (size_t)rows + 8 * (size_t)std::min(rows, rkv::kAttendFew));
+}
+// Sums of whole rows, if any, and the records of each row and head, for prefixes and own slots or one of these; rounded up to where partial sums may begin.
+size_t rows_bytes(const rkv_attend* a, int sums, int records) {
+  return (sizeof(float) * (rkv::kHeadDim * sums + 4 * records) * (size_t)a->n_rows * (size_t)a->n_q_heads + 255) & ~size_t(255);
+}
+size_t dealt_bytes(const rkv_pages* p, const rkv_attend* a) {
+  if (nothing_to_do(a) || !dealt(p, a)) return 0;
+  return rows_bytes(a, 0, 1) + parts_bytes(part_rows(p, a, false));
 }
 
 // Rows of a call that moves them, and the launch; the rows are written by a read.
@@ -225,7 +245,7 @@ int read_rows(const Pages* pages, const rkv_rows* rows, void* stream) {
 }
 
 // A launch over the row tiles of a call that has been checked, but for its workspace.
-rkv::AttendLaunch attend_launch(const Pool& pool, const rkv_attend* a, bool groups = false) {
+rkv::AttendLaunch attend_launch(const Pool& pool, const rkv_attend* a) {
   const rkv_pages* p = &pool.p;
   rkv::AttendLaunch L{};
   L.p = pool.p;
@@ -238,16 +258,17 @@ rkv::AttendLaunch attend_launch(const Pool& pool, const rkv_attend* a, bool grou
   L.n_tiles = (int32_t)row_tiles(p, a);
   L.few_long = 2 * full_tiles(p, a) < L.n_tiles;
   L.n_places = (int32_t)places(p, a);
-  L.slot_rows = part_rows(p, a, groups);
+  L.slot_rows = part_rows(p, a, false);
   // A part of 128 rows is written and read again, as many bytes as four key tiles: not for less than eight.  Few rows
   // cost nothing beside a tile (one token after 1K: 15 us with shares of one, 17 of four, 21 of eight).
   L.least = usual_rows(p, a) > 32 ? 8 : 1;
   return L;
 }
-void set_parts(rkv::AttendLaunch& L, size_t need, void* ws) {
-  if (!need) return;
-  L.records = static_cast<int32_t*>(ws);
-  L.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + kRecordBytes);
+void set_parts(rkv::AttendLaunch& L, int32_t rows, char* at) {
+  L.slot_rows = rows;
+  L.few_rows = std::min(rows, rkv::kAttendFew);
+  L.parts = reinterpret_cast<float*>(at);
+  L.few_parts = L.parts + 2 * (size_t)rkv::kAttendShares * rows * (rkv::kHeadDim + 2);
 }
 int check_workspace(size_t need, const void* ws, size_t ws_bytes) {
   if (need && !ws) return rkv::fail(RKV_ERR_WORKSPACE, "workspace is null");
@@ -256,14 +277,31 @@ int check_workspace(size_t need, const void* ws, size_t ws_bytes) {
   return RKV_OK;
 }
 
+// A launch without prefixes, in a workspace of what it needs.
+int launch_alone(const Pool& pool, const rkv_attend* a, size_t need, char* ws, void* stream) {
+  rkv::AttendLaunch L = attend_launch(pool, a);
+  if (pool.codes) {
+    if (need) {
+      L.sum_records = reinterpret_cast<float*>(ws);
+      set_parts(L, part_rows(&pool.p, a, false), ws + rows_bytes(a, 0, 1));
+    }
+    return rkv::launch_attend8(L, stream);
+  }
+  if (need) {
+    L.records = reinterpret_cast<int32_t*>(ws);
+    L.parts = reinterpret_cast<float*>(ws + kRecordBytes);
+  }
+  return rkv::launch_attend(L, stream);
+}
+
 template <class Pages>
 int attend_size(const Pages* pages, const rkv_attend* a, size_t* bytes) {
   rkv::clear_error();
   if (!bytes) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
   if (int st = check_pages(pages)) return st;
   const Pool pool = pool_of(pages);
-  if (int st = check_attend(&pool.p, a)) return st;
-  *bytes = attend_bytes(&pool.p, a);
+  if (int st = check_attend(&pool.p, a, pool.codes ? dealt : shared_out)) return st;
+  *bytes = pool.codes ? dealt_bytes(&pool.p, a) : attend_bytes(&pool.p, a);
   return RKV_OK;
 }
 template <class Pages>
@@ -271,14 +309,12 @@ int attend(const Pages* pages, const rkv_attend* a, void* ws, size_t ws_bytes, v
   rkv::clear_error();
   if (int st = check_pages(pages)) return st;
   const Pool pool = pool_of(pages);
-  if (int st = check_attend(&pool.p, a)) return st;
+  if (int st = check_attend(&pool.p, a, pool.codes ? dealt : shared_out)) return st;
   if (nothing_to_do(a)) return RKV_OK;
   if (!a->q || !a->out || !a->lens || (a->max_pages && !a->table)) return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
-  const size_t need = attend_bytes(&pool.p, a);
+  const size_t need = pool.codes ? dealt_bytes(&pool.p, a) : attend_bytes(&pool.p, a);
   if (int st = check_workspace(need, ws, ws_bytes)) return st;
-  rkv::AttendLaunch L = attend_launch(pool, a);
-  set_parts(L, need, ws);
-  return launched(pool.codes ? rkv::launch_attend8(L, stream) : rkv::launch_attend(L, stream));
+  return launched(launch_alone(pool, a, need, static_cast<char*>(ws), stream));
 }
 
 // ---- shared prefixes: the groups' rows over their prefixes, then each sequence's rows over its own slots, from those sums on
@@ -297,7 +333,7 @@ rkv_attend over_prefixes(const rkv_attend* a, const rkv_shared* g) {
   return b;
 }
 int check_shared(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
-  if (int st = check_attend(p, a)) return st;
+  if (int st = check_attend(p, a, dealt)) return st;
   if (!g) return rkv::fail(RKV_ERR_INVALID_ARG, "null shared");
   if (g->n_groups < 0 || g->max_pages < 0 || g->max_len < 0 || g->table_stride < 0) return rkv::fail(RKV_ERR_INVALID_ARG, "negative size");
   if (a->prefix_lens || a->first_keys) return rkv::fail(RKV_ERR_UNSUPPORTED, "prefix_lens and first_keys do not go with shared prefixes");
@@ -305,7 +341,7 @@ int check_shared(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
   if (((int64_t)g->max_pages + a->max_pages) * p->page_size >= kIntEnd - 1024)
     return rkv::fail(RKV_ERR_UNSUPPORTED, "a prefix and a sequence hold fewer than 2^31 - 1024 slots together");
   const rkv_attend b = over_prefixes(a, g);
-  if (!nothing_to_do(&b) && !shared_out(p, &b) && places(p, &b) * p->n_kv_heads >= kGridEnd)
+  if (!nothing_to_do(&b) && !dealt(p, &b) && places(p, &b) * p->n_kv_heads >= kGridEnd)
     return rkv::fail(RKV_ERR_UNSUPPORTED, "too many groups for one launch");
   return RKV_OK;
 }
@@ -314,20 +350,14 @@ int check_shared(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
 bool both_at_once(const rkv_pages* p, const rkv_attend* a, const rkv_attend* b) {
   const int64_t own = row_tiles(p, a), over = row_tiles(p, b);
   auto tiles = [&](int64_t pages) { return std::max<int64_t>(1, (pages * p->page_size + 63) / 64); };
-  return usual_rows(p, a) <= 64 && own + over <= rkv::kAttendListed && own * tiles(a->max_pages) + over * tiles(b->max_pages) < kIntEnd &&
+  return usual_rows(p, a) <= 64 && own + over <= rkv::kAttendDealt && own * tiles(a->max_pages) + over * tiles(b->max_pages) < kIntEnd &&
          p->n_kv_heads < (1 << 20);
 }
-size_t parts_bytes(int32_t rows) { return kRecordBytes + sizeof(float) * 2 * rkv::kAttendShares * (size_t)rows * (rkv::kHeadDim + 2); }
-// The sums of every row with their records, of one kind or both, rounded up to where the shares' records may begin; then the workspace of
-// the launches.
-size_t sums_bytes(const rkv_attend* a, bool both) {
-  return (sizeof(float) * (rkv::kHeadDim + 4) * (both ? 2 : 1) * (size_t)a->n_rows * (size_t)a->n_q_heads + 255) & ~size_t(255);
-}
-size_t shared_bytes(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
+size_t shared_bytes(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g, bool codes) {
   const rkv_attend b = over_prefixes(a, g);
-  if (nothing_to_do(a) || nothing_to_do(&b)) return attend_bytes(p, a);
-  if (both_at_once(p, a, &b)) return sums_bytes(a, true) + parts_bytes(part_rows(p, &b, true));
-  return sums_bytes(a, false) + std::max(attend_bytes(p, a), attend_bytes(p, &b, true));
+  if (nothing_to_do(a) || nothing_to_do(&b)) return codes ? dealt_bytes(p, a) : attend_bytes(p, a);
+  if (both_at_once(p, a, &b)) return rows_bytes(a, 2, 2) + parts_bytes(part_rows(p, &b, true));
+  return rows_bytes(a, 1, 1) + std::max(dealt(p, a) ? parts_bytes(part_rows(p, a, false)) : 0, dealt(p, &b) ? parts_bytes(part_rows(p, &b, true)) : 0);
 }
 
 template <class Pages>
@@ -337,7 +367,7 @@ int shared_size(const Pages* pages, const rkv_attend* a, const rkv_shared* g, si
   if (int st = check_pages(pages)) return st;
   const Pool pool = pool_of(pages);
   if (int st = check_shared(&pool.p, a, g)) return st;
-  *bytes = shared_bytes(&pool.p, a, g);
+  *bytes = shared_bytes(&pool.p, a, g, pool.codes);
   return RKV_OK;
 }
 template <class Pages>
@@ -350,39 +380,35 @@ int attend_shared(const Pages* pages, const rkv_attend* a, const rkv_shared* g, 
   if (nothing_to_do(a)) return RKV_OK;
   if (!a->q || !a->out || !a->lens || (a->max_pages && !a->table) || (g->n_groups && (!g->lens || !g->cu_seqs || (g->max_pages && !g->table))))
     return rkv::fail(RKV_ERR_INVALID_ARG, "null pointer");
-  if (int st = check_workspace(shared_bytes(p, a, g), ws, ws_bytes)) return st;
-  rkv::AttendLaunch L = attend_launch(pool, a);
+  const size_t need = shared_bytes(p, a, g, pool.codes);
+  if (int st = check_workspace(need, ws, ws_bytes)) return st;
   const rkv_attend b = over_prefixes(a, g);
-  if (nothing_to_do(&b)) {
-    set_parts(L, attend_bytes(p, a), ws);
-    return launched(pool.codes ? rkv::launch_attend8(L, stream) : rkv::launch_attend(L, stream));
-  }
+  if (nothing_to_do(&b)) return launched(launch_alone(pool, a, need, static_cast<char*>(ws), stream));
   auto* launch = pool.codes ? rkv::launch_attend8_shared : rkv::launch_attend_shared;
   const bool both = both_at_once(p, a, &b);
+  rkv::AttendLaunch L = attend_launch(pool, a);
   L.g = *g;
   L.sums = static_cast<float*>(ws);
   L.sum_records = L.sums + (both ? 2 : 1) * (size_t)a->n_rows * a->n_q_heads * rkv::kHeadDim;
-  char* rest = static_cast<char*>(ws) + sums_bytes(a, both);
+  char* rest = static_cast<char*>(ws) + rows_bytes(a, both ? 2 : 1, both ? 2 : 1);
   if (both) {
     L.stage = rkv::kBoth;
     L.n_group_tiles = (int32_t)row_tiles(p, &b);
     L.n_tiles += L.n_group_tiles;
-    L.slot_rows = part_rows(p, &b, true);
     L.least = 1;
-    set_parts(L, parts_bytes(L.slot_rows), rest);
+    set_parts(L, part_rows(p, &b, true), rest);
     return launched(launch(L, stream));
   }
-  const rkv::AttendLaunch tiles = attend_launch(pool, &b, true);
+  const rkv::AttendLaunch tiles = attend_launch(pool, &b);
   rkv::AttendLaunch G = L;
   G.n_tiles = G.n_group_tiles = tiles.n_tiles;
   G.few_long = tiles.few_long;
   G.n_places = tiles.n_places;
-  G.slot_rows = tiles.slot_rows;
   G.least = tiles.least;
   G.stage = rkv::kOverPrefix;
   L.stage = rkv::kOverOwn;
-  set_parts(G, attend_bytes(p, &b, true), rest);
-  set_parts(L, attend_bytes(p, a), rest);
+  if (dealt(p, &b)) set_parts(G, part_rows(p, &b, true), rest);
+  if (dealt(p, a)) set_parts(L, part_rows(p, a, false), rest);
   if (int st = launched(launch(G, stream))) return st;
   return launched(launch(L, stream));
 }

@@ -45,6 +45,8 @@ int launch_read8(const WriteLaunch& W, void* stream);
 constexpr int kAttendRows = 128;       // rows (tokens x query heads of a group) of a tile
 constexpr int kAttendShares = 512;     // workgroups that share the key tiles of a short list of row tiles: two a CU
 constexpr int kAttendListed = 1024;    // row tiles such a list may have
+constexpr int kAttendDealt = 768;      // and one of 8-bit pools or shared prefixes
+constexpr int kAttendFew = 16;         // rows that a wave takes by itself there
 // The launches of a call whose sequences share prefixes: over the prefixes, and over the own slots from the sums of the first on; or over both, whose
 // sums a join brings together.
 enum { kAlone = 0, kOverPrefix = 1, kOverOwn = 2, kBoth = 3 };
@@ -61,6 +63,8 @@ struct AttendLaunch {
   int32_t least;       // key tiles of a share, at least
   int32_t* records;    // [kAttendShares][4], then
   float* parts;        // [2 kAttendShares] partial sums; null: a workgroup per row tile
+  int32_t few_rows;    // of a wave's partial sum, an even number
+  float* few_parts;    // [8 kAttendShares] of these
   // Shared prefixes.  Row tiles of the groups are those of all their sequences' rows; a launch has the tiles of the groups, of the
   // sequences, or of both (the groups' first).
   int32_t stage;

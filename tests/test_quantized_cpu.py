@@ -182,15 +182,15 @@ def test_calls_of_nothing_need_no_gpu():
 
 @pytest.mark.parametrize("cu_q", [None, P])
 def test_the_workspace_of_a_shared_call_holds_its_sums_and_is_checked(cu_q):
-    """528 bytes a row and head for the prefixes and for the own slots, rounded up to 256; then 512 records and 1024 partial sums of up to
-    128 rows, all rows of a group among them, also where sequences have one row each."""
+    """528 bytes a row and head for the prefixes and for the own slots, rounded up to 256; then 1024 partial sums of up to 128 rows, all
+    rows of a group among them, also where sequences have one row each, and 4096 of at most 16."""
     L, n = _abi.lib(), C.c_size_t()
     a = attend(n_seqs=40, n_rows=40, cu_q=cu_q)
     g = shared(max_pages=4000, table_stride=4000)
     for call, size, pool in ((L.rkv_qpages_attend_shared, L.rkv_qpages_attend_shared_workspace_size, qpages()),
                              (L.rkv_pages_attend_shared, L.rkv_pages_attend_shared_workspace_size, pages())):
         assert size(C.byref(pool), C.byref(a), C.byref(g), C.byref(n)) == 0
-        assert n.value == (2 * 528 * 40 * 4 + 255) // 256 * 256 + 512 * 16 + 1024 * 80 * 130 * 4
+        assert n.value == (2 * 528 * 40 * 4 + 255) // 256 * 256 + (1024 * 80 + 4096 * 16) * 130 * 4
         refused(5, call(C.byref(pool), C.byref(a), C.byref(g), None, n.value, None))
         refused(5, call(C.byref(pool), C.byref(a), C.byref(g), C.c_void_p(P + 16), n.value, None))
         refused(5, call(C.byref(pool), C.byref(a), C.byref(g), C.c_void_p(P), n.value - 1, None))
