@@ -21,23 +21,44 @@ constexpr int kDealt = kAttendDealt;
 // all) and these bits, then the first part's share and from bit 16 the row among its tile's.
 constexpr int kParts = 4095, kHasPrefix = 1 << 16, kFewRows = 1 << 17;
 
+// What an item costs besides its key tiles, in key tiles: it begins with a table, then keys, each waited for, and ends with stores (some 5 us
+// of a workgroup where a key tile takes 1.5, 9 us of a wave where one takes 3 to 4).  Shares of many tiles count it, as units before the first
+// one; where there is little to do for all, shares are as small as can be.
+constexpr int kItem = 3;
+
 // The list of row tiles that every workgroup makes: those of the groups over their prefixes, then those of the sequences.
 struct Deal {
   int32_t row0[kDealt + 2];       // first row of each group and behind the last, then of each sequence
   int32_t slots[kDealt];          // of each prefix, then of each sequence
-  int32_t wide[kDealt + 1];       // key tiles of a head before row tile i, of those with more than 16 rows
+  int32_t wide[kDealt + 1];       // units of a head before row tile i, of those with more than 16 rows
   int32_t few[kDealt + 1];        // and of the others
   uint16_t seq[kDealt];           // group or sequence of row tile i, and kPrefixed
-  int32_t sums[2][kDealt / 64];
+  int32_t sums[4][kDealt / 64];
   int32_t early;                  // whether some sequence has rows before its last prefix slot
 };
 constexpr int kPrefixed = 1 << 15;
 
+// Of a head: key tiles and row tiles of either kind; workgroups (of an XCD's) for the wide ones; units besides the key tiles that an item counts for.
 struct Totals {
-  int wide, few;
+  int wide, few, wide_items, few_items, n_wide, wide_extra, few_extra;
 };
-// Fills the list; the key tiles of a head, fewer than 2^31 (the host lets no other call here).
-template <bool kShared>
+// Workgroups (of the kShares / 8 of an XCD) for the wide tiles, so that either side ends at the same time.  Measured, us: a wide tile's 64 keys
+// take a workgroup 1.5, in 8 bits 2.1 (their way into LDS is by registers); those of a narrow one take a wave 5 to 6, or 3 to 4 in 8 bits, as long
+// as the chip's memory does not bound them, and a narrow item 9 besides.
+template <Pool kPool>
+__device__ __forceinline__ int wide_workgroups(const Totals& all) {
+  constexpr int kMost = kShares / 8;
+  if (!all.wide) return 0;
+  if (!all.few) return kMost;
+  const float wide = (in_codes(kPool) ? 2.1f : 1.5f) * (float)(all.wide + kItem * all.wide_items);
+  const float few = (in_codes(kPool) ? 0.9f : 1.4f) * (float)all.few + 2.2f * (float)all.few_items;
+  return min(max((int)(wide / (wide + few) * kMost + 0.5f), 1), kMost - 1);
+}
+__device__ __forceinline__ int extra_units(int tiles, int items, int heads, int shares) {
+  return ((int64_t)tiles + kItem * items) * heads >= (int64_t)2 * kItem * shares ? kItem : 0;
+}
+// Fills the list; the units of a head, fewer than 2^31 (the host lets no other call here).
+template <Pool kPool, bool kShared>
 __device__ __forceinline__ Totals deal(const AttendLaunch& A, Deal& L, int groups, int seqs) {
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, own0 = groups ? groups + 1 : 0;
   int first_prefixed = 0, end_prefixed = 0;
@@ -60,7 +81,7 @@ __device__ __forceinline__ Totals deal(const AttendLaunch& A, Deal& L, int group
     __syncthreads();
   }
   // A tile a thread: 256 at a time, as many times as there are tiles.
-  int cost[kDealt / 256], x_wide[kDealt / 256], x_few[kDealt / 256];
+  int cost[kDealt / 256], x_wide[kDealt / 256], x_few[kDealt / 256], i_wide[kDealt / 256], i_few[kDealt / 256];
   bool narrow[kDealt / 256];
 #pragma unroll
   for (int i = 0; i < kDealt / 256; ++i) {
@@ -97,31 +118,56 @@ __device__ __forceinline__ Totals deal(const AttendLaunch& A, Deal& L, int group
         }
       }
     }
+    const uint64_t few = __ballot(narrow[i]), wide = __ballot(cost[i] && !narrow[i]), below = ((uint64_t)1 << lane) - 1;
+    i_wide[i] = (int)__popcll(wide & below);      // row tiles before this one
+    i_few[i] = (int)__popcll(few & below);
     if (lane == 63) {
       L.sums[0][4 * i + wv] = x_wide[i];
       L.sums[1][4 * i + wv] = x_few[i];
+      L.sums[2][4 * i + wv] = (int)__popcll(wide);
+      L.sums[3][4 * i + wv] = (int)__popcll(few);
     }
   }
   __syncthreads();
-  Totals all = {0, 0};
+  Totals all = {};
 #pragma unroll
   for (int i = 0; i < kDealt / 256; ++i) {
     if (256 * i >= A.n_tiles) break;
-    int wide = all.wide, few = all.few;
+    x_wide[i] += all.wide - (narrow[i] ? 0 : cost[i]);
+    x_few[i] += all.few - (narrow[i] ? cost[i] : 0);
+    i_wide[i] += all.wide_items;
+    i_few[i] += all.few_items;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
+      const int wide = L.sums[0][4 * i + j], few = L.sums[1][4 * i + j], wide_items = L.sums[2][4 * i + j], few_items = L.sums[3][4 * i + j];
       if (j < wv) {
-        wide += L.sums[0][4 * i + j];
-        few += L.sums[1][4 * i + j];
+        x_wide[i] += wide;
+        x_few[i] += few;
+        i_wide[i] += wide_items;
+        i_few[i] += few_items;
       }
-      all.wide += L.sums[0][4 * i + j];
-      all.few += L.sums[1][4 * i + j];
+      all.wide += wide;
+      all.few += few;
+      all.wide_items += wide_items;
+      all.few_items += few_items;
     }
-    L.wide[256 * i + tid] = wide + x_wide[i] - (narrow[i] ? 0 : cost[i]);
-    L.few[256 * i + tid] = few + x_few[i] - (narrow[i] ? cost[i] : 0);
   }
   all.wide = uniform(all.wide);
   all.few = uniform(all.few);
+  all.wide_items = uniform(all.wide_items);
+  all.few_items = uniform(all.few_items);
+  all.n_wide = uniform(wide_workgroups<kPool>(all));
+  all.wide_extra = extra_units(all.wide, all.wide_items, A.p.n_kv_heads, 8 * all.n_wide);
+  all.few_extra = extra_units(all.few, all.few_items, A.p.n_kv_heads, 4 * (kShares - 8 * all.n_wide));
+#pragma unroll
+  for (int i = 0; i < kDealt / 256; ++i) {
+    if (256 * i >= A.n_tiles) break;
+    L.wide[256 * i + tid] = x_wide[i] + all.wide_extra * i_wide[i];
+    L.few[256 * i + tid] = x_few[i] + all.few_extra * i_few[i];
+  }
+  __syncthreads();      // what a thread of no tile wrote is behind the last one's
+  all.wide += all.wide_extra * all.wide_items;      // units from here on
+  all.few += all.few_extra * all.few_items;
   if (tid == 0) {
     L.wide[A.n_tiles] = all.wide;
     L.few[A.n_tiles] = all.few;
@@ -130,18 +176,13 @@ __device__ __forceinline__ Totals deal(const AttendLaunch& A, Deal& L, int group
   return all;
 }
 
-// Workgroups (of the kShares / 8 of an XCD) for the wide tiles.  A key tile of up to 128 rows keeps a workgroup for 1.1 us; one of few rows
-// is 16 or 32 KiB of memory, of which a workgroup's share of the chip's rate takes 1.4 or 2.8 us.
-template <Pool kPool>
-__device__ __forceinline__ int wide_workgroups(Totals all) {
-  constexpr int kMost = kShares / 8;
-  if (!all.wide) return 0;
-  if (!all.few) return kMost;
-  const float wide = 1.1f * (float)all.wide, few = (in_codes(kPool) ? 1.4f : 2.8f) * (float)all.few;
-  return min(max((int)(wide / (wide + few) * kMost + 0.5f), 1), kMost - 1);
+// a / b for a >= 0 and b > 0; two 64-bit divisions are a third of a microsecond.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  if ((a | b) >> 32 == 0) return (uint32_t)a / (uint32_t)b;
+  return a / b;
 }
 
-// Shares of the row tiles' key tiles, in the order (head, row tile, key tile): equal, consecutive ones.  Workgroup b runs on XCD b % 8 and
+// Shares of the row tiles' units, in the order (head, row tile, key tile): equal, consecutive ones.  Workgroup b runs on XCD b % 8 and
 // takes shares that follow those of the XCD before, so that the tiles of a head, which read the same keys, meet in one L2.
 template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared>
 __global__ __launch_bounds__(256, 2) void attend_dealt_kernel(const AttendLaunch A) {
@@ -149,18 +190,18 @@ __global__ __launch_bounds__(256, 2) void attend_dealt_kernel(const AttendLaunch
   __shared__ Bounds bounds;
   __shared__ Deal L;
   const int groups = kShared && A.stage != kOverOwn ? A.g.n_groups : 0, seqs = kShared && A.stage == kOverPrefix ? 0 : A.a.n_seqs;
-  const Totals all = deal<kShared>(A, L, groups, seqs);
-  const int xcd = blockIdx.x % 8, at_xcd = blockIdx.x / 8, n_wide = uniform(wide_workgroups<kPool>(all));
+  const Totals all = deal<kPool, kShared>(A, L, groups, seqs);
+  const int xcd = blockIdx.x % 8, at_xcd = blockIdx.x / 8, n_wide = all.n_wide;
   // This workgroup's shares, or this wave's.
-  auto take = [&](auto few, const int32_t* before, int count_all, int w, int shares, int least) __attribute__((always_inline)) {
+  auto take = [&](auto few, const int32_t* before, int units, int extra, int w, int shares, int least) __attribute__((always_inline)) {
     constexpr bool kFew = decltype(few)::value;
     const int tid = kFew ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t total = (int64_t)count_all * A.p.n_kv_heads;
-    const int64_t share = max((int64_t)least, (total + shares - 1) / shares);
+    const int64_t total = (int64_t)units * A.p.n_kv_heads;
+    const int64_t share = max((int64_t)least, divide(total + shares - 1, shares));
     int64_t pos = w * share;
     const int64_t end = min(total, pos + share);
     while (pos < end) {
-      const int h = uniform((int)(pos / count_all)), rem = uniform((int)(pos - (int64_t)h * count_all));
+      const int h = uniform((int)divide(pos, units)), rem = uniform((int)(pos - (int64_t)h * units));
       int lo = 0, hi = A.n_tiles;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -170,14 +211,17 @@ __global__ __launch_bounds__(256, 2) void attend_dealt_kernel(const AttendLaunch
       const int tile = uniform(lo), named = uniform(L.seq[tile]), seq = named & ~kPrefixed;
       const bool over = kShared && tile < A.n_group_tiles;
       const int v = over || !groups ? seq : groups + 1 + seq, at = over || !kShared ? tile : tile - A.n_group_tiles;
-      const int u0 = rem - uniform(before[tile]), count = uniform(before[tile + 1]) - uniform(before[tile]);
-      const int n = (int)min((int64_t)(count - u0), end - pos);
+      const int x0 = rem - uniform(before[tile]), count = uniform(before[tile + 1]) - uniform(before[tile]);
+      const int x = (int)min((int64_t)(count - x0), end - pos);
+      const int u0 = max(0, x0 - extra), n = max(0, x0 + x - extra) - u0;      // key tiles
+      pos += x;
+      if (n == 0) continue;      // the next share begins it
       const int row0 = uniform(L.row0[v]), n_q = uniform(L.row0[v + 1]) - row0, r0 = (at - tile_start(A, row0, seq)) * kRows;
       float* part = nullptr;
       int word = 0;
-      if (n < count) {
+      if (n < count - extra) {
         part = kFew ? few_slot(A, 2 * w + (u0 == 0)) : part_slot(A, 2 * w + (u0 == 0));
-        if (u0 == 0) word = ((int)((pos + count - 1) / share) - w + 1) | (kFew ? kFewRows : 0);
+        if (u0 == 0) word = ((int)divide(pos - x - x0 + count - 1, share) - w + 1) | (kFew ? kFewRows : 0);
       }
       if (u0 == 0) {
         if (named & kPrefixed) word |= kHasPrefix;
@@ -189,14 +233,13 @@ __global__ __launch_bounds__(256, 2) void attend_dealt_kernel(const AttendLaunch
       const int n_kv = uniform(L.slots[over ? seq : groups + seq]);
       attend_rows<kF16, kCap, kBias, kPool, kShared, kFew, kFew>(A, smem, bounds, seq, row0, n_q, n_kv, r0, h, u0, n, part, over, kShared && L.early);
       if constexpr (!kFew) lds_sync();   // the memory that rows left by is the next tiles'
-      pos += n;
     }
   };
   if (at_xcd < n_wide) {
-    take(Flag<false>{}, L.wide, all.wide, xcd * n_wide + at_xcd, 8 * n_wide, A.least);
+    take(Flag<false>{}, L.wide, all.wide, all.wide_extra, xcd * n_wide + at_xcd, 8 * n_wide, A.least + all.wide_extra);
   } else {
     const int n_few = kShares / 8 - n_wide;
-    take(Flag<true>{}, L.few, all.few, 4 * (xcd * n_few + at_xcd - n_wide) + uniform(threadIdx.x >> 6), 32 * n_few, 1);
+    take(Flag<true>{}, L.few, all.few, all.few_extra, 4 * (xcd * n_few + at_xcd - n_wide) + uniform(threadIdx.x >> 6), 32 * n_few, 1 + all.few_extra);
   }
 }
 
@@ -221,10 +264,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const AttendLau
     const int64_t row = (in ? id : task) / a.n_q_heads;
     const int hq = (int)((in ? id : task) - row * a.n_q_heads);
     const f32x4 own = *reinterpret_cast<const f32x4*>(sums_scale(A, row, hq, both));
-    const int own_word = __float_as_int(own[2]), own_parts = own_word & kParts;
     f32x4 pre = {0.f, 0.f, 0.f, 0.f};
+    if (both) pre = *reinterpret_cast<const f32x4*>(sums_scale(A, row, hq));      // undefined without a prefix
+    const int own_word = __float_as_int(own[2]), own_parts = own_word & kParts;
     const bool with_prefix = both && (own_word & kHasPrefix);
-    if (with_prefix) pre = *reinterpret_cast<const f32x4*>(sums_scale(A, row, hq));
     const int pre_word = __float_as_int(pre[2]), pre_parts = pre_word & kParts;
     const int n_pre = with_prefix ? max(1, pre_parts) : 0, n = n_pre + (both ? max(1, own_parts) : own_parts);   // alone, a whole row is finished
     float m = -__builtin_inff(), l = 0.f;

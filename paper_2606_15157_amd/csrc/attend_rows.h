@@ -285,6 +285,11 @@ __device__ __forceinline__ u32x4 widen8(uint32_t lo, uint32_t hi, float scale) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
 }
+// n strides on, both not negative and below 2^32: one multiply-add.
+template <class T>
+__device__ __forceinline__ T* far_by(T* from, int n, int64_t stride) {
+  return from + (uint64_t)(uint32_t)n * (uint32_t)stride;
+}
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // Probability 0 times what a hidden slot holds is no 0 if that is infinite or NaN.  A tile whose rows see different slots and
@@ -633,7 +638,6 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
       };
       // Whether some of this lane's keys from `key` on is visible to some row, and their page is one.
       auto held = [&](int key, int page) { return key + kEach > b_lo && key < min(b_hi, end) && (uint32_t)page < (uint32_t)p.n_pages; };
-      auto far_by = [](auto* from, int n, int64_t stride) { return from + (uint64_t)(uint32_t)n * (uint32_t)stride; };      // both below 2^32
       auto load_k = [&](int key0, const Places& at, Block& x) __attribute__((always_inline)) {
         const char* row = nullptr;
         if constexpr (kDense) {
@@ -1027,18 +1031,33 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
     uint32_t scale;
   };
   Raw raw_k, raw_v;
-  int page_near = -1, page_far = -1;      // of this lane's row of the next tile of V and of K to be loaded
   const int q_row = 16 * wv + (lane >> 2), q_c = lane & 3;
-  auto q_look = [&](int tl) __attribute__((always_inline)) { return table[div_by(min(max(tl * kKeys + q_row, b_lo), b_hi - 1), A.by_page)]; };
-  auto q_load = [&](int tl, int page, Raw& raw, const char* rows, int64_t page_stride, int64_t slot, const Scales& scales) __attribute__((always_inline)) {
-    const int key = tl * kKeys + q_row;
-    const bool in = key >= b_lo && key < b_hi && (uint32_t)page < (uint32_t)p.n_pages;
-    const int at = key - div_by(in ? key : 0, A.by_page) * p.page_size;
-    const char* src = in ? rows + page * page_stride + at * slot : zeros;
-    const uint8_t* byte = in ? scales.at + page * scales.page + h * scales.head + at * scales.slot : reinterpret_cast<const uint8_t*>(zeros);
-    raw.c[0] = *reinterpret_cast<const u32x4*>(src + 16 * q_c);
-    raw.c[1] = *reinterpret_cast<const u32x4*>(src + 64 + 16 * q_c);
-    raw.scale = *byte;
+  // Where this lane's row of a tile lies (a page that is none: a row of zeros): of the next tile of V to be loaded, of K, and of the one after.
+  struct Spot {
+    int page, at;
+  };
+  Spot spot_v, spot_k;
+  const uint8_t *k_scales = A.ks.at + h * A.ks.head, *v_scales = A.vs.at + h * A.vs.head;
+  auto q_look = [&](int tl) __attribute__((always_inline)) {
+    const int key = tl * kKeys + q_row, c = div_by(min(max(key, b_lo), b_hi - 1), A.by_page);
+    return Spot{key >= b_lo && key < b_hi ? table[c] : -1, key - c * p.page_size};
+  };
+  auto q_load = [&](const Spot& x, Raw& raw, const char* rows, int64_t page_stride, int64_t slot, const uint8_t* scales, const Scales& s) __attribute__((always_inline)) {
+    const bool in = (uint32_t)x.page < (uint32_t)p.n_pages;
+    const char* src;
+    const uint8_t* byte;
+    if constexpr (kPool == kCodes8) {
+      const int page = in ? x.page : 0, at = in ? x.at : 0;
+      src = far_by(far_by(rows, page, page_stride), at, slot);
+      byte = far_by(scales, page, s.page) + at;
+    } else {
+      src = rows + x.page * page_stride + x.at * slot;
+      byte = scales + x.page * s.page + x.at * s.slot;
+    }
+    src = (in ? src : zeros) + 16 * q_c;
+    raw.c[0] = *reinterpret_cast<const u32x4*>(src);
+    raw.c[1] = *reinterpret_cast<const u32x4*>(src + 64);
+    raw.scale = *(in ? byte : reinterpret_cast<const uint8_t*>(zeros));
   };
   auto q_store = [&](const Raw& raw, uint32_t to, int swizzle) __attribute__((always_inline)) {
     const float scale = scale_of(raw.scale);
@@ -1051,18 +1070,18 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   };
   auto q_store_k = [&](int buf) __attribute__((always_inline)) { q_store(raw_k, buf * kTileBytes, q_row & 15); };
   auto q_store_v = [&](int buf) __attribute__((always_inline)) { q_store(raw_v, (2 + buf) * kTileBytes, 4 * (q_row & 3)); };
-  auto q_load_k = [&](int tl) __attribute__((always_inline)) { q_load(tl, page_far, raw_k, kp, p.k_page, p.k_slot, A.ks); };
-  auto q_load_v = [&](int tl) __attribute__((always_inline)) { q_load(tl, page_near, raw_v, vp, p.v_page, p.v_slot, A.vs); };
+  auto q_load_k = [&](const Spot& x) __attribute__((always_inline)) { q_load(x, raw_k, kp, p.k_page, p.k_slot, k_scales, A.ks); };
+  auto q_load_v = [&](const Spot& x) __attribute__((always_inline)) { q_load(x, raw_v, vp, p.v_page, p.v_slot, v_scales, A.vs); };
   Place here, next;
   auto advance = [&](int tl, int b) __attribute__((always_inline)) {   // b = (tl + 1 - t0) % 2
     if constexpr (kQuant) {
       lds_sync();
       if (tl + 2 < t1) q_store_k(1 - b);
       if (tl + 1 < t1 && tl >= t0) q_store_v(b);
-      if (tl + 3 < t1) q_load_k(tl + 3);
-      if (tl + 2 < t1) q_load_v(tl + 2);
-      page_near = page_far;
-      if (tl + 4 < t1) page_far = q_look(tl + 4);
+      if (tl + 3 < t1) q_load_k(spot_k);
+      if (tl + 2 < t1) q_load_v(spot_v);
+      spot_v = spot_k;
+      if (tl + 4 < t1) spot_k = q_look(tl + 4);
       return;
     }
     tile_sync();
@@ -1073,14 +1092,14 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
   };
   if (t0 < t1) {
     if constexpr (kQuant) {
-      page_near = page_far = q_look(t0);
-      q_load_k(t0);
-      q_load_v(t0);
-      page_near = t0 + 1 < t1 ? q_look(t0 + 1) : -1;      // of V's second tile, and K's
-      page_far = t0 + 2 < t1 ? q_look(t0 + 2) : -1;
+      const Spot first = q_look(t0);
+      spot_v = q_look(t0 + 1);      // of V's second tile, and K's
+      spot_k = q_look(t0 + 2);
+      q_load_k(first);
+      q_load_v(first);
       q_store_k(0);
       q_store_v(0);
-      if (t0 + 1 < t1) q_load(t0 + 1, page_near, raw_k, kp, p.k_page, p.k_slot, A.ks);
+      if (t0 + 1 < t1) q_load_k(spot_v);
     } else {
       find(t0, here);
       if (t0 + 1 < t1) find(t0 + 1, next);

@@ -167,7 +167,7 @@ size_t attend_bytes(const rkv_pages* p, const rkv_attend* a) {
 // 8-bit pools and shared prefixes: whether a launch's key tiles are dealt out (attend_dealt_kernel and a join).
 bool dealt(const rkv_pages* p, const rkv_attend* a) {
   const int64_t tiles = row_tiles(p, a), most = ((int64_t)a->max_pages * p->page_size + 63) / 64;
-  if (tiles > rkv::kAttendDealt || tiles * std::max<int64_t>(1, most) >= kIntEnd || p->n_kv_heads >= (1 << 20)) return false;
+  if (tiles > rkv::kAttendDealt || tiles * (4 + most) >= kIntEnd || p->n_kv_heads >= (1 << 20)) return false;   // an item's units, and at least one tile
   return shared_out(p, a);
 }
 // Partial sums of workgroups and of waves: of `rows` rows, the most that a row tile has.
@@ -349,7 +349,7 @@ int check_shared(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
 // sequence cost more in launches than in sums of whole rows that go through memory.
 bool both_at_once(const rkv_pages* p, const rkv_attend* a, const rkv_attend* b) {
   const int64_t own = row_tiles(p, a), over = row_tiles(p, b);
-  auto tiles = [&](int64_t pages) { return std::max<int64_t>(1, (pages * p->page_size + 63) / 64); };
+  auto tiles = [&](int64_t pages) { return 4 + (pages * p->page_size + 63) / 64; };
   return usual_rows(p, a) <= 64 && own + over <= rkv::kAttendDealt && own * tiles(a->max_pages) + over * tiles(b->max_pages) < kIntEnd &&
          p->n_kv_heads < (1 << 20);
 }
