@@ -592,16 +592,24 @@ def pages_read(cache, slots, *, k_out=None, v_out=None, stream=None):
     if ctx is not None:
         with ctx:
             return pages_read(cache, slots, k_out=k_out, v_out=v_out)
-    if slots.dim() not in (1, 2):
+    have = slots.shape
+    if len(have) == 2:
+        if not slots.is_contiguous():
+            raise ValueError("slots must be contiguous")
+        slots = slots.view(-1)
+    elif len(have) != 1:
         raise ValueError("slots must have shape [T] or [B, n]")
-    _check_int32("slots", slots, tuple(slots.shape), dev)
-    if not slots.is_contiguous():
-        raise ValueError("slots must be contiguous")
-    shape = (*slots.shape, cache.n_kv_heads, cache.head_dim)
-    k, v = (_T.empty(shape, dtype=cache.dtype, device=dev) if x is None else x for x in (k_out, v_out))
+    shape = (*have, cache.n_kv_heads, cache.head_dim)
+    k, v = k_out, v_out
+    if k is None and v is None:
+        k, v = _T.empty((2, *shape), dtype=cache.dtype, device=dev).unbind(0)
+    elif k is None:
+        k = _T.empty(shape, dtype=cache.dtype, device=dev)
+    elif v is None:
+        v = _T.empty(shape, dtype=cache.dtype, device=dev)
     if k.shape != shape:
         raise ValueError(f"k_out and v_out must have shape {list(shape)}")
-    check(cache._read(cache._pack, _rows_pack(cache, k, v, slots.reshape(-1), "k_out and v_out"), _raw_stream(dev)))
+    check(cache._read(cache._pack, _rows_pack(cache, k, v, slots, "k_out and v_out"), _raw_stream(dev)))
     return k, v
 
 

@@ -43,15 +43,15 @@ struct Totals {
   int wide, few, wide_items, few_items, n_wide, wide_extra, few_extra;
 };
 // Workgroups (of the kShares / 8 of an XCD) for the wide tiles, so that either side ends at the same time.  Measured, us: a wide tile's 64 keys
-// take a workgroup 1.5, in 8 bits 2.1 (their way into LDS is by registers); those of a narrow one take a wave 5 to 6, or 3 to 4 in 8 bits, as long
-// as the chip's memory does not bound them, and a narrow item 9 besides.
+// take a workgroup 1.6, in 8 bits 2.3 (their way into LDS is by registers); those of a narrow one take a wave 5 to 6, or 3 in 8 bits, as long
+// as the chip's memory does not bound them, and a narrow item 6 to 8 besides; a workgroup has four waves.
 template <Pool kPool>
 __device__ __forceinline__ int wide_workgroups(const Totals& all) {
   constexpr int kMost = kShares / 8;
   if (!all.wide) return 0;
   if (!all.few) return kMost;
-  const float wide = (in_codes(kPool) ? 2.1f : 1.5f) * (float)(all.wide + kItem * all.wide_items);
-  const float few = (in_codes(kPool) ? 0.9f : 1.4f) * (float)all.few + 2.2f * (float)all.few_items;
+  const float wide = (in_codes(kPool) ? 2.3f : 1.6f) * (float)(all.wide + kItem * all.wide_items);
+  const float few = (in_codes(kPool) ? 0.75f : 1.4f) * (float)all.few + (in_codes(kPool) ? 1.6f : 2.f) * (float)all.few_items;
   return min(max((int)(wide / (wide + few) * kMost + 0.5f), 1), kMost - 1);
 }
 __device__ __forceinline__ int extra_units(int tiles, int items, int heads, int shares) {
@@ -62,21 +62,32 @@ template <Pool kPool, bool kShared>
 __device__ __forceinline__ Totals deal(const AttendLaunch& A, Deal& L, int groups, int seqs) {
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, own0 = groups ? groups + 1 : 0;
   int first_prefixed = 0, end_prefixed = 0;
+  bool early = false;
   if constexpr (kShared) {
     first_prefixed = A.g.cu_seqs[0];
     end_prefixed = A.g.cu_seqs[A.g.n_groups];
-    if (groups) {
-      for (int s = tid; s <= groups; s += 256) L.row0[s] = first_row<kShared>(A, s, true);
-      for (int s = tid; s < groups; s += 256) L.slots[s] = slots_of<kShared>(A, s, true);
+  }
+  // What a thread loads of a group and of a sequence it loads at once: one wait, and one more for the groups' rows.
+  const int32_t* cu = A.a.cu_q;
+  for (int s = tid; s <= max(groups, A.a.n_seqs); s += 256) {
+    const int last = A.a.n_seqs - 1;
+    const int c0 = cu ? cu[min(s, last + 1)] : s, c1 = cu ? cu[min(s, last) + 1] : s + 1, n_kv = last >= 0 ? slots_of(A, min(s, last)) : 0;
+    if constexpr (kShared) {
+      if (s <= groups && groups) {
+        const int member = A.g.cu_seqs[s], slots = slots_of<kShared>(A, min(s, groups - 1), true);
+        L.row0[s] = min(max(cu ? cu[min(max(member, 0), A.a.n_seqs)] : min(max(member, 0), A.a.n_seqs), 0), A.a.n_rows);
+        if (s < groups) L.slots[s] = slots;
+      }
+      early |= groups && s <= last && A.a.causal && c1 - c0 > n_kv + 1;
+    }
+    if (s <= seqs && seqs) {
+      L.row0[own0 + s] = min(max(c0, 0), A.a.n_rows);
+      if (s < seqs) L.slots[groups + s] = n_kv;
     }
   }
-  if (seqs) {
-    for (int s = tid; s <= seqs; s += 256) L.row0[own0 + s] = first_row<kShared>(A, s, false);
-    for (int s = tid; s < seqs; s += 256) L.slots[groups + s] = slots_of(A, s);
-  }
   if constexpr (kShared) {
-    const int early = __syncthreads_or(groups && early_rows(A, 0, A.a.n_seqs, tid, 256));
-    if (tid == 0) L.early = early;
+    const int some = __syncthreads_or(early);
+    if (tid == 0) L.early = some;
   } else {
     __syncthreads();
   }

@@ -765,6 +765,7 @@ __device__ __forceinline__ void attend_rows(const AttendLaunch& A, unsigned char
 #pragma unroll
         for (int i = 0; i < kEach; ++i) x[i] = score(s[i >> 2][i & 3], i, far);
         if (key0 < all_lo || key0 + kBlock > all_hi) {
+          asm volatile("");      // a branch: few blocks come here
           const int from = lo - key0 - kEach * lg, to = hi - key0 - kEach * lg;
 #pragma unroll
           for (int i = 0; i < kEach; ++i)
