@@ -193,7 +193,42 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
   return a / b;
 }
 
-// Shares of the row tiles' units, in the order (head, row tile, key tile): equal, consecutive ones.  Workgroup b runs on XCD b % 8 and
+// How units are shared out.  Of a CU's two workgroups the one that came first is served first: with equal shares of 512 tokens after 32768 the
+// first ones took 257 us and the others 322, of four sequences of 131072 146 and 171.  So shares go by weights, 5 to 4 for workgroups and 7 to 6 for
+// waves, where even the smaller ones hold `least` units; else all hold as many as need be for that.
+struct Cut {
+  int64_t total, share;      // share: of every one, or 0
+  int n, n_first, first, second;      // shares of an XCD, those of its CUs' first workgroups, and weights
+  __device__ __forceinline__ int weight() const { return n_first * first + (n - n_first) * second; }      // of an XCD
+  __device__ __forceinline__ void set(int64_t units, int shares, int of_first, int w_first, int w_second, int least) {
+    total = units;
+    n = shares;
+    n_first = of_first;
+    first = w_first;
+    second = w_second;
+    const double smallest = (double)total * second / (8 * weight());
+    share = smallest >= least + 1 ? 0 : max((int64_t)least, divide(total + 8 * n - 1, 8 * n));
+  }
+  // The first unit of share w.
+  __device__ __forceinline__ int64_t begin(int w) const {
+    if (share) return min(total, w * share);
+    if (w >= 8 * n) return total;
+    const int x = w / n, j = w - x * n;
+    const int before = x * weight() + (j < n_first ? j * first : n_first * first + (j - n_first) * second);
+    return (int64_t)((double)total * before / (8 * weight()));
+  }
+  // The share that unit p belongs to.
+  __device__ __forceinline__ int of(int64_t p) const {
+    if (share) return (int)divide(p, share);
+    const int at = (int)((double)p * (8 * weight()) / (double)total), x = min(at / weight(), 7), r = at - x * weight();
+    int w = x * n + min(r < n_first * first ? r / first : n_first + (r - n_first * first) / second, n - 1);
+    while (begin(w) > p) --w;
+    while (begin(w + 1) <= p) ++w;
+    return w;
+  }
+};
+
+// Shares of the row tiles' units, in the order (head, row tile, key tile), are consecutive.  Workgroup b runs on XCD b % 8 and
 // takes shares that follow those of the XCD before, so that the tiles of a head, which read the same keys, meet in one L2.
 template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared>
 __global__ __launch_bounds__(256, 2) void attend_dealt_kernel(const AttendLaunch A) {
@@ -204,13 +239,11 @@ __global__ __launch_bounds__(256, 2) void attend_dealt_kernel(const AttendLaunch
   const Totals all = deal<kPool, kShared>(A, L, groups, seqs);
   const int xcd = blockIdx.x % 8, at_xcd = blockIdx.x / 8, n_wide = all.n_wide;
   // This workgroup's shares, or this wave's.
-  auto take = [&](auto few, const int32_t* before, int units, int extra, int w, int shares, int least) __attribute__((always_inline)) {
+  auto take = [&](auto few, const int32_t* before, int units, int extra, int w, const Cut& cut) __attribute__((always_inline)) {
     constexpr bool kFew = decltype(few)::value;
     const int tid = kFew ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t total = (int64_t)units * A.p.n_kv_heads;
-    const int64_t share = max((int64_t)least, divide(total + shares - 1, shares));
-    int64_t pos = w * share;
-    const int64_t end = min(total, pos + share);
+    int64_t pos = cut.begin(w);
+    const int64_t end = cut.begin(w + 1);
     while (pos < end) {
       const int h = uniform((int)divide(pos, units)), rem = uniform((int)(pos - (int64_t)h * units));
       int lo = 0, hi = A.n_tiles;
@@ -232,7 +265,7 @@ __global__ __launch_bounds__(256, 2) void attend_dealt_kernel(const AttendLaunch
       int word = 0;
       if (n < count - extra) {
         part = kFew ? few_slot(A, 2 * w + (u0 == 0)) : part_slot(A, 2 * w + (u0 == 0));
-        if (u0 == 0) word = ((int)divide(pos - x - x0 + count - 1, share) - w + 1) | (kFew ? kFewRows : 0);
+        if (u0 == 0) word = (cut.of(pos - x - x0 + count - 1) - w + 1) | (kFew ? kFewRows : 0);
       }
       if (u0 == 0) {
         if (named & kPrefixed) word |= kHasPrefix;
@@ -246,11 +279,15 @@ __global__ __launch_bounds__(256, 2) void attend_dealt_kernel(const AttendLaunch
       if constexpr (!kFew) lds_sync();   // the memory that rows left by is the next tiles'
     }
   };
+  constexpr int kFirst = kShares / 16;      // workgroups of an XCD that are their CU's first
+  Cut cut;
   if (at_xcd < n_wide) {
-    take(Flag<false>{}, L.wide, all.wide, all.wide_extra, xcd * n_wide + at_xcd, 8 * n_wide, A.least + all.wide_extra);
+    cut.set((int64_t)all.wide * A.p.n_kv_heads, n_wide, min(n_wide, kFirst), 5, 4, A.least + all.wide_extra);
+    take(Flag<false>{}, L.wide, all.wide, all.wide_extra, xcd * n_wide + at_xcd, cut);
   } else {
     const int n_few = kShares / 8 - n_wide;
-    take(Flag<true>{}, L.few, all.few, all.few_extra, 4 * (xcd * n_few + at_xcd - n_wide) + uniform(threadIdx.x >> 6), 32 * n_few, 1 + all.few_extra);
+    cut.set((int64_t)all.few * A.p.n_kv_heads, 4 * n_few, 4 * max(0, kFirst - n_wide), 7, 6, 1 + all.few_extra);
+    take(Flag<true>{}, L.few, all.few, all.few_extra, 4 * (xcd * n_few + at_xcd - n_wide) + uniform(threadIdx.x >> 6), cut);
   }
 }
 
