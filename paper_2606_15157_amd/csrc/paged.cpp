@@ -193,6 +193,7 @@ int check_rows(const Pool& pool, const rkv_rows* rows, bool written) {
     return rkv::fail(RKV_ERR_UNSUPPORTED, "at most 2^28 - 16 rows a call, each head's counted");
   if (int st = check_layout("k rows", rows->k, {rows->k_outer, rows->k_token, rows->k_head})) return st;
   if (int st = check_layout("v rows", rows->v, {rows->v_outer, rows->v_token, rows->v_head})) return st;
+  if (written && rows->k == rows->v) return rkv::fail(RKV_ERR_INVALID_ARG, "k and v are read into the same rows");
   const int32_t heads = pool.p.n_kv_heads;
   if (written && (!rows_nest<3>({{{rows->k_outer, rows->n_outer}, {rows->k_token, rows->n_tokens}, {rows->k_head, heads}}}) ||
                   !rows_nest<3>({{{rows->v_outer, rows->n_outer}, {rows->v_token, rows->n_tokens}, {rows->v_head, heads}}})))

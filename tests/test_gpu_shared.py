@@ -7,7 +7,7 @@ import torch
 
 import paper_2606_15157_amd as rkv
 from oracle import pages as OG
-from test_gpu_paged import Case, NAN, compare, f64, ints
+from test_gpu_paged import Case, HALF, NAN, compare, f64, ints
 from test_gpu_quantized import QCase
 
 pytestmark = pytest.mark.gpu
@@ -260,6 +260,54 @@ def test_a_served_prompt_with_many_answers():
     full = [torch.cat([x.expand(n, -1, -1, -1), torch.stack([o[i] for o in own], 1)], 1).transpose(1, 2) for i, x in enumerate((k[None], v[None]))]
     want, log, weight, reach = OG.attend(f64(full[0]), f64(full[1]), f64(qt), [[b] for b in range(n)], [P + steps] * n)
     compare(y, lse, want, log, weight, reach, torch.bfloat16, most=P + steps)
+
+
+def near(a, b, size, dtype, steps=2):
+    """Two results of one definition: each is off by half a step of its type of itself, and by half a step of the probabilities' of
+    sum p |v| (`size`, which is itself a result in that type: 1.02 times); sums in 32 bits are far below both."""
+    half = HALF[dtype]
+    assert ((a.float() - b.float()).abs() <= steps * half * 1.02 * (1.02 * size.float() + b.float().abs()) + 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("quant", [False, True], ids=["rows", "codes"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n,groups,own,kw", [(64, 3, 900, dict()), (256, 2, 40, dict()), (100, 90, 700, dict(window=3000)), (40, 2, 2500, dict(softcap=20.0)),
+                                             (48, 2, 300, dict(q=7))], ids=["few", "many", "groups", "capped", "drafts"])
+def test_large_batches_equal_attention_over_whole_caches(n, groups, own, kw, dtype, quant):
+    """Shares of many items, of both kinds, whose sizes count: against calls in which every sequence's table begins with its prefix's pages."""
+    kw = dict(kw)
+    m, hq, hkv, page, g = kw.pop("q", 1), 32, 8, 16, torch.Generator(device="cuda").manual_seed(n)
+    rng = np.random.default_rng(n)
+    prefixes = [int(x) * page for x in rng.integers(64, 300, groups)]
+    lens = [int(x) for x in rng.integers(m, own + m, n)]
+    cuts = [0, *sorted(rng.choice(np.arange(1, n), groups - 1, replace=False).tolist()), n]
+    total = sum(prefixes) // page + sum(-(-x // page) for x in lens)
+    k, v = (torch.randn((total, hkv, page, 128), device="cuda", generator=g).to(dtype) for _ in range(2))
+    if quant:
+        cache = rkv.QuantizedCache.empty(total, hkv, page, dtype)
+        slots = torch.arange(total * page, device="cuda", dtype=torch.int32)
+        rkv.pages_write(cache, *(x.transpose(1, 2).reshape(-1, hkv, 128) for x in (k, v)), slots)
+        k, v = (x.view(total, page, hkv, 128).transpose(1, 2) for x in rkv.pages_read(cache, slots))
+    plain, sizes = rkv.PagedCache(k, v), rkv.PagedCache(k, v.abs())
+    cache = cache if quant else plain
+    ids, width = iter(rng.permutation(total).tolist()), max(prefixes) // page + own // page + 2
+    shared = [[next(ids) for _ in range(p // page)] for p in prefixes]
+    table = [[next(ids) for _ in range(-(-x // page))] for x in lens]
+    group = np.repeat(np.arange(groups), np.diff(cuts))
+    pad = lambda rows, w: ints([r + [-1] * (w - len(r)) for r in rows])  # noqa: E731
+    whole, all_lens = pad([shared[x] + t for x, t in zip(group, table)], width), ints([prefixes[x] + y for x, y in zip(group, lens)])
+    q = torch.randn((n * m, hq, 128), device="cuda", generator=g).to(dtype)
+    cu = ints([m * i for i in range(n + 1)])
+    want, log = rkv.pages_attend(plain, q, whole, all_lens, cu, return_lse=True, **kw)
+    size = rkv.pages_attend(sizes, q, whole, all_lens, cu, **kw)
+    args = (q, pad(shared, max(prefixes) // page), ints(prefixes), ints(cuts), pad(table, own // page + 2), ints(lens), cu)
+    got, lse = rkv.pages_attend_shared(cache, *args, return_lse=True, max_q=m, **kw)
+    near(got, want, size, dtype)
+    assert (lse - log).abs().max() <= 1e-4
+    if quant:      # and the same call without sharing, in 8 bits
+        got, lse = rkv.pages_attend(cache, q, whole, all_lens, cu, return_lse=True, max_q=m, **kw)
+        near(got, want, size, dtype)
+        assert (lse - log).abs().max() <= 1e-4
 
 
 def test_gradients_are_refused():

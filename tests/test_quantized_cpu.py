@@ -114,10 +114,15 @@ def test_bad_rows_are_refused(status, bad):
     refused(status, L.rkv_pages_read(C.byref(pages()), C.byref(rows(**bad)), None))
 
 
+def test_k_and_v_are_not_read_into_the_same_rows():
+    for call, pool in ((_abi.lib().rkv_qpages_read, qpages()), (_abi.lib().rkv_pages_read, pages())):
+        refused(1, call(C.byref(pool), C.byref(rows()), None), "same")
+
+
 @pytest.mark.parametrize("bad", [dict(k_token=128), dict(k_head=64), dict(v_token=0), dict(n_outer=2), dict(n_outer=2, k_outer=768, v_outer=512)])
 def test_rows_that_run_into_each_other_are_not_read_into(bad):
     for call, pool in ((_abi.lib().rkv_qpages_read, qpages()), (_abi.lib().rkv_pages_read, pages())):
-        refused(1, call(C.byref(pool), C.byref(rows(**bad)), None), "overlap")
+        refused(1, call(C.byref(pool), C.byref(rows(**{"v": 2 * P, **bad})), None), "overlap")
 
 
 @pytest.mark.parametrize("bad", [dict(k_slot=0), dict(v_slot=112), dict(k_head=0), dict(v_page=2048), dict(ks_slot=0), dict(vs_head=8), dict(ks_page=16),
