@@ -194,8 +194,8 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
 }
 
 // How units are shared out.  Of a CU's two workgroups the one that came first is served first: with equal shares of 512 tokens after 32768 the
-// first ones took 257 us and the others 322, of four sequences of 131072 146 and 171.  So shares go by weights, 5 to 4 for workgroups and 7 to 6 for
-// waves, where even the smaller ones hold `least` units; else all hold as many as need be for that.
+// first ones took 257 us and the others 322, of four sequences of 131072 146 and 171.  So shares go by weights, 4 to 3, where even the smaller ones
+// hold `least` units; else all hold as many as need be for that.
 struct Cut {
   int64_t total, share;      // share: of every one, or 0
   int n, n_first, first, second;      // shares of an XCD, those of its CUs' first workgroups, and weights
@@ -282,11 +282,11 @@ __global__ __launch_bounds__(256, 2) void attend_dealt_kernel(const AttendLaunch
   constexpr int kFirst = kShares / 16;      // workgroups of an XCD that are their CU's first
   Cut cut;
   if (at_xcd < n_wide) {
-    cut.set((int64_t)all.wide * A.p.n_kv_heads, n_wide, min(n_wide, kFirst), 5, 4, A.least + all.wide_extra);
+    cut.set((int64_t)all.wide * A.p.n_kv_heads, n_wide, min(n_wide, kFirst), 4, 3, A.least + all.wide_extra);
     take(Flag<false>{}, L.wide, all.wide, all.wide_extra, xcd * n_wide + at_xcd, cut);
   } else {
     const int n_few = kShares / 8 - n_wide;
-    cut.set((int64_t)all.few * A.p.n_kv_heads, 4 * n_few, 4 * max(0, kFirst - n_wide), 7, 6, 1 + all.few_extra);
+    cut.set((int64_t)all.few * A.p.n_kv_heads, 4 * n_few, 4 * max(0, kFirst - n_wide), 4, 3, 1 + all.few_extra);
     take(Flag<true>{}, L.few, all.few, all.few_extra, 4 * (xcd * n_few + at_xcd - n_wide) + uniform(threadIdx.x >> 6), cut);
   }
 }
