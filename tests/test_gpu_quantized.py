@@ -133,6 +133,27 @@ def test_read_of_a_16_bit_pool_and_of_batches(dtype, given):
         assert (held[:, :, 0] == 7).all() and (held[:, :, 4] == 7).all() and (held[:, :, :, 0] == 7).all()
 
 
+@pytest.mark.parametrize("quant", [False, True])
+def test_reads_of_more_than_the_caches_hold(quant):
+    """Rows that go past the L2 caches, slots in any order."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    n, hkv, page = 9001, 8, 100
+    k, v = (torch.randn((n, hkv, 128), device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    slots = torch.randperm(9100, device="cuda", generator=g)[:n].to(torch.int32)
+    if quant:
+        cache = rkv.QuantizedCache.empty(91, hkv, page)
+    else:
+        pool = torch.empty((2, 91, hkv, page, 128), dtype=torch.bfloat16, device="cuda")
+        cache = rkv.PagedCache(pool[0], pool[1])
+    rkv.pages_write(cache, k, v, slots)
+    whole = rkv.pages_read(cache, slots)
+    for part in range(0, n, 3001):      # calls of less
+        for x, y in zip(whole, rkv.pages_read(cache, slots[part:part + 3001])):
+            assert torch.equal(x[part:part + 3001], y)
+    for x, y in zip(whole, (k, v)):
+        assert torch.equal(x, y) if not quant else np.array_equal(f64(x), OG.decode(*OG.encode(f64(y), "bf16")))
+
+
 def test_calls_of_nothing():
     cache = pool_of(3, 2, 4, torch.bfloat16)
     before = bits(cache.k_pages).copy()
