@@ -84,6 +84,16 @@ def test_masks_and_scores(what, kw, width, quant):
 
 
 @pytest.mark.parametrize("quant", [False, True], ids=["rows", "codes"])
+@pytest.mark.parametrize("width", [0, 16384], ids=["tiles", "shares"])
+@pytest.mark.parametrize("page", [16, 30])
+@pytest.mark.parametrize("kw", [dict(), dict(window=64), dict(window=200, slopes=[0.3] * 16), dict(softcap=3.0), dict(causal=False, window=100)],
+                         ids=lambda d: "-".join(d) or "plain")
+def test_more_rows_than_go_at_once(kw, page, width, quant):
+    """Over 2048 rows of a KV head: the prefixes first, then the own slots from those sums on."""
+    Shared(**PROMPTS, hq=16, hkv=1, page=page, seed=17, width=width // page, quant=quant).check(**kw)
+
+
+@pytest.mark.parametrize("quant", [False, True], ids=["rows", "codes"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_long_prefixes_that_share_the_chip(dtype, quant):
     """Prefixes and own slots both split over shares, more rows than a tile, and a group of one sequence."""
@@ -156,10 +166,11 @@ def test_sinks_in_the_prefix_and_in_the_own_slots(dtype, quant):
 @pytest.mark.parametrize("quant", [False, True], ids=["rows", "codes"])
 @pytest.mark.parametrize("window", [0, 120])
 @pytest.mark.parametrize("width", [0, 16384])
-def test_nan_reaches_only_the_rows_that_see_it(window, width, quant):
+@pytest.mark.parametrize("hq", [4, 64], ids=["at-once", "in-two"])
+def test_nan_reaches_only_the_rows_that_see_it(hq, window, width, quant):
     """V of a few slots of the prefix and of the own slots is NaN: windows hide the prefix's from some rows of a tile."""
     lens = [(40, 60), (1, 30), (30, 200), (3, 5)]
-    s = Shared(lens, [100], [4], hq=4, hkv=2, seed=31, width=width // 16, quant=quant)
+    s = Shared(lens, [100], [4], hq=hq, hkv=2, seed=31, width=width // 16, quant=quant)
     kw = dict(window=window) if window else {}
     want, log, weight, reach = s.oracle(**kw)
     bad = [(-1, 40, 5), (-1, 95, 9), (0, 50, 64), (2, 150, 0), (3, 4, 33)]
@@ -192,9 +203,12 @@ def test_pages_outside_the_pool_and_queries_before_the_first_slot():
 @pytest.mark.parametrize("kw", [dict(), dict(window=30), dict(slopes=SLOPES[:4]), dict(causal=False), dict(causal=False, window=30)],
                          ids=lambda d: "-".join(d) or "plain")
 @pytest.mark.parametrize("width", [0, 16384], ids=["tiles", "shares"])
-def test_queries_among_the_prefix(kw, width, quant):
+@pytest.mark.parametrize("hq,hkv", [(4, 2), (16, 1)], ids=["at-once", "in-two"])
+def test_queries_among_the_prefix(hq, hkv, kw, width, quant):
     """More rows than own slots: the first ones' positions lie in the prefix, or before its first slot."""
-    s = Shared([(40, 4), (1, 0), (3, 0), (2, 1), (90, 3), (1, 30)], [70, 20], [4, 2], hq=4, hkv=2, seed=13, width=width // 16, quant=quant)
+    if "slopes" in kw:
+        kw = dict(kw, slopes=[SLOPES[i % 4] for i in range(hq)])
+    s = Shared([(40, 4), (1, 0), (3, 0), (2, 1), (90, 3), (1, 30)], [70, 20], [4, 2], hq=hq, hkv=hkv, seed=13, width=width // 16, quant=quant)
     s.check(**kw)
 
 
@@ -272,7 +286,8 @@ def near(a, b, size, dtype, steps=2):
 @pytest.mark.parametrize("quant", [False, True], ids=["rows", "codes"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("n,groups,own,kw", [(64, 3, 900, dict()), (256, 2, 40, dict()), (100, 90, 700, dict(window=3000)), (40, 2, 2500, dict(softcap=20.0)),
-                                             (48, 2, 300, dict(q=7))], ids=["few", "many", "groups", "capped", "drafts"])
+                                             (48, 2, 300, dict(q=7)), (48, 2, 300, dict(q=40)), (70, 60, 500, dict(q=16, window=2000))],
+                         ids=["few", "many", "groups", "capped", "drafts", "in-two", "groups-in-two"])
 def test_large_batches_equal_attention_over_whole_caches(n, groups, own, kw, dtype, quant):
     """Shares of many items, of both kinds, whose sizes count: against calls in which every sequence's table begins with its prefix's pages."""
     kw = dict(kw)
@@ -290,7 +305,7 @@ def test_large_batches_equal_attention_over_whole_caches(n, groups, own, kw, dty
         k, v = (x.view(total, page, hkv, 128).transpose(1, 2) for x in rkv.pages_read(cache, slots))
     plain, sizes = rkv.PagedCache(k, v), rkv.PagedCache(k, v.abs())
     cache = cache if quant else plain
-    ids, width = iter(rng.permutation(total).tolist()), max(prefixes) // page + own // page + 2
+    ids, width = iter(rng.permutation(total).tolist()), max(prefixes) // page + (own + m) // page + 2
     shared = [[next(ids) for _ in range(p // page)] for p in prefixes]
     table = [[next(ids) for _ in range(-(-x // page))] for x in lens]
     group = np.repeat(np.arange(groups), np.diff(cuts))
@@ -300,7 +315,7 @@ def test_large_batches_equal_attention_over_whole_caches(n, groups, own, kw, dty
     cu = ints([m * i for i in range(n + 1)])
     want, log = rkv.pages_attend(plain, q, whole, all_lens, cu, return_lse=True, **kw)
     size = rkv.pages_attend(sizes, q, whole, all_lens, cu, **kw)
-    args = (q, pad(shared, max(prefixes) // page), ints(prefixes), ints(cuts), pad(table, own // page + 2), ints(lens), cu)
+    args = (q, pad(shared, max(prefixes) // page), ints(prefixes), ints(cuts), pad(table, (own + m) // page + 2), ints(lens), cu)
     got, lse = rkv.pages_attend_shared(cache, *args, return_lse=True, max_q=m, **kw)
     near(got, want, size, dtype)
     assert (lse - log).abs().max() <= 1e-4
