@@ -315,7 +315,9 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
     if constexpr (in_codes(kPool)) {
       const uint8_t byte = scales.at[page * scales.page + h * scales.head + at * scales.slot];
       const uint16_t two = reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(x) + page * page_stride + h * head + at * slot)[lane];
-      return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8((uint32_t)two, scale_of(byte), false));
+      // in the type that the tiles take, where a scale of no write may be infinite
+      if constexpr (kF16) return widen<kF16>(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)two, scale_of(byte), false)));
+      else return widen<kF16>(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)two, scale_of(byte), false)));
     } else {
       return widen<kF16>(reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(x) + page * page_stride + h * head + at * slot)[lane]);
     }

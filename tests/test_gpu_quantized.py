@@ -308,6 +308,30 @@ def test_nan_reaches_only_the_rows_that_see_it(kw, wide):
     compare(filled, lse, want, log, weight, reach, torch.bfloat16, most=200)
 
 
+@pytest.mark.parametrize("wide", [0, 16384])
+def test_a_value_beyond_the_type_reaches_only_the_rows_that_see_it(wide):
+    """448 times 2^23, a scale that no write gives, is finite in 32 bits and infinite in fp16, also where rows that do not see it meet it."""
+    lens = [(150, 150), (40, 200), (3, 90)]
+    c = QCase(lens, hq=4, hkv=2, page=16, dtype=torch.float16, seed=32, width=wide // 16)
+    bad = [(0, 70, 5), (0, 140, 127), (1, 180, 64), (2, 88, 33)]
+    for s, j, d in bad:
+        page, at = int(c.table[s, j // 16]), j % 16
+        c.v[page, :, at] = 0
+        codes = c.cache.v_pages.view(torch.uint8)
+        codes[page, :, at], c.cache.v_scales[page, :, at] = 0, 150
+        codes[page, :, at, d] = 126
+    want, log, weight, reach = OG.attend(f64(c.k), f64(c.v), f64(c.q), c.table, [n for _, n in lens], c.cu)
+    got, lse = rkv.pages_attend(c.cache, c.q, ints(c.table.tolist()), ints([n for _, n in lens]), ints(c.cu), return_lse=True)
+    filled, row = got.clone(), 0
+    for s, (m, n) in enumerate(lens):
+        for i in range(m):
+            hit = [d for t, j, d in bad if t == s and j <= n - m + i]
+            assert not torch.isfinite(got[row][:, hit]).any()
+            filled[row][:, hit] = torch.from_numpy(want[row][:, hit]).to("cuda", torch.float16)
+            row += 1
+    compare(filled, lse, want, log, weight, reach, torch.float16, most=200)
+
+
 def test_pages_outside_the_pool_read_as_zeros():
     c = QCase([(2, 64), (2, 64)], seed=12)
     c.table[0, 1], c.table[0, 2] = 1 << 30, -5
