@@ -436,7 +436,7 @@ typedef struct {
 /* rkv_pages_write into 8 bits.  A row x gets the exponent e, the least with max |x_i| <= 448 2^e (over finite x_i; all zeros: the least there
  * is), cut to [-117, 120] for bf16 and [-15, 8] for fp16, the byte e + 127, and codes x_i 2^-e rounded to nearest even (at the largest e
  * cut to 240 2^e first), NaN for what is not finite.  An x_i is so off by at most 2^-4 of it, or 2^(e - 10) where that is more, and every value
- * is exact in dtype.  Any other bytes stand for what they say, rounded to dtype where they are read.
+ * is exact in dtype.  Any other bytes stand for what they say, rounded to dtype where they are read (255: NaN).
  * rkv_qpages_read gives the values back.  Errors: as rkv_pages_write and rkv_pages_read; null scales, negative scale strides or
  * scales that overlap are RKV_ERR_INVALID_ARG. */
 int rkv_qpages_write(const rkv_qpages* pages, const rkv_rows* rows, void* stream);

@@ -115,6 +115,17 @@ def test_every_code_at_every_scale_reads_as_what_it_stands_for(dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_codes_at_any_other_scale_are_rounded_to_the_type(dtype):
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda").view(2, 128).repeat(256, 1).view(512, 1, 1, 128)
+    scales = torch.arange(256, device="cuda").to(torch.uint8).repeat_interleave(2).view(512, 1, 1)
+    cache = rkv.QuantizedCache(codes.view(E4M3), codes.view(E4M3), scales, scales, dtype)
+    want = torch.from_numpy(OG.decode(codes.cpu().numpy(), scales.cpu().numpy())[:, 0]).to(dtype)      # one rounding: 32 bits hold them all
+    want[510:] = NAN
+    for x in rkv.pages_read(cache, torch.arange(512, dtype=torch.int32, device="cuda")):
+        assert np.array_equal(f64(x), f64(want), equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("given", [False, True])
 def test_read_of_a_16_bit_pool_and_of_batches(dtype, given):
     g = torch.Generator(device="cuda").manual_seed(3)
