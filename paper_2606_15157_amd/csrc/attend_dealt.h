@@ -339,7 +339,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const AttendLau
         const float *from_o = sums_row(A, row, hq, both && !over), *from_m = sums_scale(A, row, hq, both && !over);
         if (word & kParts) {      // cut to the workspace, whatever cu_q and cu_seqs hold
           const bool few = word & kFewRows;
-          const int share = min((where & 0xffff) + k, (few ? 4 : 1) * kShares - 1), rows = few ? A.few_rows : A.slot_rows, at = min(where >> 16, rows - 1);
+          const int share = min((where & 0xffff) + k, (few ? 4 : 1) * kShares - 1), rows = few ? A.few_rows : A.slot_rows, at = min((int)((uint32_t)where >> 16), rows - 1);
           const float* from = few ? few_slot(A, k ? 2 * share : 2 * share + 1) : part_slot(A, k ? 2 * share : 2 * share + 1);
           from_o = from + at * kHeadDim;
           from_m = from + rows * kHeadDim + 2 * at;
