@@ -220,6 +220,25 @@ def test_cu_seqs_outside_their_range_are_cut():
     assert torch.equal(rkv.pages_attend_shared(s.c.cache, q, shared, plens, ints([-5, 1 << 30]), table, lens, cu), want)
 
 
+@pytest.mark.parametrize("what", SETS)
+@pytest.mark.parametrize("quant", [False, True], ids=["rows", "codes"])
+def test_pages_behind_4_gib(quant, what):
+    """The same pages at the end of a pool of more than 2^32 bytes give the same bits, few rows and many."""
+    s = Shared(**SETS[what], hq=8, hkv=2, quant=quant, seed=41)
+    small, held = s.c.cache, ("k_pages", "v_pages") + (("k_scales", "v_scales") if quant else ())
+    pools = [getattr(small, x) for x in held]
+    first = 2 ** 32 // (pools[0][0].numel() * pools[0].element_size()) + 1
+    far = [torch.empty((first + small.n_pages, *x.shape[1:]), dtype=x.dtype, device="cuda") for x in pools]
+    for x, y in zip(far, pools):
+        x.view(torch.uint8)[first:] = y.contiguous().view(torch.uint8)
+    cache = rkv.QuantizedCache(*far, s.dtype) if quant else rkv.PagedCache(*far)
+    q, shared, plens, cu_seqs, table, lens, cu = s.args()
+    for kw in (dict(), dict(window=40)):
+        want = rkv.pages_attend_shared(small, *s.args(), return_lse=True, **kw)
+        got = rkv.pages_attend_shared(cache, q, shared + first, plens, cu_seqs, table + first, lens, cu, return_lse=True, **kw)
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
 @pytest.mark.parametrize("quant", [False, True], ids=["rows", "codes"])
 def test_repeats_graphs_and_streams_give_the_same_bits(quant):
     """Eager, on a side stream, and in two captured graphs that run beside each other, with other work between replays."""
