@@ -416,7 +416,8 @@ int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream);
 
 /* The way back: row (o, t, h) of `rows` (whose k and v are written) becomes what lies in slot slots[o n_tokens + t], zeros for a slot outside
  * [0, n_pages * page_size).  Slots may repeat.  Errors: as rkv_pages_write, with the rows' own dimensions in the place of the pool's: they may not
- * run into each other, nor k's into v's (one pointer for both is refused), while an overlapping pool can be read. */
+ * run into each other, while an overlapping pool can be read; nor may k's rows run into v's (RKV_ERR_INVALID_ARG): they lie apart, or between each
+ * other by the same strides ([tokens, 2, heads, d], slices of one buffer).  The rows may not lie in slots that are read. */
 int rkv_pages_read(const rkv_pages* pages, const rkv_rows* rows, void* stream);
 
 /* A pool held in 8 bits: rows of 128 codes in OCP e4m3 (no infinities, NaN 0x7f and 0xff), one byte each, and for each row of K

@@ -584,7 +584,8 @@ def pages_write(cache, k, v, slots, *, stream=None):
 def pages_read(cache, slots, *, k_out=None, v_out=None, stream=None):
     """Rows back from their slots (rkv_pages_read, rkv_qpages_read): slots int32 [T] or [B, n], zeros for a slot outside the pool (-1); the
     same slot may come twice.  Returns k, v [T, Hkv, d] or [B, n, Hkv, d] of the pool's type: k_out and v_out if given, of any strides that are
-    multiples of 8 (out.permute(0, 2, 1, 3) of [B, Hkv, n, d], what evict_prefill takes).  No backward pass: tensors that require
+    multiples of 8 (out.permute(0, 2, 1, 3) of [B, Hkv, n, d], what evict_prefill takes).  k_out and v_out share no element (refused): two
+    pieces of memory, or slices of one buffer with the same strides.  Neither lies in slots that are read.  No backward pass: tensors that require
     gradients are refused unless gradients are off."""
     dev = cache.device
     _refuse_gradients("pages_read", cache.k_pages, cache.v_pages, k_out, v_out)

@@ -45,6 +45,42 @@ bool rows_nest(std::array<Dim, kDims> dims, __int128 extent = rkv::kHeadDim) {
   return true;
 }
 
+// Rows of `extent` elements of `size` bytes from `at` on, told apart by their dimensions as above.
+struct Rows {
+  const void* at;
+  int size;
+  __int128 extent;
+  std::array<Dim, 3> dims;
+};
+// Whether a row of x and a row of y may share a byte, from the i-th largest stride of each on, y `apart` elements behind x.  Apart they are
+// where all of one lies behind all of the other; else, of slices along one stride that both have, each can only meet the two that
+// are less than it away, for a slice is no longer than the stride.  Where both lie in one piece of memory by different strides they count as met.
+bool slices_meet(const std::array<Dim, 4>& x, const std::array<Dim, 4>& y, const std::array<__int128, 4>& x_extent, const std::array<__int128, 4>& y_extent, int i,
+                 __int128 apart) {
+  if (apart >= x_extent[i] || -apart >= y_extent[i]) return false;
+  const Dim &dx = x[i], &dy = y[i];
+  if (dx.count == 0 || dx.stride != dy.stride) return true;     // rows, or strides that differ
+  const __int128 s = dx.stride;
+  __int128 d = -apart / s - (-apart % s < 0);                  // rounded down
+  for (int k = 0; k < 2; ++k, ++d)
+    if (d > -dx.count && d < dy.count && slices_meet(x, y, x_extent, y_extent, i + 1, apart + d * s)) return true;
+  return false;
+}
+bool rows_meet(const Rows& x, const Rows& y) {
+  std::array<Dim, 4> dims[2] = {};           // those of more than one entry, the largest stride first, then {0, 0}
+  std::array<__int128, 4> extents[2] = {};   // of what the strides from i on reach
+  for (int k = 0; k < 2; ++k) {
+    const Rows& r = k ? y : x;
+    int n = 0;
+    for (const Dim& d : r.dims)
+      if (d.count > 1) dims[k][n++] = d;
+    std::sort(dims[k].begin(), dims[k].begin() + n, [](const Dim& a, const Dim& b) { return a.stride > b.stride; });
+    extents[k].fill(r.extent);
+    for (int i = n - 1; i >= 0; --i) extents[k][i] = extents[k][i + 1] + (__int128)dims[k][i].stride * (dims[k][i].count - 1);
+  }
+  return slices_meet(dims[0], dims[1], extents[0], extents[1], 0, ((__int128)(uintptr_t)y.at - (__int128)(uintptr_t)x.at) / x.size);
+}
+
 template <class Pages>
 int check_pool(const Pages* p) {
   if (!p) return rkv::fail(RKV_ERR_INVALID_ARG, "null pages");
@@ -197,9 +233,12 @@ int check_rows(const Pool& pool, const rkv_rows* rows, bool written) {
   if (int st = check_layout("v rows", rows->v, {rows->v_outer, rows->v_token, rows->v_head})) return st;
   if (written && rows->k == rows->v) return rkv::fail(RKV_ERR_INVALID_ARG, "k and v are read into the same rows");
   const int32_t heads = pool.p.n_kv_heads;
-  if (written && (!rows_nest<3>({{{rows->k_outer, rows->n_outer}, {rows->k_token, rows->n_tokens}, {rows->k_head, heads}}}) ||
-                  !rows_nest<3>({{{rows->v_outer, rows->n_outer}, {rows->v_token, rows->n_tokens}, {rows->v_head, heads}}})))
+  const Rows k{rows->k, 2, rkv::kHeadDim, {{{rows->k_outer, rows->n_outer}, {rows->k_token, rows->n_tokens}, {rows->k_head, heads}}}};
+  const Rows v{rows->v, 2, rkv::kHeadDim, {{{rows->v_outer, rows->n_outer}, {rows->v_token, rows->n_tokens}, {rows->v_head, heads}}}};
+  if (written && (!rows_nest(k.dims) || !rows_nest(v.dims)))
     return rkv::fail(RKV_ERR_INVALID_ARG, "the rows to be read into overlap (no stride may be less than the extent of the smaller ones)");
+  if (written && rows_meet(k, v))
+    return rkv::fail(RKV_ERR_INVALID_ARG, "k's rows to be read into overlap v's (they lie apart, or between each other by the same strides)");
   return RKV_OK;
 }
 int check_written(const Pool& pool) {

@@ -145,6 +145,28 @@ def test_read_of_a_16_bit_pool_and_of_batches(dtype, given):
 
 
 @pytest.mark.parametrize("quant", [False, True])
+def test_k_and_v_are_read_between_each_other_but_not_into_each_other(quant):
+    """Slices of one buffer with the same strides, beside each other in its tokens, its heads and its rows."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    pool = torch.randn((2, 9, 3, 7, 128), device="cuda", generator=g).to(torch.bfloat16)
+    cache = pool_of(9, 3, 7, torch.bfloat16, seed=6) if quant else rkv.PagedCache(pool[0], pool[1])
+    slots = torch.randint(-4, 67, (11,), device="cuda", generator=g).to(torch.int32)
+    want = rkv.pages_read(cache, slots)
+    empty = lambda *s: torch.full((*s, 128), 7.0, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    tokens, heads, rows, even = empty(11, 2, 3), empty(11, 8), empty(11, 3, 2), empty(30, 3)
+    for k, v in ((tokens[:, 0], tokens[:, 1]), (heads[:, 4:7], heads[:, 1:4]), (rows[:, :, 1], rows[:, :, 0]), (even[::2][:11], even[7::2][:11])):
+        for x, y in zip(rkv.pages_read(cache, slots, k_out=k, v_out=v), want):
+            assert torch.equal(x.view(torch.int16), y.view(torch.int16))      # also what is NaN
+    assert (heads[:, [0, 7]] == 7).all() and (even[[1, 3, 5, 22, 24, 26, 28]] == 7).all()
+    for k, v in ((heads[:, 0:3], heads[:, 2:5]), (even[::2][:11], even[6::2][:11]), (even[:11], even[10:21]), (heads[:, :3], heads[:, :3])):
+        before = [x.clone() for x in (heads, even)]
+        with pytest.raises(rkv.RkvError):
+            rkv.pages_read(cache, slots, k_out=k, v_out=v)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in zip(before, (heads, even)))
+
+
+@pytest.mark.parametrize("quant", [False, True])
 def test_reads_of_more_than_the_caches_hold(quant):
     """Rows that go past the L2 caches, slots in any order."""
     g = torch.Generator(device="cuda").manual_seed(9)

@@ -125,6 +125,58 @@ def test_rows_that_run_into_each_other_are_not_read_into(bad):
         refused(1, call(C.byref(pool), C.byref(rows(**{"v": 2 * P, **bad})), None), "overlap")
 
 
+LAYOUTS = [
+    (0, dict(v=2 * P)), (1, dict(v=P + 2 * 64)), (1, dict(v=P + 2 * 384)), (1, dict(v=P + 2 * 760)), (0, dict(v=P + 2 * 768)), (0, dict(v=P - 2 * 768)), (1, dict(v=P - 2 * 760)),
+    # heads 2 .. 3 and 1 .. 2 of one buffer of four; 0 .. 1 and 2 .. 3
+    (1, dict(k=P + 512, v=P + 256, k_token=512, v_token=512)), (0, dict(v=P + 512, k_token=512, v_token=512)),
+    # [tokens, heads, 2, d], even and odd tokens, and even ones with later even ones
+    (0, dict(v=P + 256, k_head=256, v_head=256, k_token=512, v_token=512)), (0, dict(v=P + 2 * 256 * 5, k_token=512, v_token=512, n_tokens=40)),
+    (1, dict(v=P + 2 * 256 * 6, k_token=512, v_token=512, n_tokens=40)), (1, dict(v=P - 2 * 256 * 6, k_token=512, v_token=512, n_tokens=40)),
+    # [batch, heads, tokens, d] of one allocation, and the second beginning in the first's last row
+    (0, dict(v=P + 2 * 768, k_head=384, k_token=128, v_head=384, v_token=128)), (1, dict(v=P + 2 * 640, k_head=384, k_token=128, v_head=384, v_token=128)),
+    # the same memory by other strides; strides of dimensions of one do not count
+    (1, dict(v=P + 2 * 128, v_token=128, v_head=512)), (0, dict(v=P + 512, k_token=512, v_token=512, k_outer=8, v_outer=1 << 40))]
+
+
+@pytest.mark.parametrize("met,layout", [x for x in LAYOUTS if x[0]])
+def test_rows_of_k_are_not_read_into_those_of_v(met, layout):
+    for call, pool in ((_abi.lib().rkv_qpages_read, qpages()), (_abi.lib().rkv_pages_read, pages())):
+        refused(1, call(C.byref(pool), C.byref(rows(**layout)), None), "overlap")
+
+
+def elements(at, counts, strides):
+    got = np.array([at])
+    for n, s in zip(counts, strides):
+        got = (got[:, None] + s * np.arange(n)).ravel()
+    return (got[:, None] + np.arange(128)).ravel()
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="without a GPU a call that is not refused ends at its launch")
+def test_rows_are_refused_for_an_element_that_k_and_v_share_and_for_no_other_reason():
+    """All layouts above, and drawn ones of equal strides, against the sets of their elements."""
+    rng = np.random.default_rng(7)
+    names = [("k_outer", "v_outer"), ("k_token", "v_token"), ("k_head", "v_head")]
+    tried = [(2, rows(**x)) for _, x in LAYOUTS]
+    for _ in range(600):
+        counts = [int(x) for x in rng.integers(1, 5, 3)]
+        strides, extent = [0] * 3, 128
+        for i in rng.permutation(3):
+            strides[i] = extent + 8 * int(rng.integers(0, 40))
+            extent += strides[i] * (counts[i] - 1)
+        far = 8 * int(rng.integers(-extent // 8 - 8, extent // 8 + 8))      # elements from k to v
+        if rng.random() < 0.5:
+            far = sum(int(d) * s for d, s in zip(rng.integers(-4, 5, 3), strides)) + 8 * int(rng.integers(-17, 18))
+        tried.append((counts[2], rows(v=P + 2 * far, n_outer=counts[0], n_tokens=counts[1], **{x: s for pair, s in zip(names, strides) for x in pair})))
+    seen = [0, 0]
+    for heads, r in tried:
+        counts = (r.n_outer, r.n_tokens, heads)
+        meet = np.intersect1d(*(elements((getattr(r, "kv"[i]) - P) // 2, counts, [getattr(r, pair[i]) for pair in names]) for i in range(2))).size > 0
+        got = _abi.lib().rkv_pages_read(C.byref(pages(n_kv_heads=heads)), C.byref(r), None)
+        assert got == (1 if meet else 6), (meet, got, [(n, getattr(r, n)) for n, _ in r._fields_])
+        seen[meet] += 1
+    assert min(seen) >= 100, seen
+
+
 @pytest.mark.parametrize("bad", [dict(k_slot=0), dict(v_slot=112), dict(k_head=0), dict(v_page=2048), dict(ks_slot=0), dict(vs_head=8), dict(ks_page=16),
                                  dict(vs_slot=2)])
 def test_overlapping_pools_are_not_written(bad):
