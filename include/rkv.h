@@ -408,8 +408,9 @@ typedef struct {
 /* Copies new K and V rows to their slots, bit-exactly.  A row whose slot is outside [0, n_pages * page_size) is
  * skipped (padding).  Slots that are not skipped must be distinct.
  * The pool's rows may not overlap: its dimensions of more than one entry taken by stride, no stride is less than the extent of
- * the smaller ones (128 elements for the smallest).  An overlapping pool can be attended.
- * Errors: RKV_ERR_INVALID_ARG (null pointers, negative sizes or strides, unknown dtype, a pool whose rows overlap), RKV_ERR_UNSUPPORTED (head_dim
+ * the smaller ones (128 elements for the smallest).  Nor may k's rows overlap v's: they lie apart, or between each other by the same strides, or
+ * k and v are one pool, which v's rows are left in.  An overlapping pool can be attended.
+ * Errors: RKV_ERR_INVALID_ARG (null pointers, negative sizes or strides, unknown dtype, pools whose rows overlap), RKV_ERR_UNSUPPORTED (head_dim
  * != 128, pointers not 16-byte aligned, strides not multiples of 8, n_outer * n_tokens * n_kv_heads above 2^28 - 16, 2^31 slots),
  * RKV_ERR_HIP. */
 int rkv_pages_write(const rkv_pages* pages, const rkv_rows* rows, void* stream);
@@ -438,8 +439,8 @@ typedef struct {
  * is), cut to [-117, 120] for bf16 and [-15, 8] for fp16, the byte e + 127, and codes x_i 2^-e rounded to nearest even (at the largest e
  * cut to 240 2^e first), NaN for what is not finite.  An x_i is so off by at most 2^-4 of it, or 2^(e - 10) where that is more, and every value
  * is exact in dtype.  Any other bytes stand for what they say, rounded to dtype where they are read (255: NaN).
- * rkv_qpages_read gives the values back.  Errors: as rkv_pages_write and rkv_pages_read; null scales, negative scale strides or
- * scales that overlap are RKV_ERR_INVALID_ARG. */
+ * rkv_qpages_read gives the values back.  Errors: as rkv_pages_write and rkv_pages_read; null scales, negative scale strides and,
+ * in writes, scales that overlap each other or codes are RKV_ERR_INVALID_ARG (one pool for k and v has one array of scales, too). */
 int rkv_qpages_write(const rkv_qpages* pages, const rkv_rows* rows, void* stream);
 int rkv_qpages_read(const rkv_qpages* pages, const rkv_rows* rows, void* stream);
 

@@ -66,7 +66,14 @@ bool slices_meet(const std::array<Dim, 4>& x, const std::array<Dim, 4>& y, const
     if (d > -dx.count && d < dy.count && slices_meet(x, y, x_extent, y_extent, i + 1, apart + d * s)) return true;
   return false;
 }
+__int128 whole(const Rows& r) {
+  __int128 extent = r.extent;
+  for (const Dim& d : r.dims) extent += (__int128)d.stride * (d.count - 1);
+  return extent;
+}
 bool rows_meet(const Rows& x, const Rows& y) {
+  const __int128 apart = ((__int128)(uintptr_t)y.at - (__int128)(uintptr_t)x.at) / x.size;
+  if (apart >= whole(x) || -apart >= whole(y)) return false;      // as in most calls
   std::array<Dim, 4> dims[2] = {};           // those of more than one entry, the largest stride first, then {0, 0}
   std::array<__int128, 4> extents[2] = {};   // of what the strides from i on reach
   for (int k = 0; k < 2; ++k) {
@@ -78,7 +85,13 @@ bool rows_meet(const Rows& x, const Rows& y) {
     extents[k].fill(r.extent);
     for (int i = n - 1; i >= 0; --i) extents[k][i] = extents[k][i + 1] + (__int128)dims[k][i].stride * (dims[k][i].count - 1);
   }
-  return slices_meet(dims[0], dims[1], extents[0], extents[1], 0, ((__int128)(uintptr_t)y.at - (__int128)(uintptr_t)x.at) / x.size);
+  return slices_meet(dims[0], dims[1], extents[0], extents[1], 0, apart);
+}
+
+bool rows_same(const Rows& x, const Rows& y) {
+  bool same = x.at == y.at;
+  for (size_t i = 0; i < x.dims.size(); ++i) same &= x.dims[i].count <= 1 || x.dims[i].stride == y.dims[i].stride;
+  return same;
 }
 
 template <class Pages>
@@ -243,12 +256,22 @@ int check_rows(const Pool& pool, const rkv_rows* rows, bool written) {
 }
 int check_written(const Pool& pool) {
   const rkv_pages& p = pool.p;
-  bool apart = rows_nest<3>({{{p.k_page, p.n_pages}, {p.k_head, p.n_kv_heads}, {p.k_slot, p.page_size}}}) &&
-               rows_nest<3>({{{p.v_page, p.n_pages}, {p.v_head, p.n_kv_heads}, {p.v_slot, p.page_size}}});
-  for (const rkv::Scales& x : {pool.ks, pool.vs})
-    apart &= !pool.codes || rows_nest<3>({{{x.page, p.n_pages}, {x.head, p.n_kv_heads}, {x.slot, p.page_size}}}, 1);
+  const int size = pool.codes ? 1 : 2;
+  auto rows = [&](const void* at, __int128 extent, int64_t page, int64_t head, int64_t slot) {
+    return Rows{at, size, extent, {{{page, p.n_pages}, {head, p.n_kv_heads}, {slot, p.page_size}}}};
+  };
+  const Rows k = rows(p.k, rkv::kHeadDim, p.k_page, p.k_head, p.k_slot), v = rows(p.v, rkv::kHeadDim, p.v_page, p.v_head, p.v_slot);
+  const Rows ks = rows(pool.ks.at, 1, pool.ks.page, pool.ks.head, pool.ks.slot), vs = rows(pool.vs.at, 1, pool.vs.page, pool.vs.head, pool.vs.slot);
+  bool apart = rows_nest(k.dims) && rows_nest(v.dims);
+  if (pool.codes) apart = apart && rows_nest(ks.dims, 1) && rows_nest(vs.dims, 1);
   if (!apart)
     return rkv::fail(RKV_ERR_INVALID_ARG, "the pool's rows overlap (no stride may be less than the extent of the smaller ones): it can be read, not written");
+  // A pool whose values are its keys is written twice by the same lanes in order; any other byte that two rows share is a race.
+  const bool one = rows_same(k, v) && (!pool.codes || rows_same(ks, vs));
+  bool met = !one && rows_meet(k, v);
+  if (pool.codes) met = met || (!one && rows_meet(ks, vs)) || rows_meet(k, ks) || rows_meet(k, vs) || rows_meet(v, ks) || rows_meet(v, vs);
+  if (met)
+    return rkv::fail(RKV_ERR_INVALID_ARG, "k's and v's pages, or their scales, overlap (they lie apart, or between each other by the same strides): they can be read, not written");
   return RKV_OK;
 }
 rkv::WriteLaunch rows_launch(const Pool& pool, const rkv_rows* rows) {

@@ -144,6 +144,26 @@ def test_read_of_a_16_bit_pool_and_of_batches(dtype, given):
         assert (held[:, :, 0] == 7).all() and (held[:, :, 4] == 7).all() and (held[:, :, :, 0] == 7).all()
 
 
+def test_a_pool_in_one_buffer_is_one_of_four():
+    """Codes and scales of K and V side by side in each slot: the same bytes as apart; the same scales for both are refused."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    record = torch.full((6, 3, 8, 272), 7, dtype=torch.uint8, device="cuda")
+    codes = [record[..., :128].view(E4M3), record[..., 128:256].view(E4M3)]
+    cache, apart = rkv.QuantizedCache(*codes, record[..., 256], record[..., 257]), pool_of(6, 3, 8, torch.bfloat16)
+    k, v = (torch.randn((30, 3, 128), device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    slots = torch.randperm(48, device="cuda", generator=g)[:30].to(torch.int32)
+    before = record.clone()
+    with pytest.raises(rkv.RkvError, match="overlap"):
+        rkv.pages_write(rkv.QuantizedCache(*codes, record[..., 256], record[..., 256]), k, v, slots)
+    torch.cuda.synchronize()
+    assert torch.equal(before, record)
+    for c in (cache, apart):
+        rkv.pages_write(c, k, v, slots)
+    assert (record[..., 258:] == 7).all()
+    for x, y in zip(rkv.pages_read(cache, slots), rkv.pages_read(apart, slots)):
+        assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("quant", [False, True])
 def test_k_and_v_are_read_between_each_other_but_not_into_each_other(quant):
     """Slices of one buffer with the same strides, beside each other in its tokens, its heads and its rows."""

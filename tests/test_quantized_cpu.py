@@ -183,6 +183,37 @@ def test_overlapping_pools_are_not_written(bad):
     refused(1, _abi.lib().rkv_qpages_write(C.byref(qpages(**bad)), C.byref(rows()), None), "overlap")
 
 
+# Pools of 4 pages of 2 heads of 16 slots: 16 KiB of codes (32 KiB in 16 bits) and 128 scales.
+APART = dict(v=2 * P, v_scale=P // 2 + 128, k_scale=P // 2)
+
+
+@pytest.mark.parametrize("bad", [dict(v=P + 128), dict(v=P + 16384 - 16), dict(v=P - 16384 + 128), dict(v_scale=P // 2), dict(v_scale=P // 2 + 127),
+                                 dict(v_scale=P + 5), dict(k_scale=P + 16383), dict(k_scale=2 * P, v_scale=2 * P + 128), dict(v=P), dict(v=P, v_scale=P // 2, k_page=8192),
+                                 dict(k_slot=144, k_head=2304, k_page=4608, k_scale=P + 127, ks_slot=144, ks_head=2304, ks_page=4608)])
+def test_written_pools_of_k_and_v_do_not_run_into_each_other(bad):
+    refused(1, _abi.lib().rkv_qpages_write(C.byref(qpages(**{**APART, **bad})), C.byref(rows()), None), "overlap")
+
+
+@pytest.mark.parametrize("bad", [dict(v=P + 256), dict(v=P + 32768 - 16), dict(v=P - 32768 + 16), dict(v=P, v_slot=256, v_head=128 * 32, v_page=128 * 64)])
+def test_written_16_bit_pools_do_not_run_into_each_other(bad):
+    pool = dict(k_page=4096, k_head=2048, k_slot=128, v_page=4096, v_head=2048, v_slot=128)
+    refused(1, _abi.lib().rkv_pages_write(C.byref(pages(**{**pool, **bad})), C.byref(rows()), None), "overlap")
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="without a GPU a call that is not refused ends at its launch")
+def test_pools_that_share_no_byte_are_written():
+    """Codes and scales in one piece of memory: a record a slot, a block a page, K and V by turns; and a pool whose values are its keys."""
+    slot = dict(k_slot=144, k_head=2304, k_page=4608, k_scale=P + 128, ks_slot=144, ks_head=2304, ks_page=4608)
+    block = dict(k_page=8192 + 64, v=P + 4096, v_page=8192 + 64, k_scale=P + 8192, ks_page=8192 + 64, v_scale=P + 8192 + 32, vs_page=8192 + 64)
+    pairs = dict(k_slot=256, k_head=4096, k_page=8192, v=P + 128, v_slot=256, v_head=4096, v_page=8192)
+    one = dict(v=P, v_scale=P // 2)
+    for good in (dict(), dict(v=P + 16384), dict(v=P - 16384, v_scale=P // 2 - 128), slot, block, pairs, one):
+        assert _abi.lib().rkv_qpages_write(C.byref(qpages(**{**APART, **good})), C.byref(rows()), None) == 6, good
+    pool = dict(k_page=4096, k_head=2048, k_slot=128, v_page=4096, v_head=2048, v_slot=128)
+    for good in (dict(), dict(v=P + 32768), dict(k_page=8192, v=P + 8192, v_page=8192), dict(k_slot=256, k_head=4096, k_page=8192, v=P + 256, v_slot=256, v_head=4096, v_page=8192)):
+        assert _abi.lib().rkv_pages_write(C.byref(pages(**{**pool, **good})), C.byref(rows()), None) == 6, good
+
+
 @pytest.mark.parametrize("status,bad", [
     (1, dict(q=None)), (1, dict(out=None)), (1, dict(lens=None)), (1, dict(table=None)), (1, dict(n_seqs=-1)), (1, dict(window=-1)), (1, dict(causal=2)),
     (1, dict(scale=float("nan"))), (1, dict(softcap=-1.0)), (4, dict(softcap=600.0)), (1, dict(out_token=0)), (2, dict(n_q_heads=3)), (2, dict(cu_q=None)),
