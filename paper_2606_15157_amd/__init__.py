@@ -646,7 +646,8 @@ def pages_attend_shared(cache, q, shared_table, shared_lens, cu_seqs, table, len
     shared_table int32 [n_groups, max_pages] and shared_lens int32 [n_groups]: pages and slots of each prefix (a sequence of `pages_init`'s
     tables, or rows of its own); cu_seqs int32 [n_groups + 1]: sequences cu_seqs[g] .. cu_seqs[g + 1] - 1 begin with prefix g, others
     with none; table, lens, cu_q and all else as in pages_attend, with only what follows the prefix in table and lens.  The result is that of
-    pages_attend on caches in which each sequence's slots follow its prefix's.  max_shared: the most slots of a prefix, if known.  No backward
+    pages_attend on caches in which each sequence's slots follow its prefix's (a row whose position there lies in the prefix sees it up to
+    that position, if causal).  max_shared: the most slots of a prefix, if known.  No backward
     pass: tensors that require gradients are refused unless gradients are off."""
     dev = cache.device
     _refuse_gradients("pages_attend_shared", q, cache.k_pages, cache.v_pages, slopes, out, lse_out)
