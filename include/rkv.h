@@ -512,9 +512,10 @@ typedef struct {
 
 /* rkv_pages_attend of sequences that share prefixes: the result is that of caches in which each sequence's own slots follow its
  * group's prefix: positions, windows and distances count from the prefix's first slot, and with causal a row at position p sees no slot behind
- * p, of the prefix or its own.  (Rows see all of a prefix but where a sequence has more rows than own slots and one: the first of these
- * have positions in the prefix, or before its first slot, where they see nothing.  With causal 0 only a window hides slots.)  Each prefix
- * is read once for the rows of all its sequences instead of once for each; a row's sums over its prefix are held in 32 bits between the two.  A group of one sequence is allowed, as is a prefix of no slots.
+ * p, of the prefix or its own.  (Windows aside, rows see all of a prefix but where a sequence has more rows than own slots and one: the
+ * first of these have positions in the prefix, or before its first slot, where they see nothing.  With causal 0 only a window hides slots.)
+ * Each prefix is read once for the rows of all its sequences instead of once for each; a row's sums over its prefix are held in 32 bits
+ * between the two.  A group of one sequence is allowed, as is a prefix of no slots.
  * ws: as rkv_pages_attend; it holds 528 or 1056 bytes for each row and query head besides.
  * Errors: as rkv_pages_attend; RKV_ERR_UNSUPPORTED also for prefix_lens or first_keys, and where a prefix and a sequence
  * could hold 2^31 - 1024 slots together; RKV_ERR_SHAPE for a shared table whose stride is less than max_pages. */

@@ -471,8 +471,10 @@ class PagedCache:
 class QuantizedCache:
     """A pool of K and V pages held in 8 bits (rkv_qpages): k_pages, v_pages torch.float8_e4m3fn [n_pages, Hkv, page_size, 128], any strides
     that are multiples of 16 with the last dimension dense; k_scales, v_scales uint8 [n_pages, Hkv, page_size], any strides: a row's
-    values are its codes times 2^(byte - 127).  dtype: bf16 or fp16, of the rows written and read and of queries.  Rows that
-    `pages_write` put here come back exact in dtype, each within 2^-4 of what was written."""
+    values are its codes times 2^(byte - 127).  dtype: bf16 or fp16, of the rows written and read and of queries.
+    A value x that `pages_write` puts here comes back exact in dtype and off by at most 2^-4 |x| or 2^(e - 10), whichever is more, where e is
+    its row's exponent (the least with max |x_i| <= 448 2^e): values below 2^-18 or so of their row's largest may come back as 0.  What is
+    not finite comes back as NaN.  A pool that is written holds k_pages, v_pages and the scales in bytes of their own (or is one for K and V)."""
 
     def __init__(self, k_pages, v_pages, k_scales, v_scales, dtype=None):
         torch = _torch()
