@@ -7,7 +7,7 @@ import torch
 
 import paper_2606_15157_amd as rkv
 from oracle import pages as OG
-from test_gpu_paged import Case, FEW, MANY, NAN, ONE, compare, f64, ints
+from test_gpu_paged import Case, FEW, HALF, MANY, NAN, ONE, compare, f64, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -403,6 +403,32 @@ def test_the_same_as_attention_over_the_rows_read_back():
     b = rkv.pages_attend(rkv.PagedCache(c.k, c.v), *args)
     # both round probabilities and outputs to bf16 (half a step each), of |p| |v| sums within 4 of the largest output here
     assert (a.float() - b.float()).abs().max() <= 4 * 2.0 ** -8 * 4 * b.float().abs().max()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("lens,width", [([(1, 500), (20, 300), (1, 64), (130, 700)], 0), ([(1, 5000), (20, 3000), (3, 4100), (1, 70)], 16384)], ids=["tiles", "shares"])
+@pytest.mark.parametrize("kw", [dict(), dict(window=300), dict(softcap=3.0)], ids=lambda d: "-".join(d) or "plain")
+def test_each_value_is_that_of_attention_over_the_rows_read_back(kw, lens, width, dtype):
+    """Both calls have the same operands: each output is off by half a step of itself, and by half a step of the probabilities of its own
+    sum p |v|; what the scores' 32-bit sums add is `compare`'s bound, for either call."""
+    c = QCase(lens, hq=8, hkv=2, seed=14, width=width // 16, dtype=dtype)
+    slots = torch.cat([t[:-(-n // 16)].long().repeat_interleave(16) * 16 + torch.arange(-(-n // 16) * 16) % 16 for t, (_, n) in zip(torch.as_tensor(c.table), lens)])
+    k, v = torch.full_like(c.k, NAN), torch.full_like(c.v, NAN)
+    for to, x in zip((k, v), rkv.pages_read(c.cache, slots.to("cuda", torch.int32))):
+        to[(slots // 16).cuda(), :, (slots % 16).cuda()] = x
+    args = (c.q, ints(c.table.tolist()), ints([n for _, n in lens]), ints(c.cu))
+    a, lse = rkv.pages_attend(c.cache, *args, return_lse=True, **kw)
+    b, log = rkv.pages_attend(rkv.PagedCache(k, v), *args, return_lse=True, **kw)
+    size = rkv.pages_attend(rkv.PagedCache(k, v.abs()), *args, **kw).float() / (1 - 2 * HALF[dtype])      # itself short by two half steps at most
+    _, _, _, reach = OG.attend(f64(c.k), f64(c.v), f64(c.q), c.table, [n for _, n in lens], c.cu, **kw)
+    reach = torch.from_numpy(reach).cuda()
+    score = 2.0 ** -24 * (148 * reach + 16 * kw.get("softcap", 0.0) + 8)
+    assert ((lse - log).abs() <= 2 * (score + 2.0 ** -13 * 0.01 + 2.0 ** -22 * log.abs())).all()
+    most = max(n for _, n in lens)
+    tiny = 2.0 ** -25 * most if dtype == torch.float16 else 0.0
+    # |a| exceeds |b| by less than what is allowed here, so that 1.02 covers half a step of either
+    bound = 2 * (HALF[dtype] * (size + b.float().abs()) * 1.02 + (2 * score[..., None] + 2.0 ** -15) * size + tiny)
+    assert ((a.float() - b.float()).abs() <= bound).all()
 
 
 def test_repeats_are_bit_equal_on_a_side_stream_and_under_a_graph():
