@@ -42,10 +42,11 @@ constexpr int kPrefixed = 1 << 15;
 struct Totals {
   int wide, few, wide_items, few_items, n_wide, wide_extra, few_extra;
 };
-// Workgroups (of the kShares / 8 of an XCD) for the wide tiles, so that either side ends at the same time.  Measured, us: a wide tile's 64 keys
-// take a workgroup 1.6, in 8 bits 2.3 (their way into LDS is by registers); those of a narrow one take a wave 5 to 6, or 3 in 8 bits, as long
-// as the chip's memory does not bound them, and a narrow item 6 to 8 besides; a workgroup has four waves.  (2.0 for 2.3: 128 requests in eight groups
-// 215 -> 196 us, all in one 115 -> 118, 64 in one 43.5 -> 47.)
+// Workgroups (of the kShares / 8 of an XCD) for the wide tiles, so that either side ends at the same time.  By time stamps, us: a wide tile's 64 keys
+// take a workgroup 1.8, in 8 bits 2.1 (their way into LDS is by registers); those of a narrow one take a wave 5 to 6, or 3 in 8 bits, as long
+// as the chip's memory does not bound them, and a narrow item 6 to 8 besides; a workgroup has four waves.  The weights below, 1.6 and 2.3, are from
+// before 8-bit codes went to LDS beside the products, and no rule for all shapes: with 2.0 for 2.3 128 requests in eight groups take 196 us for
+// 215, but all in one 118 for 115, and 64 in one 47 for 43.5.
 template <Pool kPool>
 __device__ __forceinline__ int wide_workgroups(const Totals& all) {
   constexpr int kMost = kShares / 8;

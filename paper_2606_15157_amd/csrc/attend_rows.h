@@ -394,8 +394,8 @@ __device__ __forceinline__ bool attend_row_by_row(const AttendLaunch& A, Bounds&
   return true;
 }
 
-// kCap: capped scores, kBias: less a slope times the distance; kShared: one of the two launches of a call whose sequences share
-// prefixes.  Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
+// kCap: capped scores, kBias: less a slope times the distance; kShared: a launch of a call whose sequences share prefixes, of its rows
+// over the prefixes (kOverPrefix), over the own slots from those sums on (kOverOwn), or of both (kBoth).  Key tiles t0 + u0 .. t0 + u0 + n - 1 of a row tile's span [t0, t1) (n < 0: all of them) for KV head h.  part: where the
 // partial sums go, null: the rows are finished (over the prefixes, their sums are).  kNarrow: at most 16 rows; kWave: those by one wave, which
 // neither waits for another nor touches LDS.
 template <bool kF16, bool kCap, bool kBias, Pool kPool, bool kShared, bool kNarrow, bool kWave = false>

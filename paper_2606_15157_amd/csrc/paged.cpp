@@ -215,7 +215,8 @@ size_t attend_bytes(const rkv_pages* p, const rkv_attend* a) {
 
 // 8-bit pools and shared prefixes: whether a launch's key tiles are dealt out (attend_dealt_kernel and a join), by the rule above; of 8-bit pools,
 // us, a workgroup per tile against dealt out: one token of one sequence of 1024 12 / 19, of 2048 18.5 / 20, of 4096 31 / 21, of 32768 233 / 32; of 16
-// of 2048 21 / 26, of 4096 35 / 40, of 8192 69 / 57; of 64 of 4096 98 / 113, of 3000 to 5000 105 / 112, of 512 to 8192 124 / 96, of 64 to 8192 86 / 57.
+// of 2048 21 / 26, of 4096 35 / 40, of 8192 69 / 57; of 64 of 1024 26 and of 2048 45, not dealt out, of 4096 98 / 113, of 3000 to 5000 105 / 112,
+// of 512 to 8192 124 / 96, of 64 to 8192 86 / 57.
 bool dealt(const rkv_pages* p, const rkv_attend* a) {
   const int64_t tiles = row_tiles(p, a), most = ((int64_t)a->max_pages * p->page_size + 63) / 64;
   if (tiles > rkv::kAttendDealt || tiles * (4 + most) >= kIntEnd || p->n_kv_heads >= (1 << 20)) return false;   // an item's units, and at least one tile
@@ -413,8 +414,9 @@ int check_shared(const rkv_pages* p, const rkv_attend* a, const rkv_shared* g) {
 // Whether one launch takes both: the rows of all sequences over the prefixes and those of each over its own slots in one list, all sums by way
 // of memory and one join.  Two launches, one after the other, pay for two lists and two ramps, but only the prefixes' sums go through
 // memory and full rows are finished where they are.  Measured on 32 query and 8 KV heads, sequences x tokens behind a prefix, 64 to 512 own slots, us,
-// one against two: 16 x 1 behind 1024 24 / 38, 64 x 1 behind 8192 43 / 57, 64 x 8 117 / 123, 8 x 64 112 / 114, 64 x 16 198 / 199, 64 x 32 372 / 314;
-// 16 x 32 behind 1024 44 / 48, 16 x 64 61 / 52; in 8 bits 64 x 1 45 / 61, 64 x 16 215 / 219, 64 x 32 382 / 351.
+// one against two: 16 x 1 behind 1024 24 / 36, 64 x 1 behind 8192 42 / 56, 64 x 8 115 / 118, 8 x 64 111 / 112, 64 x 16 194 / 187, 64 x 32 369 / 302;
+// 16 x 32 behind 1024 44 / 48, 16 x 64 61 / 53; in 8 bits 64 x 1 44 / 59, 64 x 8 122 / 125, 8 x 64 116 / 118, 64 x 16 200 / 197, 64 x 32 376 / 320;
+// 16 x 32 behind 1024 46 / 49, 16 x 64 64 / 56.
 bool both_at_once(const rkv_pages* p, const rkv_attend* a, const rkv_attend* b) {
   const int64_t own = row_tiles(p, a), over = row_tiles(p, b), rows = (int64_t)a->n_rows * (a->n_q_heads / p->n_kv_heads);
   auto tiles = [&](int64_t pages) { return 4 + (pages * p->page_size + 63) / 64; };

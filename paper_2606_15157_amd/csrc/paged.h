@@ -1,4 +1,4 @@
-// Declarations of the paged caches: paged.cpp checks, pages.hip and attend.hip compute.
+// Declarations of the paged caches: paged.cpp checks, pages.hip moves rows and the attend*.hip instances of attend_rows.h and attend_dealt.h compute.
 #pragma once
 
 #include "rkv_internal.h"
